@@ -39,12 +39,13 @@ typedef enum {
   RG_ERR_ALIGNMENT = 5,     /* pointer or leading dimension breaks a 16-byte rule */
   RG_ERR_WORKSPACE = 6,     /* workspace missing or too small */
   RG_ERR_CUDA = 7,          /* the CUDA runtime or driver reported an error */
-  RG_ERR_TIMEOUT = 8        /* a bounded device-side wait gave up (see rg_device_status) */
+  RG_ERR_TIMEOUT = 8,       /* a bounded device-side wait gave up (see rg_device_status) */
+  RG_ERR_PAGE = 9           /* a sequence's length or block table reached outside the cache (see rg_device_status) */
 } rg_status_t;
 
 /* RG_F16 = IEEE binary16.  RG_F8E4M3 = 8-bit float, 1-4-3, bias 7, no infinities, NaN = S.1111.111
  * (the fp8 input type of Sec. 2); it is an operand type only (A and B of rg_gemm). */
-typedef enum { RG_BF16 = 0, RG_F32 = 1, RG_F16 = 2, RG_F8E4M3 = 3 } rg_dtype_t;
+typedef enum { RG_BF16 = 0, RG_F32 = 1, RG_F16 = 2, RG_F8E4M3 = 3, RG_I32 = 16, RG_I64 = 17 } rg_dtype_t;   /* RG_I32, RG_I64: positions (rg_rope) */
 
 /* The tree that combines values (split-K partials in rg_gemm, the leaves of a row in
  * rg_reduce_rows).  Sec. 3.1: a reduction order is a binary tree up to swapping an addition's
@@ -267,6 +268,124 @@ typedef struct {
 rg_status_t rg_attention(const rg_attn_desc_t* d, const rg_tensor_t* Q, const rg_tensor_t* K, const rg_tensor_t* Vt,
                          const rg_tensor_t* O, void* cuda_stream);
 
+/* ---- Positions, a paged cache of keys and values, and attention over it ----------------------------------
+ * The operators of a serving step around rg_gemm: rotate the new rows by their positions, put keys and values
+ * into pages, and let the new rows attend to everything their sequence holds.  (The paper treats attention with
+ * contiguous keys; rg_attention is that form.)  As everywhere in this library a row's bits depend on its own
+ * numbers and on the descriptor, not on the other rows of the batch, on how many new rows come at once, on where
+ * the pages lie, on the run, or on max_q and max_len.
+ *
+ * rg_rows_t: rows [tokens][heads][dim]; elements of one head are contiguous, the other strides are in elements
+ * and free (a slice of a fused product's output will do).  rg_cache_t: [pages][page_size][heads][dim] with any
+ * strides for the first three, so both [page][slot][head] and [page][head][slot] memory orders are this type.
+ * dim is at most 1024, heads at most 65535. */
+typedef struct {
+  void* ptr;
+  int32_t dtype;
+  int64_t tokens, heads, dim;
+  int64_t token_stride, head_stride;
+} rg_rows_t;
+typedef struct {
+  void* ptr;
+  int32_t dtype;
+  int64_t pages, page_size, heads, dim;
+  int64_t page_stride, slot_stride, head_stride;
+} rg_cache_t;
+
+/* The sequences of a batch.  All arrays are DEVICE memory and read when the kernels run, so a captured graph
+ * replays with what they hold by then.  Rows cu_q[s] .. cu_q[s+1]-1 are the new tokens of sequence s (cu_q
+ * starts at 0 and never falls; sequences without new tokens are fine; rows from cu_q[n_seqs] on belong to none:
+ * nothing is written for them).  seq_lens[s] counts the tokens of sequence s with the new ones: row r of its n
+ * new rows stands at place seq_lens[s] - n + r, in page block_table[s * table_ld + place / page_size].  Entries
+ * of pages behind the last token are not read.
+ *   max_q    the host's upper bound of new tokens in one sequence (0: the number of rows).  It picks tile
+ *            heights and never changes a bit or an answer.
+ *   max_len  the host's upper bound of seq_lens (0: table_cols * page_size).  It sizes the workspace.
+ * What only the device sees is checked there: a token without a place (seq_lens[s] < its count of new rows), a
+ * length beyond max_len or beyond the table, a page outside the cache.  Nothing out of bounds is touched; the
+ * health word (rg_device_status) then holds RG_PAGE_CODE_APPEND or RG_PAGE_CODE_ATTEND and the call's answer for
+ * that sequence is not meaningful: its key or value is not written, a page outside the cache reads as zeros, a
+ * length counts as its bound, a row without a place gives zeros (and -inf).
+ * A page may serve several sequences (a shared prefix) as long as no two tokens of one call write one slot. */
+typedef struct {
+  const int32_t* block_table;
+  int64_t table_ld;
+  int32_t table_cols;
+  int32_t n_seqs;
+  const int32_t* seq_lens;
+  const int32_t* cu_q;            /* n_seqs + 1 */
+  int64_t max_q;
+  int64_t max_len;
+} rg_paged_seqs_t;
+#define RG_PAGE_CODE_APPEND 0x2A00u
+#define RG_PAGE_CODE_ATTEND 0x2B00u
+
+/* Rotary positions: pair j (of rot_dim / 2) of every head turns by pos[axis(j)][token] * inv_freq[j] radians,
+ * (a, b) -> (a cos - b sin, b cos + a sin); elements from rot_dim on pass through.  RG_ROPE_HALF pairs elements
+ * j and j + rot_dim / 2, RG_ROPE_PAIRS elements 2j and 2j + 1.  The pairs of axis 0 come first, then axis 1's,
+ * ...: sections[a] pairs each, summing to rot_dim / 2.  With inverse = 1 the angle's sign is turned: the
+ * transpose, which takes the gradient of the rotated rows to the gradient of the rows.
+ * The angle is computed in 64 bits (exact to about 2^-52 of its size), sine, cosine and the rotation in fp32
+ * with one rounding to the output type.  rot_dim is even, at most 512 and at most dim; dim is even. */
+typedef enum { RG_ROPE_HALF = 0, RG_ROPE_PAIRS = 1 } rg_rope_style_t;
+typedef struct {
+  uint32_t size;          /* = sizeof(rg_rope_desc_t) */
+  uint32_t rot_dim;
+  uint32_t sections[4];
+  uint8_t style;          /* rg_rope_style_t */
+  uint8_t n_axes;         /* 1..4 */
+  uint8_t inverse;        /* 0 or 1 */
+  uint8_t _pad;
+} rg_rope_desc_t;
+
+/* out = x rotated.  x and out: bf16, fp16 or fp32 of one type, same shape, any strides; out may be x itself, else
+ * they do not overlap.  pos: RG_I32 or RG_I64, rows = axes, cols = tokens, `ld` elements between axes.  inv_freq:
+ * DEVICE pointer to rot_dim / 2 doubles.  Asynchronous on `cuda_stream`. */
+rg_status_t rg_rope(const rg_rope_desc_t* d, const rg_rows_t* x, const rg_tensor_t* pos, const double* inv_freq,
+                    const rg_rows_t* out, void* cuda_stream);
+
+/* Puts the new tokens' keys (rotated) and values into their pages, and rotates the queries into q_out, in one
+ * launch.  k, v: [tokens][kv heads][dim]; q, q_out (both or neither): [tokens][query heads][dim]; all of the
+ * caches' type (bf16, fp16 or fp32), any strides; q_out may be q itself.  pos as in rg_rope, or NULL: a token's
+ * position is its place in its sequence (then n_axes is 1).  d NULL: nothing turns (then q, q_out, pos and inv_freq
+ * are NULL too).  d->inverse must be 0.  Asynchronous on `cuda_stream`. */
+rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_rows_t* v, const rg_tensor_t* pos, const double* inv_freq,
+                         const rg_cache_t* k_cache, const rg_cache_t* v_cache, const rg_paged_seqs_t* seqs,
+                         const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream);
+
+/* Attention of the new rows over the cache (which holds their own keys and values already: rg_kv_append first).
+ * Query head h reads key head h / (query heads / kv heads).  A row at place p sees keys t <= p (mask = 1) or all
+ * keys of its sequence (mask = 0), and with window > 0 (mask = 1 only) of those the last `window`: t > p - window.
+ * Keys are walked in blocks of 128 places; with s_t = scale * (q . k_t) in fp32 from tensor-core chains over dim,
+ *   p_t = exp(s_t - m),   l += sum of the block's p_t,   O += (P . V)_block,   P = p narrowed to the cache's type
+ * where m is a running maximum that moves (and O and l are rescaled, in fp32) only when a block's maximum exceeds
+ * it by more than 8 / log2(e); the answer is O / l, rounded once.  exp is the hardware's base-two exponential for some of the
+ * elements and a polynomial of IEEE operations for the others, by the key's place: bits repeat on this architecture.
+ * lse (may be NULL): [tokens][query heads] of stride lse_ld, fp32: the natural logarithm of the sum of exp(s_t).  A row that
+ * sees no key gives zeros and -inf.  What a row does not see never reaches it, infinities and NaN in masked keys and
+ * values included; where a NaN or infinite value is seen the answer's element is NaN or infinite.
+ *   split   0, or a multiple of 128: keys [i * split, (i + 1) * split) form a part with a maximum, sum and product of
+ *           its own, and the parts are joined in ascending order.  It decides bits (rows of one `split` have the same
+ *           bits alone and in a chunk) and it spreads few rows with many keys over the GPU: 256 to 512 for single
+ *           tokens, 0 for long chunks.
+ * q, out: [tokens][query heads][dim]; q of the caches' type, bf16 or fp16; out of that type or fp32.  dim is a
+ * multiple of 8 up to 128; query heads a multiple of kv heads, at most 128 for each; page_size a multiple of 8.
+ * q and caches: 16-byte aligned, strides multiples of 8 elements, else RG_ERR_ALIGNMENT.  ws: at least
+ * rg_paged_attention_workspace_bytes(...), 16-byte aligned; calls (or graphs) that share one must not overlap.
+ * Asynchronous on `cuda_stream`. */
+typedef struct {
+  uint32_t size;          /* = sizeof(rg_paged_attn_desc_t) */
+  uint32_t split;
+  uint32_t window;        /* 0 = none */
+  float scale;            /* finite, > 0 */
+  uint8_t mask;           /* 0 = none, 1 = causal at the sequence's end */
+  uint8_t _pad[3];
+} rg_paged_attn_desc_t;
+size_t rg_paged_attention_workspace_bytes(const rg_paged_attn_desc_t* d, const rg_paged_seqs_t* seqs, int64_t page_size,
+                                          int64_t tokens, int64_t q_heads, int64_t dim);
+rg_status_t rg_paged_attention(const rg_paged_attn_desc_t* d, const rg_rows_t* q, const rg_cache_t* k_cache, const rg_cache_t* v_cache,
+                               const rg_paged_seqs_t* seqs, const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream);
+
 /* Host-buffer forms of rg_gemm and rg_reduce_rows, for callers whose data lives in host memory.
  * Every tensor / epilogue / args pointer is a HOST pointer (pinned memory makes the copies
  * asynchronous).  `dev_scratch` is a caller-owned DEVICE buffer of at least
@@ -338,7 +457,8 @@ rg_status_t rg_selftest_exp(int32_t form, const float* x, float* y, int64_t n, v
 /* Device-side health word of the current device.  Every wait inside the kernels is bounded; a
  * wait that gives up records a code here, lets the kernel drain and return, and leaves the
  * context usable.  Copies the word to *code (0 = healthy) and clears it.  Synchronises the
- * device.  Returns RG_ERR_TIMEOUT if the word was non-zero. */
+ * device.  Returns RG_ERR_TIMEOUT if the word was non-zero; if all it holds is a code of the paged
+ * operators (RG_PAGE_CODE_APPEND, RG_PAGE_CODE_ATTEND), RG_ERR_PAGE. */
 rg_status_t rg_device_status(uint32_t* code);
 
 const char* rg_status_string(rg_status_t s);

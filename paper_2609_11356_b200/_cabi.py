@@ -13,8 +13,12 @@ LIB_PATH = os.path.join(_HERE, "librg.so")
 
 RG_OK = 0
 STATUS_NAMES = {0: "RG_OK", 1: "RG_ERR_NULL", 2: "RG_ERR_INVALID_DESC", 3: "RG_ERR_UNSUPPORTED", 4: "RG_ERR_SHAPE",
-                5: "RG_ERR_ALIGNMENT", 6: "RG_ERR_WORKSPACE", 7: "RG_ERR_CUDA", 8: "RG_ERR_TIMEOUT"}
+                5: "RG_ERR_ALIGNMENT", 6: "RG_ERR_WORKSPACE", 7: "RG_ERR_CUDA", 8: "RG_ERR_TIMEOUT",
+                9: "RG_ERR_PAGE"}
 RG_BF16, RG_F32, RG_F16, RG_F8E4M3 = 0, 1, 2, 3
+RG_I32, RG_I64 = 16, 17
+RG_ROPE_HALF, RG_ROPE_PAIRS = 0, 1
+RG_PAGE_CODE_APPEND, RG_PAGE_CODE_ATTEND = 0x2A00, 0x2B00
 RG_TREE_LEFT, RG_TREE_BALANCED = 0, 1
 RG_ATOM_TC_BF16_K16, RG_ATOM_SCALAR, RG_ATOM_TC_F8_K32 = 0, 1, 2
 RG_COLOP_SUM, RG_COLOP_DOT = 0, 1
@@ -27,7 +31,8 @@ RG_SELFTEST_WAIT_CODE = 0xE00
 EXPORTS = ["rg_desc_init", "rg_desc_validate", "rg_desc_class", "rg_gemm_workspace_bytes", "rg_gemm",
            "rg_reduce_rows", "rg_gemm_host_scratch_bytes", "rg_gemm_host", "rg_reduce_rows_host_scratch_bytes",
            "rg_reduce_rows_host", "rg_device_status", "rg_status_string", "rg_gemm_noalloc",
-           "rg_reduce_cols_workspace_bytes", "rg_reduce_cols", "rg_attention", "rg_selftest_bounded_wait", "rg_selftest_exp"]
+           "rg_reduce_cols_workspace_bytes", "rg_reduce_cols", "rg_attention", "rg_selftest_bounded_wait", "rg_selftest_exp",
+           "rg_rope", "rg_kv_append", "rg_paged_attention_workspace_bytes", "rg_paged_attention"]
 
 
 class rg_attn_desc_t(C.Structure):
@@ -59,6 +64,31 @@ class rg_reduce_args_t(C.Structure):
     _fields_ = [("weight", C.c_void_p), ("weight_dtype", C.c_int32), ("eps", C.c_float), ("aux_out", C.c_void_p)]
 
 
+class rg_rows_t(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int32), ("tokens", C.c_int64), ("heads", C.c_int64), ("dim", C.c_int64),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class rg_cache_t(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int32), ("pages", C.c_int64), ("page_size", C.c_int64), ("heads", C.c_int64), ("dim", C.c_int64),
+                ("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class rg_paged_seqs_t(C.Structure):
+    _fields_ = [("block_table", C.c_void_p), ("table_ld", C.c_int64), ("table_cols", C.c_int32), ("n_seqs", C.c_int32),
+                ("seq_lens", C.c_void_p), ("cu_q", C.c_void_p), ("max_q", C.c_int64), ("max_len", C.c_int64)]
+
+
+class rg_rope_desc_t(C.Structure):
+    _fields_ = [("size", C.c_uint32), ("rot_dim", C.c_uint32), ("sections", C.c_uint32 * 4),
+                ("style", C.c_uint8), ("n_axes", C.c_uint8), ("inverse", C.c_uint8), ("_pad", C.c_uint8)]
+
+
+class rg_paged_attn_desc_t(C.Structure):
+    _fields_ = [("size", C.c_uint32), ("split", C.c_uint32), ("window", C.c_uint32), ("scale", C.c_float),
+                ("mask", C.c_uint8), ("_pad", C.c_uint8 * 3)]
+
+
 _lib = None
 
 
@@ -87,6 +117,11 @@ def load():
     L.rg_reduce_cols_workspace_bytes.restype = sz; L.rg_reduce_cols_workspace_bytes.argtypes = [i64, i64]
     L.rg_reduce_cols.restype = C.c_int; L.rg_reduce_cols.argtypes = [D, C.c_int, T, T, T, vp, sz, vp]
     L.rg_attention.restype = C.c_int; L.rg_attention.argtypes = [C.POINTER(rg_attn_desc_t), T, T, T, T, vp]
+    R, H, S, RD, PD = C.POINTER(rg_rows_t), C.POINTER(rg_cache_t), C.POINTER(rg_paged_seqs_t), C.POINTER(rg_rope_desc_t), C.POINTER(rg_paged_attn_desc_t)
+    L.rg_rope.restype = C.c_int; L.rg_rope.argtypes = [RD, R, T, vp, R, vp]
+    L.rg_kv_append.restype = C.c_int; L.rg_kv_append.argtypes = [RD, R, R, T, vp, H, H, S, R, R, vp]
+    L.rg_paged_attention_workspace_bytes.restype = sz; L.rg_paged_attention_workspace_bytes.argtypes = [PD, S, i64, i64, i64, i64]
+    L.rg_paged_attention.restype = C.c_int; L.rg_paged_attention.argtypes = [PD, R, H, H, S, R, vp, i64, vp, sz, vp]
     L.rg_gemm_noalloc.restype = C.c_int; L.rg_gemm_noalloc.argtypes = [D, T, T, T, E, vp]
     L.rg_selftest_bounded_wait.restype = C.c_int; L.rg_selftest_bounded_wait.argtypes = [C.c_uint64, vp, vp]
     L.rg_selftest_exp.restype = C.c_int; L.rg_selftest_exp.argtypes = [C.c_int32, vp, vp, C.c_int64, vp]

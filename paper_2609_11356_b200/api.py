@@ -234,3 +234,140 @@ def rg_reduce_rows_host(d: K.rg_desc_t, op: int, x, out, dev_scratch, *, weight=
 def rg_reduce_rows_host_scratch_bytes(op, x, out) -> int:
     xt, ot = _tensor(x), _tensor(out)
     return int(K.load().rg_reduce_rows_host_scratch_bytes(int(op), C.byref(xt), C.byref(ot)))
+
+
+# ---------------------------------------------------------------- positions, paged cache, attention over it
+def _rows(t) -> K.rg_rows_t:
+    if t.dim() != 3:
+        raise ValueError(f"rows are [tokens, heads, dim], got a tensor of {t.dim()} dimensions")
+    n, h, d = t.shape
+    st, sh, sd = t.stride()
+    if sd != 1 and d > 1:
+        raise ValueError("the elements of a head must be contiguous")
+    return K.rg_rows_t(t.data_ptr(), _dtype_code(t), n, h, d, st, sh)
+
+
+def _cache(t) -> K.rg_cache_t:
+    if t.dim() != 4:
+        raise ValueError(f"a cache is [pages, page_size, heads, dim], got a tensor of {t.dim()} dimensions")
+    if t.stride(3) != 1 and t.shape[3] > 1:
+        raise ValueError("the elements of a head must be contiguous")
+    return K.rg_cache_t(t.data_ptr(), _dtype_code(t), *t.shape, *t.stride()[:3])
+
+
+def _positions(pos) -> K.rg_tensor_t:
+    import torch
+    code = K.RG_I32 if pos.dtype == torch.int32 else K.RG_I64 if pos.dtype == torch.int64 else None
+    if code is None:
+        raise TypeError(f"positions are int32 or int64, got {pos.dtype}")
+    if pos.dim() not in (1, 2) or (pos.shape[-1] > 1 and pos.stride(-1) != 1):
+        raise ValueError("positions are [tokens] or [axes, tokens], contiguous along the tokens")
+    if pos.dim() == 1:
+        return K.rg_tensor_t(pos.data_ptr(), code, 1, pos.shape[0], pos.shape[0])
+    return K.rg_tensor_t(pos.data_ptr(), code, pos.shape[0], pos.shape[1], pos.stride(0))
+
+
+def _frequencies(inv_freq, d) -> int:
+    import torch
+    if inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous() or inv_freq.numel() != d.rot_dim // 2:
+        raise ValueError(f"inv_freq is a contiguous float64 tensor of rot_dim / 2 = {d.rot_dim // 2} elements")
+    return inv_freq.data_ptr()
+
+
+def _call(where: str, fn, device, *args):
+    """One C call with `device` current and on its current stream."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError(f"{where}: tensors must be on a CUDA device, got {device}")
+    if device.index == torch.cuda.current_device():
+        st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    _check(st, where)
+
+
+def _one_device(where: str, *tensors):
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"{where}: tensors on {device} and {t.device}")
+    return device
+
+
+def rg_rope_desc(*, rot_dim: int, style: int = K.RG_ROPE_HALF, sections: Sequence[int] = (), inverse: int = 0) -> K.rg_rope_desc_t:
+    """Rotary positions (see include/rg.h): `sections` gives the pairs of each axis (default: one axis with all of them)."""
+    d = K.rg_rope_desc_t()
+    sections = tuple(sections) or (rot_dim // 2,)
+    if len(sections) > 4 or rot_dim < 0 or any(n < 0 for n in sections):
+        raise RgError(2, "rg_rope_desc")
+    d.size, d.rot_dim, d.style, d.n_axes, d.inverse = C.sizeof(K.rg_rope_desc_t), rot_dim, style, len(sections), int(inverse)
+    for i, n in enumerate(sections):
+        d.sections[i] = n
+    return d
+
+
+def rg_rope(d: K.rg_rope_desc_t, x, pos, inv_freq, out):
+    """out = x [tokens, heads, dim] rotated by `pos` ([tokens] or [axes, tokens], int32 or int64); inv_freq: float64 [rot_dim / 2],
+    radians per position.  out may be x."""
+    device = _one_device("rg_rope", x, pos, inv_freq, out)
+    _call("rg_rope", K.load().rg_rope, device, C.byref(d), C.byref(_rows(x)), C.byref(_positions(pos)), _frequencies(inv_freq, d), C.byref(_rows(out)))
+    return out
+
+
+class rg_paged_seqs:
+    """The sequences of a batch (see include/rg.h): int32 CUDA tensors block_table [n, pages], seq_lens [n] and cu_q [n + 1], and the
+    host's bounds of new tokens in one sequence and of seq_lens (0: none known).  The tensors are read when the kernels run."""
+    __slots__ = ("block_table", "seq_lens", "cu_q", "device", "c")
+
+    def __init__(self, block_table, seq_lens, cu_q, *, max_q: int = 0, max_len: int = 0):
+        import torch
+        for name, t, dims in (("block_table", block_table, 2), ("seq_lens", seq_lens, 1), ("cu_q", cu_q, 1)):
+            if t.dtype != torch.int32 or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+                raise ValueError(f"{name} is a contiguous int32 tensor of {dims} dimension(s)")
+        n = seq_lens.shape[0]
+        if block_table.shape[0] != n or cu_q.shape[0] != n + 1:
+            raise ValueError(f"{n} sequences need block_table [{n}, pages] and cu_q [{n + 1}], got {tuple(block_table.shape)} and {tuple(cu_q.shape)}")
+        self.device = _one_device("rg_paged_seqs", seq_lens, block_table, cu_q)
+        self.block_table, self.seq_lens, self.cu_q = block_table, seq_lens, cu_q
+        self.c = K.rg_paged_seqs_t(block_table.data_ptr(), max(block_table.stride(0), block_table.shape[1]) if n > 1 else block_table.shape[1], block_table.shape[1], n,
+                                   seq_lens.data_ptr(), cu_q.data_ptr(), max_q, max_len)
+
+
+def rg_kv_append(d, k, v, inv_freq, k_cache, v_cache, seqs: rg_paged_seqs, *, pos=None, q=None, q_out=None):
+    """Put keys (rotated) and values of the new tokens into their pages; rotate q into q_out.  d None: nothing is rotated."""
+    if (q is None) != (q_out is None):
+        raise ValueError("rg_kv_append: q and q_out go together")
+    device = _one_device("rg_kv_append", k, v, inv_freq, k_cache, v_cache, seqs, pos, q, q_out)
+    _call("rg_kv_append", K.load().rg_kv_append, device, C.byref(d) if d is not None else None, C.byref(_rows(k)), C.byref(_rows(v)),
+          C.byref(_positions(pos)) if pos is not None else None, _frequencies(inv_freq, d) if inv_freq is not None and d is not None else None,
+          C.byref(_cache(k_cache)), C.byref(_cache(v_cache)), C.byref(seqs.c),
+          C.byref(_rows(q)) if q is not None else None, C.byref(_rows(q_out)) if q_out is not None else None)
+
+
+def rg_paged_attn_desc(*, scale: float, split: int = 0, window: int = 0, mask: int = 1) -> K.rg_paged_attn_desc_t:
+    """Attention over a paged cache: `split` keys for each part (0: one part), a causal mask (mask=1) of the last `window` keys (0: all)."""
+    if split < 0 or window < 0:
+        raise RgError(2, "rg_paged_attn_desc")
+    return K.rg_paged_attn_desc_t(C.sizeof(K.rg_paged_attn_desc_t), split, window, scale, mask)
+
+
+def rg_paged_attention_workspace_bytes(d: K.rg_paged_attn_desc_t, seqs: rg_paged_seqs, tokens: int, q_heads: int, dim: int, page_size: int = 0) -> int:
+    """Bytes of workspace; `page_size` is needed where seqs has no max_len."""
+    if page_size <= 0:
+        if seqs.c.max_len <= 0 and d.split:
+            raise ValueError("rg_paged_attention_workspace_bytes: give page_size, or seqs a max_len")
+        page_size = 1 << 20                              # max_len is the bound
+    return int(K.load().rg_paged_attention_workspace_bytes(C.byref(d), C.byref(seqs.c), page_size, tokens, q_heads, dim))
+
+
+def rg_paged_attention(d: K.rg_paged_attn_desc_t, q, k_cache, v_cache, seqs: rg_paged_seqs, out, *, lse=None, ws=None):
+    """out = attention of the rows q [tokens, heads, dim] over their sequences' pages; lse: float32 [tokens, heads] or None."""
+    import torch
+    device = _one_device("rg_paged_attention", q, k_cache, v_cache, seqs, out, lse, ws)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or (lse.shape[1] > 1 and lse.stride(1) != 1)):
+        raise ValueError("lse is float32 [tokens, heads], contiguous along the heads")
+    _call("rg_paged_attention", K.load().rg_paged_attention, device, C.byref(d), C.byref(_rows(q)), C.byref(_cache(k_cache)), C.byref(_cache(v_cache)),
+          C.byref(seqs.c), C.byref(_rows(out)), lse.data_ptr() if lse is not None else None, max(lse.stride(0), lse.shape[1]) if lse is not None else 0,
+          ws.data_ptr() if ws is not None else None, ws.numel() * ws.element_size() if ws is not None else 0)
+    return out

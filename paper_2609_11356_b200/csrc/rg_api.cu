@@ -445,6 +445,204 @@ rg_status_t rg_attention(const rg_attn_desc_t* d, const rg_tensor_t* Q, const rg
   return rg::launch_attention_fixed((int)d->block_n, (int)d->exp_base, (int)d->mask, d->scale, (int)H, Q, K, Vt, O, static_cast<cudaStream_t>(cuda_stream));
 }
 
+// ------------------------------------------------------------ rotary positions and the paged cache
+namespace {
+
+constexpr int64_t STRIDE_LIMIT = int64_t(1) << 46;         // elements: byte offsets stay within 64 bits
+
+rg_status_t check_rows(const rg_rows_t* t) {
+  if (!t) return RG_ERR_NULL;
+  if (!dtype_ok(t->dtype)) return RG_ERR_SHAPE;
+  if (t->tokens < 0 || t->tokens > DIM_LIMIT || t->heads < 1 || t->heads > 65535 || t->dim < 1 || t->dim > 1024) return RG_ERR_SHAPE;
+  if (t->token_stride < 0 || t->head_stride < 0 || t->token_stride > STRIDE_LIMIT || t->head_stride > STRIDE_LIMIT) return RG_ERR_SHAPE;
+  if (t->tokens > 0 && !t->ptr) return RG_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(t->ptr) % esize(t->dtype)) return RG_ERR_ALIGNMENT;
+  return RG_OK;
+}
+
+// what is written: two elements must not share an address
+rg_status_t check_rows_out(const rg_rows_t* t) {
+  rg_status_t s = check_rows(t);
+  if (s != RG_OK) return s;
+  const bool head_inner = t->head_stride >= t->dim && (t->tokens < 2 || t->token_stride >= (t->heads - 1) * t->head_stride + t->dim);
+  const bool token_inner = t->token_stride >= t->dim && (t->heads < 2 || t->head_stride >= (t->tokens - 1) * t->token_stride + t->dim);
+  const bool one = t->heads == 1 && (t->tokens < 2 || t->token_stride >= t->dim);
+  return head_inner || token_inner || one ? RG_OK : RG_ERR_SHAPE;
+}
+
+rg_status_t check_cache(const rg_cache_t* c) {
+  if (!c) return RG_ERR_NULL;
+  if (!dtype_ok(c->dtype)) return RG_ERR_SHAPE;
+  if (c->pages < 0 || c->pages > DIM_LIMIT || c->page_size < 1 || c->page_size > (1 << 20) || c->heads < 1 || c->heads > 65535 || c->dim < 1 || c->dim > 1024)
+    return RG_ERR_SHAPE;
+  const int64_t st[3] = {c->page_stride, c->slot_stride, c->head_stride};
+  for (int64_t x : st) if (x < 0 || x > STRIDE_LIMIT) return RG_ERR_SHAPE;
+  if (c->pages > 0 && !c->ptr) return RG_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(c->ptr) % esize(c->dtype)) return RG_ERR_ALIGNMENT;
+  return RG_OK;
+}
+
+rg_status_t check_seqs(const rg_paged_seqs_t* q) {
+  if (!q) return RG_ERR_NULL;
+  if (q->n_seqs < 0 || q->table_cols < 0 || q->table_ld < 0 || q->max_q < 0 || q->max_len < 0) return RG_ERR_SHAPE;
+  if (q->table_ld < q->table_cols && q->n_seqs > 1) return RG_ERR_SHAPE;
+  if (q->n_seqs > 0 && (!q->seq_lens || !q->cu_q || (q->table_cols > 0 && !q->block_table))) return RG_ERR_NULL;
+  return RG_OK;
+}
+
+rg_status_t check_rope_desc(const rg_rope_desc_t* d, int64_t dim) {
+  if (!d) return RG_ERR_NULL;
+  if (d->size != sizeof(rg_rope_desc_t) || d->style > RG_ROPE_PAIRS || d->n_axes < 1 || d->n_axes > 4 || d->inverse > 1) return RG_ERR_INVALID_DESC;
+  if (d->rot_dim < 2 || d->rot_dim % 2) return RG_ERR_INVALID_DESC;
+  uint64_t pairs = 0;
+  for (int a = 0; a < d->n_axes; ++a) pairs += d->sections[a];
+  if (pairs != d->rot_dim / 2) return RG_ERR_INVALID_DESC;
+  if (d->rot_dim > 512) return RG_ERR_UNSUPPORTED;
+  if (d->rot_dim > dim || dim % 2) return RG_ERR_SHAPE;
+  return RG_OK;
+}
+
+rg_status_t check_positions(const rg_rope_desc_t* d, const rg_tensor_t* pos, int64_t tokens) {
+  if (pos->dtype != RG_I32 && pos->dtype != RG_I64) return RG_ERR_SHAPE;
+  if (pos->rows != d->n_axes || pos->cols != tokens || (d->n_axes > 1 && pos->ld < tokens)) return RG_ERR_SHAPE;
+  if (tokens > 0 && !pos->ptr) return RG_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(pos->ptr) % (pos->dtype == RG_I64 ? 8 : 4)) return RG_ERR_ALIGNMENT;
+  return RG_OK;
+}
+
+void set_rotation(rg::RopeParams* p, const rg_rope_desc_t* d, const rg_tensor_t* pos, const double* inv_freq) {
+  p->rot = (int32_t)d->rot_dim; p->style = d->style; p->inverse = d->inverse;
+  uint32_t end = 0;
+  for (int a = 0; a < 3; ++a) {
+    if (a < d->n_axes) end += d->sections[a];
+    p->axis_end[a] = a + 1 < d->n_axes ? (int32_t)end : INT32_MAX;
+  }
+  p->inv_freq = inv_freq;
+  if (pos) { p->pos = pos->ptr; p->pos64 = pos->dtype == RG_I64; p->pos_ld = pos->ld; }
+}
+
+bool same_shape(const rg_rows_t* a, const rg_rows_t* b) {
+  return a->dtype == b->dtype && a->tokens == b->tokens && a->heads == b->heads && a->dim == b->dim;
+}
+
+int64_t bound_of_len(const rg_paged_seqs_t* q, int64_t page_size) {
+  const int64_t all = (int64_t)q->table_cols * page_size;
+  return q->max_len > 0 ? std::min(q->max_len, all) : all;
+}
+
+rg_status_t check_paged_desc(const rg_paged_attn_desc_t* d) {
+  if (!d) return RG_ERR_NULL;
+  if (d->size != sizeof(rg_paged_attn_desc_t) || d->mask > 1) return RG_ERR_INVALID_DESC;
+  if (!(d->scale > 0.0f) || d->scale > 3.0e38f) return RG_ERR_INVALID_DESC;
+  if (d->split % 128 || d->split > (1u << 30) || d->window > (1u << 30)) return RG_ERR_INVALID_DESC;
+  if (d->window && !d->mask) return RG_ERR_INVALID_DESC;
+  return RG_OK;
+}
+
+}  // namespace
+
+rg_status_t rg_rope(const rg_rope_desc_t* d, const rg_rows_t* x, const rg_tensor_t* pos, const double* inv_freq,
+                    const rg_rows_t* out, void* cuda_stream) {
+  rg_status_t s;
+  if (!d || !pos || !inv_freq) return RG_ERR_NULL;
+  if ((s = check_rows(x)) != RG_OK || (s = check_rows_out(out)) != RG_OK) return s;
+  if ((s = check_rope_desc(d, x->dim)) != RG_OK || (s = check_positions(d, pos, x->tokens)) != RG_OK) return s;
+  if (!same_shape(x, out)) return RG_ERR_SHAPE;
+  if (reinterpret_cast<uintptr_t>(inv_freq) % 8) return RG_ERR_ALIGNMENT;
+  if (x->tokens == 0) return RG_OK;
+  rg::RopeParams p{};
+  p.st[0] = {x->ptr, out->ptr, x->token_stride, x->head_stride, 0, out->token_stride, out->head_stride, (int32_t)x->heads, 1, 0};
+  p.n_streams = 1; p.tokens = x->tokens; p.d = (int32_t)x->dim;
+  set_rotation(&p, d, pos, inv_freq);
+  return rg::launch_rope(p, x->dtype, false, static_cast<cudaStream_t>(cuda_stream));
+}
+
+rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_rows_t* v, const rg_tensor_t* pos, const double* inv_freq,
+                         const rg_cache_t* k_cache, const rg_cache_t* v_cache, const rg_paged_seqs_t* seqs,
+                         const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream) {
+  rg_status_t s;
+  if ((s = check_rows(k)) != RG_OK || (s = check_rows(v)) != RG_OK || (s = check_cache(k_cache)) != RG_OK || (s = check_cache(v_cache)) != RG_OK ||
+      (s = check_seqs(seqs)) != RG_OK)
+    return s;
+  if (!same_shape(k, v) || k->dtype != k_cache->dtype || k->dtype != v_cache->dtype) return RG_ERR_SHAPE;
+  if (k_cache->pages != v_cache->pages || k_cache->page_size != v_cache->page_size || k_cache->heads != k->heads || v_cache->heads != k->heads ||
+      k_cache->dim != k->dim || v_cache->dim != k->dim || k->dim % 2)
+    return RG_ERR_SHAPE;
+  if (!q != !q_out) return RG_ERR_NULL;
+  if (d) {
+    if ((s = check_rope_desc(d, k->dim)) != RG_OK) return s;
+    if (d->inverse) return RG_ERR_UNSUPPORTED;
+    if (!inv_freq) return RG_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(inv_freq) % 8) return RG_ERR_ALIGNMENT;
+    if (pos) { if ((s = check_positions(d, pos, k->tokens)) != RG_OK) return s; }
+    else if (d->n_axes != 1) return RG_ERR_INVALID_DESC;
+  } else if (q || pos || inv_freq) {
+    return RG_ERR_INVALID_DESC;
+  }
+  if (q) {
+    if ((s = check_rows(q)) != RG_OK || (s = check_rows_out(q_out)) != RG_OK) return s;
+    if (!same_shape(q, q_out) || q->tokens != k->tokens || q->dim != k->dim || q->dtype != k->dtype) return RG_ERR_SHAPE;
+  }
+  if (k->tokens == 0 || seqs->n_seqs == 0) return RG_OK;
+  rg::RopeParams p{};
+  int n = 0;
+  p.st[n++] = {k->ptr, k_cache->ptr, k->token_stride, k->head_stride, k_cache->page_stride, k_cache->slot_stride, k_cache->head_stride, (int32_t)k->heads, d ? 1 : 0, 1};
+  p.st[n++] = {v->ptr, v_cache->ptr, v->token_stride, v->head_stride, v_cache->page_stride, v_cache->slot_stride, v_cache->head_stride, (int32_t)v->heads, 0, 1};
+  if (q) p.st[n++] = {q->ptr, q_out->ptr, q->token_stride, q->head_stride, 0, q_out->token_stride, q_out->head_stride, (int32_t)q->heads, 1, 0};
+  p.n_streams = n; p.tokens = k->tokens; p.d = (int32_t)k->dim;
+  if (d) set_rotation(&p, d, pos, inv_freq);
+  p.table = seqs->block_table; p.table_ld = seqs->table_ld; p.table_cols = seqs->table_cols;
+  p.seq_lens = seqs->seq_lens; p.cu_q = seqs->cu_q; p.n_seqs = seqs->n_seqs;
+  p.pages = k_cache->pages; p.page_size = (int32_t)k_cache->page_size;
+  return rg::launch_rope(p, k->dtype, true, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t rg_paged_attention_workspace_bytes(const rg_paged_attn_desc_t* d, const rg_paged_seqs_t* seqs, int64_t page_size,
+                                          int64_t tokens, int64_t q_heads, int64_t dim) {
+  if (check_paged_desc(d) != RG_OK || check_seqs(seqs) != RG_OK || page_size < 1 || tokens < 1 || q_heads < 1 || dim < 1) return 0;
+  if (d->split == 0) return 0;
+  const int64_t n = (bound_of_len(seqs, page_size) + d->split - 1) / d->split;
+  if (n <= 1) return 0;
+  return align_up((size_t)tokens * q_heads * n * (size_t)(dim + 2) * sizeof(float), 256);
+}
+
+rg_status_t rg_paged_attention(const rg_paged_attn_desc_t* d, const rg_rows_t* q, const rg_cache_t* k_cache, const rg_cache_t* v_cache,
+                               const rg_paged_seqs_t* seqs, const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream) {
+  rg_status_t s;
+  if ((s = check_paged_desc(d)) != RG_OK) return s;
+  if ((s = check_rows(q)) != RG_OK || (s = check_rows_out(out)) != RG_OK || (s = check_cache(k_cache)) != RG_OK || (s = check_cache(v_cache)) != RG_OK ||
+      (s = check_seqs(seqs)) != RG_OK)
+    return s;
+  if (q->dtype == RG_F32) return RG_ERR_UNSUPPORTED;
+  if (k_cache->dtype != q->dtype || v_cache->dtype != q->dtype || (out->dtype != q->dtype && out->dtype != RG_F32)) return RG_ERR_SHAPE;
+  if (out->tokens != q->tokens || out->heads != q->heads || out->dim != q->dim) return RG_ERR_SHAPE;
+  if (k_cache->pages != v_cache->pages || k_cache->page_size != v_cache->page_size || k_cache->heads != v_cache->heads || k_cache->dim != q->dim || v_cache->dim != q->dim)
+    return RG_ERR_SHAPE;
+  if (q->heads % k_cache->heads) return RG_ERR_SHAPE;
+  if (q->dim % 8 || q->dim > 128 || k_cache->page_size % 8 || q->heads / k_cache->heads > 128) return RG_ERR_UNSUPPORTED;
+  if (lse && (lse_ld < q->heads || reinterpret_cast<uintptr_t>(lse) % 4)) return RG_ERR_SHAPE;
+  const int64_t strides[] = {q->token_stride, q->head_stride, k_cache->page_stride, k_cache->slot_stride, k_cache->head_stride,
+                             v_cache->page_stride, v_cache->slot_stride, v_cache->head_stride};
+  for (int64_t x : strides) if (x % 8) return RG_ERR_ALIGNMENT;
+  if ((reinterpret_cast<uintptr_t>(q->ptr) | reinterpret_cast<uintptr_t>(k_cache->ptr) | reinterpret_cast<uintptr_t>(v_cache->ptr)) & 15) return RG_ERR_ALIGNMENT;
+  const int64_t max_len = bound_of_len(seqs, k_cache->page_size);
+  if (max_len > DIM_LIMIT / 2) return RG_ERR_SHAPE;
+  if (q->tokens == 0 || seqs->n_seqs == 0) return RG_OK;
+  rg::PagedAttnArgs a{};
+  a.q = q; a.k = k_cache; a.v = v_cache; a.seqs = seqs; a.out = out; a.lse = lse; a.lse_ld = lse_ld;
+  a.max_q = seqs->max_q > 0 ? std::min(seqs->max_q, q->tokens) : q->tokens;
+  a.max_len = max_len;
+  a.split = d->split; a.window = d->window; a.scale = d->scale; a.causal = d->mask;
+  a.segments = d->split ? (int32_t)((max_len + d->split - 1) / d->split) : 1;
+  if (a.segments < 1) a.segments = 1;
+  if (a.segments > 1) {
+    if (!ws || ws_bytes < rg_paged_attention_workspace_bytes(d, seqs, k_cache->page_size, q->tokens, q->heads, q->dim)) return RG_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws) & 15) return RG_ERR_ALIGNMENT;
+    a.ws = ws;
+  }
+  return rg::launch_paged_attention(a, static_cast<cudaStream_t>(cuda_stream));
+}
+
 // ------------------------------------------------------------ host-buffer forms
 size_t rg_gemm_host_scratch_bytes(const rg_desc_t* d, int64_t M, int64_t N, int64_t K, int32_t c_dtype,
                                   const rg_epilogue_t* epi) {
@@ -605,8 +803,11 @@ rg_status_t rg_device_status(uint32_t* code) {
   if (s2 == RG_ERR_CUDA) return s2;
   const rg_status_t s3 = rg::read_and_clear_attn_status(&c);
   if (s3 == RG_ERR_CUDA) return s3;
-  if (code) *code = a ? a : (b ? b : c);
-  return (a || b || c) ? RG_ERR_TIMEOUT : RG_OK;
+  uint32_t e = 0, f = 0;
+  if (rg::read_and_clear_paged_attn_status(&e) == RG_ERR_CUDA || rg::read_and_clear_paged_status(&f) == RG_ERR_CUDA) return RG_ERR_CUDA;
+  const uint32_t waits = a ? a : (b ? b : (c ? c : (e != RG_PAGE_CODE_ATTEND ? e : 0)));   // a wait that gave up goes before a bad page
+  if (code) *code = waits ? waits : (e ? e : f);
+  return waits ? RG_ERR_TIMEOUT : (e || f) ? RG_ERR_PAGE : RG_OK;
 }
 
 const char* rg_status_string(rg_status_t s) {
@@ -620,6 +821,7 @@ const char* rg_status_string(rg_status_t s) {
     case RG_ERR_WORKSPACE: return "workspace missing or too small";
     case RG_ERR_CUDA: return "CUDA runtime or driver error";
     case RG_ERR_TIMEOUT: return "a bounded device-side wait gave up";
+    case RG_ERR_PAGE: return "a sequence's length or block table reached outside the cache";
   }
   return "unknown status";
 }

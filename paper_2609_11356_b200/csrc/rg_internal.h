@@ -65,6 +65,55 @@ bool make_operand_tmap(CUtensorMap_st* map, const void* ptr, int dtype, int64_t 
 rg_status_t launch_attention_fixed(int block_n, int exp_base, int causal, float scale, int heads, const rg_tensor_t* Q, const rg_tensor_t* K,
                                    const rg_tensor_t* Vt, const rg_tensor_t* O, cudaStream_t st);
 rg_status_t read_and_clear_attn_status(uint32_t* code);
+
+// ---- rotary positions, paged cache (rg_rope.cu, rg_paged_attention.cu)
+struct RopeStream {
+  const void* src;
+  void* dst;
+  int64_t src_tok, src_head;           // strides in elements
+  int64_t dst_page, dst_tok, dst_head; // dst_tok: between slots of a page, or between rows
+  int32_t heads;
+  int32_t rotate;
+  int32_t paged;                       // dst is a cache
+};
+struct RopeParams {
+  RopeStream st[3];
+  int32_t n_streams, heads_all;
+  int64_t tokens;
+  int32_t d, rot, style, inverse;
+  int32_t axis_end[3];                 // first pair of the axes 1, 2, 3
+  int32_t pos64;
+  const void* pos;
+  int64_t pos_ld;
+  const double* inv_freq;
+  const int32_t* table;
+  int64_t table_ld;
+  const int32_t* seq_lens;
+  const int32_t* cu_q;
+  int64_t pages;
+  int32_t table_cols, n_seqs, page_size;
+  int32_t tile, head_group;            // tokens and heads of a CTA
+};
+rg_status_t launch_rope(RopeParams p, int dtype, bool paged, cudaStream_t st);
+rg_status_t read_and_clear_paged_status(uint32_t* code);
+
+struct PagedAttnArgs {
+  const rg_rows_t* q;
+  const rg_cache_t* k;
+  const rg_cache_t* v;
+  const rg_paged_seqs_t* seqs;
+  const rg_rows_t* out;
+  float* lse;
+  int64_t lse_ld;
+  void* ws;
+  int64_t max_q, max_len;              // resolved bounds
+  int32_t segments;                    // most parts of a row (1: no workspace)
+  uint32_t split, window;
+  float scale;
+  int32_t causal;
+};
+rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st);
+rg_status_t read_and_clear_paged_attn_status(uint32_t* code);
 rg_status_t read_and_clear_status(uint32_t* code);
 rg_status_t launch_wait_selftest(uint64_t limit_ns, uint32_t code, unsigned int* left_early, cudaStream_t st);
 // y[i] = FORM(x[i]) by the device functions the kernels use (forms 0-2 and 6; the attention kernel's forms 3-5)
