@@ -448,7 +448,7 @@ rg_status_t rg_attention(const rg_attn_desc_t* d, const rg_tensor_t* Q, const rg
 // ------------------------------------------------------------ rotary positions and the paged cache
 namespace {
 
-constexpr int64_t STRIDE_LIMIT = int64_t(1) << 46;         // elements: byte offsets stay within 64 bits
+constexpr int64_t STRIDE_LIMIT = int64_t(1) << 38;         // elements: what a tensor map can hold in bytes
 
 rg_status_t check_rows(const rg_rows_t* t) {
   if (!t) return RG_ERR_NULL;
@@ -624,8 +624,11 @@ rg_status_t rg_paged_attention(const rg_paged_attn_desc_t* d, const rg_rows_t* q
   const int64_t strides[] = {q->token_stride, q->head_stride, k_cache->page_stride, k_cache->slot_stride, k_cache->head_stride,
                              v_cache->page_stride, v_cache->slot_stride, v_cache->head_stride};
   for (int64_t x : strides) if (x % 8) return RG_ERR_ALIGNMENT;
+  // a dimension that repeats one address has no tensor map
+  const int64_t sizes[] = {q->tokens, q->heads, k_cache->pages, k_cache->page_size, k_cache->heads, v_cache->pages, v_cache->page_size, v_cache->heads};
+  for (int i = 0; i < 8; ++i) if (strides[i] == 0 && sizes[i] > 1) return RG_ERR_UNSUPPORTED;
   if ((reinterpret_cast<uintptr_t>(q->ptr) | reinterpret_cast<uintptr_t>(k_cache->ptr) | reinterpret_cast<uintptr_t>(v_cache->ptr)) & 15) return RG_ERR_ALIGNMENT;
-  const int64_t max_len = bound_of_len(seqs, k_cache->page_size);
+  const int64_t max_len = k_cache->pages > 0 ? bound_of_len(seqs, k_cache->page_size) : 0;
   if (max_len > DIM_LIMIT / 2) return RG_ERR_SHAPE;
   if (q->tokens == 0 || seqs->n_seqs == 0) return RG_OK;
   rg::PagedAttnArgs a{};

@@ -1846,6 +1846,20 @@ rg_status_t launch_silu_selftest(const float* x, float* y, int64_t n, cudaStream
 }
 
 // The same tensor map for other kernels of the library (boxes of 64 columns x box_rows rows, 128-byte swizzle).
+// 4-D tensor map over 16-bit elements (innermost dimension contiguous, strides of the others in elements), 128-byte swizzle, zero fill
+// outside.  The stride of a dimension of one entry is never used and may be anything.
+bool make_tmap_4d(CUtensorMap_st* map, const void* ptr, int dtype, const int64_t (&dims)[4], const int64_t (&strides)[3], const int (&box)[4]) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return false;
+  cuuint64_t d[4], st[3];
+  cuuint32_t b[4];
+  const cuuint32_t es[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 4; ++i) { d[i] = (cuuint64_t)dims[i]; b[i] = (cuuint32_t)box[i]; }
+  for (int i = 0; i < 3; ++i) st[i] = dims[i + 1] > 1 ? (cuuint64_t)strides[i] * 2 : 16;
+  return fn(map, dtype == RG_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), d, st, b, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool make_operand_tmap(CUtensorMap_st* map, const void* ptr, int dtype, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
   return cached_tmap(map, ptr, dtype, rows, cols, ld, box_rows);
 }
