@@ -41,6 +41,7 @@ namespace {
 
 constexpr int BLK = 128;                       // keys of a block
 constexpr float LAG = 8.0f;                    // how far, in powers of two, a score may exceed the running maximum
+constexpr int ITEMS = 4;                       // work items that the producer can be ahead
 constexpr int FLAGS = 8;                       // masked blocks' items that the fixer can be ahead of the softmax warps (below half the ring's slots)
 
 // ---------------------------------------------------------------- PTX
@@ -73,6 +74,11 @@ __device__ __forceinline__ void pa_ld32(uint32_t taddr, uint32_t* r) {
         "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void pa_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void pa_st32(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
@@ -83,7 +89,6 @@ __device__ __forceinline__ void pa_st32(uint32_t taddr, const uint32_t* r) {
         "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
       : "memory");
 }
-__device__ __forceinline__ void pa_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void pa_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float pa_ex2(float x) {
   float y;
@@ -107,9 +112,9 @@ __device__ __forceinline__ uint64_t pa_desc(uint32_t smem_addr, uint32_t lead) {
   d |= static_cast<uint64_t>(2) << 61;
   return d;
 }
-// 16-bit x 16-bit -> fp32, M = 128, N = n; `transposed`: second operand MN-major
-__host__ __device__ constexpr uint32_t pa_idesc(int n, bool bf16, bool transposed) {
-  return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (transposed ? 1u << 16 : 0u) | (static_cast<uint32_t>(n >> 3) << 17) | (8u << 24);
+// 16-bit x 16-bit -> fp32, M = 128, N = n; `transposed`: that operand is MN-major
+__host__ __device__ constexpr uint32_t pa_idesc(int n, bool bf16, bool a_transposed, bool b_transposed) {
+  return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (a_transposed ? 1u << 15 : 0u) | (b_transposed ? 1u << 16 : 0u) | (static_cast<uint32_t>(n >> 3) << 17) | (8u << 24);
 }
 
 // ---------------------------------------------------------------- arguments and work items
@@ -134,15 +139,16 @@ struct Params {
   int64_t v_page, v_slot, v_head;
 };
 
-struct Item {
+struct alignas(16) Item {
   int32_t seq, head, seg;
   int32_t tok;                           // first token of the CTA's rows
-  int32_t n_tok;                         // tokens of this CTA
+  int32_t n_tok;                         // tokens of this CTA; 0: no more items
   int32_t pos;                           // place of the first one
   int32_t len, lo, hi;                   // keys some row sees, within this part: lo .. hi (hi < lo: none)
   int32_t b0, b1;                        // blocks
-  bool multi;                            // the sequence has several parts: results go to the workspace
+  int32_t multi;                         // the sequence has several parts: results go to the workspace
 };
+static_assert(sizeof(Item) == 48, "three 16-byte words");
 
 // How a sequence's rows see its keys.
 struct SeqView {
@@ -167,11 +173,11 @@ __device__ __forceinline__ void parts_of(const Params& p, const SeqView& v, int3
   if (p.split && hi >= lo) { *g0 = (int32_t)(lo / p.split); *n = (int32_t)(hi / p.split) - *g0 + 1; }
 }
 
-// The items of this CTA: number blockIdx.x, + gridDim.x, ... in the order sequence, tile (the last, longest first), part, head.  Every warp
-// that needs them walks the same list; 32 sequences at a time, one a lane.
+// The items of this CTA: number blockIdx.x, + gridDim.x, ... in the order sequence, tile (the last, longest first), part, head; 32 sequences at a
+// time, one a lane.  The producer walks them and hands them to the other warps in shared memory.
 struct Walk {
-  int64_t next;                          // number of the next item, counted from the first item of the lane group
-  int64_t before, count, total;          // this lane's sequence: items before it in the group, its own; the group's
+  uint32_t next;                         // number of the next item, counted from the first item of the lane group
+  uint32_t before, count, total;          // this lane's sequence: items before it in the group, its own; the group's
   int32_t base;                          // first sequence of the group
   SeqView mine;                          // this lane's sequence
   __device__ __forceinline__ void load(const Params& p, int tile_tokens) {
@@ -183,12 +189,12 @@ struct Walk {
       if (bad) atomicCAS(&g_paged_attn_status_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
       int32_t g0, n;
       parts_of(p, v, &g0, &n);
-      count = (int64_t)((v.n + tile_tokens - 1) / tile_tokens) * n * p.hkv;
+      count = (uint32_t)((v.n + tile_tokens - 1) / tile_tokens) * n * p.hkv;
     }
-    int64_t sum = count;
+    uint32_t sum = count;
 #pragma unroll
     for (int x = 1; x < 32; x <<= 1) {
-      const int64_t up = __shfl_up_sync(0xffffffffu, sum, x);
+      const uint32_t up = __shfl_up_sync(0xffffffffu, sum, x);
       if (lane >= x) sum += up;
     }
     before = sum - count;
@@ -203,7 +209,7 @@ struct Walk {
       load(p, tile_tokens);
     }
     const int owner = __ffs(__ballot_sync(0xffffffffu, next >= before && next < before + count)) - 1;
-    const int64_t local = next - __shfl_sync(0xffffffffu, before, owner);
+    const uint32_t local = next - __shfl_sync(0xffffffffu, before, owner);
     next += gridDim.x;
     it.seq = base + owner;
     SeqView v;
@@ -212,10 +218,10 @@ struct Walk {
     v.first = v.len - v.n;
     int32_t g0, n;
     parts_of(p, v, &g0, &n);
-    it.head = (int32_t)(local % p.hkv);
-    const int64_t rest = local / p.hkv;
-    it.seg = (int32_t)(rest % n);
-    const int32_t tiles = (v.n + tile_tokens - 1) / tile_tokens, tile = tiles - 1 - (int32_t)(rest / n);
+    const uint32_t rest = local / (uint32_t)p.hkv;
+    it.head = (int32_t)(local - rest * p.hkv);
+    it.seg = (int32_t)(rest % (uint32_t)n);
+    const int32_t tiles = (v.n + tile_tokens - 1) / tile_tokens, tile = tiles - 1 - (int32_t)(rest / (uint32_t)n);
     const int32_t t0 = tile * tile_tokens;
     it.n_tok = min(tile_tokens, v.n - t0);
     it.tok = v.tok + t0;
@@ -261,105 +267,164 @@ __device__ __forceinline__ float2 poly_ex2(float2 x) {
   return make_float2(__int_as_float(__float_as_int(q.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(q.y) + (__float_as_int(t.y) << 23)));
 }
 
-struct Row {
-  float m, l;                            // running maximum of the scores (before scaling) and sum
-};
+constexpr int QW = 32;                         // scores are taken 32 keys at a time: a quarter of a block, with a sum of its own
 
-// Scores of one row and block -> probabilities.  s: the block's 128 scores; packed: the narrowed probabilities, two a word.  first ..
-// last: the columns the row sees (MASKED).  Returns the factor that O takes first.
-template <int DT, bool MASKED>
-__device__ __forceinline__ float softmax_block(uint32_t (&s)[BLK], uint32_t (&packed)[BLK / 2], int first, int last, float c, Row& row) {
-  if (MASKED) {
-#pragma unroll
-    for (int i = 0; i < BLK; ++i) s[i] = (i >= first && i <= last) ? s[i] : 0xff800000u;
-  }
-  float mx[4];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    mx[q] = __uint_as_float(s[32 * q]);
-#pragma unroll
-    for (int i = 1; i + 1 < 32; i += 2) mx[q] = max3(mx[q], __uint_as_float(s[32 * q + i]), __uint_as_float(s[32 * q + i + 1]));
-    mx[q] = max3(mx[q], __uint_as_float(s[32 * q + 31]), __uint_as_float(s[32 * q + 31]));
-  }
-  const float mb = max3(max3(mx[0], mx[1], mx[2]), mx[3], mx[3]);
-  float alpha = 1.0f;
-  if (f_mul(f_add(mb, -row.m), c) > LAG) {                 // from -inf: any number; -inf and NaN: never
-    alpha = pa_ex2(f_mul(f_add(row.m, -mb), c));
-    row.m = mb;
-  }
-  const float shift = row.m == -INFINITY ? 0.0f : -f_mul(row.m, c);
-  const float2 c2 = make_float2(c, c), sh2 = make_float2(shift, shift);
-  float2 sum[4];
-#pragma unroll
-  for (int i = 0; i < BLK / 2; ++i) {
-    const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, sh2);
-    float2 e;
-    // which of the two exponentials a key takes follows from its place alone: the hardware unit gives 4 results a cycle and
-    // quarter of the SM, the polynomial takes the rest off it
-    if ((i & 3) == 3) e = poly_ex2(x);
-    else e = make_float2(pa_ex2(x.x), pa_ex2(x.y));
-    if (MASKED) {
-      e.x = (2 * i >= first && 2 * i <= last) ? e.x : 0.0f;
-      e.y = (2 * i + 1 >= first && 2 * i + 1 <= last) ? e.y : 0.0f;
-    }
-    sum[i & 3] = i < 4 ? e : __fadd2_rn(sum[i & 3], e);
-    packed[i] = pack_16x2(e.x, e.y, DT);
-  }
-  const float2 t = __fadd2_rn(__fadd2_rn(sum[0], sum[1]), __fadd2_rn(sum[2], sum[3]));
-  float total = f_add(t.x, t.y);
-  // a NaN or an infinity among the scores: the row is NaN; nothing above -inf so far: no sum
-  total = mb != mb || mb == INFINITY ? __int_as_float(0x7fffffff) : row.m == -INFINITY ? 0.0f : total;
-  row.l = f_fma(row.l, alpha, total);
-  return alpha;
+// A quarter of a row's scores from tensor memory; what follows cannot be moved in front of the wait.
+__device__ __forceinline__ void load_quarter(uint32_t taddr, uint32_t (&s)[QW]) {
+  pa_ld32(taddr, s);
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(s[0]), "+r"(s[1]), "+r"(s[2]), "+r"(s[3]), "+r"(s[4]), "+r"(s[5]), "+r"(s[6]), "+r"(s[7]), "+r"(s[8]), "+r"(s[9]), "+r"(s[10]), "+r"(s[11]),
+                 "+r"(s[12]), "+r"(s[13]), "+r"(s[14]), "+r"(s[15]), "+r"(s[16]), "+r"(s[17]), "+r"(s[18]), "+r"(s[19]), "+r"(s[20]), "+r"(s[21]), "+r"(s[22]),
+                 "+r"(s[23]), "+r"(s[24]), "+r"(s[25]), "+r"(s[26]), "+r"(s[27]), "+r"(s[28]), "+r"(s[29])
+               :: "memory");
+  asm volatile("" : "+r"(s[30]), "+r"(s[31]) :: "memory");
 }
 
-// ---------------------------------------------------------------- the kernel
-template <int HDP, int NT>
-struct Form {
-  static constexpr int DB = HDP / 64;                              // 64-column boxes of a head
-  static constexpr int ROWS = NT == 2 ? 128 : 32;                  // rows of a tile that hold queries
-  static constexpr int SOFT = NT == 2 ? 8 : 1;                     // softmax warps
-  static constexpr int THREADS = (SOFT + 3) * 32;
-  static constexpr uint32_t Q_BOX = ROWS * 128, Q_TILE = DB * Q_BOX, Q_BYTES = NT * Q_TILE;
-  static constexpr uint32_t KV_BOX = BLK * 128, SLOT = DB * KV_BOX;
-  // wide: one CTA an SM; narrow: two.  The narrow form's query tile is read as 128 rows, the last 96 of them being whatever the ring
-  // behind it holds: their scores stay in lanes that nobody reads.
-  static constexpr int SLOTS = NT == 2 ? (HDP == 128 ? 5 : 10) : (HDP == 128 ? 3 : 6);
-  static constexpr uint32_t COLS = NT == 2 ? 512 : 256;            // tensor memory: S_t (P_t over it) at 128 t, O_t at 128 (NT + t)
-  static constexpr size_t SMEM = 1024 + Q_BYTES + SLOTS * SLOT + 512;
+// The largest of a quarter's scores, NaN if one is; first .. last: the columns of the quarter that the row sees (MASKED).
+template <bool MASKED>
+__device__ __forceinline__ float quarter_max(const uint32_t (&s)[QW], int first, int last) {
+  float v[QW];
+#pragma unroll
+  for (int i = 0; i < QW; ++i) v[i] = MASKED && (i < first || i > last) ? -INFINITY : __uint_as_float(s[i]);
+  float a = v[0], b = v[1];
+#pragma unroll
+  for (int i = 2; i < QW; i += 4) { a = max3(a, v[i], v[i + 1]); if (i + 3 < QW) b = max3(b, v[i + 2], v[i + 3]); }
+  return max3(a, b, b);
+}
+
+// The block's maximum mb -> the running maximum; returns the factor that sums and O take (1 nearly always).
+__device__ __forceinline__ float move_max(float& m, float mb, float c) {
+  float alpha = 1.0f;
+  if (f_mul(f_add(mb, -m), c) > LAG) {                     // from -inf: any number; -inf and NaN: never
+    alpha = pa_ex2(f_mul(f_add(m, -mb), c));
+    m = mb;
+  }
+  return alpha;
+}
+__device__ __forceinline__ float shift_of(float m, float c) { return m == -INFINITY ? 0.0f : -f_mul(m, c); }
+
+// The exponentials of two scores.  Which of the two forms a key takes follows from its place alone: the hardware unit gives 16 results a
+// cycle and SM, and the last quarter of every block is taken off it.
+template <bool POLY>
+__device__ __forceinline__ float2 prob2(float2 s, float c, float shift0, float shift1) {
+  const float2 x = __ffma2_rn(s, make_float2(c, c), make_float2(shift0, shift1));
+  return POLY ? poly_ex2(x) : make_float2(pa_ex2(x.x), pa_ex2(x.y));
+}
+
+// Probabilities of a quarter, narrowed two to a word; returns their fp32 sum, in the order of a butterfly over the 32 keys (key with key + 16 first).
+template <int DT, bool MASKED, bool POLY>
+__device__ __forceinline__ float quarter_probs(const uint32_t (&s)[QW], uint32_t (&packed)[QW / 2], int first, int last, float c, float shift) {
+  float2 e[QW / 2];
+#pragma unroll
+  for (int i = 0; i < QW / 2; ++i) {
+    e[i] = prob2<POLY>(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c, shift, shift);
+    if (MASKED) {
+      e[i].x = (2 * i >= first && 2 * i <= last) ? e[i].x : 0.0f;
+      e[i].y = (2 * i + 1 >= first && 2 * i + 1 <= last) ? e[i].y : 0.0f;
+    }
+    packed[i] = pack_16x2(e[i].x, e[i].y, DT);
+  }
+#pragma unroll
+  for (int n = QW / 4; n >= 1; n >>= 1)
+#pragma unroll
+    for (int i = 0; i < n; ++i) e[i] = __fadd2_rn(e[i], e[i + n]);
+  return f_add(e[0].x, e[0].y);
+}
+// A quarter's running sum.  A NaN or an infinity among the block's scores makes the row NaN; nothing above -inf so far: no sum.
+__device__ __forceinline__ float add_quarter(float l, float alpha, float total, float m, float mb) {
+  total = mb != mb || mb == INFINITY ? __int_as_float(0x7fffffff) : m == -INFINITY ? 0.0f : total;
+  return f_fma(l, alpha, total);
+}
+__device__ __forceinline__ float join_quarters(float a, float b, float c, float d) { return f_add(f_add(a, b), f_add(c, d)); }
+
+// O = alpha O for one lane's columns
+template <int HDP>
+__device__ __forceinline__ void rescale(uint32_t t_o, float alpha) {
+#pragma unroll
+  for (int q = 0; q < HDP / QW; ++q) {
+    uint32_t o[QW];
+    load_quarter(t_o + 32u * q, o);
+#pragma unroll
+    for (int i = 0; i < QW; ++i) o[i] = __float_as_uint(f_mul(__uint_as_float(o[i]), alpha));
+    pa_st32(t_o + 32u * q, o);
+  }
+}
+
+// The fixer's work on a block of V in shared memory (n 16-byte words, 128-byte rows of 64 elements, box after box): elements that are not finite
+// become zero.  Whether one of them belongs to a key of lo .. hi.
+template <int DT>
+__device__ __forceinline__ bool fix_values(uint4* base, uint32_t n, int32_t key0, int32_t lo, int32_t hi) {
+  constexpr uint32_t EXP = DT == RG_BF16 ? 0x7f807f80u : 0x7c007c00u, ONE = DT == RG_BF16 ? 0x00800080u : 0x04000400u;      // exponent fields, and what makes a full one carry
+  bool seen = false;
+#pragma unroll 4
+  for (uint32_t i = threadIdx.x & 31; i < n; i += 32) {
+    uint4 w = base[i];
+    const uint32_t hit = (((w.x & EXP) + ONE) | ((w.y & EXP) + ONE) | ((w.z & EXP) + ONE) | ((w.w & EXP) + ONE)) & 0x80008000u;
+    if (hit) {
+      auto clean = [&](uint32_t x) { const uint32_t h = ((x & EXP) + ONE) & 0x80008000u; return x & ~((h >> 15) * 0xffffu); };
+      w.x = clean(w.x); w.y = clean(w.y); w.z = clean(w.z); w.w = clean(w.w);
+      base[i] = w;
+      const int32_t key = key0 + (int32_t)(i / 8 % BLK);
+      seen |= key >= lo && key <= hi;
+    }
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  return __any_sync(0xffffffffu, seen);
+}
+
+// A position in a ring of N barriers.
+template <int N>
+struct Ring {
+  uint32_t slot = 0, phase = 0;
+  __device__ __forceinline__ void step() { if (++slot == N) { slot = 0; phase ^= 1u; } }
 };
 
-template <int HDP, int NT, int DT>
-__global__ void __launch_bounds__(Form<HDP, NT>::THREADS, NT == 2 ? 1 : 2)
-paged_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+// ---------------------------------------------------------------- the kernel for many rows
+template <int HDP>
+struct Wide {
+  static constexpr int DB = HDP / 64;                              // 64-column boxes of a head
+  static constexpr int NT = 2, SOFT = 4 * NT;                      // tiles of 128 rows, softmax warps
+  static constexpr int PRODUCER = SOFT, MMA = SOFT + 1, FIXER = SOFT + 2, WARPS = SOFT + 3, THREADS = WARPS * 32;
+  static constexpr uint32_t Q_BOX = 128 * 128, Q_TILE = DB * Q_BOX;
+  static constexpr uint32_t KV_BOX = BLK * 128, SLOT = DB * KV_BOX;
+  static constexpr int SLOTS = HDP == 128 ? 5 : 10;
+  static constexpr uint32_t COLS = 512;                            // tensor memory: S_t, and P_t over it, at 128 t, O_t at 128 (2 + t)
+  static constexpr uint32_t KV_AT = NT * Q_TILE, ITEM_AT = KV_AT + SLOTS * SLOT, BAR_AT = ITEM_AT + ITEMS * sizeof(Item), N_BAR = 10 + 3 * SLOTS + 2 * ITEMS,
+                            FLAG_AT = BAR_AT + 8 * N_BAR, LAST = FLAG_AT + 4 * (2 + FLAGS);
+  static constexpr size_t SMEM = 1024 + LAST;
+  static_assert(SMEM <= 232448 && SLOTS / 2 + 1 < FLAGS, "fits the SM; the fixer cannot be a whole turn of flags ahead");
+};
+
+template <int HDP, int DT>
+__global__ void __launch_bounds__(Wide<HDP>::THREADS, 1)
+paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                        const __grid_constant__ Params p) {
-  using F = Form<HDP, NT>;
-  constexpr int DB = F::DB, SLOTS = F::SLOTS, WARPS_T = F::SOFT / NT;
-  constexpr uint32_t IDESC_S = pa_idesc(BLK, DT == RG_BF16, false), IDESC_O = pa_idesc(HDP, DT == RG_BF16, true);
+  using F = Wide<HDP>;
+  constexpr int DB = F::DB, SLOTS = F::SLOTS, NT = F::NT;
+  constexpr uint32_t IDESC_S = pa_idesc(BLK, DT == RG_BF16, false, false), IDESC_O = pa_idesc(HDP, DT == RG_BF16, false, true);
 
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
-  const uint32_t sQ = smem_base, sKV = sQ + F::Q_BYTES;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem_gen + F::Q_BYTES + SLOTS * F::SLOT);
-  const uint32_t bar0 = smem_u32(bars);
-  const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_s = bar0 + 16, b_p = bar0 + 32, b_o_full = bar0 + 48, b_o_empty = bar0 + 64;   // two each from b_s on
-  const uint32_t b_full = bar0 + 80, b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 10 + 3 * SLOTS);
+  const uint32_t sQ = smem_base, sKV = smem_base + F::KV_AT;
+  Item* items = reinterpret_cast<Item*>(smem_gen + F::ITEM_AT);
+  const uint32_t bar0 = smem_base + F::BAR_AT;
+  const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_s = bar0 + 16, b_p = bar0 + 32, b_o_full = bar0 + 48, b_o_empty = bar0 + 64, b_full = bar0 + 80;   // two each from b_s to b_o_empty
+  const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + F::FLAG_AT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* not_finite = reinterpret_cast<volatile int*>(tmem_slot + 2);          // [FLAGS]
-  static_assert((10 + 3 * SLOTS) * 8 + 4 * (2 + FLAGS) <= 512, "barriers and flags fit behind the ring");
-  static_assert(SLOTS / 2 + 1 < FLAGS, "the fixer cannot be a whole turn of flags ahead");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     mbar_init(b_q_full, 1); mbar_init(b_q_empty, 1);
-    for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 8 * t, WARPS_T); mbar_init(b_o_full + 8 * t, 1); mbar_init(b_o_empty + 8 * t, WARPS_T); }
+    for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 8 * t, 4); mbar_init(b_o_full + 8 * t, 1); mbar_init(b_o_empty + 8 * t, 4); }
     for (int s = 0; s < SLOTS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_ready + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
+    for (int s = 0; s < ITEMS; ++s) { mbar_init(b_item + 8 * s, 1); mbar_init(b_free + 8 * s, F::WARPS - 1); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == F::SOFT + 1) {
+  if (warp == F::MMA) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(F::COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -368,30 +433,44 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_
   pa_fence_after();
   const uint32_t tmem = *tmem_slot;
   const int cta_tokens = NT * p.tile_tokens;
-  Walk walk;
-  Item it;
-  walk.start(p, cta_tokens);
 
-  if (warp == F::SOFT) {
+  // Next item, for the warps that get it from the producer; false: none left, or a wait gave up.
+  Ring<ITEMS> ir;
+  auto next_item = [&](Item& it, bool& alive) -> bool {
+    if (!warp_mbar_wait(b_item + 8 * ir.slot, ir.phase, abort_flag, &g_paged_attn_status_word, 0x2000u)) { alive = false; return false; }
+    it = items[ir.slot];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(b_free + 8 * ir.slot);
+    ir.step();
+    return it.n_tok > 0;
+  };
+  Item it;
+  bool alive = true;
+
+  if (warp == F::PRODUCER) {
     // ------------------------------------------------------------ producer
     const int pieces = BLK / p.box;                                // TMA boxes along the keys of a block
     const int piece = lane % pieces, col = lane / pieces;          // col < DB: this lane issues a box
-    uint32_t ring = 0, items = 0;
-    bool alive = true;
-    while (alive && walk.get(p, cta_tokens, it)) {
+    Ring<SLOTS> kv;
+    uint32_t q_phase = 1;
+    Walk walk;
+    walk.start(p, cta_tokens);
+    while (alive) {
+      const bool more = walk.get(p, cta_tokens, it);
+      if (!more) it.n_tok = 0;
+      alive = warp_mbar_wait(b_free + 8 * ir.slot, ir.phase ^ 1u, abort_flag, &g_paged_attn_status_word, 0x2080u);
+      if (!alive) break;
+      if (lane == 0) { items[ir.slot] = it; mbar_arrive(b_item + 8 * ir.slot); }
+      ir.step();
+      if (!more) break;
       if (it.b1 == it.b0) continue;
       const int32_t* row = p.table + (int64_t)it.seq * p.table_ld;
-      auto page_of = [&](int b) -> int32_t {                       // page of this lane's keys, out of the cache's range where there is none
-        const int32_t k = b * BLK + piece * p.box;
-        if (k > it.hi || k + p.box <= it.lo) return -1;
-        const int32_t id = row[k / p.page_size];
-        if (id >= 0 && id < p.pages) return id;
-        if (col == 0) atomicCAS(&g_paged_attn_status_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
-        return p.pages;                                            // behind the last page: the copy fills in zeros
-      };
-      int32_t page = page_of(it.b0);
-      alive = warp_mbar_wait(b_q_empty, (items & 1) ^ 1u, abort_flag, &g_paged_attn_status_word, 0x2100u);
+      auto wanted = [&](int b) -> bool { const int32_t k = b * BLK + piece * p.box; return col < DB && k <= it.hi && k + p.box > it.lo; };
+      auto entry = [&](int b) -> int32_t { return row[(b * BLK + piece * p.box) / p.page_size]; };
+      int32_t ahead = wanted(it.b0) ? entry(it.b0) : 0;
+      alive = warp_mbar_wait(b_q_empty, q_phase, abort_flag, &g_paged_attn_status_word, 0x2100u);
       if (!alive) break;
+      q_phase ^= 1u;
       const int tiles = NT == 2 && it.n_tok > p.tile_tokens ? 2 : 1;
       if (lane == 0) mbar_expect_tx(b_q_full, (uint32_t)(tiles * DB * p.tile_tokens * p.group) * 128u);
       __syncwarp();
@@ -399,36 +478,41 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_
         const int t = lane / DB, b = lane % DB;
         pa_tma_4d(sQ + t * F::Q_TILE + b * F::Q_BOX, &tmap_q, b * 64, 0, it.tok + t * p.tile_tokens, it.head, b_q_full);
       }
-      ++items;
       for (int b = it.b0; b < it.b1 && alive; ++b) {
-        const int32_t ahead = b + 1 < it.b1 ? page_of(b + 1) : -1;
-        const bool mine = col < DB && page >= 0;
+        const bool mine = wanted(b);
+        int32_t page = ahead;
+        if (b + 1 < it.b1 && wanted(b + 1)) ahead = entry(b + 1);  // looked up a block ahead of its use
+        if (mine && (page < 0 || page >= p.pages)) {               // not a page: the copy from behind the last one fills in zeros
+          if (col == 0) atomicCAS(&g_paged_attn_status_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
+          page = p.pages;
+        }
         const int32_t at = (b * BLK + piece * p.box) % p.page_size;
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)p.box * 128u;
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const uint32_t slot = ring % SLOTS, turn = ring / SLOTS;
-          alive = warp_mbar_wait(b_empty + 8 * slot, (turn & 1) ^ 1u, abort_flag, &g_paged_attn_status_word, 0x2200u | slot);
+        for (int which = 0; which < 2; ++which) {
+          alive = warp_mbar_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, &g_paged_attn_status_word, 0x2200u | kv.slot);
           if (!alive) break;
-          if (lane == 0) mbar_expect_tx(b_full + 8 * slot, bytes);
+          if (lane == 0) mbar_expect_tx(b_full + 8 * kv.slot, bytes);
           __syncwarp();
-          if (mine) pa_tma_4d(sKV + slot * F::SLOT + col * F::KV_BOX + piece * p.box * 128, kv ? &tmap_v : &tmap_k, col * 64, at, it.head, page, b_full + 8 * slot);
-          ++ring;
+          if (mine) pa_tma_4d(sKV + kv.slot * F::SLOT + col * F::KV_BOX + piece * p.box * 128, which ? &tmap_v : &tmap_k, col * 64, at, it.head, page, b_full + 8 * kv.slot);
+          kv.step();
         }
-        page = ahead;
       }
     }
-  } else if (warp == F::SOFT + 1) {
+  } else if (warp == F::MMA) {
     // ------------------------------------------------------------ MMA issuer: the warp walks converged, an elected lane issues
     const bool leader = elect_one();
-    uint32_t ring = 0, items = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};
-    bool alive = true;
-    auto slot_ready = [&](uint32_t r) -> uint32_t {                // waits for ring position r, returns its address
-      const uint32_t slot = r % SLOTS, par = (r / SLOTS) & 1;
-      if (alive) alive = warp_mbar_wait(b_ready + 8 * slot, par, abort_flag, &g_paged_attn_status_word, 0x2300u | slot);
-      if (alive) alive = warp_mbar_wait(b_full + 8 * slot, par, abort_flag, &g_paged_attn_status_word, 0x2380u | slot);
+    Ring<SLOTS> kv;
+    uint32_t q_phase = 0, p_phase[2] = {0, 0}, o_phase[2] = {1, 1};
+    // Waits for the next slot; its address comes out warp-uniform, so that the descriptors stay in uniform registers.
+    auto next_slot = [&](uint32_t& bar) -> uint32_t {
+      const uint32_t slot = __shfl_sync(0xffffffffu, kv.slot, 0);
+      alive = warp_mbar_wait(b_ready + 8 * slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x2300u | slot);
+      if (alive) alive = warp_mbar_wait(b_full + 8 * slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x2380u | slot);
       pa_fence_after();
-      return sKV + slot * F::SLOT;
+      bar = b_empty + 8 * slot;
+      kv.step();
+      return __shfl_sync(0xffffffffu, sKV + slot * F::SLOT, 0);
     };
     auto scores = [&](int t, uint32_t sK) {
 #pragma unroll
@@ -439,25 +523,27 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_
       }
       if (leader) pa_commit(b_s + 8 * t);
     };
-    while (alive && walk.get(p, cta_tokens, it)) {
-      if (it.b1 == it.b0) continue;
-      const int tiles = NT == 2 && it.n_tok > p.tile_tokens ? 2 : 1, nb = it.b1 - it.b0;
-      alive = warp_mbar_wait(b_q_full, items & 1, abort_flag, &g_paged_attn_status_word, 0x2400u);
-      ++items;
+    while (alive && next_item(it, alive)) {
+      const int nb = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
+      if (nb == 0) continue;
+      const int tiles = NT == 2 && __shfl_sync(0xffffffffu, it.n_tok, 0) > p.tile_tokens ? 2 : 1;
+      alive = warp_mbar_wait(b_q_full, q_phase, abort_flag, &g_paged_attn_status_word, 0x2400u);
+      q_phase ^= 1u;
       if (!alive) break;
-      uint32_t sK = slot_ready(ring);
+      uint32_t k_bar, v_bar, sK = next_slot(k_bar);
       if (!alive) break;
       for (int t = 0; t < tiles; ++t) scores(t, sK);
-      if (leader) { pa_commit(b_empty + 8 * (ring % SLOTS)); if (nb == 1) pa_commit(b_q_empty); }
+      if (leader) { pa_commit(k_bar); if (nb == 1) pa_commit(b_q_empty); }
       for (int j = 0; j < nb && alive; ++j) {
-        const uint32_t rv = ring + 1 + 2 * j, rk = ring + 2 + 2 * j;
         const bool more = j + 1 < nb;
-        const uint32_t sV = slot_ready(rv);
+        const uint32_t sV = next_slot(v_bar);
         if (!alive) break;
-        for (int t = 0; t < tiles; ++t) {
-          alive = warp_mbar_wait(b_p + 8 * t, n_p[t] & 1, abort_flag, &g_paged_attn_status_word, 0x2500u | t);
-          ++n_p[t];
-          if (alive && j == 0) { alive = warp_mbar_wait(b_o_empty + 8 * t, (n_o[t] & 1) ^ 1u, abort_flag, &g_paged_attn_status_word, 0x2580u | t); ++n_o[t]; }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (t >= tiles) break;
+          alive = warp_mbar_wait(b_p + 8 * t, p_phase[t], abort_flag, &g_paged_attn_status_word, 0x2500u | t);
+          p_phase[t] ^= 1u;
+          if (alive && j == 0) { alive = warp_mbar_wait(b_o_empty + 8 * t, o_phase[t], abort_flag, &g_paged_attn_status_word, 0x2580u | t); o_phase[t] ^= 1u; }
           if (!alive) break;
           pa_fence_after();
           const uint64_t v = pa_desc(sV, F::KV_BOX);
@@ -466,130 +552,115 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_
             if (leader) pa_mma_ts(tmem + 128u * (NT + t), tmem + 128u * t + 8u * e, v + (uint64_t)(e * (2048 >> 4)), IDESC_O, (j | e) ? 1u : 0u);
           if (!more && leader) pa_commit(b_o_full + 8 * t);
           if (more) {
-            if (t == 0) sK = slot_ready(rk);
+            if (t == 0) sK = next_slot(k_bar);
             if (!alive) break;
             scores(t, sK);
           }
         }
         if (!alive) break;
         if (leader) {
-          pa_commit(b_empty + 8 * (rv % SLOTS));
-          if (more) pa_commit(b_empty + 8 * (rk % SLOTS));
+          pa_commit(v_bar);
+          if (more) pa_commit(k_bar);
           if (j + 2 == nb) pa_commit(b_q_empty);
         }
       }
-      ring += 2 * nb;
     }
-  } else if (warp == F::SOFT + 2) {
+  } else if (warp == F::FIXER) {
     // ------------------------------------------------------------ fixer
-    uint32_t ring = 0, flags = 0;
-    bool alive = true;
-    while (alive && walk.get(p, cta_tokens, it)) {
+    Ring<SLOTS> kv;
+    uint32_t flags = 0;
+    while (alive && next_item(it, alive)) {
       bool any_masked = false;
       for (int b = it.b0; b < it.b1 && alive; ++b) {
         const bool masked = masked_block(p, it, b);
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const uint32_t slot = ring % SLOTS, turn = ring / SLOTS;
-          alive = warp_mbar_wait(b_full + 8 * slot, turn & 1, abort_flag, &g_paged_attn_status_word, 0x2600u | slot);
+        for (int which = 0; which < 2; ++which) {
+          alive = warp_mbar_wait(b_full + 8 * kv.slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x2600u | kv.slot);
           if (!alive) break;
-          if (kv == 1 && masked) {
-            constexpr uint32_t EXP = DT == RG_BF16 ? 0x7f807f80u : 0x7c007c00u, ONE = DT == RG_BF16 ? 0x00800080u : 0x04000400u;
-            uint4* base = reinterpret_cast<uint4*>(smem_gen + F::Q_BYTES + slot * F::SLOT);
-            bool seen = false;
-#pragma unroll 4
-            for (uint32_t i = lane; i < F::SLOT / 16; i += 32) {
-              uint4 w = base[i];
-              const uint32_t hit = (((w.x & EXP) + ONE) | ((w.y & EXP) + ONE) | ((w.z & EXP) + ONE) | ((w.w & EXP) + ONE)) & 0x80008000u;
-              if (hit) {
-                auto clean = [&](uint32_t x) { const uint32_t h = ((x & EXP) + ONE) & 0x80008000u; return x & ~((h >> 15) * 0xffffu); };
-                w.x = clean(w.x); w.y = clean(w.y); w.z = clean(w.z); w.w = clean(w.w);
-                base[i] = w;
-                const int32_t key = b * BLK + (int32_t)(((i * 16) % F::KV_BOX) / 128);
-                seen |= key >= it.lo && key <= it.hi;
-              }
-            }
-            seen = __any_sync(0xffffffffu, seen);
+          if (which == 1 && masked) {
+            const bool seen = fix_values<DT>(reinterpret_cast<uint4*>(smem_gen + F::KV_AT + kv.slot * F::SLOT), F::SLOT / 16, b * BLK, it.lo, it.hi);
             if (lane == 0) not_finite[flags % FLAGS] = any_masked ? (not_finite[flags % FLAGS] | (seen ? 1 : 0)) : (seen ? 1 : 0);
             any_masked = true;
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(b_ready + 8 * slot);
-          ++ring;
+          if (lane == 0) mbar_arrive(b_ready + 8 * kv.slot);
+          kv.step();
         }
       }
       if (any_masked) ++flags;
     }
   } else {
     // ------------------------------------------------------------ softmax and output rows
-    const int t = NT == 2 ? warp >> 2 : 0;                         // tile
+    const int t = warp >> 2;                                       // tile
     const int r = (warp & 3) * 32 + lane;                          // row of the tile, and its lane in tensor memory
-    const uint32_t t_s = tmem + 128u * t + (static_cast<uint32_t>((warp & 3) * 32) << 16), t_o = t_s + 128u * NT;
+    const uint32_t t_s = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128u * t, t_o = t_s + 128u * NT;
     const int my_tok = r / p.group, my_head = r - my_tok * p.group;
-    uint32_t n_s = 0, n_o = 0, flags = 0;
-    bool alive = true;
-    while (alive && walk.get(p, cta_tokens, it)) {
+    uint32_t s_phase = 0, o_phase = 0, flags = 0;
+    while (alive && next_item(it, alive)) {
       const int tok = t * p.tile_tokens + my_tok;                  // within the item
       const bool live = my_tok < p.tile_tokens && tok < it.n_tok;
       const bool warp_live = __any_sync(0xffffffffu, live);
       const bool tile_live = t * p.tile_tokens < it.n_tok;
       const int32_t place = it.pos + tok;
       const int32_t hi = live ? min(last_seen(p, place, it.len), it.hi) : -1, lo = max(first_seen(p, place), it.lo);
-      Row row = {-INFINITY, 0.0f};
-      bool any_masked = false;
+      float m = -INFINITY, l[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      bool any_masked = masked_block(p, it, it.b0) && it.b1 > it.b0;
+      if (it.b1 > it.b0 + 1) any_masked |= masked_block(p, it, it.b1 - 1);      // what is masked lies at the ends
       if (tile_live) {
         for (int b = it.b0; b < it.b1; ++b) {
           const bool masked = masked_block(p, it, b);
-          any_masked |= masked;
-          alive = warp_mbar_wait(b_s + 8 * t, n_s & 1, abort_flag, &g_paged_attn_status_word, 0x2700u | t);
-          ++n_s;
+          alive = warp_mbar_wait(b_s + 8 * t, s_phase, abort_flag, &g_paged_attn_status_word, 0x2700u | t);
           if (!alive) break;
+          const int first = lo - b * BLK, last = hi - b * BLK;     // columns of the block that the row sees
+          pa_fence_after();
           if (warp_live) {
-            pa_fence_after();
-            uint32_t s[BLK], packed[BLK / 2];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) pa_ld32(t_s + 32u * q, s + 32 * q);
-            pa_wait_ld();
-            float alpha;
+            uint32_t s[QW], packed[QW / 2];
+            float mq[4];
             if (masked) {
-              alpha = softmax_block<DT, true>(s, packed, lo - b * BLK, hi - b * BLK, p.c, row);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) { load_quarter(t_s + 32u * q, s); mq[q] = quarter_max<true>(s, first - 32 * q, last - 32 * q); }
             } else {
-              alpha = softmax_block<DT, false>(s, packed, 0, BLK - 1, p.c, row);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) { load_quarter(t_s + 32u * q, s); mq[q] = quarter_max<false>(s, 0, 0); }
             }
-            __syncwarp();
-            pa_st32(t_s, packed);
-            pa_st32(t_s + 32u, packed + 32);
-            // the scores of this block are complete, so the product of the block before is too: O may be rescaled
-            if (b > it.b0 && __any_sync(0xffffffffu, live && alpha != 1.0f)) {
+            const float mb = max3(max3(mq[0], mq[1], mq[2]), mq[3], mq[3]);
+            const float alpha = move_max(m, mb, p.c), shift = shift_of(m, p.c);
+            // probabilities go over scores that have been read: quarter q's words end at column 16 (q + 1)
+            if (masked) {
 #pragma unroll
-              for (int q = 0; q < HDP / 32; ++q) {
-                uint32_t o[32];
-                pa_ld32(t_o + 32u * q, o);
-                pa_wait_ld();
+              for (int q = 0; q < 4; ++q) {
+                load_quarter(t_s + 32u * q, s);
+                l[q] = add_quarter(l[q], alpha, q == 3 ? quarter_probs<DT, true, true>(s, packed, first - 96, last - 96, p.c, shift) : quarter_probs<DT, true, false>(s, packed, first - 32 * q, last - 32 * q, p.c, shift), m, mb);
+                pa_st16(t_s + 16u * q, packed);
+              }
+            } else {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(f_mul(__uint_as_float(o[i]), alpha));
-                pa_st32(t_o + 32u * q, o);
+              for (int q = 0; q < 4; ++q) {
+                load_quarter(t_s + 32u * q, s);
+                l[q] = add_quarter(l[q], alpha, q == 3 ? quarter_probs<DT, false, true>(s, packed, 0, 0, p.c, shift) : quarter_probs<DT, false, false>(s, packed, 0, 0, p.c, shift), m, mb);
+                pa_st16(t_s + 16u * q, packed);
               }
             }
+            // the scores of this block are complete, so the product of the block before is too: O may be rescaled
+            if (b > it.b0 && __any_sync(0xffffffffu, live && alpha != 1.0f)) rescale<HDP>(t_o, alpha);
             pa_wait_st();
             pa_fence_before();
           }
+          s_phase ^= 1u;
           __syncwarp();
           if (lane == 0) mbar_arrive(b_p + 8 * t);
         }
         if (!alive) break;
       }
       const int slot_flag = flags % FLAGS;
-      bool add_back = false;
-      if (NT == 2 && !tile_live) {                                 // keep count of the flags all the same
-        for (int b = it.b0; b < it.b1; ++b) any_masked |= masked_block(p, it, b);
-      }
       if (any_masked) ++flags;
       if (!tile_live) continue;
-      if (it.b1 > it.b0) {
-        alive = warp_mbar_wait(b_o_full + 8 * t, n_o & 1, abort_flag, &g_paged_attn_status_word, 0x2780u | t);
-        ++n_o;
+      const bool blocks = it.b1 > it.b0;
+      const float sum = join_quarters(l[0], l[1], l[2], l[3]);
+      bool add_back = false;
+      if (blocks) {
+        alive = warp_mbar_wait(b_o_full + 8 * t, o_phase, abort_flag, &g_paged_attn_status_word, 0x2780u | t);
+        o_phase ^= 1u;
         if (!alive) break;
         pa_fence_after();
         add_back = any_masked && not_finite[slot_flag] != 0;
@@ -598,18 +669,18 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_
         const int64_t token = (int64_t)it.tok + tok;
         const int head = it.head * p.group + my_head;
         const int64_t grow = token * p.hq + head;
-        const bool none = !(row.l > 0.0f) && row.l == row.l;       // no key seen
-        const float inv = it.multi ? 1.0f : none ? 0.0f : __frcp_rn(row.l);
+        const bool none = !(sum > 0.0f) && sum == sum;             // no key seen
+        const float inv = it.multi ? 1.0f : none ? 0.0f : __frcp_rn(sum);
         float* part = it.multi ? p.part_o + (grow * p.segments + it.seg) * p.d : nullptr;
 #pragma unroll 1
-        for (int q = 0; q < HDP / 32; ++q) {
+        for (int q = 0; q < HDP / QW; ++q) {
           if (32 * q >= p.d) break;
-          uint32_t raw[32];
+          uint32_t raw[QW];
           __syncwarp();
-          if (it.b1 > it.b0) { pa_ld32(t_o + 32u * q, raw); pa_wait_ld(); }
-          float o[32];
+          if (blocks) load_quarter(t_o + 32u * q, raw);
+          float o[QW];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = none || it.b1 == it.b0 ? 0.0f : f_mul(__uint_as_float(raw[i]), inv);
+          for (int i = 0; i < QW; ++i) o[i] = none || !blocks ? 0.0f : f_mul(__uint_as_float(raw[i]), inv);
           if (add_back && live) {
             // the elements of V that the fixer took out and this row sees
             for (int b = it.b0; b < it.b1; ++b) {
@@ -619,7 +690,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_
                 if (id < 0 || id >= p.pages) continue;
                 const uint16_t* v = p.v + id * p.v_page + (k % p.page_size) * p.v_slot + it.head * p.v_head;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
+                for (int i = 0; i < QW; ++i) {
                   if (32 * q + i >= p.d) break;
                   const float x = DT == RG_BF16 ? bf16_bits_to_f32(v[32 * q + i]) : f16_bits_to_f32(v[32 * q + i]);
                   if (!(f_add(x, -x) == 0.0f)) o[i] = f_add(o[i], x);
@@ -627,41 +698,41 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_
               }
             }
           }
-          const int n = live ? min(32, p.d - 32 * q) : 0;
+          const int n = live ? min(QW, p.d - 32 * q) : 0;
           if (n == 0) {
           } else if (it.multi) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4)
+            for (int i = 0; i < QW; i += 4)
               if (i < n) *reinterpret_cast<float4*>(part + 32 * q + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
           } else if (p.o_dtype == RG_F32) {
             float* dst = static_cast<float*>(p.out) + token * p.o_tok + head * p.o_head + 32 * q;
             if (p.o_vec) {
 #pragma unroll
-              for (int i = 0; i < 32; i += 4) if (i < n) *reinterpret_cast<float4*>(dst + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+              for (int i = 0; i < QW; i += 4) if (i < n) *reinterpret_cast<float4*>(dst + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
             } else {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) if (i < n) dst[i] = o[i];
+              for (int i = 0; i < QW; ++i) if (i < n) dst[i] = o[i];
             }
           } else {
             uint16_t* dst = static_cast<uint16_t*>(p.out) + token * p.o_tok + head * p.o_head + 32 * q;
-            uint32_t w[16];
+            uint32_t w[QW / 2];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = pack_16x2(o[2 * i], o[2 * i + 1], DT);
+            for (int i = 0; i < QW / 2; ++i) w[i] = pack_16x2(o[2 * i], o[2 * i + 1], DT);
             if (p.o_vec) {
 #pragma unroll
-              for (int i = 0; i < 16; i += 4) if (2 * i < n) *reinterpret_cast<uint4*>(dst + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+              for (int i = 0; i < QW / 2; i += 4) if (2 * i < n) *reinterpret_cast<uint4*>(dst + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
             } else {
 #pragma unroll
-              for (int i = 0; i < 16; ++i) if (2 * i < n) { dst[2 * i] = (uint16_t)(w[i] & 0xffffu); dst[2 * i + 1] = (uint16_t)(w[i] >> 16); }
+              for (int i = 0; i < QW / 2; ++i) if (2 * i < n) { dst[2 * i] = (uint16_t)(w[i] & 0xffffu); dst[2 * i + 1] = (uint16_t)(w[i] >> 16); }
             }
           }
         }
         if (live) {
-          if (it.multi) p.part_ml[grow * p.segments + it.seg] = make_float2(row.m, row.l);
-          else if (p.lse) p.lse[token * p.lse_ld + head] = none ? -INFINITY : f_add(f_mul(row.m, p.scale), logf(row.l));
+          if (it.multi) p.part_ml[grow * p.segments + it.seg] = make_float2(m, sum);
+          else if (p.lse) p.lse[token * p.lse_ld + head] = none ? -INFINITY : f_add(f_mul(m, p.scale), logf(sum));
         }
       }
-      if (it.b1 > it.b0) {
+      if (blocks) {
         pa_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(b_o_empty + 8 * t);
@@ -676,7 +747,431 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_
     while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
     __syncthreads();
   }
-  if (warp == F::SOFT + 1) {
+  if (warp == F::MMA) {
+    pa_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(F::COLS) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------- the form for few rows
+// Single tokens and drafts: up to ROWS rows of a key head.  The operands change places: a block's keys are the 128 rows of the first product and
+// the head's elements the 128 rows of the second, the queries the narrow side (N = 16 or 32) of both, so that the tensor core reads every K and
+// V element from shared memory once and little else:
+//   S' = K_j Q^T       lane = key, column = row of queries
+//   O' += V_j^T P^T    lane = element of the head, column = row of queries; V is read transposed, P from shared memory
+// A softmax thread is one key of the block and holds its score with every row; maxima and sums over the keys go through butterflies
+// in which lanes trade rows (after five steps a lane holds one row's value), and the four warps' maxima through shared memory.
+template <int HDP, int ROWS>
+struct Few {
+  static constexpr int DB = HDP / 64;
+  static constexpr int PRODUCER = 4, MMA = 5, FIXER = 6, WARPS = 7, THREADS = WARPS * 32;
+  static constexpr int N = ROWS < 16 ? 16 : ROWS;                  // narrow side of the products
+  static constexpr uint32_t Q_BOX = N * 128, P_BOX = N * 128, P_BUF = 2 * P_BOX;      // rows of 64 elements, 64 keys
+  static constexpr uint32_t KV_BOX = BLK * 128, SLOT = DB * KV_BOX;
+  static constexpr int SLOTS = HDP == 128 ? 3 : 5;
+  static constexpr uint32_t COLS = 128;                            // tensor memory: S' of even and odd blocks at 0 and 32, O' of even and odd items at 64 and 96
+  static constexpr uint32_t Q_AT = SLOTS * SLOT, P_AT = Q_AT + DB * Q_BOX, ITEM_AT = P_AT + 2 * P_BUF, BAR_AT = ITEM_AT + ITEMS * sizeof(Item),
+                            N_BAR = 12 + 3 * SLOTS + 2 * ITEMS, FLAG_AT = BAR_AT + 8 * N_BAR, MAX_AT = (FLAG_AT + 4 * (2 + FLAGS) + 15) & ~15u, SUM_AT = MAX_AT + 2 * 128 * 4,
+                            LAST = SUM_AT + 2 * 128 * 4;
+  static constexpr size_t SMEM = 1024 + LAST;
+  static_assert(SMEM <= 115712 && SLOTS / 2 + 1 < FLAGS, "two CTAs fit the SM; the fixer cannot be a whole turn of flags ahead");
+};
+
+template <int N>
+__device__ __forceinline__ void pa_ld_cols(uint32_t taddr, uint32_t (&r)[N]);
+template <>
+__device__ __forceinline__ void pa_ld_cols<8>(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+}
+template <>
+__device__ __forceinline__ void pa_ld_cols<16>(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                 "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+template <>
+__device__ __forceinline__ void pa_ld_cols<32>(uint32_t taddr, uint32_t (&r)[32]) { load_quarter(taddr, r); }
+template <int N>
+__device__ __forceinline__ void pa_st_cols(uint32_t taddr, const uint32_t (&r)[N]) {
+  if constexpr (N == 32) pa_st32(taddr, r);
+  else if constexpr (N == 16) pa_st16(taddr, r);
+  else
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr) : "memory");
+}
+
+// Butterfly over the warp's lanes for ROWS values a lane, lanes trading halves of what they still hold: lane i ends with the whole value of
+// row i >> (5 - log2 ROWS).  Every level combines lane i's value with lane i ^ x's, x = 16, 8, 4, 2, 1.
+template <int ROWS, bool MAX>
+__device__ __forceinline__ float reduce_rows(float (&v)[ROWS]) {
+  const int lane = threadIdx.x & 31;
+  int n = ROWS;
+#pragma unroll
+  for (int x = 16; x; x >>= 1) {
+    if (n > 1) {
+      n >>= 1;
+      const bool upper = lane & x;
+#pragma unroll
+      for (int i = 0; i < ROWS / 2; ++i) {
+        if (i >= n) break;
+        const float keep = upper ? v[i + n] : v[i], send = upper ? v[i] : v[i + n];
+        const float got = __shfl_xor_sync(0xffffffffu, send, x);
+        v[i] = MAX ? max3(keep, got, got) : f_add(keep, got);
+      }
+    } else {
+      const float got = __shfl_xor_sync(0xffffffffu, v[0], x);
+      v[0] = MAX ? max3(v[0], got, got) : f_add(v[0], got);
+    }
+  }
+  return v[0];
+}
+
+template <int HDP, int ROWS, int DT>
+__global__ void __launch_bounds__(Few<HDP, ROWS>::THREADS, 2)
+paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                           const __grid_constant__ Params p) {
+  using F = Few<HDP, ROWS>;
+  constexpr int DB = F::DB, SLOTS = F::SLOTS;
+  constexpr uint32_t IDESC_S = pa_idesc(F::N, DT == RG_BF16, false, false), IDESC_O = pa_idesc(F::N, DT == RG_BF16, true, false);
+
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
+  const uint32_t sKV = smem_base, sQ = smem_base + F::Q_AT, sP = smem_base + F::P_AT;
+  Item* items = reinterpret_cast<Item*>(smem_gen + F::ITEM_AT);
+  const uint32_t bar0 = smem_base + F::BAR_AT;
+  const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_x = bar0 + 16, b_y = bar0 + 24, b_s = bar0 + 32, b_p = bar0 + 48, b_pv = bar0 + 64, b_o_empty = bar0 + 80, b_full = bar0 + 96;   // two each from b_s to b_o_empty
+  const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + F::FLAG_AT);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* not_finite = reinterpret_cast<volatile int*>(tmem_slot + 2);          // [FLAGS]
+  float* xm = reinterpret_cast<float*>(smem_gen + F::MAX_AT);                          // [2][4][32]: the warps' maxima of a block, by its parity
+  float* xl = reinterpret_cast<float*>(smem_gen + F::SUM_AT);                          // [2][4][32]: their sums, by the item's parity
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(b_q_full, 1); mbar_init(b_q_empty, 1); mbar_init(b_x, 4); mbar_init(b_y, 4);
+    for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 8 * t, 4); mbar_init(b_pv + 8 * t, 1); mbar_init(b_o_empty + 8 * t, 4); }
+    for (int s = 0; s < SLOTS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_ready + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
+    for (int s = 0; s < ITEMS; ++s) { mbar_init(b_item + 8 * s, 1); mbar_init(b_free + 8 * s, F::WARPS - 1); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == F::MMA) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(F::COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pa_fence_before();
+  __syncthreads();
+  pa_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  Ring<ITEMS> ir;
+  auto next_item = [&](Item& it, bool& alive) -> bool {
+    if (!warp_mbar_wait(b_item + 8 * ir.slot, ir.phase, abort_flag, &g_paged_attn_status_word, 0x3000u)) { alive = false; return false; }
+    it = items[ir.slot];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(b_free + 8 * ir.slot);
+    ir.step();
+    return it.n_tok > 0;
+  };
+  Item it;
+  bool alive = true;
+
+  if (warp == F::PRODUCER) {
+    // ------------------------------------------------------------ producer: K_0, K_1, V_0, K_2, V_1, ..., as they are used
+    const int pieces = BLK / p.box;
+    const int piece = lane % pieces, col = lane / pieces;
+    Ring<SLOTS> kv;
+    uint32_t q_phase = 1;
+    Walk walk;
+    walk.start(p, p.tile_tokens);
+    while (alive) {
+      const bool more = walk.get(p, p.tile_tokens, it);
+      if (!more) it.n_tok = 0;
+      alive = warp_mbar_wait(b_free + 8 * ir.slot, ir.phase ^ 1u, abort_flag, &g_paged_attn_status_word, 0x3080u);
+      if (!alive) break;
+      if (lane == 0) { items[ir.slot] = it; mbar_arrive(b_item + 8 * ir.slot); }
+      ir.step();
+      if (!more) break;
+      if (it.b1 == it.b0) continue;
+      const int32_t* row = p.table + (int64_t)it.seq * p.table_ld;
+      auto wanted = [&](int b) -> bool { const int32_t k = b * BLK + piece * p.box; return col < DB && b < it.b1 && k <= it.hi && k + p.box > it.lo; };
+      auto entry = [&](int b) -> int32_t { return row[(b * BLK + piece * p.box) / p.page_size]; };
+      int32_t page = wanted(it.b0) ? entry(it.b0) : 0, next = wanted(it.b0 + 1) ? entry(it.b0 + 1) : 0;      // looked up a block ahead of their use
+      alive = warp_mbar_wait(b_q_empty, q_phase, abort_flag, &g_paged_attn_status_word, 0x3100u);
+      if (!alive) break;
+      q_phase ^= 1u;
+      if (lane == 0) mbar_expect_tx(b_q_full, (uint32_t)(DB * p.tile_tokens * p.group) * 128u);
+      __syncwarp();
+      if (lane < DB) pa_tma_4d(sQ + lane * F::Q_BOX, &tmap_q, lane * 64, 0, it.tok, it.head, b_q_full);
+      auto copy = [&](const CUtensorMap* map, int b, int32_t& id) {
+        const bool mine = wanted(b);
+        if (mine && (id < 0 || id >= p.pages)) {                   // not a page: the copy from behind the last one fills in zeros
+          if (col == 0) atomicCAS(&g_paged_attn_status_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
+          id = p.pages;
+        }
+        const int32_t at = (b * BLK + piece * p.box) % p.page_size;
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)p.box * 128u;
+        alive = warp_mbar_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, &g_paged_attn_status_word, 0x3200u | kv.slot);
+        if (!alive) return;
+        if (lane == 0) mbar_expect_tx(b_full + 8 * kv.slot, bytes);
+        __syncwarp();
+        if (mine) pa_tma_4d(sKV + kv.slot * F::SLOT + col * F::KV_BOX + piece * p.box * 128, map, col * 64, at, it.head, id, b_full + 8 * kv.slot);
+        kv.step();
+      };
+      copy(&tmap_k, it.b0, page);
+      for (int b = it.b0; b < it.b1 && alive; ++b) {
+        const int32_t later = wanted(b + 2) ? entry(b + 2) : 0;
+        if (b + 1 < it.b1) copy(&tmap_k, b + 1, next);
+        if (alive) copy(&tmap_v, b, page);
+        page = next;
+        next = later;
+      }
+    }
+  } else if (warp == F::MMA) {
+    // ------------------------------------------------------------ MMA issuer
+    const bool leader = elect_one();
+    Ring<SLOTS> kv;
+    uint32_t q_phase = 0, block = 0, n_item = 0;
+    auto next_slot = [&](uint32_t& bar) -> uint32_t {
+      const uint32_t slot = __shfl_sync(0xffffffffu, kv.slot, 0);
+      alive = warp_mbar_wait(b_ready + 8 * slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x3300u | slot);
+      if (alive) alive = warp_mbar_wait(b_full + 8 * slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x3380u | slot);
+      pa_fence_after();
+      bar = b_empty + 8 * slot;
+      kv.step();
+      return __shfl_sync(0xffffffffu, sKV + slot * F::SLOT, 0);
+    };
+    // The scores of block number c go to columns 32 (c & 1): those of c - 2 have been read, since the product of c - 2 was issued.
+    auto scores = [&](uint32_t c, uint32_t sK, uint32_t k_bar) {
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        const uint64_t k = pa_desc(sK + b * F::KV_BOX, 16), q = pa_desc(sQ + b * F::Q_BOX, 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (leader) pa_mma_ss(tmem + 32u * (c & 1), k + 2u * e, q + 2u * e, IDESC_S, (b | e) ? 1u : 0u);
+      }
+      if (leader) { pa_commit(b_s + 8 * (c & 1)); pa_commit(k_bar); }
+    };
+    while (alive && next_item(it, alive)) {
+      const int nb = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
+      if (nb == 0) continue;
+      alive = warp_mbar_wait(b_q_full, q_phase, abort_flag, &g_paged_attn_status_word, 0x3400u);
+      q_phase ^= 1u;
+      if (!alive) break;
+      uint32_t bar, sK = next_slot(bar);
+      if (!alive) break;
+      scores(block, sK, bar);
+      if (nb == 1 && leader) pa_commit(b_q_empty);
+      const uint32_t t_o = tmem + 64u + 32u * (n_item & 1);
+      for (int j = 0; j < nb; ++j, ++block) {
+        if (j + 1 < nb) {
+          sK = next_slot(bar);
+          if (!alive) break;
+          scores(block + 1, sK, bar);
+          if (j + 2 == nb && leader) pa_commit(b_q_empty);
+        }
+        const uint32_t sV = next_slot(bar);
+        if (alive) alive = warp_mbar_wait(b_p + 8 * (block & 1), (block >> 1) & 1, abort_flag, &g_paged_attn_status_word, 0x3500u);
+        if (alive && j == 0) alive = warp_mbar_wait(b_o_empty + 8 * (n_item & 1), ((n_item >> 1) & 1) ^ 1u, abort_flag, &g_paged_attn_status_word, 0x3580u);
+        if (!alive) break;
+        pa_fence_after();
+        // heads of up to 64 elements: the upper 64 lanes repeat the lower ones (distance 0 between the column groups), nobody reads them
+        const uint64_t v = pa_desc(sV, HDP == 128 ? F::KV_BOX : 0), pr = pa_desc(sP + (block & 1) * F::P_BUF, 16);
+#pragma unroll
+        for (int e = 0; e < BLK / 16; ++e)
+          if (leader) pa_mma_ss(t_o, v + (uint64_t)(e * (2048 >> 4)), pr + (uint64_t)((e >> 2) * (F::P_BOX >> 4) + 2 * (e & 3)), IDESC_O, (j | e) ? 1u : 0u);
+        if (leader) { pa_commit(b_pv + 8 * (block & 1)); pa_commit(bar); }
+      }
+      ++n_item;
+    }
+  } else if (warp == F::FIXER) {
+    // ------------------------------------------------------------ fixer
+    Ring<SLOTS> kv;
+    uint32_t flags = 0;
+    while (alive && next_item(it, alive)) {
+      bool any_masked = false;
+      const int nb = it.b1 - it.b0;
+      for (int i = 0; i < 2 * nb && alive; ++i) {                  // K_0, K_1, V_0, K_2, V_1, ..., V of the last two
+        const bool is_v = i == 2 * nb - 1 || (i >= 2 && !(i & 1));
+        const int b = it.b0 + (i == 2 * nb - 1 ? nb - 1 : (i >> 1) - 1);
+        alive = warp_mbar_wait(b_full + 8 * kv.slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x3600u | kv.slot);
+        if (!alive) break;
+        if (is_v && masked_block(p, it, b)) {
+          const bool seen = fix_values<DT>(reinterpret_cast<uint4*>(smem_gen + kv.slot * F::SLOT), F::SLOT / 16, b * BLK, it.lo, it.hi);
+          if (lane == 0) not_finite[flags % FLAGS] = any_masked ? (not_finite[flags % FLAGS] | (seen ? 1 : 0)) : (seen ? 1 : 0);
+          any_masked = true;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_ready + 8 * kv.slot);
+        kv.step();
+      }
+      if (any_masked) ++flags;
+    }
+  } else {
+    // ------------------------------------------------------------ softmax and output rows
+    constexpr int SH = ROWS == 8 ? 2 : ROWS == 16 ? 1 : 0;         // lane i looks after row i >> SH
+    const int r = lane >> SH;
+    const int my_tok = r / p.group;
+    const uint32_t t_lane = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+    uint32_t block = 0, n_item = 0, flags = 0;
+    uint8_t* p_row = smem_gen + F::P_AT + (warp >> 1) * F::P_BOX + (lane & 7) * 2;     // this key's place in the rows of P: 16-byte pieces of 8 keys, swizzled
+    const int p_piece = (warp & 1) * 4 + (lane >> 3);
+    while (alive && next_item(it, alive)) {
+      const bool live = my_tok < it.n_tok && my_tok < p.tile_tokens;
+      const int32_t place = it.pos + my_tok;
+      const int32_t hi = live ? min(last_seen(p, place, it.len), it.hi) : -1, lo = max(first_seen(p, place), it.lo);
+      const bool blocks = it.b1 > it.b0;
+      const uint32_t t_o = t_lane + 64u + 32u * (n_item & 1);
+      float m = -INFINITY, l = 0.0f;                               // of row r; l over this warp's keys
+      bool any_masked = blocks && (masked_block(p, it, it.b0) || masked_block(p, it, it.b1 - 1));       // what is masked lies at the ends
+      for (int b = it.b0; b < it.b1; ++b, ++block) {
+        const uint32_t buf = block & 1, phase = (block >> 1) & 1;
+        alive = warp_mbar_wait(b_s + 8 * buf, phase, abort_flag, &g_paged_attn_status_word, 0x3700u);
+        if (!alive) break;
+        pa_fence_after();
+        uint32_t s[ROWS];
+        pa_ld_cols<ROWS>(t_lane + 32u * buf, s);
+        const bool masked = masked_block(p, it, b);
+        const int32_t key = b * BLK + warp * 32 + lane;
+        uint32_t seen = 0xffffffffu;                               // rows that see this key
+        if (masked) {
+          seen = 0;
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) {
+            const int32_t from = __shfl_sync(0xffffffffu, lo, i << SH), to = __shfl_sync(0xffffffffu, hi, i << SH);
+            if (key >= from && key <= to) seen |= 1u << i;
+            else s[i] = 0xff800000u;
+          }
+        }
+        float v[ROWS];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) v[i] = __uint_as_float(s[i]);
+        float* x = xm + buf * 128;                                 // a warp is at most one block ahead of another
+        x[warp * 32 + lane] = reduce_rows<ROWS, true>(v);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_x);
+        alive = warp_mbar_wait(b_x, block & 1, abort_flag, &g_paged_attn_status_word, 0x3640u);
+        if (!alive) break;
+        const float mb = max3(max3(x[lane], x[32 + lane], x[64 + lane]), x[96 + lane], x[96 + lane]);
+        const float alpha = move_max(m, mb, p.c), shift = shift_of(m, p.c);
+        uint8_t* row = p_row + buf * F::P_BUF;
+#pragma unroll
+        for (int i = 0; i < ROWS; i += 2) {
+          const float s0 = __shfl_sync(0xffffffffu, shift, i << SH), s1 = __shfl_sync(0xffffffffu, shift, (i + 1) << SH);
+          const float2 sc = make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+          float2 e = warp == 3 ? prob2<true>(sc, p.c, s0, s1) : prob2<false>(sc, p.c, s0, s1);
+          if (masked) { e.x = (seen >> i) & 1u ? e.x : 0.0f; e.y = (seen >> (i + 1)) & 1u ? e.y : 0.0f; }
+          v[i] = e.x; v[i + 1] = e.y;
+          const uint32_t w = pack_16x2(e.x, e.y, DT);
+          *reinterpret_cast<uint16_t*>(row + i * 128 + ((p_piece ^ (i & 7)) << 4)) = (uint16_t)(w & 0xffffu);
+          *reinterpret_cast<uint16_t*>(row + (i + 1) * 128 + ((p_piece ^ ((i + 1) & 7)) << 4)) = (uint16_t)(w >> 16);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        if (b > it.b0 && __any_sync(0xffffffffu, live && alpha != 1.0f)) {
+          // O' takes the factor once the product of the block before is complete; the one of this block waits for this warp
+          alive = warp_mbar_wait(b_pv + 8 * (buf ^ 1), ((block - 1) >> 1) & 1, abort_flag, &g_paged_attn_status_word, 0x3680u);
+          if (!alive) break;
+          pa_fence_after();
+          uint32_t o[ROWS];
+          pa_ld_cols<ROWS>(t_o, o);
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) o[i] = __float_as_uint(f_mul(__uint_as_float(o[i]), __shfl_sync(0xffffffffu, alpha, i << SH)));
+          pa_st_cols<ROWS>(t_o, o);
+          pa_wait_st();
+        }
+        pa_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_p + 8 * buf);
+        l = add_quarter(l, alpha, reduce_rows<ROWS, false>(v), m, mb);
+      }
+      if (!alive) break;
+      const int slot_flag = flags % FLAGS;
+      if (any_masked) ++flags;
+      float sum = 0.0f;
+      bool add_back = false;
+      if (blocks) {
+        float* x = xl + (n_item & 1) * 128;
+        x[warp * 32 + lane] = l;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_y);
+        alive = warp_mbar_wait(b_y, n_item & 1, abort_flag, &g_paged_attn_status_word, 0x3740u);
+        if (!alive) break;
+        sum = join_quarters(x[lane], x[32 + lane], x[64 + lane], x[96 + lane]);
+        alive = warp_mbar_wait(b_pv + 8 * ((block - 1) & 1), ((block - 1) >> 1) & 1, abort_flag, &g_paged_attn_status_word, 0x3780u);      // the last block's product
+        if (!alive) break;
+        pa_fence_after();
+        add_back = any_masked && not_finite[slot_flag] != 0;
+      }
+      const bool none = !(sum > 0.0f) && sum == sum;               // no key seen
+      const float inv = it.multi ? 1.0f : none ? 0.0f : __frcp_rn(sum);
+      const int col = warp * 32 + lane;                            // element of the head
+      const int n_rows = it.n_tok * p.group;
+      if (warp * 32 < p.d) {
+        uint32_t raw[ROWS];
+        if (blocks) pa_ld_cols<ROWS>(t_o, raw);
+        float o[ROWS];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+          const bool zero = __shfl_sync(0xffffffffu, (int)none, i << SH) || !blocks;
+          const float f = __shfl_sync(0xffffffffu, inv, i << SH);
+          o[i] = zero ? 0.0f : f_mul(__uint_as_float(raw[i]), f);
+        }
+        if (add_back) {
+          // the elements of V that the fixer took out, for the rows that see them
+          for (int b = it.b0; b < it.b1; ++b) {
+            if (!masked_block(p, it, b)) continue;
+            for (int32_t k = max(it.lo, b * BLK); k <= min(it.hi, b * BLK + BLK - 1); ++k) {
+              const int64_t id = p.table[(int64_t)it.seq * p.table_ld + k / p.page_size];
+              const bool there = id >= 0 && id < p.pages && col < p.d;
+              const float x = there ? load_scalar(p.v, DT, id * p.v_page + (int64_t)(k % p.page_size) * p.v_slot + it.head * p.v_head + col) : 0.0f;
+              const bool odd = !(f_add(x, -x) == 0.0f);
+#pragma unroll
+              for (int i = 0; i < ROWS; ++i) {
+                const int32_t from = __shfl_sync(0xffffffffu, lo, i << SH), to = __shfl_sync(0xffffffffu, hi, i << SH);
+                if (odd && k >= from && k <= to) o[i] = f_add(o[i], x);
+              }
+            }
+          }
+        }
+        if (col < p.d) {
+          int tok = 0, head = 0;
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) {
+            if (i < n_rows) {
+              const int64_t token = (int64_t)it.tok + tok;
+              const int h = it.head * p.group + head;
+              if (it.multi) p.part_o[((token * p.hq + h) * p.segments + it.seg) * p.d + col] = o[i];
+              else store_scalar(p.out, p.o_dtype, token * p.o_tok + h * p.o_head + col, o[i]);
+              if (++head == p.group) { head = 0; ++tok; }
+            }
+          }
+        }
+      }
+      if (warp == 0 && live && (lane & ((1 << SH) - 1)) == 0) {
+        const int64_t token = (int64_t)it.tok + my_tok;
+        const int h = it.head * p.group + r - my_tok * p.group;
+        if (it.multi) p.part_ml[(token * p.hq + h) * p.segments + it.seg] = make_float2(m, sum);
+        else if (p.lse) p.lse[token * p.lse_ld + h] = none ? -INFINITY : f_add(f_mul(m, p.scale), logf(sum));
+      }
+      if (blocks) {
+        pa_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_o_empty + 8 * (n_item & 1));
+        ++n_item;
+      }
+    }
+  }
+
+  // ---------------------------------------------------------------- teardown
+  __syncthreads();
+  if (*abort_flag) {                                               // a wait gave up: let copies and products in flight end
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == F::MMA) {
     pa_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(F::COLS) : "memory");
   }
@@ -739,19 +1234,43 @@ __global__ void __launch_bounds__(128) join_parts_kernel(const __grid_constant__
 }
 
 // ---------------------------------------------------------------- host
-template <int HDP, int NT, int DT>
-cudaError_t launch_form(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
-  using F = Form<HDP, NT>;
-  static DeviceOnce configured;
+template <typename F, typename Kernel>
+cudaError_t launch_form(Kernel kernel, DeviceOnce& configured, int ctas_per_sm, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most,
+                        cudaStream_t st) {
   const DeviceInfo dev = current_device();
   if (!configured.has(dev.dev)) {
-    cudaError_t e = cudaFuncSetAttribute(paged_attention_kernel<HDP, NT, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::SMEM);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::SMEM);
     if (e != cudaSuccess) return e;
     configured.set(dev.dev);
   }
-  const int64_t grid = std::min<int64_t>(most, (int64_t)dev.sms * (NT == 2 ? 1 : 2));
-  paged_attention_kernel<HDP, NT, DT><<<(unsigned)grid, F::THREADS, F::SMEM, st>>>(q, k, v, p);
+  kernel<<<(unsigned)std::min<int64_t>(most, (int64_t)dev.sms * ctas_per_sm), F::THREADS, F::SMEM, st>>>(q, k, v, p);
   return cudaGetLastError();
+}
+template <int HDP, int DT>
+cudaError_t launch_wide(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
+  static DeviceOnce configured;
+  return launch_form<Wide<HDP>>(paged_attention_wide_kernel<HDP, DT>, configured, 1, q, k, v, p, most, st);
+}
+template <int HDP, int ROWS, int DT>
+cudaError_t launch_few(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
+  static DeviceOnce configured;
+  return launch_form<Few<HDP, ROWS>>(paged_attention_few_kernel<HDP, ROWS, DT>, configured, 2, q, k, v, p, most, st);
+}
+template <int DT>
+cudaError_t launch_any(int rows, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
+  if (p.d <= 64) {
+    switch (rows) {
+      case 8: return launch_few<64, 8, DT>(q, k, v, p, most, st);
+      case 16: return launch_few<64, 16, DT>(q, k, v, p, most, st);
+      case 32: return launch_few<64, 32, DT>(q, k, v, p, most, st);
+    }
+    return launch_wide<64, DT>(q, k, v, p, most, st);
+  }
+  switch (rows) {
+    case 8: return launch_few<128, 8, DT>(q, k, v, p, most, st);
+    case 16: return launch_few<128, 16, DT>(q, k, v, p, most, st);
+  }
+  return launch_wide<128, DT>(q, k, v, p, most, st);
 }
 
 }  // namespace
@@ -775,9 +1294,11 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   if (a.ws) p.part_ml = reinterpret_cast<float2*>(p.part_o + T * p.hq * (int64_t)a.segments * d);
   p.v = static_cast<const uint16_t*>(a.v->ptr); p.v_page = a.v->page_stride; p.v_slot = a.v->slot_stride; p.v_head = a.v->head_stride;
 
-  // one tile of 32 rows where a sequence's new rows fit it: two CTAs an SM, no second tile to wait for
-  const bool narrow = G <= 32 && a.max_q * G <= 32;
-  const int rows = narrow ? 32 : 128;
+  // The form for few rows where a sequence's new rows of a key head fit one of its tiles: 8, 16 or (heads of 64: the tile's operands have to
+  // fit half an SM) 32 rows.
+  const int64_t need = a.max_q * G;
+  const int rows = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 && d <= 64 ? 32 : 128;
+  const bool narrow = rows < 128;
   p.tile_tokens = rows / G;
   int box = page & -page;                                  // the largest power of two that divides the page size: boxes never cross pages
   p.box = box = box < BLK ? box : BLK;
@@ -794,15 +1315,8 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   // no more CTAs than there can be items
   const int cta_tokens = p.tile_tokens * (narrow ? 1 : 2);
   const int64_t most = std::min<int64_t>(T, (T + cta_tokens - 1) / cta_tokens + p.n_seqs) * hkv * a.segments;
-  cudaError_t e;
-  const bool bf = a.q->dtype == RG_BF16;
-  if (narrow) {
-    if (d <= 64) e = bf ? launch_form<64, 1, RG_BF16>(tq, tk, tv, p, most, st) : launch_form<64, 1, RG_F16>(tq, tk, tv, p, most, st);
-    else e = bf ? launch_form<128, 1, RG_BF16>(tq, tk, tv, p, most, st) : launch_form<128, 1, RG_F16>(tq, tk, tv, p, most, st);
-  } else {
-    if (d <= 64) e = bf ? launch_form<64, 2, RG_BF16>(tq, tk, tv, p, most, st) : launch_form<64, 2, RG_F16>(tq, tk, tv, p, most, st);
-    else e = bf ? launch_form<128, 2, RG_BF16>(tq, tk, tv, p, most, st) : launch_form<128, 2, RG_F16>(tq, tk, tv, p, most, st);
-  }
+  if (most >= (int64_t(1) << 31)) return RG_ERR_SHAPE;     // items are counted in 32 bits
+  const cudaError_t e = a.q->dtype == RG_BF16 ? launch_any<RG_BF16>(rows, tq, tk, tv, p, most, st) : launch_any<RG_F16>(rows, tq, tk, tv, p, most, st);
   if (e != cudaSuccess) return RG_ERR_CUDA;
   if (a.segments > 1) {
     join_parts_kernel<<<(unsigned)((T * p.hq + 3) / 4), 128, 0, st>>>(p);
