@@ -90,6 +90,21 @@ __device__ __forceinline__ void pa_st32(uint32_t taddr, const uint32_t* r) {
       : "memory");
 }
 __device__ __forceinline__ void pa_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// The library's bounded wait, made by a whole warp and without a function call (a kernel that moves registers between its warps cannot have one).
+__device__ __forceinline__ bool pa_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t code) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  uint64_t t0 = 0;
+  for (uint32_t turn = 1;; ++turn) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if ((turn & 255u) == 0) {
+      const uint64_t now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      const bool late = now - t0 > WAIT_LIMIT_NS;
+      if (late) { *abort_flag = 1; atomicCAS(&g_paged_attn_status_word, 0u, code); }
+      if (__any_sync(0xffffffffu, late || *abort_flag)) return false;
+    }
+  }
+}
 __device__ __forceinline__ float pa_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -249,22 +264,21 @@ __device__ __forceinline__ bool masked_block(const Params& p, const Item& it, in
 
 // ---------------------------------------------------------------- one row, one block
 // 2^x for x <= LAG or NaN by its own steps: the nearest integer by a magic addition, a polynomial of degree 5 for the rest (equal to 1
-// at 0; largest relative error 1.7e-7, fitted by iteratively reweighted least squares), the integer added to the exponent.  Below
-// -125 the answer is that of -125: at most 2^-125, where the hardware's instruction has 0.  Two at a time.  The integer sum at the end
-// (and not a multiplication) keeps the assembler from contracting it with the addition that follows.  NaN comes out as some number: a row
-// with a NaN among its scores is marked in its sum.
+// at 0; largest relative error 1.7e-7, fitted by iteratively reweighted least squares), the integer added to the exponent; 0 below -125.
+// Two at a time.  The integer sum at the end (and not a multiplication) keeps the assembler from contracting it with the addition that
+// follows.  NaN comes out as some number: a row with a NaN among its scores is marked in its sum.
 __device__ __forceinline__ float2 poly_ex2(float2 x) {
   const float2 magic = make_float2(12582912.0f, 12582912.0f), unmagic = make_float2(-12582912.0f, -12582912.0f);
-  const float2 y = make_float2(fmaxf(x.x, -125.0f), fmaxf(x.y, -125.0f));
-  const float2 t = __fadd2_rn(y, magic), n = __fadd2_rn(t, unmagic);
-  const float2 f = __ffma2_rn(n, make_float2(-1.0f, -1.0f), y);
+  const float2 t = __fadd2_rn(x, magic), n = __fadd2_rn(t, unmagic);
+  const float2 f = __ffma2_rn(n, make_float2(-1.0f, -1.0f), x);
   float2 q = make_float2(0x1.5bba14p-10f, 0x1.5bba14p-10f);
   q = __ffma2_rn(q, f, make_float2(0x1.3cea88p-7f, 0x1.3cea88p-7f));
   q = __ffma2_rn(q, f, make_float2(0x1.c6b752p-5f, 0x1.c6b752p-5f));
   q = __ffma2_rn(q, f, make_float2(0x1.ebf9bcp-3f, 0x1.ebf9bcp-3f));
   q = __ffma2_rn(q, f, make_float2(0x1.62e42ap-1f, 0x1.62e42ap-1f));
   q = __ffma2_rn(q, f, make_float2(1.0f, 1.0f));
-  return make_float2(__int_as_float(__float_as_int(q.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(q.y) + (__float_as_int(t.y) << 23)));
+  const float a = __int_as_float(__float_as_int(q.x) + (__float_as_int(t.x) << 23)), b = __int_as_float(__float_as_int(q.y) + (__float_as_int(t.y) << 23));
+  return make_float2(x.x < -125.0f ? 0.0f : a, x.y < -125.0f ? 0.0f : b);
 }
 
 constexpr int QW = 32;                         // scores are taken 32 keys at a time: a quarter of a block, with a sum of its own
@@ -280,15 +294,21 @@ __device__ __forceinline__ void load_quarter(uint32_t taddr, uint32_t (&s)[QW]) 
   asm volatile("" : "+r"(s[30]), "+r"(s[31]) :: "memory");
 }
 
-// The largest of a quarter's scores, NaN if one is; first .. last: the columns of the quarter that the row sees (MASKED).
-template <bool MASKED>
-__device__ __forceinline__ float quarter_max(const uint32_t (&s)[QW], int first, int last) {
-  float v[QW];
+// Waits for loads from tensor memory; what uses a row's scores cannot be moved in front of the wait.
+__device__ __forceinline__ void wait_scores(uint32_t (&s)[BLK]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < QW; ++i) v[i] = MASKED && (i < first || i > last) ? -INFINITY : __uint_as_float(s[i]);
-  float a = v[0], b = v[1];
+  for (int i = 0; i < BLK; i += 16)
+    asm volatile("" : "+r"(s[i]), "+r"(s[i + 1]), "+r"(s[i + 2]), "+r"(s[i + 3]), "+r"(s[i + 4]), "+r"(s[i + 5]), "+r"(s[i + 6]), "+r"(s[i + 7]), "+r"(s[i + 8]),
+                 "+r"(s[i + 9]), "+r"(s[i + 10]), "+r"(s[i + 11]), "+r"(s[i + 12]), "+r"(s[i + 13]), "+r"(s[i + 14]), "+r"(s[i + 15]));
+}
+
+// The largest of a quarter's scores, NaN if one is.
+__device__ __forceinline__ float quarter_max(const uint32_t* s) {
+  float a = __uint_as_float(s[0]), b = __uint_as_float(s[1]);
 #pragma unroll
-  for (int i = 2; i < QW; i += 4) { a = max3(a, v[i], v[i + 1]); if (i + 3 < QW) b = max3(b, v[i + 2], v[i + 3]); }
+  for (int i = 2; i + 3 < QW; i += 4) { a = max3(a, __uint_as_float(s[i]), __uint_as_float(s[i + 1])); b = max3(b, __uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])); }
+  a = max3(a, __uint_as_float(s[QW - 2]), __uint_as_float(s[QW - 1]));
   return max3(a, b, b);
 }
 
@@ -303,32 +323,35 @@ __device__ __forceinline__ float move_max(float& m, float mb, float c) {
 }
 __device__ __forceinline__ float shift_of(float m, float c) { return m == -INFINITY ? 0.0f : -f_mul(m, c); }
 
-// The exponentials of two scores.  Which of the two forms a key takes follows from its place alone: the hardware unit gives 16 results a
-// cycle and SM, and the last quarter of every block is taken off it.
+// The exponentials of two scores.  Which of the two forms a key takes follows from its place alone: the last 8 of every 32 the polynomial,
+// which takes them off the hardware unit (16 results a cycle and SM, where a block of both tiles wants 32768 in 2048 cycles of the tensor core).
+constexpr int POLY_FROM = 24;
 template <bool POLY>
 __device__ __forceinline__ float2 prob2(float2 s, float c, float shift0, float shift1) {
   const float2 x = __ffma2_rn(s, make_float2(c, c), make_float2(shift0, shift1));
   return POLY ? poly_ex2(x) : make_float2(pa_ex2(x.x), pa_ex2(x.y));
 }
 
-// Probabilities of a quarter, narrowed two to a word; returns their fp32 sum, in the order of a butterfly over the 32 keys (key with key + 16 first).
-template <int DT, bool MASKED, bool POLY>
-__device__ __forceinline__ float quarter_probs(const uint32_t (&s)[QW], uint32_t (&packed)[QW / 2], int first, int last, float c, float shift) {
-  float2 e[QW / 2];
+// Probabilities of a quarter, narrowed two to a word (masked scores are -inf and give exact zeros); returns their fp32 sum, in the order of a
+// butterfly over the 32 keys: key with key + 16 first, neighbours last.
+template <int DT>
+__device__ __forceinline__ float quarter_probs(const uint32_t* s, uint32_t* packed, float c, float shift) {
+  float2 t[8];
 #pragma unroll
-  for (int i = 0; i < QW / 2; ++i) {
-    e[i] = prob2<POLY>(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c, shift, shift);
-    if (MASKED) {
-      e[i].x = (2 * i >= first && 2 * i <= last) ? e[i].x : 0.0f;
-      e[i].y = (2 * i + 1 >= first && 2 * i + 1 <= last) ? e[i].y : 0.0f;
-    }
-    packed[i] = pack_16x2(e[i].x, e[i].y, DT);
+  for (int i = 0; i < 8; ++i) {
+    const int j = i + 8;
+    const float2 a = prob2<false>(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c, shift, shift);
+    const float2 sj = make_float2(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1]));
+    const float2 b = 2 * j >= POLY_FROM ? prob2<true>(sj, c, shift, shift) : prob2<false>(sj, c, shift, shift);
+    packed[i] = pack_16x2(a.x, a.y, DT);
+    packed[j] = pack_16x2(b.x, b.y, DT);
+    t[i] = __fadd2_rn(a, b);
   }
 #pragma unroll
-  for (int n = QW / 4; n >= 1; n >>= 1)
+  for (int n = 4; n >= 1; n >>= 1)
 #pragma unroll
-    for (int i = 0; i < n; ++i) e[i] = __fadd2_rn(e[i], e[i + n]);
-  return f_add(e[0].x, e[0].y);
+    for (int i = 0; i < n; ++i) t[i] = __fadd2_rn(t[i], t[i + n]);
+  return f_add(t[0].x, t[0].y);
 }
 // A quarter's running sum.  A NaN or an infinity among the block's scores makes the row NaN; nothing above -inf so far: no sum.
 __device__ __forceinline__ float add_quarter(float l, float alpha, float total, float m, float mb) {
@@ -384,7 +407,7 @@ template <int HDP>
 struct Wide {
   static constexpr int DB = HDP / 64;                              // 64-column boxes of a head
   static constexpr int NT = 2, SOFT = 4 * NT;                      // tiles of 128 rows, softmax warps
-  static constexpr int PRODUCER = SOFT, MMA = SOFT + 1, FIXER = SOFT + 2, WARPS = SOFT + 3, THREADS = WARPS * 32;
+  static constexpr int PRODUCER = SOFT, MMA = SOFT + 1, FIXER = SOFT + 2, WARPS = SOFT + 3, THREADS = (SOFT + 4) * 32;   // the last warp does nothing
   static constexpr uint32_t Q_BOX = 128 * 128, Q_TILE = DB * Q_BOX;
   static constexpr uint32_t KV_BOX = BLK * 128, SLOT = DB * KV_BOX;
   static constexpr int SLOTS = HDP == 128 ? 5 : 10;
@@ -437,7 +460,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   // Next item, for the warps that get it from the producer; false: none left, or a wait gave up.
   Ring<ITEMS> ir;
   auto next_item = [&](Item& it, bool& alive) -> bool {
-    if (!warp_mbar_wait(b_item + 8 * ir.slot, ir.phase, abort_flag, &g_paged_attn_status_word, 0x2000u)) { alive = false; return false; }
+    if (!pa_wait(b_item + 8 * ir.slot, ir.phase, abort_flag, 0x2000u)) { alive = false; return false; }
     it = items[ir.slot];
     __syncwarp();
     if (lane == 0) mbar_arrive(b_free + 8 * ir.slot);
@@ -446,7 +469,9 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   };
   Item it;
   bool alive = true;
-
+  // A softmax thread holds a row's 128 scores: its warps take registers from the other four (168 a thread at launch: 2 * 216 + 72 = 3 * 168).
+  if (warp >= F::SOFT) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   if (warp == F::PRODUCER) {
     // ------------------------------------------------------------ producer
     const int pieces = BLK / p.box;                                // TMA boxes along the keys of a block
@@ -458,7 +483,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
     while (alive) {
       const bool more = walk.get(p, cta_tokens, it);
       if (!more) it.n_tok = 0;
-      alive = warp_mbar_wait(b_free + 8 * ir.slot, ir.phase ^ 1u, abort_flag, &g_paged_attn_status_word, 0x2080u);
+      alive = pa_wait(b_free + 8 * ir.slot, ir.phase ^ 1u, abort_flag, 0x2080u);
       if (!alive) break;
       if (lane == 0) { items[ir.slot] = it; mbar_arrive(b_item + 8 * ir.slot); }
       ir.step();
@@ -468,7 +493,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
       auto wanted = [&](int b) -> bool { const int32_t k = b * BLK + piece * p.box; return col < DB && k <= it.hi && k + p.box > it.lo; };
       auto entry = [&](int b) -> int32_t { return row[(b * BLK + piece * p.box) / p.page_size]; };
       int32_t ahead = wanted(it.b0) ? entry(it.b0) : 0;
-      alive = warp_mbar_wait(b_q_empty, q_phase, abort_flag, &g_paged_attn_status_word, 0x2100u);
+      alive = pa_wait(b_q_empty, q_phase, abort_flag, 0x2100u);
       if (!alive) break;
       q_phase ^= 1u;
       const int tiles = NT == 2 && it.n_tok > p.tile_tokens ? 2 : 1;
@@ -490,7 +515,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)p.box * 128u;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-          alive = warp_mbar_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, &g_paged_attn_status_word, 0x2200u | kv.slot);
+          alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x2200u | kv.slot);
           if (!alive) break;
           if (lane == 0) mbar_expect_tx(b_full + 8 * kv.slot, bytes);
           __syncwarp();
@@ -507,8 +532,8 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
     // Waits for the next slot; its address comes out warp-uniform, so that the descriptors stay in uniform registers.
     auto next_slot = [&](uint32_t& bar) -> uint32_t {
       const uint32_t slot = __shfl_sync(0xffffffffu, kv.slot, 0);
-      alive = warp_mbar_wait(b_ready + 8 * slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x2300u | slot);
-      if (alive) alive = warp_mbar_wait(b_full + 8 * slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x2380u | slot);
+      alive = pa_wait(b_ready + 8 * slot, kv.phase, abort_flag, 0x2300u | slot);
+      if (alive) alive = pa_wait(b_full + 8 * slot, kv.phase, abort_flag, 0x2380u | slot);
       pa_fence_after();
       bar = b_empty + 8 * slot;
       kv.step();
@@ -527,7 +552,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
       const int nb = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
       if (nb == 0) continue;
       const int tiles = NT == 2 && __shfl_sync(0xffffffffu, it.n_tok, 0) > p.tile_tokens ? 2 : 1;
-      alive = warp_mbar_wait(b_q_full, q_phase, abort_flag, &g_paged_attn_status_word, 0x2400u);
+      alive = pa_wait(b_q_full, q_phase, abort_flag, 0x2400u);
       q_phase ^= 1u;
       if (!alive) break;
       uint32_t k_bar, v_bar, sK = next_slot(k_bar);
@@ -541,9 +566,9 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           if (t >= tiles) break;
-          alive = warp_mbar_wait(b_p + 8 * t, p_phase[t], abort_flag, &g_paged_attn_status_word, 0x2500u | t);
+          alive = pa_wait(b_p + 8 * t, p_phase[t], abort_flag, 0x2500u | t);
           p_phase[t] ^= 1u;
-          if (alive && j == 0) { alive = warp_mbar_wait(b_o_empty + 8 * t, o_phase[t], abort_flag, &g_paged_attn_status_word, 0x2580u | t); o_phase[t] ^= 1u; }
+          if (alive && j == 0) { alive = pa_wait(b_o_empty + 8 * t, o_phase[t], abort_flag, 0x2580u | t); o_phase[t] ^= 1u; }
           if (!alive) break;
           pa_fence_after();
           const uint64_t v = pa_desc(sV, F::KV_BOX);
@@ -575,7 +600,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         const bool masked = masked_block(p, it, b);
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-          alive = warp_mbar_wait(b_full + 8 * kv.slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x2600u | kv.slot);
+          alive = pa_wait(b_full + 8 * kv.slot, kv.phase, abort_flag, 0x2600u | kv.slot);
           if (!alive) break;
           if (which == 1 && masked) {
             const bool seen = fix_values<DT>(reinterpret_cast<uint4*>(smem_gen + F::KV_AT + kv.slot * F::SLOT), F::SLOT / 16, b * BLK, it.lo, it.hi);
@@ -589,8 +614,10 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
       }
       if (any_masked) ++flags;
     }
+  }
   } else {
     // ------------------------------------------------------------ softmax and output rows
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const int t = warp >> 2;                                       // tile
     const int r = (warp & 3) * 32 + lane;                          // row of the tile, and its lane in tensor memory
     const uint32_t t_s = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128u * t, t_o = t_s + 128u * NT;
@@ -609,37 +636,27 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
       if (tile_live) {
         for (int b = it.b0; b < it.b1; ++b) {
           const bool masked = masked_block(p, it, b);
-          alive = warp_mbar_wait(b_s + 8 * t, s_phase, abort_flag, &g_paged_attn_status_word, 0x2700u | t);
+          alive = pa_wait(b_s + 8 * t, s_phase, abort_flag, 0x2700u | t);
           if (!alive) break;
           const int first = lo - b * BLK, last = hi - b * BLK;     // columns of the block that the row sees
           pa_fence_after();
           if (warp_live) {
-            uint32_t s[QW], packed[QW / 2];
-            float mq[4];
+            uint32_t s[BLK];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) pa_ld32(t_s + 32u * q, s + 32 * q);
+            wait_scores(s);
             if (masked) {
 #pragma unroll
-              for (int q = 0; q < 4; ++q) { load_quarter(t_s + 32u * q, s); mq[q] = quarter_max<true>(s, first - 32 * q, last - 32 * q); }
-            } else {
-#pragma unroll
-              for (int q = 0; q < 4; ++q) { load_quarter(t_s + 32u * q, s); mq[q] = quarter_max<false>(s, 0, 0); }
+              for (int i = 0; i < BLK; ++i) s[i] = i >= first && i <= last ? s[i] : 0xff800000u;
             }
-            const float mb = max3(max3(mq[0], mq[1], mq[2]), mq[3], mq[3]);
+            const float mb = max3(max3(quarter_max(s), quarter_max(s + 32), quarter_max(s + 64)), quarter_max(s + 96), -INFINITY);
             const float alpha = move_max(m, mb, p.c), shift = shift_of(m, p.c);
-            // probabilities go over scores that have been read: quarter q's words end at column 16 (q + 1)
-            if (masked) {
+            // probabilities go over scores, which have been read
 #pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                load_quarter(t_s + 32u * q, s);
-                l[q] = add_quarter(l[q], alpha, q == 3 ? quarter_probs<DT, true, true>(s, packed, first - 96, last - 96, p.c, shift) : quarter_probs<DT, true, false>(s, packed, first - 32 * q, last - 32 * q, p.c, shift), m, mb);
-                pa_st16(t_s + 16u * q, packed);
-              }
-            } else {
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                load_quarter(t_s + 32u * q, s);
-                l[q] = add_quarter(l[q], alpha, q == 3 ? quarter_probs<DT, false, true>(s, packed, 0, 0, p.c, shift) : quarter_probs<DT, false, false>(s, packed, 0, 0, p.c, shift), m, mb);
-                pa_st16(t_s + 16u * q, packed);
-              }
+            for (int q = 0; q < 4; ++q) {
+              uint32_t packed[QW / 2];
+              l[q] = add_quarter(l[q], alpha, quarter_probs<DT>(s + 32 * q, packed, p.c, shift), m, mb);
+              pa_st16(t_s + 16u * q, packed);
             }
             // the scores of this block are complete, so the product of the block before is too: O may be rescaled
             if (b > it.b0 && __any_sync(0xffffffffu, live && alpha != 1.0f)) rescale<HDP>(t_o, alpha);
@@ -659,7 +676,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
       const float sum = join_quarters(l[0], l[1], l[2], l[3]);
       bool add_back = false;
       if (blocks) {
-        alive = warp_mbar_wait(b_o_full + 8 * t, o_phase, abort_flag, &g_paged_attn_status_word, 0x2780u | t);
+        alive = pa_wait(b_o_full + 8 * t, o_phase, abort_flag, 0x2780u | t);
         o_phase ^= 1u;
         if (!alive) break;
         pa_fence_after();
@@ -869,7 +886,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
 
   Ring<ITEMS> ir;
   auto next_item = [&](Item& it, bool& alive) -> bool {
-    if (!warp_mbar_wait(b_item + 8 * ir.slot, ir.phase, abort_flag, &g_paged_attn_status_word, 0x3000u)) { alive = false; return false; }
+    if (!pa_wait(b_item + 8 * ir.slot, ir.phase, abort_flag, 0x3000u)) { alive = false; return false; }
     it = items[ir.slot];
     __syncwarp();
     if (lane == 0) mbar_arrive(b_free + 8 * ir.slot);
@@ -890,7 +907,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     while (alive) {
       const bool more = walk.get(p, p.tile_tokens, it);
       if (!more) it.n_tok = 0;
-      alive = warp_mbar_wait(b_free + 8 * ir.slot, ir.phase ^ 1u, abort_flag, &g_paged_attn_status_word, 0x3080u);
+      alive = pa_wait(b_free + 8 * ir.slot, ir.phase ^ 1u, abort_flag, 0x3080u);
       if (!alive) break;
       if (lane == 0) { items[ir.slot] = it; mbar_arrive(b_item + 8 * ir.slot); }
       ir.step();
@@ -900,7 +917,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       auto wanted = [&](int b) -> bool { const int32_t k = b * BLK + piece * p.box; return col < DB && b < it.b1 && k <= it.hi && k + p.box > it.lo; };
       auto entry = [&](int b) -> int32_t { return row[(b * BLK + piece * p.box) / p.page_size]; };
       int32_t page = wanted(it.b0) ? entry(it.b0) : 0, next = wanted(it.b0 + 1) ? entry(it.b0 + 1) : 0;      // looked up a block ahead of their use
-      alive = warp_mbar_wait(b_q_empty, q_phase, abort_flag, &g_paged_attn_status_word, 0x3100u);
+      alive = pa_wait(b_q_empty, q_phase, abort_flag, 0x3100u);
       if (!alive) break;
       q_phase ^= 1u;
       if (lane == 0) mbar_expect_tx(b_q_full, (uint32_t)(DB * p.tile_tokens * p.group) * 128u);
@@ -914,7 +931,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         }
         const int32_t at = (b * BLK + piece * p.box) % p.page_size;
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)p.box * 128u;
-        alive = warp_mbar_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, &g_paged_attn_status_word, 0x3200u | kv.slot);
+        alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x3200u | kv.slot);
         if (!alive) return;
         if (lane == 0) mbar_expect_tx(b_full + 8 * kv.slot, bytes);
         __syncwarp();
@@ -937,8 +954,8 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     uint32_t q_phase = 0, block = 0, n_item = 0;
     auto next_slot = [&](uint32_t& bar) -> uint32_t {
       const uint32_t slot = __shfl_sync(0xffffffffu, kv.slot, 0);
-      alive = warp_mbar_wait(b_ready + 8 * slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x3300u | slot);
-      if (alive) alive = warp_mbar_wait(b_full + 8 * slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x3380u | slot);
+      alive = pa_wait(b_ready + 8 * slot, kv.phase, abort_flag, 0x3300u | slot);
+      if (alive) alive = pa_wait(b_full + 8 * slot, kv.phase, abort_flag, 0x3380u | slot);
       pa_fence_after();
       bar = b_empty + 8 * slot;
       kv.step();
@@ -957,7 +974,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     while (alive && next_item(it, alive)) {
       const int nb = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
       if (nb == 0) continue;
-      alive = warp_mbar_wait(b_q_full, q_phase, abort_flag, &g_paged_attn_status_word, 0x3400u);
+      alive = pa_wait(b_q_full, q_phase, abort_flag, 0x3400u);
       q_phase ^= 1u;
       if (!alive) break;
       uint32_t bar, sK = next_slot(bar);
@@ -973,8 +990,8 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
           if (j + 2 == nb && leader) pa_commit(b_q_empty);
         }
         const uint32_t sV = next_slot(bar);
-        if (alive) alive = warp_mbar_wait(b_p + 8 * (block & 1), (block >> 1) & 1, abort_flag, &g_paged_attn_status_word, 0x3500u);
-        if (alive && j == 0) alive = warp_mbar_wait(b_o_empty + 8 * (n_item & 1), ((n_item >> 1) & 1) ^ 1u, abort_flag, &g_paged_attn_status_word, 0x3580u);
+        if (alive) alive = pa_wait(b_p + 8 * (block & 1), (block >> 1) & 1, abort_flag, 0x3500u);
+        if (alive && j == 0) alive = pa_wait(b_o_empty + 8 * (n_item & 1), ((n_item >> 1) & 1) ^ 1u, abort_flag, 0x3580u);
         if (!alive) break;
         pa_fence_after();
         // heads of up to 64 elements: the upper 64 lanes repeat the lower ones (distance 0 between the column groups), nobody reads them
@@ -996,7 +1013,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       for (int i = 0; i < 2 * nb && alive; ++i) {                  // K_0, K_1, V_0, K_2, V_1, ..., V of the last two
         const bool is_v = i == 2 * nb - 1 || (i >= 2 && !(i & 1));
         const int b = it.b0 + (i == 2 * nb - 1 ? nb - 1 : (i >> 1) - 1);
-        alive = warp_mbar_wait(b_full + 8 * kv.slot, kv.phase, abort_flag, &g_paged_attn_status_word, 0x3600u | kv.slot);
+        alive = pa_wait(b_full + 8 * kv.slot, kv.phase, abort_flag, 0x3600u | kv.slot);
         if (!alive) break;
         if (is_v && masked_block(p, it, b)) {
           const bool seen = fix_values<DT>(reinterpret_cast<uint4*>(smem_gen + kv.slot * F::SLOT), F::SLOT / 16, b * BLK, it.lo, it.hi);
@@ -1028,21 +1045,18 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       bool any_masked = blocks && (masked_block(p, it, it.b0) || masked_block(p, it, it.b1 - 1));       // what is masked lies at the ends
       for (int b = it.b0; b < it.b1; ++b, ++block) {
         const uint32_t buf = block & 1, phase = (block >> 1) & 1;
-        alive = warp_mbar_wait(b_s + 8 * buf, phase, abort_flag, &g_paged_attn_status_word, 0x3700u);
+        alive = pa_wait(b_s + 8 * buf, phase, abort_flag, 0x3700u);
         if (!alive) break;
         pa_fence_after();
         uint32_t s[ROWS];
         pa_ld_cols<ROWS>(t_lane + 32u * buf, s);
         const bool masked = masked_block(p, it, b);
         const int32_t key = b * BLK + warp * 32 + lane;
-        uint32_t seen = 0xffffffffu;                               // rows that see this key
         if (masked) {
-          seen = 0;
 #pragma unroll
           for (int i = 0; i < ROWS; ++i) {
             const int32_t from = __shfl_sync(0xffffffffu, lo, i << SH), to = __shfl_sync(0xffffffffu, hi, i << SH);
-            if (key >= from && key <= to) seen |= 1u << i;
-            else s[i] = 0xff800000u;
+            s[i] = key >= from && key <= to ? s[i] : 0xff800000u;
           }
         }
         float v[ROWS];
@@ -1052,7 +1066,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         x[warp * 32 + lane] = reduce_rows<ROWS, true>(v);
         __syncwarp();
         if (lane == 0) mbar_arrive(b_x);
-        alive = warp_mbar_wait(b_x, block & 1, abort_flag, &g_paged_attn_status_word, 0x3640u);
+        alive = pa_wait(b_x, block & 1, abort_flag, 0x3640u);
         if (!alive) break;
         const float mb = max3(max3(x[lane], x[32 + lane], x[64 + lane]), x[96 + lane], x[96 + lane]);
         const float alpha = move_max(m, mb, p.c), shift = shift_of(m, p.c);
@@ -1061,8 +1075,8 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         for (int i = 0; i < ROWS; i += 2) {
           const float s0 = __shfl_sync(0xffffffffu, shift, i << SH), s1 = __shfl_sync(0xffffffffu, shift, (i + 1) << SH);
           const float2 sc = make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
-          float2 e = warp == 3 ? prob2<true>(sc, p.c, s0, s1) : prob2<false>(sc, p.c, s0, s1);
-          if (masked) { e.x = (seen >> i) & 1u ? e.x : 0.0f; e.y = (seen >> (i + 1)) & 1u ? e.y : 0.0f; }
+          const float2 eh = prob2<false>(sc, p.c, s0, s1), ep = prob2<true>(sc, p.c, s0, s1);
+          const float2 e = lane >= POLY_FROM ? ep : eh;
           v[i] = e.x; v[i + 1] = e.y;
           const uint32_t w = pack_16x2(e.x, e.y, DT);
           *reinterpret_cast<uint16_t*>(row + i * 128 + ((p_piece ^ (i & 7)) << 4)) = (uint16_t)(w & 0xffffu);
@@ -1071,7 +1085,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         if (b > it.b0 && __any_sync(0xffffffffu, live && alpha != 1.0f)) {
           // O' takes the factor once the product of the block before is complete; the one of this block waits for this warp
-          alive = warp_mbar_wait(b_pv + 8 * (buf ^ 1), ((block - 1) >> 1) & 1, abort_flag, &g_paged_attn_status_word, 0x3680u);
+          alive = pa_wait(b_pv + 8 * (buf ^ 1), ((block - 1) >> 1) & 1, abort_flag, 0x3680u);
           if (!alive) break;
           pa_fence_after();
           uint32_t o[ROWS];
@@ -1096,10 +1110,10 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         x[warp * 32 + lane] = l;
         __syncwarp();
         if (lane == 0) mbar_arrive(b_y);
-        alive = warp_mbar_wait(b_y, n_item & 1, abort_flag, &g_paged_attn_status_word, 0x3740u);
+        alive = pa_wait(b_y, n_item & 1, abort_flag, 0x3740u);
         if (!alive) break;
         sum = join_quarters(x[lane], x[32 + lane], x[64 + lane], x[96 + lane]);
-        alive = warp_mbar_wait(b_pv + 8 * ((block - 1) & 1), ((block - 1) >> 1) & 1, abort_flag, &g_paged_attn_status_word, 0x3780u);      // the last block's product
+        alive = pa_wait(b_pv + 8 * ((block - 1) & 1), ((block - 1) >> 1) & 1, abort_flag, 0x3780u);      // the last block's product
         if (!alive) break;
         pa_fence_after();
         add_back = any_masked && not_finite[slot_flag] != 0;
