@@ -323,9 +323,9 @@ __device__ __forceinline__ float move_max(float& m, float mb, float c) {
 }
 __device__ __forceinline__ float shift_of(float m, float c) { return m == -INFINITY ? 0.0f : -f_mul(m, c); }
 
-// The exponentials of two scores.  Which of the two forms a key takes follows from its place alone: the last 8 of every 32 the polynomial,
+// The exponentials of two scores.  Which of the two forms a key takes follows from its place alone: the last 4 of every 32 the polynomial,
 // which takes them off the hardware unit (16 results a cycle and SM, where a block of both tiles wants 32768 in 2048 cycles of the tensor core).
-constexpr int POLY_FROM = 24;
+constexpr int POLY_FROM = 28;
 template <bool POLY>
 __device__ __forceinline__ float2 prob2(float2 s, float c, float shift0, float shift1) {
   const float2 x = __ffma2_rn(s, make_float2(c, c), make_float2(shift0, shift1));
@@ -363,7 +363,7 @@ __device__ __forceinline__ float join_quarters(float a, float b, float c, float 
 // O = alpha O for one lane's columns
 template <int HDP>
 __device__ __forceinline__ void rescale(uint32_t t_o, float alpha) {
-#pragma unroll
+#pragma unroll 1
   for (int q = 0; q < HDP / QW; ++q) {
     uint32_t o[QW];
     load_quarter(t_o + 32u * q, o);
@@ -412,7 +412,7 @@ struct Wide {
   static constexpr uint32_t KV_BOX = BLK * 128, SLOT = DB * KV_BOX;
   static constexpr int SLOTS = HDP == 128 ? 5 : 10;
   static constexpr uint32_t COLS = 512;                            // tensor memory: S_t, and P_t over it, at 128 t, O_t at 128 (2 + t)
-  static constexpr uint32_t KV_AT = NT * Q_TILE, ITEM_AT = KV_AT + SLOTS * SLOT, BAR_AT = ITEM_AT + ITEMS * sizeof(Item), N_BAR = 10 + 3 * SLOTS + 2 * ITEMS,
+  static constexpr uint32_t KV_AT = NT * Q_TILE, ITEM_AT = KV_AT + SLOTS * SLOT, BAR_AT = ITEM_AT + ITEMS * sizeof(Item), N_BAR = 12 + 3 * SLOTS + 2 * ITEMS,
                             FLAG_AT = BAR_AT + 8 * N_BAR, LAST = FLAG_AT + 4 * (2 + FLAGS);
   static constexpr size_t SMEM = 1024 + LAST;
   static_assert(SMEM <= 232448 && SLOTS / 2 + 1 < FLAGS, "fits the SM; the fixer cannot be a whole turn of flags ahead");
@@ -432,7 +432,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   const uint32_t sQ = smem_base, sKV = smem_base + F::KV_AT;
   Item* items = reinterpret_cast<Item*>(smem_gen + F::ITEM_AT);
   const uint32_t bar0 = smem_base + F::BAR_AT;
-  const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_s = bar0 + 16, b_p = bar0 + 32, b_o_full = bar0 + 48, b_o_empty = bar0 + 64, b_full = bar0 + 80;   // two each from b_s to b_o_empty
+  const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_s = bar0 + 16, b_o_full = bar0 + 32, b_o_empty = bar0 + 48, b_p = bar0 + 64, b_full = bar0 + 96;   // one a tile from b_s on; b_p: and half of the keys
   const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + F::FLAG_AT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -441,7 +441,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     mbar_init(b_q_full, 1); mbar_init(b_q_empty, 1);
-    for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 8 * t, 4); mbar_init(b_o_full + 8 * t, 1); mbar_init(b_o_empty + 8 * t, 4); }
+    for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 16 * t, 4); mbar_init(b_p + 16 * t + 8, 4); mbar_init(b_o_full + 8 * t, 1); mbar_init(b_o_empty + 8 * t, 4); }
     for (int s = 0; s < SLOTS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_ready + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
     for (int s = 0; s < ITEMS; ++s) { mbar_init(b_item + 8 * s, 1); mbar_init(b_free + 8 * s, F::WARPS - 1); }
     *abort_flag = 0;
@@ -566,15 +566,19 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           if (t >= tiles) break;
-          alive = pa_wait(b_p + 8 * t, p_phase[t], abort_flag, 0x2500u | t);
-          p_phase[t] ^= 1u;
+          alive = pa_wait(b_p + 16 * t, p_phase[t], abort_flag, 0x2500u | t);
           if (alive && j == 0) { alive = pa_wait(b_o_empty + 8 * t, o_phase[t], abort_flag, 0x2580u | t); o_phase[t] ^= 1u; }
           if (!alive) break;
           pa_fence_after();
           const uint64_t v = pa_desc(sV, F::KV_BOX);
 #pragma unroll
-          for (int e = 0; e < BLK / 16; ++e)
-            if (leader) pa_mma_ts(tmem + 128u * (NT + t), tmem + 128u * t + 8u * e, v + (uint64_t)(e * (2048 >> 4)), IDESC_O, (j | e) ? 1u : 0u);
+          for (int half = 0; half < 2; ++half) {                   // the first 64 keys' product runs while the others' probabilities are computed
+            if (half) { alive = pa_wait(b_p + 16 * t + 8, p_phase[t], abort_flag, 0x2540u | t); p_phase[t] ^= 1u; if (!alive) break; pa_fence_after(); }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (leader) pa_mma_ts(tmem + 128u * (NT + t), tmem + 128u * t + 32u * half + 8u * e, v + (uint64_t)((4 * half + e) * (2048 >> 4)), IDESC_O, (j | half | e) ? 1u : 0u);
+          }
+          if (!alive) break;
           if (!more && leader) pa_commit(b_o_full + 8 * t);
           if (more) {
             if (t == 0) sK = next_slot(k_bar);
@@ -657,15 +661,23 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
               uint32_t packed[QW / 2];
               l[q] = add_quarter(l[q], alpha, quarter_probs<DT>(s + 32 * q, packed, p.c, shift), m, mb);
               pa_st16(t_s + 16u * q, packed);
+              if (q == 1) {
+                // the scores of this block are complete, so the product of the block before is too: O may be rescaled
+                if (b > it.b0 && __any_sync(0xffffffffu, live && alpha != 1.0f)) rescale<HDP>(t_o, alpha);
+                pa_wait_st();
+                pa_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(b_p + 16 * t);
+              }
             }
-            // the scores of this block are complete, so the product of the block before is too: O may be rescaled
-            if (b > it.b0 && __any_sync(0xffffffffu, live && alpha != 1.0f)) rescale<HDP>(t_o, alpha);
             pa_wait_st();
             pa_fence_before();
+          } else if (lane == 0) {
+            mbar_arrive(b_p + 16 * t);
           }
           s_phase ^= 1u;
           __syncwarp();
-          if (lane == 0) mbar_arrive(b_p + 8 * t);
+          if (lane == 0) mbar_arrive(b_p + 16 * t + 8);
         }
         if (!alive) break;
       }
