@@ -365,7 +365,7 @@ rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_r
  * sees no key gives zeros and -inf.  What a row does not see never reaches it, infinities and NaN in masked keys and
  * values included; where a NaN or infinite value is seen the answer's element is NaN or infinite.
  *   split   0, or a multiple of 128: keys [i * split, (i + 1) * split) form a part with a maximum, sum and product of
- *           its own, and the parts are joined in ascending order.  It decides bits (rows of one `split` have the same
+ *           its own, and the parts are joined in ascending order (by sixteens, and the sixteens then).  It decides bits (rows of one `split` have the same
  *           bits alone and in a chunk) and it spreads few rows with many keys over the GPU: 256 to 512 for single
  *           tokens, 0 for long chunks.
  * q, out: [tokens][query heads][dim]; q of the caches' type, bf16 or fp16; out of that type or fp32.  dim is a

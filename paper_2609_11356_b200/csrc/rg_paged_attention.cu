@@ -455,6 +455,8 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   __syncthreads();
   pa_fence_after();
   const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");               // the set-up ran under the tail of the kernel in front; from here on its results are read
+  if (p.segments > 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int cta_tokens = NT * p.tile_tokens;
 
   // Next item, for the warps that get it from the producer; false: none left, or a wait gave up.
@@ -895,6 +897,8 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
   __syncthreads();
   pa_fence_after();
   const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");               // the set-up ran under the tail of the kernel in front; from here on its results are read
+  if (p.segments > 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   Ring<ITEMS> ir;
   auto next_item = [&](Item& it, bool& alive) -> bool {
@@ -1203,10 +1207,17 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
   }
 }
 
-// Joins the parts of a row in ascending order.  A warp a row, four columns a lane.
-__global__ void __launch_bounds__(128) join_parts_kernel(const __grid_constant__ Params p) {
-  const int lane = threadIdx.x & 31;
-  const int64_t grow = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+// Joins the parts of a row: parts of one sixteen (by their number) in ascending order, then the sixteens in ascending order.  A warp sums a
+// sixteen, four columns a lane and sixteen loads in flight; WARPS of them take the sixteens of one row in turn.  With WARPS = 1 (no sequence can have
+// more than 16 parts) every warp of a CTA has a row of its own: 2048 rows of up to 16 parts; a single long row would leave most of them without work.
+constexpr int JOIN_THREADS = 256;
+template <int WARPS>
+__global__ void __launch_bounds__(JOIN_THREADS) join_parts_kernel(const __grid_constant__ Params p) {
+  __shared__ float4 s_o[WARPS > 1 ? WARPS : 1][32];
+  __shared__ float s_l[WARPS > 1 ? WARPS : 1], s_m[WARPS > 1 ? WARPS : 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  asm volatile("griddepcontrol.wait;" ::: "memory");               // the parts are the kernel's in front
+  const int64_t grow = WARPS > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (JOIN_THREADS / 32) + warp;
   if (grow >= p.tokens * p.hq) return;
   const int64_t token = grow / p.hq;
   const int head = (int)(grow - token * p.hq);
@@ -1223,40 +1234,86 @@ __global__ void __launch_bounds__(128) join_parts_kernel(const __grid_constant__
   const int ga = hi >= lo ? lo / p.split : 0, gb = hi >= lo ? hi / p.split + 1 : 0;
   const float2* ml = p.part_ml + grow * p.segments;
   float m = -INFINITY;
-  for (int g = ga + lane; g < gb; g += 32) m = fmaxf(m, ml[g].x);
+  for (int g = ga + (WARPS > 1 ? (int)threadIdx.x : lane); g < gb; g += WARPS > 1 ? JOIN_THREADS : 32) m = fmaxf(m, ml[g].x);
 #pragma unroll
   for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+  if (WARPS > 1) {
+    if (lane == 0) s_m[warp] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) m = fmaxf(m, s_m[w]);
+  }
   float l = 0.0f;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   const bool mine = 4 * lane < p.d;
   const float* po = p.part_o + grow * p.segments * p.d + 4 * lane;
-  for (int base = ga; base < gb; base += 32) {
+  for (int base = ga / 16; base * 16 < gb; base += WARPS) {        // sixteens base .. base + WARPS - 1
+    const int first = 16 * (base + (WARPS > 1 ? warp : 0));
     float w = 0.0f, wl = 0.0f;
-    if (base + lane < gb) {
-      const float2 x = ml[base + lane];
+    const int g = first + (lane & 15);
+    if (g >= ga && g < gb) {
+      const float2 x = ml[g];
       w = x.x == -INFINITY ? 0.0f : pa_ex2(f_mul(f_add(x.x, -m), p.c));
       wl = f_mul(w, x.y);
     }
-    const int count = min(32, gb - base);
-#pragma unroll 8
-    for (int i = 0; i < count; ++i) {
+    float4 x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      x[i] = mine && first + i >= ga && first + i < gb ? *reinterpret_cast<const float4*>(po + (int64_t)(first + i) * p.d) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float al = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
       const float wi = __shfl_sync(0xffffffffu, w, i);
-      l = f_add(l, __shfl_sync(0xffffffffu, wl, i));
-      if (mine) {
-        const float4 x = *reinterpret_cast<const float4*>(po + (int64_t)(base + i) * p.d);
-        o.x = f_fma(wi, x.x, o.x); o.y = f_fma(wi, x.y, o.y); o.z = f_fma(wi, x.z, o.z); o.w = f_fma(wi, x.w, o.w);
+      al = f_add(al, __shfl_sync(0xffffffffu, wl, i));
+      a.x = f_fma(wi, x[i].x, a.x); a.y = f_fma(wi, x[i].y, a.y); a.z = f_fma(wi, x[i].z, a.z); a.w = f_fma(wi, x[i].w, a.w);
+    }
+    if (WARPS > 1) {
+      s_o[warp][lane] = a;
+      if (lane == 0) s_l[warp] = al;
+      __syncthreads();
+      if (warp == 0) {
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) {                          // a sixteen without parts is zeros
+          const float4 y = s_o[k][lane];
+          o.x = f_add(o.x, y.x); o.y = f_add(o.y, y.y); o.z = f_add(o.z, y.z); o.w = f_add(o.w, y.w);
+          l = f_add(l, s_l[k]);
+        }
       }
+      __syncthreads();
+    } else {
+      o.x = f_add(o.x, a.x); o.y = f_add(o.y, a.y); o.z = f_add(o.z, a.z); o.w = f_add(o.w, a.w);
+      l = f_add(l, al);
     }
   }
+  if (WARPS > 1 && warp) return;
   const bool none = !(l > 0.0f) && l == l;
   const float inv = none ? 0.0f : __frcp_rn(l);
   if (mine) {
     const float r[4] = {none ? 0.0f : f_mul(o.x, inv), none ? 0.0f : f_mul(o.y, inv), none ? 0.0f : f_mul(o.z, inv), none ? 0.0f : f_mul(o.w, inv)};
     const int64_t at = token * p.o_tok + head * p.o_head + 4 * lane;
+    if (p.o_vec && p.o_dtype == RG_F32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = make_float4(r[0], r[1], r[2], r[3]);
+    else if (p.o_vec) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = make_uint2(pack_16x2(r[0], r[1], p.o_dtype), pack_16x2(r[2], r[3], p.o_dtype));
+    else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) store_scalar(p.out, p.o_dtype, at + i, r[i]);
+      for (int i = 0; i < 4; ++i) store_scalar(p.out, p.o_dtype, at + i, r[i]);
+    }
   }
   if (p.lse && lane == 0) p.lse[token * p.lse_ld + head] = none ? -INFINITY : f_add(f_mul(m, p.scale), logf(l));
+}
+template <int WARPS>
+cudaError_t launch_join(const Params& p, cudaStream_t st) {
+  const int64_t rows = p.tokens * p.hq;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(WARPS > 1 ? rows : (rows + JOIN_THREADS / 32 - 1) / (JOIN_THREADS / 32)), 1, 1);
+  cfg.blockDim = dim3(JOIN_THREADS, 1, 1);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // its launch runs under the main kernel, which it waits for
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, join_parts_kernel<WARPS>, p);
 }
 
 // ---------------------------------------------------------------- host
@@ -1269,8 +1326,17 @@ cudaError_t launch_form(Kernel kernel, DeviceOnce& configured, int ctas_per_sm, 
     if (e != cudaSuccess) return e;
     configured.set(dev.dev);
   }
-  kernel<<<(unsigned)std::min<int64_t>(most, (int64_t)dev.sms * ctas_per_sm), F::THREADS, F::SMEM, st>>>(q, k, v, p);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)std::min<int64_t>(most, (int64_t)dev.sms * ctas_per_sm), 1, 1);
+  cfg.blockDim = dim3(F::THREADS, 1, 1);
+  cfg.dynamicSmemBytes = F::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, q, k, v, p);
 }
 template <int HDP, int DT>
 cudaError_t launch_wide(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
@@ -1344,10 +1410,7 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   if (most >= (int64_t(1) << 31)) return RG_ERR_SHAPE;     // items are counted in 32 bits
   const cudaError_t e = a.q->dtype == RG_BF16 ? launch_any<RG_BF16>(rows, tq, tk, tv, p, most, st) : launch_any<RG_F16>(rows, tq, tk, tv, p, most, st);
   if (e != cudaSuccess) return RG_ERR_CUDA;
-  if (a.segments > 1) {
-    join_parts_kernel<<<(unsigned)((T * p.hq + 3) / 4), 128, 0, st>>>(p);
-    if (cudaGetLastError() != cudaSuccess) return RG_ERR_CUDA;
-  }
+  if (a.segments > 1 && (a.segments <= 16 ? launch_join<1>(p, st) : launch_join<JOIN_THREADS / 32>(p, st)) != cudaSuccess) return RG_ERR_CUDA;
   return RG_OK;
 }
 
