@@ -117,11 +117,11 @@ def load():
     L.rg_reduce_cols_workspace_bytes.restype = sz; L.rg_reduce_cols_workspace_bytes.argtypes = [i64, i64]
     L.rg_reduce_cols.restype = C.c_int; L.rg_reduce_cols.argtypes = [D, C.c_int, T, T, T, vp, sz, vp]
     L.rg_attention.restype = C.c_int; L.rg_attention.argtypes = [C.POINTER(rg_attn_desc_t), T, T, T, T, vp]
-    R, H, S, RD, PD = C.POINTER(rg_rows_t), C.POINTER(rg_cache_t), C.POINTER(rg_paged_seqs_t), C.POINTER(rg_rope_desc_t), C.POINTER(rg_paged_attn_desc_t)
-    L.rg_rope.restype = C.c_int; L.rg_rope.argtypes = [RD, R, T, vp, R, vp]
-    L.rg_kv_append.restype = C.c_int; L.rg_kv_append.argtypes = [RD, R, R, T, vp, H, H, S, R, R, vp]
-    L.rg_paged_attention_workspace_bytes.restype = sz; L.rg_paged_attention_workspace_bytes.argtypes = [PD, S, i64, i64, i64, i64]
-    L.rg_paged_attention.restype = C.c_int; L.rg_paged_attention.argtypes = [PD, R, H, H, S, R, vp, i64, vp, sz, vp]
+    # structures of these four are passed by reference or as packed bytes
+    L.rg_rope.restype = C.c_int; L.rg_rope.argtypes = [vp] * 6
+    L.rg_kv_append.restype = C.c_int; L.rg_kv_append.argtypes = [vp] * 11
+    L.rg_paged_attention_workspace_bytes.restype = sz; L.rg_paged_attention_workspace_bytes.argtypes = [vp, vp, i64, i64, i64, i64]
+    L.rg_paged_attention.restype = C.c_int; L.rg_paged_attention.argtypes = [vp] * 7 + [i64, vp, sz, vp]
     L.rg_gemm_noalloc.restype = C.c_int; L.rg_gemm_noalloc.argtypes = [D, T, T, T, E, vp]
     L.rg_selftest_bounded_wait.restype = C.c_int; L.rg_selftest_bounded_wait.argtypes = [C.c_uint64, vp, vp]
     L.rg_selftest_exp.restype = C.c_int; L.rg_selftest_exp.argtypes = [C.c_int32, vp, vp, C.c_int64, vp]

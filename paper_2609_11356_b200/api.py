@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional, Sequence
 
 from . import _cabi as K
@@ -237,34 +238,48 @@ def rg_reduce_rows_host_scratch_bytes(op, x, out) -> int:
 
 
 # ---------------------------------------------------------------- positions, paged cache, attention over it
-def _rows(t) -> K.rg_rows_t:
+# These calls are a few microseconds of GPU work in a decode step: their C structures are packed in one go (a ctypes structure
+# costs a microsecond more) and passed as bytes.
+_ROWS, _CACHE, _TENSOR = struct.Struct("@Pi5q"), struct.Struct("@Pi7q"), struct.Struct("@Pi3q")
+_CODES = {}
+
+
+def _code(t) -> int:
+    c = _CODES.get(t.dtype)
+    if c is None:
+        c = _CODES[t.dtype] = _dtype_code(t)
+    return c
+
+
+def _rows(t) -> bytes:
     if t.dim() != 3:
         raise ValueError(f"rows are [tokens, heads, dim], got a tensor of {t.dim()} dimensions")
     n, h, d = t.shape
     st, sh, sd = t.stride()
     if sd != 1 and d > 1:
         raise ValueError("the elements of a head must be contiguous")
-    return K.rg_rows_t(t.data_ptr(), _dtype_code(t), n, h, d, st, sh)
+    return _ROWS.pack(t.data_ptr(), _code(t), n, h, d, st, sh)
 
 
-def _cache(t) -> K.rg_cache_t:
+def _cache(t) -> bytes:
     if t.dim() != 4:
         raise ValueError(f"a cache is [pages, page_size, heads, dim], got a tensor of {t.dim()} dimensions")
-    if t.stride(3) != 1 and t.shape[3] > 1:
+    n, page, h, d = t.shape
+    sn, sp, sh, sd = t.stride()
+    if sd != 1 and d > 1:
         raise ValueError("the elements of a head must be contiguous")
-    return K.rg_cache_t(t.data_ptr(), _dtype_code(t), *t.shape, *t.stride()[:3])
+    return _CACHE.pack(t.data_ptr(), _code(t), n, page, h, d, sn, sp, sh)
 
 
-def _positions(pos) -> K.rg_tensor_t:
+def _positions(pos) -> bytes:
     import torch
     code = K.RG_I32 if pos.dtype == torch.int32 else K.RG_I64 if pos.dtype == torch.int64 else None
     if code is None:
         raise TypeError(f"positions are int32 or int64, got {pos.dtype}")
     if pos.dim() not in (1, 2) or (pos.shape[-1] > 1 and pos.stride(-1) != 1):
         raise ValueError("positions are [tokens] or [axes, tokens], contiguous along the tokens")
-    if pos.dim() == 1:
-        return K.rg_tensor_t(pos.data_ptr(), code, 1, pos.shape[0], pos.shape[0])
-    return K.rg_tensor_t(pos.data_ptr(), code, pos.shape[0], pos.shape[1], pos.stride(0))
+    n = pos.shape[-1]
+    return _TENSOR.pack(pos.data_ptr(), code, 1 if pos.dim() == 1 else pos.shape[0], n, n if pos.dim() == 1 else pos.stride(0))
 
 
 def _frequencies(inv_freq, d) -> int:
@@ -274,24 +289,26 @@ def _frequencies(inv_freq, d) -> int:
     return inv_freq.data_ptr()
 
 
-def _call(where: str, fn, device, *args):
+def _call(where: str, fn, device: int, *args):
     """One C call with `device` current and on its current stream."""
     import torch
-    if device.type != "cuda":
-        raise ValueError(f"{where}: tensors must be on a CUDA device, got {device}")
-    if device.index == torch.cuda.current_device():
-        st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    raw_stream = torch._C._cuda_getCurrentRawStream      # torch.cuda.current_stream(device).cuda_stream without the Python object around it
+    if device == torch.cuda.current_device():
+        st = fn(*args, raw_stream(device))
     else:
         with torch.cuda.device(device):
-            st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
-    _check(st, where)
+            st = fn(*args, raw_stream(device))
+    if st != K.RG_OK:
+        raise RgError(st, where)
 
 
-def _one_device(where: str, *tensors):
-    device = tensors[0].device
+def _one_device(where: str, *tensors) -> int:
+    device = tensors[0].get_device()
     for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"{where}: tensors on {device} and {t.device}")
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{where}: tensors on different devices")
+    if device < 0:
+        raise ValueError(f"{where}: tensors must be on a CUDA device")
     return device
 
 
@@ -311,7 +328,7 @@ def rg_rope(d: K.rg_rope_desc_t, x, pos, inv_freq, out):
     """out = x [tokens, heads, dim] rotated by `pos` ([tokens] or [axes, tokens], int32 or int64); inv_freq: float64 [rot_dim / 2],
     radians per position.  out may be x."""
     device = _one_device("rg_rope", x, pos, inv_freq, out)
-    _call("rg_rope", K.load().rg_rope, device, C.byref(d), C.byref(_rows(x)), C.byref(_positions(pos)), _frequencies(inv_freq, d), C.byref(_rows(out)))
+    _call("rg_rope", K.load().rg_rope, device, C.byref(d), _rows(x), _positions(pos), _frequencies(inv_freq, d), _rows(out))
     return out
 
 
@@ -319,6 +336,9 @@ class rg_paged_seqs:
     """The sequences of a batch (see include/rg.h): int32 CUDA tensors block_table [n, pages], seq_lens [n] and cu_q [n + 1], and the
     host's bounds of new tokens in one sequence and of seq_lens (0: none known).  The tensors are read when the kernels run."""
     __slots__ = ("block_table", "seq_lens", "cu_q", "device", "c")
+
+    def get_device(self) -> int:
+        return self.device
 
     def __init__(self, block_table, seq_lens, cu_q, *, max_q: int = 0, max_len: int = 0):
         import torch
@@ -328,7 +348,9 @@ class rg_paged_seqs:
         n = seq_lens.shape[0]
         if block_table.shape[0] != n or cu_q.shape[0] != n + 1:
             raise ValueError(f"{n} sequences need block_table [{n}, pages] and cu_q [{n + 1}], got {tuple(block_table.shape)} and {tuple(cu_q.shape)}")
-        self.device = _one_device("rg_paged_seqs", seq_lens, block_table, cu_q)
+        if not block_table.device == seq_lens.device == cu_q.device:
+            raise ValueError("rg_paged_seqs: tensors on different devices")
+        self.device = seq_lens.get_device()
         self.block_table, self.seq_lens, self.cu_q = block_table, seq_lens, cu_q
         self.c = K.rg_paged_seqs_t(block_table.data_ptr(), max(block_table.stride(0), block_table.shape[1]) if n > 1 else block_table.shape[1], block_table.shape[1], n,
                                    seq_lens.data_ptr(), cu_q.data_ptr(), max_q, max_len)
@@ -339,10 +361,9 @@ def rg_kv_append(d, k, v, inv_freq, k_cache, v_cache, seqs: rg_paged_seqs, *, po
     if (q is None) != (q_out is None):
         raise ValueError("rg_kv_append: q and q_out go together")
     device = _one_device("rg_kv_append", k, v, inv_freq, k_cache, v_cache, seqs, pos, q, q_out)
-    _call("rg_kv_append", K.load().rg_kv_append, device, C.byref(d) if d is not None else None, C.byref(_rows(k)), C.byref(_rows(v)),
-          C.byref(_positions(pos)) if pos is not None else None, _frequencies(inv_freq, d) if inv_freq is not None and d is not None else None,
-          C.byref(_cache(k_cache)), C.byref(_cache(v_cache)), C.byref(seqs.c),
-          C.byref(_rows(q)) if q is not None else None, C.byref(_rows(q_out)) if q_out is not None else None)
+    _call("rg_kv_append", K.load().rg_kv_append, device, C.byref(d) if d is not None else None, _rows(k), _rows(v),
+          _positions(pos) if pos is not None else None, _frequencies(inv_freq, d) if inv_freq is not None and d is not None else None,
+          _cache(k_cache), _cache(v_cache), C.byref(seqs.c), _rows(q) if q is not None else None, _rows(q_out) if q_out is not None else None)
 
 
 def rg_paged_attn_desc(*, scale: float, split: int = 0, window: int = 0, mask: int = 1) -> K.rg_paged_attn_desc_t:
@@ -367,7 +388,7 @@ def rg_paged_attention(d: K.rg_paged_attn_desc_t, q, k_cache, v_cache, seqs: rg_
     device = _one_device("rg_paged_attention", q, k_cache, v_cache, seqs, out, lse, ws)
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or (lse.shape[1] > 1 and lse.stride(1) != 1)):
         raise ValueError("lse is float32 [tokens, heads], contiguous along the heads")
-    _call("rg_paged_attention", K.load().rg_paged_attention, device, C.byref(d), C.byref(_rows(q)), C.byref(_cache(k_cache)), C.byref(_cache(v_cache)),
-          C.byref(seqs.c), C.byref(_rows(out)), lse.data_ptr() if lse is not None else None, max(lse.stride(0), lse.shape[1]) if lse is not None else 0,
+    _call("rg_paged_attention", K.load().rg_paged_attention, device, C.byref(d), _rows(q), _cache(k_cache), _cache(v_cache), C.byref(seqs.c), _rows(out),
+          lse.data_ptr() if lse is not None else None, max(lse.stride(0), lse.shape[1]) if lse is not None else 0,
           ws.data_ptr() if ws is not None else None, ws.numel() * ws.element_size() if ws is not None else 0)
     return out

@@ -140,7 +140,7 @@ struct Params {
   int32_t hq, hkv, group, d;
   int32_t tile_tokens;                   // tokens of one tile: floor(rows of a tile / group)
   int32_t box;                           // keys of one TMA box
-  int32_t split, segments, causal;
+  int32_t split, segments, causal, levels;
   int32_t window;
   float scale, c;                        // c = scale * log2(e)
   void* out;
@@ -188,24 +188,47 @@ __device__ __forceinline__ void parts_of(const Params& p, const SeqView& v, int3
   if (p.split && hi >= lo) { *g0 = (int32_t)(lo / p.split); *n = (int32_t)(hi / p.split) - *g0 + 1; }
 }
 
-// The items of this CTA: number blockIdx.x, + gridDim.x, ... in the order sequence, tile (the last, longest first), part, head; 32 sequences at a
-// time, one a lane.  The producer walks them and hands them to the other warps in shared memory.
+// The items of this CTA out of the list level, sequence, tile (the last, longest first), part, head.  Every CTA takes one of each gridDim.x of
+// them, from the front and from the back in turn.  A level holds the tiles that see a like number of keys, the most first: work of unlike
+// size then comes out even (9 prompts' chunks of 45 to 986 rows: the busiest CTA has 1.08 times the mean's work, with sequences just
+// taken in turn 1.44).  Parts are alike and many sequences even out by themselves: one level.  32 sequences at a time, one a lane.  The
+// producer walks the list and hands the items to the other warps in shared memory.
 struct Walk {
-  uint32_t next;                         // number of the next item, counted from the first item of the lane group
-  uint32_t before, count, total;          // this lane's sequence: items before it in the group, its own; the group's
-  int32_t base;                          // first sequence of the group
+  uint32_t next, step[2];                // number of the next item, counted from the first item of the lane group, and how far the ones after it are
+  uint32_t before, count, total;         // this lane's sequence: items before it in the group, its own; the group's
+  int32_t base, level;                   // first sequence of the group
+  int32_t most;                          // keys of the longest tile, about
+  int32_t t_end;                         // this lane's sequence: end of its tiles of the level
   SeqView mine;                          // this lane's sequence
-  __device__ __forceinline__ void load(const Params& p, int tile_tokens) {
-    const int lane = threadIdx.x & 31, s = base + lane;
-    count = 0;
+  // keys that tile i sees, about, and never fewer than the tile before: tiles that see fewer than x
+  __device__ __forceinline__ int32_t below(const Params& p, int tile_tokens, int32_t tiles, int32_t x) const {
+    const int32_t cap = p.window ? p.window + tile_tokens : INT32_MAX;
+    if (!p.causal || x > cap) return x > (p.causal ? cap : mine.len) ? tiles : 0;
+    return min(max((x - mine.first + tile_tokens - 1) / tile_tokens - 1, 0), tiles);
+  }
+  __device__ __forceinline__ void look_up(const Params& p) {
+    const int s = base + (threadIdx.x & 31);
+    mine = SeqView{0, 0, 0, 0};
     if (s < p.n_seqs) {
       bool bad;
-      const SeqView v = mine = view_of(p, s, &bad);
+      mine = view_of(p, s, &bad);
       if (bad) atomicCAS(&g_paged_attn_status_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
-      int32_t g0, n;
-      parts_of(p, v, &g0, &n);
-      count = (uint32_t)((v.n + tile_tokens - 1) / tile_tokens) * n * p.hkv;
     }
+  }
+  __device__ __forceinline__ void load(const Params& p, int tile_tokens) {
+    const int lane = threadIdx.x & 31;
+    if (p.n_seqs > 32 || p.levels == 1) look_up(p);
+    int32_t g0, n;
+    parts_of(p, mine, &g0, &n);
+    const int32_t tiles = (mine.n + tile_tokens - 1) / tile_tokens;
+    int32_t t0 = 0;
+    t_end = tiles;
+    if (p.levels > 1 && mine.n > 0) {
+      t0 = below(p, tile_tokens, tiles, (int32_t)((int64_t)most * level / p.levels));
+      if (level + 1 < p.levels) t_end = max(t0, below(p, tile_tokens, tiles, (int32_t)((int64_t)most * (level + 1) / p.levels)));
+      if (level == 0) t0 = 0;
+    }
+    count = (uint32_t)(t_end - t0) * n * p.hkv;
     uint32_t sum = count;
 #pragma unroll
     for (int x = 1; x < 32; x <<= 1) {
@@ -215,17 +238,38 @@ struct Walk {
     before = sum - count;
     total = __shfl_sync(0xffffffffu, sum, 31);
   }
-  __device__ __forceinline__ void start(const Params& p, int tile_tokens) { base = 0; next = blockIdx.x; load(p, tile_tokens); }
+  __device__ __forceinline__ void start(const Params& p, int tile_tokens) {
+    most = 0;
+    if (p.levels > 1) {
+      for (base = 0; base < p.n_seqs; base += 32) {
+        look_up(p);
+        const int32_t all = mine.n ? mine.len + tile_tokens : 0;
+        most = max(most, __reduce_max_sync(0xffffffffu, p.causal && p.window ? min(all, p.window + tile_tokens) : all));
+      }
+    }
+    base = 0;
+    level = p.levels - 1;
+    next = blockIdx.x;
+    step[0] = 2 * (gridDim.x - 1 - blockIdx.x) + 1;
+    step[1] = 2 * blockIdx.x + 1;
+    load(p, tile_tokens);
+  }
   __device__ __forceinline__ bool get(const Params& p, int tile_tokens, Item& it) {
     while (next >= total) {
       next -= total;
       base += 32;
-      if (base >= p.n_seqs) return false;
+      if (base >= p.n_seqs) {
+        base = 0;
+        if (--level < 0) return false;
+      }
       load(p, tile_tokens);
     }
     const int owner = __ffs(__ballot_sync(0xffffffffu, next >= before && next < before + count)) - 1;
     const uint32_t local = next - __shfl_sync(0xffffffffu, before, owner);
-    next += gridDim.x;
+    next += step[0];
+    const uint32_t swap = step[0];
+    step[0] = step[1];
+    step[1] = swap;
     it.seq = base + owner;
     SeqView v;
     v.tok = __shfl_sync(0xffffffffu, mine.tok, owner); v.len = __shfl_sync(0xffffffffu, mine.len, owner);
@@ -236,7 +280,7 @@ struct Walk {
     const uint32_t rest = local / (uint32_t)p.hkv;
     it.head = (int32_t)(local - rest * p.hkv);
     it.seg = (int32_t)(rest % (uint32_t)n);
-    const int32_t tiles = (v.n + tile_tokens - 1) / tile_tokens, tile = tiles - 1 - (int32_t)(rest / (uint32_t)n);
+    const int32_t tile = __shfl_sync(0xffffffffu, t_end, owner) - 1 - (int32_t)(rest / (uint32_t)n);
     const int32_t t0 = tile * tile_tokens;
     it.n_tok = min(tile_tokens, v.n - t0);
     it.tok = v.tok + t0;
@@ -1386,10 +1430,9 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   if (a.ws) p.part_ml = reinterpret_cast<float2*>(p.part_o + T * p.hq * (int64_t)a.segments * d);
   p.v = static_cast<const uint16_t*>(a.v->ptr); p.v_page = a.v->page_stride; p.v_slot = a.v->slot_stride; p.v_head = a.v->head_stride;
 
-  // The form for few rows where a sequence's new rows of a key head fit one of its tiles: 8, 16 or (heads of 64: the tile's operands have to
-  // fit half an SM) 32 rows.
   const int64_t need = a.max_q * G;
-  const int rows = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 && d <= 64 ? 32 : 128;
+  const int most_rows = d <= 64 ? 32 : 16, FEW_TILES = 1;
+  const int rows = need <= 8 ? 8 : need <= 16 ? 16 : G <= most_rows && need <= FEW_TILES * most_rows ? most_rows : 128;
   const bool narrow = rows < 128;
   p.tile_tokens = rows / G;
   int box = page & -page;                                  // the largest power of two that divides the page size: boxes never cross pages
@@ -1404,6 +1447,7 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
       !make_tmap_4d(&tv, vp, a.q->dtype, {d, page, hkv, pages}, {a.v->slot_stride, a.v->head_stride, a.v->page_stride}, {64, box, 1, 1}))
     return RG_ERR_CUDA;
 
+  p.levels = a.split == 0 && p.n_seqs <= 128 ? 16 : 1;
   // no more CTAs than there can be items
   const int cta_tokens = p.tile_tokens * (narrow ? 1 : 2);
   const int64_t most = std::min<int64_t>(T, (T + cta_tokens - 1) / cta_tokens + p.n_seqs) * hkv * a.segments;
