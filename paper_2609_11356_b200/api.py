@@ -241,7 +241,7 @@ def rg_reduce_rows_host_scratch_bytes(op, x, out) -> int:
 # These calls are a few microseconds of GPU work in a decode step: their C structures are packed in one go (a ctypes structure
 # costs a microsecond more) and passed as bytes.
 _ROWS, _CACHE, _TENSOR = struct.Struct("@Pi5q"), struct.Struct("@Pi7q"), struct.Struct("@Pi3q")
-_CODES = {}
+_CODES, _POSITION_CODES = {}, {}
 
 
 def _code(t) -> int:
@@ -272,14 +272,20 @@ def _cache(t) -> bytes:
 
 
 def _positions(pos) -> bytes:
-    import torch
-    code = K.RG_I32 if pos.dtype == torch.int32 else K.RG_I64 if pos.dtype == torch.int64 else None
+    code = _POSITION_CODES.get(pos.dtype)
     if code is None:
-        raise TypeError(f"positions are int32 or int64, got {pos.dtype}")
-    if pos.dim() not in (1, 2) or (pos.shape[-1] > 1 and pos.stride(-1) != 1):
+        import torch
+        _POSITION_CODES.update({torch.int32: K.RG_I32, torch.int64: K.RG_I64})
+        if pos.dtype not in _POSITION_CODES:
+            raise TypeError(f"positions are int32 or int64, got {pos.dtype}")
+        code = _POSITION_CODES[pos.dtype]
+    shape, stride = pos.shape, pos.stride()
+    n = shape[-1] if shape else 0
+    if len(shape) not in (1, 2) or (n > 1 and stride[-1] != 1):
         raise ValueError("positions are [tokens] or [axes, tokens], contiguous along the tokens")
-    n = pos.shape[-1]
-    return _TENSOR.pack(pos.data_ptr(), code, 1 if pos.dim() == 1 else pos.shape[0], n, n if pos.dim() == 1 else pos.stride(0))
+    if len(shape) == 1:
+        return _TENSOR.pack(pos.data_ptr(), code, 1, n, n)
+    return _TENSOR.pack(pos.data_ptr(), code, shape[0], n, stride[0])
 
 
 def _frequencies(inv_freq, d) -> int:

@@ -94,6 +94,7 @@ struct RopeParams {
   int64_t pages;
   int32_t table_cols, n_seqs, page_size;
   int32_t tile, head_group;            // tokens and heads of a CTA
+  uint32_t inv_units, inv_per_tok;     // 2^32 over a head's units and over a token's units of the CTA, rounded up; 0 for one unit
 };
 rg_status_t launch_rope(RopeParams p, int dtype, bool paged, cudaStream_t st);
 rg_status_t read_and_clear_paged_status(uint32_t* code);

@@ -11,6 +11,9 @@
 // computed once per CTA into shared memory (about 100 instructions for each pair, against all heads that use it) and
 // every thread then moves 2 * VEC elements of one head at a time with 16-byte accesses.  One launch rotates the
 // queries, rotates the keys into their pages and copies the values into theirs.
+#include <algorithm>
+#include <type_traits>
+
 #include "rg_common.cuh"
 #include "rg_internal.h"
 
@@ -83,18 +86,68 @@ __device__ __forceinline__ bool place_of(const RopeParams& p, int64_t t, int& se
   return true;
 }
 
+// Units a thread has in flight before the CTA works out its angles.  Alone the rotation gains by four (8192 tokens of 32 heads of 128, 134 MB:
+// 28 -> 23.4 us, 5.7 TB/s).  With the cache (three sets of strides, places to look up) the registers they take cost more than they bring (257 MB: 49 us
+// without, 54 with); there more CTAs at once do it.
+template <bool PAGED> constexpr int BATCH = PAGED ? 1 : 4;
+constexpr int PAGED_UNITS = 8;                         // units of a thread with the cache, one after the other (257 MB: 48 us with four, 46.7 with eight)
+
 template <int DT, int VEC, bool PAGED>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constant__ RopeParams p) {
+__global__ void __launch_bounds__(ROPE_THREADS, PAGED ? 6 : 4) rope_kernel(const __grid_constant__ RopeParams p) {
   using P = Pack<DT, VEC>;
   using Raw = typename P::Raw;
-  constexpr int ES = DT == RG_F32 ? 4 : 2;
-  extern __shared__ float2 cs[];                        // [tokens of the CTA][rot / 2] (cos, sin)
+  constexpr int ES = DT == RG_F32 ? 4 : 2, FLY = BATCH<PAGED>;
+  extern __shared__ __align__(16) float2 cs[];                        // [tokens of the CTA][rot / 2] (cos, sin)
   __shared__ int64_t s_page[ROPE_TOKENS];               // page of the token's slot; -1: no place for its key and value; -2: not a row at all
   __shared__ int32_t s_slot[ROPE_TOKENS];
   __shared__ int64_t s_pos[ROPE_TOKENS];
   const int64_t t0 = (int64_t)blockIdx.x * p.tile;
   const int n_tok = (int)min((int64_t)p.tile, p.tokens - t0);
   const int half = p.rot >> 1;
+  const int h0 = blockIdx.y * p.head_group, n_heads = min(p.head_group, p.heads_all - h0);
+  const int units = p.d / (2 * VEC), turned = half / VEC;   // a unit is 2 * VEC elements of one head
+  const int per_tok = p.head_group * units, all = n_tok * per_tok;      // the last group of heads may be short: its missing heads are passed over
+
+  // the i-th unit of the CTA: token, stream, head, unit of the head
+  auto find = [&](int i, int& t, int& k, int& h, int& u) -> bool {
+    t = p.inv_per_tok ? (int)__umulhi((uint32_t)i, p.inv_per_tok) : i;      // exact divisions: dividend times divisor stays below 2^32; 0: by one
+    const int r = i - t * per_tok;
+    h = p.inv_units ? (int)__umulhi((uint32_t)r, p.inv_units) : r;
+    u = r - h * units;
+    if (h >= n_heads) return false;
+    h += h0;
+    k = 0;
+    if (PAGED) {
+      if (h >= p.st[0].heads) { h -= p.st[0].heads; k = 1; }
+      if (k == 1 && h >= p.st[1].heads) { h -= p.st[1].heads; k = 2; }
+    }
+    return true;
+  };
+  // Where pair j's cosine and sine lie in the token's row: units side by side, so that the lanes of a warp, which hold neighbouring units, read
+  // neighbouring words (pair by pair they would read every 64th byte: four-way bank conflicts took a third of the time).
+  auto spot = [&](int j) -> int { return VEC == 1 ? j : ((j % VEC >> 1) * turned + j / VEC) * 2 + (j & 1); };
+  // element offsets of a unit's two vectors
+  auto offsets = [&](bool turn, int u, int& ea, int& eb) {
+    if (turn && p.style == RG_ROPE_HALF) { ea = u * VEC; eb = half + u * VEC; }
+    else { ea = 2 * u * VEC; eb = ea + VEC; }
+  };
+  Raw ra[FLY], rb[FLY];
+  auto load = [&](int first) {
+#pragma unroll
+    for (int q = 0; q < FLY; ++q) {
+      const int i = first + q * ROPE_THREADS;
+      if (i >= all) break;
+      int t, k, h, u, ea, eb;
+      if (!find(i, t, k, h, u)) continue;
+      const RopeStream& st = p.st[k];
+      offsets(u < turned && st.rotate, u, ea, eb);
+      const char* src = static_cast<const char*>(st.src) + ((t0 + t) * st.src_tok + h * st.src_head) * ES;
+      ra[q] = *reinterpret_cast<const Raw*>(src + ea * ES);
+      rb[q] = *reinterpret_cast<const Raw*>(src + eb * ES);
+    }
+  };
+  if (!PAGED) load(threadIdx.x);                        // on their way while the angles are worked out
+
   if (PAGED) {
     const int w = threadIdx.x >> 5;
     if (w < n_tok) {
@@ -126,70 +179,75 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
     const float frac = (float)(turns - rint(turns));
     float s, c;
     sincospif(2.0f * frac, &s, &c);
-    cs[i] = make_float2(c, p.inverse ? -s : s);
+    cs[t * half + spot(j)] = make_float2(c, p.inverse ? -s : s);
   }
   __syncthreads();
 
-  const int h0 = blockIdx.y * p.head_group, n_heads = min(p.head_group, p.heads_all - h0);
-  const int units = p.d / (2 * VEC), turned = half / VEC;   // a unit is 2 * VEC elements of one head
-  const int per_tok = n_heads * units;
-  for (int i = threadIdx.x; i < n_tok * per_tok; i += ROPE_THREADS) {
-    const int t = i / per_tok, r = i - t * per_tok;
-    int h = r / units;
-    const int u = r - h * units;
-    h += h0;
-    int k = 0;
-    if (PAGED) {
-      if (h >= p.st[0].heads) { h -= p.st[0].heads; k = 1; }
-      if (k == 1 && h >= p.st[1].heads) { h -= p.st[1].heads; k = 2; }
-    }
-    const RopeStream& st = p.st[k];
-    const char* src = static_cast<const char*>(st.src) + ((t0 + t) * st.src_tok + h * st.src_head) * ES;
-    char* dst = static_cast<char*>(st.dst) + h * st.dst_head * ES;
-    if (PAGED) {
-      const int64_t page = s_page[t];
-      if (page == -2 || (st.paged && page < 0)) continue;
-      dst += st.paged ? (page * st.dst_page + s_slot[t] * st.dst_tok) * ES : (t0 + t) * st.dst_tok * ES;
-    } else {
-      dst += (t0 + t) * st.dst_tok * ES;
-    }
-    // element offsets of the unit's two vectors
-    int ea, eb;
-    const bool turn = u < turned && st.rotate;
-    if (turn && p.style == RG_ROPE_HALF) { ea = u * VEC; eb = half + u * VEC; }
-    else { ea = 2 * u * VEC; eb = ea + VEC; }
-    Raw ra = *reinterpret_cast<const Raw*>(src + ea * ES), rb = *reinterpret_cast<const Raw*>(src + eb * ES);
-    if (turn) {
-      const float2* f = cs + t * half + u * VEC;
-      float a[VEC], b[VEC];
-      P::get(ra, a); P::get(rb, b);
-      if (p.style == RG_ROPE_HALF || VEC == 1) {
+  for (int first = threadIdx.x; first < all; first += FLY * ROPE_THREADS) {
+    if (PAGED || first != threadIdx.x) load(first);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float2 w = f[e];
-          const float x = a[e], y = b[e];
-          a[e] = f_fma(-y, w.y, f_mul(x, w.x));
-          b[e] = f_fma(x, w.y, f_mul(y, w.x));
-        }
+    for (int q = 0; q < FLY; ++q) {
+      const int i = first + q * ROPE_THREADS;
+      if (i >= all) break;
+      int t, k, h, u, ea, eb;
+      if (!find(i, t, k, h, u)) continue;
+      const RopeStream& st = p.st[k];
+      const bool turn = u < turned && st.rotate;
+      offsets(turn, u, ea, eb);
+      char* dst = static_cast<char*>(st.dst) + h * st.dst_head * ES;
+      if (PAGED) {
+        const int64_t page = s_page[t];
+        if (page == -2 || (st.paged && page < 0)) continue;
+        dst += st.paged ? (page * st.dst_page + s_slot[t] * st.dst_tok) * ES : (t0 + t) * st.dst_tok * ES;
       } else {
-        constexpr int H = VEC > 1 ? VEC / 2 : 1;
-        float v[2 * VEC];
+        dst += (t0 + t) * st.dst_tok * ES;
+      }
+      Raw wa = ra[q], wb = rb[q];
+      if (turn) {
+        float2 f[VEC];
+        if constexpr (VEC == 1) {
+          f[0] = cs[t * half + u];
+        } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) { v[e] = a[e]; v[VEC + e] = b[e]; }
-#pragma unroll
-        for (int e = 0; e < 2 * H; ++e) {
-          const float2 w = f[e];
-          const float x = v[2 * e], y = v[2 * e + 1];
-          v[2 * e] = f_fma(-y, w.y, f_mul(x, w.x));
-          v[2 * e + 1] = f_fma(x, w.y, f_mul(y, w.x));
+          for (int e = 0; e < VEC; e += 2) {
+            const float4 w = *reinterpret_cast<const float4*>(cs + t * half + ((e >> 1) * turned + u) * 2);
+            f[e] = make_float2(w.x, w.y);
+            f[e + 1 < VEC ? e + 1 : e] = make_float2(w.z, w.w);
+          }
         }
+        float v[2 * VEC];
+        {
+          float a[VEC], b[VEC];
+          P::get(wa, a); P::get(wb, b);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) { v[e] = a[e]; v[VEC + e] = b[e]; }
+        }
+        // pair e of the unit: elements e and VEC + e, or the neighbours 2e and 2e + 1
+        if (p.style == RG_ROPE_HALF || VEC == 1) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const float2 w = f[e];
+            const float x = v[e], y = v[VEC + e];
+            v[e] = f_fma(-y, w.y, f_mul(x, w.x));
+            v[VEC + e] = f_fma(x, w.y, f_mul(y, w.x));
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const float2 w = f[e];
+            const float x = v[2 * e], y = v[2 * e + 1];
+            v[2 * e] = f_fma(-y, w.y, f_mul(x, w.x));
+            v[2 * e + 1] = f_fma(x, w.y, f_mul(y, w.x));
+          }
+        }
+        float a[VEC], b[VEC];
 #pragma unroll
         for (int e = 0; e < VEC; ++e) { a[e] = v[e]; b[e] = v[VEC + e]; }
+        wa = P::put(a); wb = P::put(b);
       }
-      ra = P::put(a); rb = P::put(b);
+      *reinterpret_cast<Raw*>(dst + ea * ES) = wa;
+      *reinterpret_cast<Raw*>(dst + eb * ES) = wb;
     }
-    *reinterpret_cast<Raw*>(dst + ea * ES) = ra;
-    *reinterpret_cast<Raw*>(dst + eb * ES) = rb;
   }
 }
 
@@ -225,16 +283,19 @@ rg_status_t launch_rope(RopeParams p, int dtype, bool paged, cudaStream_t st) {
   for (int k = 0; k < p.n_streams; ++k) p.heads_all += p.st[k].heads;
   const int units = p.d / (2 * vec);
   const int sms = current_device().sms;
-  // tokens of a CTA: as many as give each thread a few units, while the grid still covers the GPU
+  // tokens of a CTA: as many as give a thread its units, while the grid still covers the GPU
   int64_t tile = 1;
-  while (tile < ROPE_TOKENS && tile * p.heads_all * units < 4 * ROPE_THREADS && (p.tokens + 2 * tile - 1) / (2 * tile) >= 4 * sms) tile *= 2;
-  // few tokens: their heads are dealt to several CTAs, one unit a thread
-  int groups = 1;
+  while (tile < ROPE_TOKENS && 2 * tile * p.heads_all * units <= (paged ? PAGED_UNITS : BATCH<false>) * ROPE_THREADS && (p.tokens + 2 * tile - 1) / (2 * tile) >= 4 * sms) tile *= 2;
+  // heads of a CTA: all, unless few tokens leave SMs without work; at most 8192 units a token keep the kernel's divisions exact
   const int64_t tiles = (p.tokens + tile - 1) / tile;
+  int groups = (int)(((int64_t)p.heads_all * units + 8191) / 8192);
   while (tiles * groups < 2 * sms && groups < p.heads_all && tile * ((p.heads_all + groups - 1) / groups) * units > ROPE_THREADS) ++groups;
   p.tile = (int)tile;
   p.head_group = (p.heads_all + groups - 1) / groups;
   groups = (p.heads_all + p.head_group - 1) / p.head_group;
+  auto inverse = [](uint32_t n) { return n > 1 ? (uint32_t)((uint64_t(1) << 32) / n + 1) : 0u; };
+  p.inv_units = inverse(units);
+  p.inv_per_tok = inverse((uint32_t)p.head_group * units);
   const dim3 grid((unsigned)tiles, (unsigned)groups, 1);
   const size_t smem = (size_t)tile * (p.rot / 2) * sizeof(float2);
   cudaError_t e;
