@@ -133,11 +133,24 @@ __host__ __device__ constexpr uint32_t pa_idesc(int n, bool bf16, bool a_transpo
 }
 
 // ---------------------------------------------------------------- arguments and work items
+// Division of numbers below 2^31 by a fixed one: n * ceil(2^(31 + s) / d) / 2^(31 + s), s = ceil(log2 d).  (The hardware has none: a
+// division is some 40 instructions in a row, and eight of them stood in front of a single token's first copy.)
+struct Div {
+  uint32_t d, mul, shift;                // mul = 0: by one
+  static Div by(uint32_t d) {
+    uint32_t s = 0;
+    while ((uint64_t(1) << s) < d) ++s;
+    return {d, d > 1 ? (uint32_t)(((uint64_t(1) << (31 + s)) + d - 1) / d) : 0u, s ? s - 1 : 0u};
+  }
+};
+__device__ __forceinline__ int32_t operator/(int32_t n, const Div& v) { return v.mul ? (int32_t)(__umulhi((uint32_t)n, v.mul) >> v.shift) : n; }
+
 struct Params {
   const int32_t *table, *seq_lens, *cu_q;
   int64_t table_ld, max_len, tokens;
   int32_t n_seqs, page_size, pages, table_cols;
   int32_t hq, hkv, group, d;
+  Div by_split, by_hkv, by_hq, by_page, by_group, by_tile;   // by_tile: a CTA's tokens
   int32_t tile_tokens;                   // tokens of one tile: floor(rows of a tile / group)
   int32_t box;                           // keys of one TMA box
   int32_t split, segments, causal, levels;
@@ -185,7 +198,7 @@ __device__ __forceinline__ int32_t first_seen(const Params& p, int32_t place) { 
 __device__ __forceinline__ void parts_of(const Params& p, const SeqView& v, int32_t* g0, int32_t* n) {
   const int32_t hi = last_seen(p, v.len - 1, v.len), lo = first_seen(p, max(v.first, 0));
   *g0 = 0; *n = 1;
-  if (p.split && hi >= lo) { *g0 = (int32_t)(lo / p.split); *n = (int32_t)(hi / p.split) - *g0 + 1; }
+  if (p.split && hi >= lo) { *g0 = lo / p.by_split; *n = hi / p.by_split - *g0 + 1; }
 }
 
 // The items of this CTA out of the list level, sequence, tile (the last, longest first), part, head.  Every CTA takes one of each gridDim.x of
@@ -204,7 +217,7 @@ struct Walk {
   __device__ __forceinline__ int32_t below(const Params& p, int tile_tokens, int32_t tiles, int32_t x) const {
     const int32_t cap = p.window ? p.window + tile_tokens : INT32_MAX;
     if (!p.causal || x > cap) return x > (p.causal ? cap : mine.len) ? tiles : 0;
-    return min(max((x - mine.first + tile_tokens - 1) / tile_tokens - 1, 0), tiles);
+    return min(max(max(x - mine.first + tile_tokens - 1, 0) / p.by_tile - 1, 0), tiles);
   }
   __device__ __forceinline__ void look_up(const Params& p) {
     const int s = base + (threadIdx.x & 31);
@@ -220,7 +233,7 @@ struct Walk {
     if (p.n_seqs > 32 || p.levels == 1) look_up(p);
     int32_t g0, n;
     parts_of(p, mine, &g0, &n);
-    const int32_t tiles = (mine.n + tile_tokens - 1) / tile_tokens;
+    const int32_t tiles = (mine.n + tile_tokens - 1) / p.by_tile;
     int32_t t0 = 0;
     t_end = tiles;
     if (p.levels > 1 && mine.n > 0) {
@@ -277,10 +290,10 @@ struct Walk {
     v.first = v.len - v.n;
     int32_t g0, n;
     parts_of(p, v, &g0, &n);
-    const uint32_t rest = local / (uint32_t)p.hkv;
-    it.head = (int32_t)(local - rest * p.hkv);
-    it.seg = (int32_t)(rest % (uint32_t)n);
-    const int32_t tile = __shfl_sync(0xffffffffu, t_end, owner) - 1 - (int32_t)(rest / (uint32_t)n);
+    const int32_t rest = (int32_t)local / p.by_hkv, turn = n > 1 ? rest / n : rest;
+    it.head = (int32_t)local - rest * p.hkv;
+    it.seg = rest - turn * n;
+    const int32_t tile = __shfl_sync(0xffffffffu, t_end, owner) - 1 - turn;
     const int32_t t0 = tile * tile_tokens;
     it.n_tok = min(tile_tokens, v.n - t0);
     it.tok = v.tok + t0;
@@ -521,7 +534,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   if (warp == F::PRODUCER) {
     // ------------------------------------------------------------ producer
     const int pieces = BLK / p.box;                                // TMA boxes along the keys of a block
-    const int piece = lane % pieces, col = lane / pieces;          // col < DB: this lane issues a box
+    const int piece = lane & (pieces - 1), col = lane / pieces;          // col < DB: this lane issues a box
     Ring<SLOTS> kv;
     uint32_t q_phase = 1;
     Walk walk;
@@ -537,7 +550,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
       if (it.b1 == it.b0) continue;
       const int32_t* row = p.table + (int64_t)it.seq * p.table_ld;
       auto wanted = [&](int b) -> bool { const int32_t k = b * BLK + piece * p.box; return col < DB && k <= it.hi && k + p.box > it.lo; };
-      auto entry = [&](int b) -> int32_t { return row[(b * BLK + piece * p.box) / p.page_size]; };
+      auto entry = [&](int b) -> int32_t { return row[(b * BLK + piece * p.box) / p.by_page]; };
       int32_t ahead = wanted(it.b0) ? entry(it.b0) : 0;
       alive = pa_wait(b_q_empty, q_phase, abort_flag, 0x2100u);
       if (!alive) break;
@@ -557,7 +570,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
           if (col == 0) atomicCAS(&g_paged_attn_status_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
           page = p.pages;
         }
-        const int32_t at = (b * BLK + piece * p.box) % p.page_size;
+        const int32_t key = b * BLK + piece * p.box, at = key - key / p.by_page * p.page_size;
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)p.box * 128u;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
@@ -671,7 +684,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
     const int t = warp >> 2;                                       // tile
     const int r = (warp & 3) * 32 + lane;                          // row of the tile, and its lane in tensor memory
     const uint32_t t_s = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128u * t, t_o = t_s + 128u * NT;
-    const int my_tok = r / p.group, my_head = r - my_tok * p.group;
+    const int my_tok = r / p.by_group, my_head = r - my_tok * p.group;
     uint32_t s_phase = 0, o_phase = 0, flags = 0;
     while (alive && next_item(it, alive)) {
       const int tok = t * p.tile_tokens + my_tok;                  // within the item
@@ -959,7 +972,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
   if (warp == F::PRODUCER) {
     // ------------------------------------------------------------ producer: K_0, K_1, V_0, K_2, V_1, ..., as they are used
     const int pieces = BLK / p.box;
-    const int piece = lane % pieces, col = lane / pieces;
+    const int piece = lane & (pieces - 1), col = lane / pieces;
     Ring<SLOTS> kv;
     uint32_t q_phase = 1;
     Walk walk;
@@ -975,7 +988,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       if (it.b1 == it.b0) continue;
       const int32_t* row = p.table + (int64_t)it.seq * p.table_ld;
       auto wanted = [&](int b) -> bool { const int32_t k = b * BLK + piece * p.box; return col < DB && b < it.b1 && k <= it.hi && k + p.box > it.lo; };
-      auto entry = [&](int b) -> int32_t { return row[(b * BLK + piece * p.box) / p.page_size]; };
+      auto entry = [&](int b) -> int32_t { return row[(b * BLK + piece * p.box) / p.by_page]; };
       int32_t page = wanted(it.b0) ? entry(it.b0) : 0, next = wanted(it.b0 + 1) ? entry(it.b0 + 1) : 0;      // looked up a block ahead of their use
       alive = pa_wait(b_q_empty, q_phase, abort_flag, 0x3100u);
       if (!alive) break;
@@ -989,7 +1002,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
           if (col == 0) atomicCAS(&g_paged_attn_status_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
           id = p.pages;
         }
-        const int32_t at = (b * BLK + piece * p.box) % p.page_size;
+        const int32_t key = b * BLK + piece * p.box, at = key - key / p.by_page * p.page_size;
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)p.box * 128u;
         alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x3200u | kv.slot);
         if (!alive) return;
@@ -1090,7 +1103,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     // ------------------------------------------------------------ softmax and output rows
     constexpr int SH = ROWS == 8 ? 2 : ROWS == 16 ? 1 : 0;         // lane i looks after row i >> SH
     const int r = lane >> SH;
-    const int my_tok = r / p.group;
+    const int my_tok = r / p.by_group;
     const uint32_t t_lane = tmem + (static_cast<uint32_t>(warp * 32) << 16);
     uint32_t block = 0, n_item = 0, flags = 0;
     uint8_t* p_row = smem_gen + F::P_AT + (warp >> 1) * F::P_BOX + (lane & 7) * 2;     // this key's place in the rows of P: 16-byte pieces of 8 keys, swizzled
@@ -1261,26 +1274,47 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_parts_kernel(const __grid_c
   __shared__ float s_l[WARPS > 1 ? WARPS : 1], s_m[WARPS > 1 ? WARPS : 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   asm volatile("griddepcontrol.wait;" ::: "memory");               // the parts are the kernel's in front
-  const int64_t grow = WARPS > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (JOIN_THREADS / 32) + warp;
-  if (grow >= p.tokens * p.hq) return;
-  const int64_t token = grow / p.hq;
-  const int head = (int)(grow - token * p.hq);
-  int before = 0;
-  for (int i = lane; i < p.n_seqs; i += 32) before += p.cu_q[i + 1] <= token ? 1 : 0;
-  const int s = __reduce_add_sync(0xffffffffu, before);
-  if (s >= p.n_seqs || token < p.cu_q[s]) return;
-  bool bad;
-  const SeqView v = view_of(p, s, &bad);
+  const int32_t grow = WARPS > 1 ? (int32_t)blockIdx.x : (int32_t)blockIdx.x * (JOIN_THREADS / 32) + warp;
+  if (grow >= (int32_t)(p.tokens * p.hq)) return;
+  const int32_t token = grow / p.by_hq;
+  const int head = grow - token * p.hq;
+  // the row's sequence: the first that ends behind it.  Its lengths come with the search.
+  SeqView v = {0, 0, 0, 0};
+  bool found = false;
+  for (int base = 0; base < p.n_seqs && !found; base += 32) {
+    bool bad;
+    if (base + lane < p.n_seqs) v = view_of(p, base + lane, &bad);
+    else v = SeqView{INT32_MAX, 0, 0, 0};
+    const uint32_t hit = __ballot_sync(0xffffffffu, v.tok <= token && token < v.tok + v.n);
+    found = hit != 0;
+    const int owner = found ? __ffs(hit) - 1 : 0;
+    v.tok = __shfl_sync(0xffffffffu, v.tok, owner); v.len = __shfl_sync(0xffffffffu, v.len, owner);
+    v.first = __shfl_sync(0xffffffffu, v.first, owner); v.n = __shfl_sync(0xffffffffu, v.n, owner);
+  }
+  if (!found) return;
   int32_t g0, n;
   parts_of(p, v, &g0, &n);
   if (n <= 1) return;                                              // written by the main kernel
-  const int32_t place = v.first + (int32_t)(token - v.tok), hi = last_seen(p, place, v.len), lo = first_seen(p, max(place, 0));
-  const int ga = hi >= lo ? lo / p.split : 0, gb = hi >= lo ? hi / p.split + 1 : 0;
-  const float2* ml = p.part_ml + grow * p.segments;
-  float m = -INFINITY;
-  for (int g = ga + (WARPS > 1 ? (int)threadIdx.x : lane); g < gb; g += WARPS > 1 ? JOIN_THREADS : 32) m = fmaxf(m, ml[g].x);
+  const int32_t place = v.first + (token - v.tok), hi = last_seen(p, place, v.len), lo = first_seen(p, max(place, 0));
+  const int ga = hi >= lo ? lo / p.by_split : 0, gb = hi >= lo ? hi / p.by_split + 1 : 0;
+  const float2* ml = p.part_ml + (int64_t)grow * p.segments;
+  const bool mine = 4 * lane < p.d;
+  const float* po = p.part_o + (int64_t)grow * p.segments * p.d + 4 * lane;
+  // a sixteen's products, maxima and sums; the first one of each warp is on its way before the row's maximum is known
+  float4 x[16];
+  float2 xml;
+  auto fetch = [&](int base) {
+    const int first = 16 * (base + (WARPS > 1 ? warp : 0)), g = first + (lane & 15);
+    xml = g >= ga && g < gb ? ml[g] : make_float2(-INFINITY, 0.0f);
 #pragma unroll
-  for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+    for (int i = 0; i < 16; ++i)
+      x[i] = mine && first + i >= ga && first + i < gb ? *reinterpret_cast<const float4*>(po + (int64_t)(first + i) * p.d) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  };
+  fetch(ga / 16);
+  float m = xml.x;
+  for (int g = ga / 16 * 16 + 16 * WARPS + (WARPS > 1 ? (int)threadIdx.x : lane); g < gb; g += WARPS > 1 ? JOIN_THREADS : 32) m = fmaxf(m, ml[g].x);
+#pragma unroll
+  for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
   if (WARPS > 1) {
     if (lane == 0) s_m[warp] = m;
     __syncthreads();
@@ -1289,21 +1323,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_parts_kernel(const __grid_c
   }
   float l = 0.0f;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  const bool mine = 4 * lane < p.d;
-  const float* po = p.part_o + grow * p.segments * p.d + 4 * lane;
   for (int base = ga / 16; base * 16 < gb; base += WARPS) {        // sixteens base .. base + WARPS - 1
-    const int first = 16 * (base + (WARPS > 1 ? warp : 0));
-    float w = 0.0f, wl = 0.0f;
-    const int g = first + (lane & 15);
-    if (g >= ga && g < gb) {
-      const float2 x = ml[g];
-      w = x.x == -INFINITY ? 0.0f : pa_ex2(f_mul(f_add(x.x, -m), p.c));
-      wl = f_mul(w, x.y);
-    }
-    float4 x[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      x[i] = mine && first + i >= ga && first + i < gb ? *reinterpret_cast<const float4*>(po + (int64_t)(first + i) * p.d) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (base != ga / 16) fetch(base);
+    const float w = xml.x == -INFINITY ? 0.0f : pa_ex2(f_mul(f_add(xml.x, -m), p.c)), wl = f_mul(w, xml.y);
     float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     float al = 0.0f;
 #pragma unroll
@@ -1335,7 +1357,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_parts_kernel(const __grid_c
   const float inv = none ? 0.0f : __frcp_rn(l);
   if (mine) {
     const float r[4] = {none ? 0.0f : f_mul(o.x, inv), none ? 0.0f : f_mul(o.y, inv), none ? 0.0f : f_mul(o.z, inv), none ? 0.0f : f_mul(o.w, inv)};
-    const int64_t at = token * p.o_tok + head * p.o_head + 4 * lane;
+    const int64_t at = (int64_t)token * p.o_tok + head * p.o_head + 4 * lane;
     if (p.o_vec && p.o_dtype == RG_F32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = make_float4(r[0], r[1], r[2], r[3]);
     else if (p.o_vec) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at) = make_uint2(pack_16x2(r[0], r[1], p.o_dtype), pack_16x2(r[2], r[3], p.o_dtype));
     else {
@@ -1343,7 +1365,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_parts_kernel(const __grid_c
       for (int i = 0; i < 4; ++i) store_scalar(p.out, p.o_dtype, at + i, r[i]);
     }
   }
-  if (p.lse && lane == 0) p.lse[token * p.lse_ld + head] = none ? -INFINITY : f_add(f_mul(m, p.scale), logf(l));
+  if (p.lse && lane == 0) p.lse[(int64_t)token * p.lse_ld + head] = none ? -INFINITY : f_add(f_mul(m, p.scale), logf(l));
 }
 template <int WARPS>
 cudaError_t launch_join(const Params& p, cudaStream_t st) {
@@ -1447,11 +1469,13 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
       !make_tmap_4d(&tv, vp, a.q->dtype, {d, page, hkv, pages}, {a.v->slot_stride, a.v->head_stride, a.v->page_stride}, {64, box, 1, 1}))
     return RG_ERR_CUDA;
 
+  p.by_split = Div::by(p.split ? p.split : 1); p.by_hkv = Div::by(p.hkv); p.by_hq = Div::by(p.hq); p.by_page = Div::by(page); p.by_group = Div::by(G);
+  p.by_tile = Div::by(p.tile_tokens * (narrow ? 1 : 2));
   p.levels = a.split == 0 && p.n_seqs <= 128 ? 16 : 1;
   // no more CTAs than there can be items
   const int cta_tokens = p.tile_tokens * (narrow ? 1 : 2);
   const int64_t most = std::min<int64_t>(T, (T + cta_tokens - 1) / cta_tokens + p.n_seqs) * hkv * a.segments;
-  if (most >= (int64_t(1) << 31)) return RG_ERR_SHAPE;     // items are counted in 32 bits
+  if (most >= (int64_t(1) << 31) || T * p.hq >= (int64_t(1) << 31)) return RG_ERR_SHAPE;     // items and rows are counted in 32 bits
   const cudaError_t e = a.q->dtype == RG_BF16 ? launch_any<RG_BF16>(rows, tq, tk, tv, p, most, st) : launch_any<RG_F16>(rows, tq, tk, tv, p, most, st);
   if (e != cudaSuccess) return RG_ERR_CUDA;
   if (a.segments > 1 && (a.segments <= 16 ? launch_join<1>(p, st) : launch_join<JOIN_THREADS / 32>(p, st)) != cudaSuccess) return RG_ERR_CUDA;
