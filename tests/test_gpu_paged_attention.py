@@ -304,3 +304,56 @@ def test_refusals():
         run(q=b.Q.cpu())
     empty = torch.zeros(0, 4, 64, dtype=BF, device=DEV)
     rg.rg_paged_attention(d, empty, b.kc, b.vc, b.seqs(), empty)                 # nothing to do is fine
+
+
+def test_what_is_visible_and_not_finite_arrives():
+    """A NaN key makes the rows that see it NaN, others keep their bits; a score of +inf likewise."""
+    for q_len, split in ((1, 0), (1, 128), (150, 0), (150, 128)):
+        b = Batch([q_len], [500], hq=4, hkv=2, d=64, page=16, seed=3)
+        ok, okz = attend(b, split=split)
+        for at in (100, 499 - q_len // 2):
+            page, slot = (x[at] for x in b.where(0))
+            keep = b.kc[page, slot].clone()
+            for bad in (float("nan"), float("inf")):
+                b.kc[page, slot, 1, 5] = bad
+                got, gz = attend(b, split=split)
+                row = max(0, at - (500 - q_len))
+                assert torch.equal(got[:row], ok[:row]) and torch.equal(got[:, :2], ok[:, :2])
+                hit = got[row:, 2:]
+                if bad != bad:
+                    assert bool(torch.isnan(hit).all()) and bool(torch.isnan(gz[row:, 2:]).all())
+                else:                                                           # +inf or -inf by the query's sign: NaN, or the key drops out
+                    up = b.Q[row:, 2:, 5] > 0
+                    assert bool(torch.isnan(hit[up]).all()) and bool(torch.isfinite(hit[~up]).all())
+                b.kc[page, slot] = keep
+
+
+@pytest.mark.parametrize("split", [0, 128])
+def test_pages_in_front_of_the_window_may_be_gone(split):
+    b = Batch([1, 20], [700, 500], hq=4, hkv=2, d=64, page=16, seed=7)
+    w = 130
+    ok, okz = attend(b, window=w, split=split)
+    check(b, ok, okz, window=w)
+    for i, (n, m) in enumerate(zip(b.q_lens, b.kv_lens)):
+        b.table[i, :(m - n - w + 1) // 16] = -1
+    got, gz = attend(b, window=w, split=split)
+    assert torch.equal(got, ok) and torch.equal(gz, okz)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_drawn_shapes(seed):
+    import random
+    r = random.Random(seed)
+    hkv = r.choice([1, 2, 3, 8])
+    n = r.choice([1, 2, 5, 40])
+    q = [r.choice([0, 1, 1, r.randint(1, 6), r.randint(1, 200)]) for _ in range(n)]
+    kv = [x + r.choice([0, r.randint(0, 300), r.randint(0, 2500)]) for x in q]
+    if sum(q) == 0:
+        q[0], kv[0] = 1, kv[0] + 1
+    b = Batch(q, kv, hq=hkv * r.choice([1, 2, 3, 4, 7, 16]), hkv=hkv, d=r.choice([16, 64, 88, 128]), page=r.choice([8, 16, 40, 128]), dtype=r.choice([BF, HF]), seed=seed,
+              heads_first=r.random() < 0.5, tail_rows=r.choice([0, 3]), spread=r.choice([0.3, 1.0, 2.0]))
+    window = r.choice([0, 0, r.randint(1, 600)])
+    mask = 1 if window else r.choice([1, 1, 0])
+    split = r.choice([0, 0, 128, 384, 512])
+    seqs = b.seqs(max_q=r.choice([0, 1, max(q)]), max_len=r.choice([0, max(kv)]))
+    check(b, *attend(b, window=window, mask=mask, split=split, seqs=seqs, out_dtype=r.choice([None, torch.float32])), window=window, mask=mask)
