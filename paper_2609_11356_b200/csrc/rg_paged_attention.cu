@@ -151,7 +151,7 @@ struct Params {
   int32_t n_seqs, page_size, pages, table_cols;
   int32_t hq, hkv, group, d;
   Div by_split, by_hkv, by_hq, by_page, by_group, by_tile;   // by_tile: a CTA's tokens
-  int32_t tile_tokens;                   // tokens of one tile: floor(rows of a tile / group)
+  int32_t tile_tokens, cta_tokens;       // tokens of one tile: floor(rows of a tile / group); of a CTA: one tile's or two tiles'
   int32_t box;                           // keys of one TMA box
   int32_t split, segments, causal, levels;
   int32_t window;
@@ -209,8 +209,9 @@ __device__ __forceinline__ void parts_of(const Params& p, const SeqView& v, int3
 struct Walk {
   uint32_t next, step[2];                // number of the next item, counted from the first item of the lane group, and how far the ones after it are
   uint32_t before, count, total;         // this lane's sequence: items before it in the group, its own; the group's
-  int32_t base, level;                   // first sequence of the group
-  int32_t most;                          // keys of the longest tile, about
+  int32_t base, level, levels;           // first sequence of the group
+  int32_t least, most;                   // keys of the shortest and of the longest tile, about
+  uint32_t left;                         // items of the list from the next one on (levels only): behind the last none is looked for
   int32_t t_end;                         // this lane's sequence: end of its tiles of the level
   SeqView mine;                          // this lane's sequence
   // keys that tile i sees, about, and never fewer than the tile before: tiles that see fewer than x
@@ -230,16 +231,16 @@ struct Walk {
   }
   __device__ __forceinline__ void load(const Params& p, int tile_tokens) {
     const int lane = threadIdx.x & 31;
-    if (p.n_seqs > 32 || p.levels == 1) look_up(p);
+    if (p.n_seqs > 32 || levels == 1) look_up(p);
     int32_t g0, n;
     parts_of(p, mine, &g0, &n);
     const int32_t tiles = (mine.n + tile_tokens - 1) / p.by_tile;
     int32_t t0 = 0;
     t_end = tiles;
-    if (p.levels > 1 && mine.n > 0) {
-      t0 = below(p, tile_tokens, tiles, (int32_t)((int64_t)most * level / p.levels));
-      if (level + 1 < p.levels) t_end = max(t0, below(p, tile_tokens, tiles, (int32_t)((int64_t)most * (level + 1) / p.levels)));
-      if (level == 0) t0 = 0;
+    if (levels > 1 && mine.n > 0) {
+      const int64_t range = (int64_t)most - least + 1;
+      if (level > 0) t0 = below(p, tile_tokens, tiles, least + (int32_t)(range * level / levels));
+      if (level + 1 < levels) t_end = max(t0, below(p, tile_tokens, tiles, least + (int32_t)(range * (level + 1) / levels)));
     }
     count = (uint32_t)(t_end - t0) * n * p.hkv;
     uint32_t sum = count;
@@ -253,21 +254,31 @@ struct Walk {
   }
   __device__ __forceinline__ void start(const Params& p, int tile_tokens) {
     most = 0;
-    if (p.levels > 1) {
+    least = INT32_MAX;
+    left = UINT32_MAX;
+    levels = p.levels;
+    if (levels > 1) {
+      left = 0;
       for (base = 0; base < p.n_seqs; base += 32) {
         look_up(p);
-        const int32_t all = mine.n ? mine.len + tile_tokens : 0;
-        most = max(most, __reduce_max_sync(0xffffffffu, p.causal && p.window ? min(all, p.window + tile_tokens) : all));
+        const int32_t cap = p.causal && p.window ? p.window + tile_tokens : INT32_MAX, first = p.causal ? mine.first + tile_tokens : mine.len;
+        most = max(most, __reduce_max_sync(0xffffffffu, mine.n ? min(p.causal ? mine.len + tile_tokens : mine.len, cap) : 0));
+        least = min(least, __reduce_min_sync(0xffffffffu, mine.n ? min(first, cap) : INT32_MAX));
+        left += __reduce_add_sync(0xffffffffu, (uint32_t)((mine.n + tile_tokens - 1) / p.by_tile) * p.hkv);
       }
+      least = min(least, most);
+      if (left <= gridDim.x) levels = 1;                           // an item each: nothing to even out
+      left -= min(left, blockIdx.x);
     }
     base = 0;
-    level = p.levels - 1;
+    level = levels - 1;
     next = blockIdx.x;
     step[0] = 2 * (gridDim.x - 1 - blockIdx.x) + 1;
     step[1] = 2 * blockIdx.x + 1;
     load(p, tile_tokens);
   }
   __device__ __forceinline__ bool get(const Params& p, int tile_tokens, Item& it) {
+    if (left == 0) return false;
     while (next >= total) {
       next -= total;
       base += 32;
@@ -280,6 +291,7 @@ struct Walk {
     const int owner = __ffs(__ballot_sync(0xffffffffu, next >= before && next < before + count)) - 1;
     const uint32_t local = next - __shfl_sync(0xffffffffu, before, owner);
     next += step[0];
+    left -= p.levels > 1 ? min(left, step[0]) : 0;
     const uint32_t swap = step[0];
     step[0] = step[1];
     step[1] = swap;
@@ -514,7 +526,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   const uint32_t tmem = *tmem_slot;
   asm volatile("griddepcontrol.wait;" ::: "memory");               // the set-up ran under the tail of the kernel in front; from here on its results are read
   if (p.segments > 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int cta_tokens = NT * p.tile_tokens;
+  const int cta_tokens = p.cta_tokens;
 
   // Next item, for the warps that get it from the producer; false: none left, or a wait gave up.
   Ring<ITEMS> ir;
@@ -1470,11 +1482,14 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
     return RG_ERR_CUDA;
 
   p.by_split = Div::by(p.split ? p.split : 1); p.by_hkv = Div::by(p.hkv); p.by_hq = Div::by(p.hq); p.by_page = Div::by(page); p.by_group = Div::by(G);
-  p.by_tile = Div::by(p.tile_tokens * (narrow ? 1 : 2));
-  p.levels = a.split == 0 && p.n_seqs <= 128 ? 16 : 1;
+  // Two tiles share the keys that a CTA reads and the tensor core works for one while the other's softmax runs; but where all tiles find an SM
+  // each, one tile alone is done sooner (about 2600 cycles a block against 3500).
+  auto items_of = [&](int64_t tokens) { return std::min<int64_t>(T, (T + tokens - 1) / tokens + p.n_seqs) * hkv * a.segments; };
+  p.cta_tokens = narrow || items_of(p.tile_tokens) <= current_device().sms ? p.tile_tokens : 2 * p.tile_tokens;
+  p.by_tile = Div::by(p.cta_tokens);
+  p.levels = a.split != 0 || p.n_seqs > 128 ? 1 : p.n_seqs > 32 ? 8 : 16;      // a level is a walk over all sequences
   // no more CTAs than there can be items
-  const int cta_tokens = p.tile_tokens * (narrow ? 1 : 2);
-  const int64_t most = std::min<int64_t>(T, (T + cta_tokens - 1) / cta_tokens + p.n_seqs) * hkv * a.segments;
+  const int64_t most = items_of(p.cta_tokens);
   if (most >= (int64_t(1) << 31) || T * p.hq >= (int64_t(1) << 31)) return RG_ERR_SHAPE;     // items and rows are counted in 32 bits
   const cudaError_t e = a.q->dtype == RG_BF16 ? launch_any<RG_BF16>(rows, tq, tk, tv, p, most, st) : launch_any<RG_F16>(rows, tq, tk, tv, p, most, st);
   if (e != cudaSuccess) return RG_ERR_CUDA;
