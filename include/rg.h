@@ -359,7 +359,7 @@ rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_r
  * Keys are walked in blocks of 128 places; with s_t = scale * (q . k_t) in fp32 from tensor-core chains over dim,
  *   p_t = exp(s_t - m),   l += sum of the block's p_t,   O += (P . V)_block,   P = p narrowed to the cache's type
  * where m is a running maximum that moves (and O and l are rescaled, in fp32) only when a block's maximum exceeds
- * it by more than 8 / log2(e); the answer is O / l, rounded once.  exp is the hardware's base-two exponential for some of the
+ * it by more than 8 / log2(e); the answer is O times 1 / l, rounded once.  exp is the hardware's base-two exponential for some of the
  * elements and a polynomial of IEEE operations for the others, by the key's place: bits repeat on this architecture.
  * lse (may be NULL): [tokens][query heads] of stride lse_ld, fp32: the natural logarithm of the sum of exp(s_t).  A row that
  * sees no key gives zeros and -inf.  What a row does not see never reaches it, infinities and NaN in masked keys and
@@ -368,9 +368,11 @@ rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_r
  *           its own, and the parts are joined in ascending order (by sixteens, and the sixteens then).  It decides bits (rows of one `split` have the same
  *           bits alone and in a chunk) and it spreads few rows with many keys over the GPU: 256 to 512 for single
  *           tokens, 0 for long chunks.
+ * Pages that lie wholly in front of every new row's window are not read; their table entries may be anything.
  * q, out: [tokens][query heads][dim]; q of the caches' type, bf16 or fp16; out of that type or fp32.  dim is a
- * multiple of 8 up to 128; query heads a multiple of kv heads, at most 128 for each; page_size a multiple of 8.
- * q and caches: 16-byte aligned, strides multiples of 8 elements, else RG_ERR_ALIGNMENT.  ws: at least
+ * multiple of 8 up to 128; query heads a multiple of kv heads, at most 128 for each; page_size a multiple of 8;
+ * tokens times query heads below 2^31.
+ * q and caches: 16-byte aligned, strides multiples of 8 elements (else RG_ERR_ALIGNMENT) and not 0.  ws: at least
  * rg_paged_attention_workspace_bytes(...), 16-byte aligned; calls (or graphs) that share one must not overlap.
  * Asynchronous on `cuda_stream`. */
 typedef struct {

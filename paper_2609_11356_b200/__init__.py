@@ -1,4 +1,4 @@
-"""rg — reduction-order-fixed GEMM and row reductions for B200 (sm_100a).
+"""rg — reduction-order-fixed GEMM, row reductions and attention for B200 (sm_100a).
 
 Thin Python binding over the C ABI of ``include/rg.h``; torch supplies device memory and
 streams only.  Every arithmetic step runs in the CUDA library.

@@ -8,21 +8,24 @@
 // and at the end O * (1 / l).  A running maximum that may lag by 2^8 costs nothing in precision (p is a floating-point number
 // below 2^8) and saves nearly every rescaling of O, which lives in tensor memory.
 //
-// A row's arithmetic is written once (softmax_block) and does not know the tile it is in: a block that the row does not
-// see adds exact zeros, so the row has the same bits as a single token, in a chunk, in any batch and on any pages.
+// The sum is kept for each quarter of a block's keys (32 of them, added as a butterfly adds them) and the four are joined at the end.  All of it is one
+// fixed order in both kernels below, and neither knows which other rows there are: a block that a row does not see adds exact zeros, so
+// a row has the same bits as a single token, in a chunk, in any batch and on any pages.
 //
-// One CTA, by warp:
+// paged_attention_wide_kernel, for many rows: two tiles of 128 rows, one CTA an SM; while one tile's softmax runs the tensor core works for the other.
 //   softmax (4 warps a tile)  scores from tensor memory into registers, probabilities back over them as the first operand
 //                             of the next product; row r of a tile is TMEM lane r, so maxima and sums need no exchange
-//   producer                  page numbers, then one TMA box for each page piece (a lane each): K and V blocks into one ring
+//   producer                  work items, page numbers, then one TMA box for each page piece (a lane each): K and V blocks into one ring
 //   MMA                       S_t = Q_t K_j^T and O_t += P_t V_j for the CTA's tiles in turn
 //   fixer                     hands each arrived slot to the MMA warp; in blocks where some row is masked it first turns V elements
 //                             that are not finite into zeros (0 * NaN would reach every row of the tile).  Rows that do see such an element
 //                             get it added back when they are stored (rare, from global memory).
-// Two forms of one kernel:
-//   wide    two tiles of 128 rows, one CTA an SM: while one tile's softmax runs the tensor core works for the other
-//   narrow  one tile of up to 32 rows (single tokens and drafts), two CTAs an SM: bound by the K and V bytes, the second CTA
-//           covers the latency of the first's chain of product, softmax, product
+//   A chunk of 4096 rows on 16384 keys, 32 heads of 128 on 8 key heads: 0.88-0.90 ms, 1.07-1.10 PFLOP/s.  What bounds it: 512 items on 148 SMs are
+//   four turns of which the last is half empty (0.86), and a tile's chain of product, commit, 112 hardware exponentials a lane and quarter-rate
+//   unit, product (about 3500 cycles for the two tiles' 2048 of the tensor core).  Tried there: all exponentials on the hardware unit 950 us, an eighth
+//   by the polynomial 896, a quarter 906-925, three eighths 985; two threads a row (16 softmax warps) 1070; scores read twice instead of held in
+//   registers 1090.
+// paged_attention_few_kernel, for single tokens and drafts: further down.
 // The grid is persistent: the work items (sequence, tile, part, key head) are counted out of the sequences' lengths on the device, so
 // nothing is read back and a captured graph follows the lengths of the day.
 #include <cuda.h>
@@ -861,6 +864,10 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
 //   O' += V_j^T P^T    lane = element of the head, column = row of queries; V is read transposed, P from shared memory
 // A softmax thread is one key of the block and holds its score with every row; maxima and sums over the keys go through butterflies
 // in which lanes trade rows (after five steps a lane holds one row's value), and the four warps' maxima through shared memory.
+// What bounds it: the K and V bytes.  64 sequences of up to 8192 keys, 8 key heads of 128 (1.14 GB): 188 us, 6.05 TB/s; 4 of up to 61000 (0.76 GB): 128 us,
+// 5.9 TB/s; one of 8192 (34 MB): 12 us, of which the copies are 5 (launch, item and page look-up, the chain of two blocks and the join are latency).
+// With the queries as the 128 rows instead (the other form, 4 of them filled) the 64 sequences took 234 us, and 278 with each row's keys dealt to
+// four warps: the tensor core then reads 128 mostly empty rows from shared memory for every step.
 template <int HDP, int ROWS>
 struct Few {
   static constexpr int DB = HDP / 64;
