@@ -146,6 +146,9 @@ __global__ void __launch_bounds__(ROPE_THREADS, PAGED ? 6 : 4) rope_kernel(const
       rb[q] = *reinterpret_cast<const Raw*>(src + eb * ES);
     }
   };
+  // what the kernel in front wrote is read from here on; the one behind may be set up meanwhile (it waits in the same way)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (!PAGED) load(threadIdx.x);                        // on their way while the angles are worked out
 
   if (PAGED) {
@@ -253,9 +256,17 @@ __global__ void __launch_bounds__(ROPE_THREADS, PAGED ? 6 : 4) rope_kernel(const
 
 template <int DT, int VEC>
 cudaError_t launch(const RopeParams& p, dim3 grid, size_t smem, bool paged, cudaStream_t st) {
-  if (paged) rope_kernel<DT, VEC, true><<<grid, ROPE_THREADS, smem, st>>>(p);
-  else rope_kernel<DT, VEC, false><<<grid, ROPE_THREADS, smem, st>>>(p);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(ROPE_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, paged ? rope_kernel<DT, VEC, true> : rope_kernel<DT, VEC, false>, p);
 }
 
 }  // namespace
