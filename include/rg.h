@@ -379,7 +379,7 @@ typedef struct {
   uint32_t size;          /* = sizeof(rg_paged_attn_desc_t) */
   uint32_t split;
   uint32_t window;        /* 0 = none */
-  float scale;            /* finite, > 0 */
+  float scale;            /* > 0, at most 2e38 */
   uint8_t mask;           /* 0 = none, 1 = causal at the sequence's end */
   uint8_t _pad[3];
 } rg_paged_attn_desc_t;

@@ -368,7 +368,7 @@ def rg_kv_append(d, k, v, inv_freq, k_cache, v_cache, seqs: rg_paged_seqs, *, po
         raise ValueError("rg_kv_append: q and q_out go together")
     device = _one_device("rg_kv_append", k, v, inv_freq, k_cache, v_cache, seqs, pos, q, q_out)
     _call("rg_kv_append", K.load().rg_kv_append, device, C.byref(d) if d is not None else None, _rows(k), _rows(v),
-          _positions(pos) if pos is not None else None, _frequencies(inv_freq, d) if inv_freq is not None and d is not None else None,
+          _positions(pos) if pos is not None else None, None if inv_freq is None else inv_freq.data_ptr() if d is None else _frequencies(inv_freq, d),
           _cache(k_cache), _cache(v_cache), C.byref(seqs.c), _rows(q) if q is not None else None, _rows(q_out) if q_out is not None else None)
 
 

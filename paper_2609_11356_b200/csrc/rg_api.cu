@@ -533,7 +533,7 @@ int64_t bound_of_len(const rg_paged_seqs_t* q, int64_t page_size) {
 rg_status_t check_paged_desc(const rg_paged_attn_desc_t* d) {
   if (!d) return RG_ERR_NULL;
   if (d->size != sizeof(rg_paged_attn_desc_t) || d->mask > 1) return RG_ERR_INVALID_DESC;
-  if (!(d->scale > 0.0f) || d->scale > 3.0e38f) return RG_ERR_INVALID_DESC;
+  if (!(d->scale > 0.0f) || d->scale > 2.0e38f) return RG_ERR_INVALID_DESC;      // times log2(e) it stays finite
   if (d->split % 128 || d->split > (1u << 30) || d->window > (1u << 30)) return RG_ERR_INVALID_DESC;
   if (d->window && !d->mask) return RG_ERR_INVALID_DESC;
   return RG_OK;

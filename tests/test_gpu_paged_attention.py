@@ -357,3 +357,36 @@ def test_drawn_shapes(seed):
     split = r.choice([0, 0, 128, 384, 512])
     seqs = b.seqs(max_q=r.choice([0, 1, max(q)]), max_len=r.choice([0, max(kv)]))
     check(b, *attend(b, window=window, mask=mask, split=split, seqs=seqs, out_dtype=r.choice([None, torch.float32])), window=window, mask=mask)
+
+
+def test_cache_without_pages():
+    """Nothing to read: every row is zeros, and the lengths that say otherwise are told."""
+    b = Batch([2, 1], [5, 1], hq=4, hkv=2, d=64, page=16, seed=1)
+    kc = torch.zeros(0, 16, 2, 64, dtype=BF, device=DEV)
+    for split in (0, 128):
+        out, z = torch.full_like(b.Q, 77.0), torch.full((3, 4), 77.0, device=DEV)
+        rg.rg_paged_attention(rg.rg_paged_attn_desc(scale=1.0, split=split), b.Q, kc, kc, b.seqs(), out, lse=z)
+        assert rg.rg_device_status() == rg.RG_PAGE_CODE_ATTEND
+        assert bool((out == 0).all()) and bool((z == float("-inf")).all())
+
+
+def test_two_calls_at_once_and_back_to_back():
+    """Calls on two streams with workspaces of their own, and calls in a row that share one, give what they give alone."""
+    a, b = Batch([1] * 8, [900 + 50 * i for i in range(8)], hq=8, hkv=2, d=128, page=16, seed=1), Batch([70, 130], [400, 1300], hq=8, hkv=2, d=128, page=16, seed=2)
+    d = rg.rg_paged_attn_desc(scale=0.09, split=128)
+    alone = [attend(x, scale=0.09, split=128)[0] for x in (a, b)]
+    torch.cuda.synchronize()
+    need = [rg.rg_paged_attention_workspace_bytes(d, x.seqs(), x.T, x.hq, x.d) for x in (a, b)]
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    ws = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in need]
+    for _ in range(10):
+        for i, x in enumerate((a, b)):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(rg.rg_paged_attention(d, x.Q, x.kc, x.vc, x.seqs(), torch.empty_like(x.Q), ws=ws[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, alone[i]) for o in outs[i])
+    shared = torch.empty(max(need), dtype=torch.uint8, device=DEV)
+    outs = [rg.rg_paged_attention(d, x.Q, x.kc, x.vc, x.seqs(), torch.empty_like(x.Q), ws=shared) for _ in range(10) for x in (a, b)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, alone[i % 2]) for i, o in enumerate(outs))

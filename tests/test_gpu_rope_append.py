@@ -196,7 +196,7 @@ def test_refusals():
     b = Batch([2], [5], hq=2, hkv=2, d=64, page=16)
     k = torch.zeros(2, 2, 64, dtype=BF, device=DEV)
     for kw in ({"d": rg.rg_rope_desc(rot_dim=64, inverse=1), "inv_freq": f}, {"d": rg.rg_rope_desc(rot_dim=64), "inv_freq": None}, {"d": rg.rg_rope_desc(rot_dim=64, sections=(16, 16)), "inv_freq": f},
-               {"d": None, "inv_freq": None, "k": k.half()}):
+               {"d": None, "inv_freq": None, "k": k.half()}, {"d": None, "inv_freq": f}):
         a = {"k": k, "v": k, "k_cache": b.kc, "v_cache": b.vc, "seqs": b.seqs()} | kw
         with pytest.raises(rg.RgError):
             rg.rg_kv_append(**a)
