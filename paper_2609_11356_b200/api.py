@@ -295,16 +295,22 @@ def _frequencies(inv_freq, d) -> int:
     return inv_freq.data_ptr()
 
 
+_get_device = _raw_stream = None
+
+
 def _call(where: str, fn, device: int, *args):
     """One C call with `device` current and on its current stream."""
-    import torch
-    raw_stream = torch._C._cuda_getCurrentRawStream      # torch.cuda.current_stream(device).cuda_stream without the Python object around it
-    if device == torch.cuda.current_device():
-        st = fn(*args, raw_stream(device))
+    global _get_device, _raw_stream
+    if _get_device is None:                              # what torch.cuda.current_device() and current_stream() come down to for initialised CUDA
+        import torch
+        _get_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    if device == _get_device():
+        st = fn(*args, _raw_stream(device))
     else:
+        import torch
         with torch.cuda.device(device):
-            st = fn(*args, raw_stream(device))
-    if st != K.RG_OK:
+            st = fn(*args, _raw_stream(device))
+    if st:
         raise RgError(st, where)
 
 
