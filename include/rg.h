@@ -297,7 +297,7 @@ typedef struct {
  * starts at 0 and never falls; sequences without new tokens are fine; rows from cu_q[n_seqs] on belong to none:
  * nothing is written for them).  seq_lens[s] counts the tokens of sequence s with the new ones: row r of its n
  * new rows stands at place seq_lens[s] - n + r, in page block_table[s * table_ld + place / page_size].  Entries
- * of pages behind the last token are not read.
+ * of pages behind the last token are not read.  table_ld is at least table_cols, or 0: one row for all sequences.
  *   max_q    the host's upper bound of new tokens in one sequence (0: the number of rows).  It picks tile
  *            heights and never changes a bit or an answer.
  *   max_len  the host's upper bound of seq_lens (0: table_cols * page_size).  It sizes the workspace.

@@ -345,8 +345,8 @@ def rg_rope(d: K.rg_rope_desc_t, x, pos, inv_freq, out):
 
 
 class rg_paged_seqs:
-    """The sequences of a batch (see include/rg.h): int32 CUDA tensors block_table [n, pages], seq_lens [n] and cu_q [n + 1], and the
-    host's bounds of new tokens in one sequence and of seq_lens (0: none known).  The tensors are read when the kernels run."""
+    """The sequences of a batch (see include/rg.h): int32 CUDA tensors block_table [n, pages] (one row expanded to n is fine: all sequences
+    read the same pages), seq_lens [n] and cu_q [n + 1], and the host's bounds of new tokens in one sequence and of seq_lens (0: none known).  The tensors are read when the kernels run."""
     __slots__ = ("block_table", "seq_lens", "cu_q", "device", "c")
 
     def get_device(self) -> int:
@@ -362,9 +362,13 @@ class rg_paged_seqs:
             raise ValueError(f"{n} sequences need block_table [{n}, pages] and cu_q [{n + 1}], got {tuple(block_table.shape)} and {tuple(cu_q.shape)}")
         if not block_table.device == seq_lens.device == cu_q.device:
             raise ValueError("rg_paged_seqs: tensors on different devices")
+        cols = block_table.shape[1]
+        table_ld = block_table.stride(0) if n > 1 else cols
+        if 0 < table_ld < cols:
+            raise ValueError(f"rows of block_table overlap: {cols} entries, {table_ld} apart")
         self.device = seq_lens.get_device()
         self.block_table, self.seq_lens, self.cu_q = block_table, seq_lens, cu_q
-        self.c = K.rg_paged_seqs_t(block_table.data_ptr(), max(block_table.stride(0), block_table.shape[1]) if n > 1 else block_table.shape[1], block_table.shape[1], n,
+        self.c = K.rg_paged_seqs_t(block_table.data_ptr(), table_ld, cols, n,
                                    seq_lens.data_ptr(), cu_q.data_ptr(), max_q, max_len)
 
 

@@ -485,7 +485,7 @@ rg_status_t check_cache(const rg_cache_t* c) {
 rg_status_t check_seqs(const rg_paged_seqs_t* q) {
   if (!q) return RG_ERR_NULL;
   if (q->n_seqs < 0 || q->table_cols < 0 || q->table_ld < 0 || q->max_q < 0 || q->max_len < 0) return RG_ERR_SHAPE;
-  if (q->table_ld < q->table_cols && q->n_seqs > 1) return RG_ERR_SHAPE;
+  if (q->table_ld < q->table_cols && q->table_ld != 0 && q->n_seqs > 1) return RG_ERR_SHAPE;      // 0: one row for all of them
   if (q->n_seqs > 0 && (!q->seq_lens || !q->cu_q || (q->table_cols > 0 && !q->block_table))) return RG_ERR_NULL;
   return RG_OK;
 }

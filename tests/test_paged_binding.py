@@ -1,0 +1,35 @@
+"""How the binding describes tensors of the paged calls whose rows share memory, and what it refuses: no GPU needed."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2609_11356_b200 as rg
+from paper_2609_11356_b200 import _cabi as K
+from tests.test_paged_host import SHAPE, append, attend, seqs
+
+I32 = dict(dtype=torch.int32)
+
+
+def _seqs(table, n):
+    return rg.rg_paged_seqs(table, torch.zeros(n, **I32), torch.zeros(n + 1, **I32), max_q=1, max_len=9)
+
+
+def test_a_table_row_that_all_sequences_share_keeps_its_stride():
+    row = torch.arange(64, **I32)[None]
+    assert _seqs(row.expand(4, -1), 4).c.table_ld == 0                        # as a dense table it would be read 192 entries past its end
+    assert _seqs(row, 1).c.table_ld == 64 and _seqs(row.repeat(4, 1), 4).c.table_ld == 64
+    assert _seqs(torch.zeros(4, 80, **I32)[:, 8:72], 4).c.table_ld == 80
+    assert _seqs(torch.zeros(8, 64, **I32)[::2], 4).c.table_ld == 128
+    assert _seqs(row[:, :1].expand(4, 1), 4).c.table_ld == 0
+    for ld in (1, 63):
+        with pytest.raises(ValueError, match="overlap"):
+            _seqs(torch.zeros(400, **I32).as_strided((4, 64), (ld, 1)), 4)
+
+
+def test_the_library_takes_one_table_row_for_all_and_no_overlapping_ones():
+    for ld in (1, 7):
+        assert append(s=seqs(table_ld=ld)) == SHAPE and attend(s=seqs(table_ld=ld)) == SHAPE
+    d = rg.rg_paged_attn_desc(scale=1.0, split=128)
+    need = lambda ld: K.load().rg_paged_attention_workspace_bytes(C.byref(d), C.byref(seqs(table_ld=ld, table_cols=9, max_len=129)), 16, 10, 4, 64)
+    assert need(8) == 0 and need(0) == need(9) > 0                            # 0: refused
