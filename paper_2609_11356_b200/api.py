@@ -401,10 +401,15 @@ def rg_paged_attention_workspace_bytes(d: K.rg_paged_attn_desc_t, seqs: rg_paged
 def rg_paged_attention(d: K.rg_paged_attn_desc_t, q, k_cache, v_cache, seqs: rg_paged_seqs, out, *, lse=None, ws=None):
     """out = attention of the rows q [tokens, heads, dim] over their sequences' pages; lse: float32 [tokens, heads] or None."""
     import torch
+    lse_ld = 0
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or (lse.shape[1] > 1 and lse.stride(1) != 1):
+            raise ValueError("lse is float32 [tokens, heads], contiguous along the heads")
+        lse_ld = lse.stride(0) if lse.shape[0] > 1 else lse.shape[1]
+        if lse_ld < lse.shape[1]:
+            raise ValueError(f"rows of lse overlap: {lse.shape[1]} heads, {lse_ld} apart")
     device = _one_device("rg_paged_attention", q, k_cache, v_cache, seqs, out, lse, ws)
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or (lse.shape[1] > 1 and lse.stride(1) != 1)):
-        raise ValueError("lse is float32 [tokens, heads], contiguous along the heads")
     _call("rg_paged_attention", K.load().rg_paged_attention, device, C.byref(d), _rows(q), _cache(k_cache), _cache(v_cache), C.byref(seqs.c), _rows(out),
-          lse.data_ptr() if lse is not None else None, max(lse.stride(0), lse.shape[1]) if lse is not None else 0,
+          lse.data_ptr() if lse is not None else None, lse_ld,
           ws.data_ptr() if ws is not None else None, ws.numel() * ws.element_size() if ws is not None else 0)
     return out

@@ -33,3 +33,21 @@ def test_the_library_takes_one_table_row_for_all_and_no_overlapping_ones():
     d = rg.rg_paged_attn_desc(scale=1.0, split=128)
     need = lambda ld: K.load().rg_paged_attention_workspace_bytes(C.byref(d), C.byref(seqs(table_ld=ld, table_cols=9, max_len=129)), 16, 10, 4, 64)
     assert need(8) == 0 and need(0) == need(9) > 0                            # 0: refused
+
+
+def _attend(lse=None, ws=None, split=0):
+    """The public call on host tensors: what it refuses for its layout comes before the refusal of the device."""
+    q, cache = torch.zeros(4, 2, 64, dtype=torch.bfloat16), torch.zeros(5, 16, 2, 64, dtype=torch.bfloat16)
+    rg.rg_paged_attention(rg.rg_paged_attn_desc(scale=1.0, split=split), q, cache, cache, _seqs(torch.zeros(1, 5, **I32), 1), torch.zeros_like(q), lse=lse, ws=ws)
+
+
+@pytest.mark.parametrize("lse", [torch.zeros(1, 2).expand(4, 2), torch.zeros(9).as_strided((4, 2), (1, 1)), torch.zeros(1, 1).expand(4, 2)])
+def test_normalisers_whose_rows_share_memory_are_refused(lse):
+    with pytest.raises(ValueError, match="lse"):                              # written as if dense, they would be written past their end
+        _attend(lse=lse)
+
+
+@pytest.mark.parametrize("lse", [torch.zeros(4, 2), torch.zeros(4, 6)[:, 1:3], torch.zeros(8, 2)[::2]])
+def test_normalisers_of_any_other_stride_are_not(lse):
+    with pytest.raises(ValueError, match="CUDA device"):
+        _attend(lse=lse)
