@@ -101,6 +101,16 @@ def _tensor(t) -> K.rg_tensor_t:
     return K.rg_tensor_t(t.data_ptr(), _dtype_code(t), t.shape[0], t.shape[1], max(ld, int(t.shape[1])))
 
 
+def _workspace(ws):
+    """Address of a workspace tensor and the bytes it has there: an expanded one has fewer than its elements say."""
+    if ws is None:
+        return None, 0
+    n = ws.numel()
+    if n and not ws.is_contiguous():
+        n = min(n, 1 + sum((size - 1) * stride for size, stride in zip(ws.shape, ws.stride())))
+    return ws.data_ptr(), n * ws.element_size()
+
+
 def _epilogue(bias, act, residual) -> Optional[K.rg_epilogue_t]:
     if bias is None and residual is None and not act:
         return None
@@ -125,8 +135,7 @@ def rg_gemm(d: K.rg_desc_t, A, B, C_out, *, bias=None, act: int = 0, residual=No
     L = K.load()
     a, b, c = _tensor(A), _tensor(B), _tensor(C_out)
     e = _epilogue(bias, act, residual)
-    ws_ptr = ws.data_ptr() if ws is not None else None
-    ws_bytes = ws.numel() * ws.element_size() if ws is not None else 0
+    ws_ptr, ws_bytes = _workspace(ws)
     st = L.rg_gemm(C.byref(d), C.byref(a), C.byref(b), C.byref(c), C.byref(e) if e is not None else None,
                    ws_ptr, ws_bytes, _stream(A))
     _check(st, "rg_gemm")
@@ -192,8 +201,7 @@ def rg_reduce_cols(d: K.rg_desc_t, op: int, x, out, *, y=None, ws=None):
     L = K.load()
     xt, ot = _tensor(x), _tensor(out)
     yt = _tensor(y) if y is not None else None
-    ws_ptr = ws.data_ptr() if ws is not None else None
-    ws_bytes = ws.numel() * ws.element_size() if ws is not None else 0
+    ws_ptr, ws_bytes = _workspace(ws)
     st = L.rg_reduce_cols(C.byref(d), int(op), C.byref(xt), C.byref(yt) if yt is not None else None, C.byref(ot),
                           ws_ptr, ws_bytes, _stream(x))
     _check(st, "rg_reduce_cols")
@@ -207,7 +215,7 @@ def rg_gemm_host(d: K.rg_desc_t, A, B, C_out, dev_scratch, *, bias=None, act: in
     a, b, c = _tensor(A), _tensor(B), _tensor(C_out)
     e = _epilogue(bias, act, residual)
     st = L.rg_gemm_host(C.byref(d), C.byref(a), C.byref(b), C.byref(c), C.byref(e) if e is not None else None,
-                        dev_scratch.data_ptr(), dev_scratch.numel() * dev_scratch.element_size(), _stream(dev_scratch))
+                        *_workspace(dev_scratch), _stream(dev_scratch))
     _check(st, "rg_gemm_host")
     return C_out
 
@@ -226,8 +234,8 @@ def rg_reduce_rows_host(d: K.rg_desc_t, op: int, x, out, dev_scratch, *, weight=
     args.eps = float(eps)
     if aux_out is not None:
         args.aux_out = aux_out.data_ptr()
-    st = L.rg_reduce_rows_host(C.byref(d), int(op), C.byref(xt), C.byref(ot), C.byref(args), dev_scratch.data_ptr(),
-                               dev_scratch.numel() * dev_scratch.element_size(), _stream(dev_scratch))
+    st = L.rg_reduce_rows_host(C.byref(d), int(op), C.byref(xt), C.byref(ot), C.byref(args),
+                               *_workspace(dev_scratch), _stream(dev_scratch))
     _check(st, "rg_reduce_rows_host")
     return out
 
@@ -408,8 +416,8 @@ def rg_paged_attention(d: K.rg_paged_attn_desc_t, q, k_cache, v_cache, seqs: rg_
         lse_ld = lse.stride(0) if lse.shape[0] > 1 else lse.shape[1]
         if lse_ld < lse.shape[1]:
             raise ValueError(f"rows of lse overlap: {lse.shape[1]} heads, {lse_ld} apart")
+    ws_ptr, ws_bytes = _workspace(ws)
     device = _one_device("rg_paged_attention", q, k_cache, v_cache, seqs, out, lse, ws)
     _call("rg_paged_attention", K.load().rg_paged_attention, device, C.byref(d), _rows(q), _cache(k_cache), _cache(v_cache), C.byref(seqs.c), _rows(out),
-          lse.data_ptr() if lse is not None else None, lse_ld,
-          ws.data_ptr() if ws is not None else None, ws.numel() * ws.element_size() if ws is not None else 0)
+          lse.data_ptr() if lse is not None else None, lse_ld, ws_ptr, ws_bytes)
     return out

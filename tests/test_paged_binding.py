@@ -5,8 +5,8 @@ import pytest
 import torch
 
 import paper_2609_11356_b200 as rg
-from paper_2609_11356_b200 import _cabi as K
-from tests.test_paged_host import SHAPE, append, attend, seqs
+from paper_2609_11356_b200 import _cabi as K, api
+from tests.test_paged_host import SHAPE, WS, append, attend, seqs
 
 I32 = dict(dtype=torch.int32)
 
@@ -51,3 +51,17 @@ def test_normalisers_whose_rows_share_memory_are_refused(lse):
 def test_normalisers_of_any_other_stride_are_not(lse):
     with pytest.raises(ValueError, match="CUDA device"):
         _attend(lse=lse)
+
+
+def test_a_workspace_has_the_bytes_that_it_holds():
+    byte, words = torch.zeros(1, dtype=torch.uint8), torch.zeros(8, 64)
+    for ws, n in ((None, 0), (byte.expand(1 << 20), 1), (words[:1].expand(100, 64), 256), (words[:, :1].expand(8, 64), 4 * (7 * 64 + 1)), (words, 2048), (words.T, 2048),
+                  (words.view(-1)[::2], 1024), (words[:0], 0), (words[:0].expand(0, 64), 0), (words[:0].T, 0)):
+        assert api._workspace(ws) == (None if ws is None else ws.data_ptr(), n)
+    a, c = torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(2, 2)
+    d = rg.rg_desc(cuts=(32,))
+    need = rg.rg_gemm_workspace_bytes(d, 2, 2)
+    for ws in (byte.expand(need), torch.zeros(need - 1, dtype=torch.uint8)):
+        with pytest.raises(rg.RgError) as e:                                  # the expanded byte passed for all of it
+            rg.rg_gemm(d, a, a, c, ws=ws)
+        assert e.value.status == WS
