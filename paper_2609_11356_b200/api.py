@@ -95,10 +95,10 @@ def _dtype_code(t) -> int:
 
 def _tensor(t) -> K.rg_tensor_t:
     if t.dim() == 1:
-        return K.rg_tensor_t(t.data_ptr(), _dtype_code(t), t.shape[0], 1, max(int(t.stride(0)), 1))
+        return K.rg_tensor_t(t.data_ptr(), _dtype_code(t), t.shape[0], 1, int(t.stride(0)) if t.shape[0] > 1 else 1)
     assert t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "rows must be contiguous"
-    ld = int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
-    return K.rg_tensor_t(t.data_ptr(), _dtype_code(t), t.shape[0], t.shape[1], max(ld, int(t.shape[1])))
+    ld = int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))      # rows that overlap are the library's to refuse
+    return K.rg_tensor_t(t.data_ptr(), _dtype_code(t), t.shape[0], t.shape[1], ld)
 
 
 def _workspace(ws):

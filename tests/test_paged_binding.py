@@ -65,3 +65,18 @@ def test_a_workspace_has_the_bytes_that_it_holds():
         with pytest.raises(rg.RgError) as e:                                  # the expanded byte passed for all of it
             rg.rg_gemm(d, a, a, c, ws=ws)
         assert e.value.status == WS
+
+
+def test_matrices_whose_rows_share_memory_are_refused():
+    """rg_gemm and the reductions: an expanded matrix is not described as a dense one."""
+    a, c, v = torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(2, 2), torch.zeros(2)
+    row = torch.zeros(1, 64, dtype=torch.bfloat16).expand(2, 64)
+    over = torch.zeros(80, dtype=torch.bfloat16).as_strided((2, 64), (16, 1))
+    for call in (lambda: rg.rg_gemm(rg.rg_desc(), row, a, c), lambda: rg.rg_gemm(rg.rg_desc(), a, over, c), lambda: rg.rg_gemm(rg.rg_desc(), a, a, c[:1].expand(2, 2)),
+                 lambda: rg.rg_reduce_rows(rg.rg_desc(), rg.RG_OP_SUM, row, v), lambda: rg.rg_reduce_rows(rg.rg_desc(), rg.RG_OP_SUM, a, v[:1].expand(2))):
+        with pytest.raises(rg.RgError) as e:
+            call()
+        assert e.value.status == SHAPE
+    for t, ld in ((a, 64), (a[:1], 64), (torch.zeros(2, 80)[:, :64], 80), (torch.zeros(1, 80)[:, :64], 80), (torch.zeros(4, 64)[::2], 128), (torch.zeros(0, 64), 64),
+                  (torch.zeros(3, 1), 1), (v, 1), (torch.zeros(6)[::3], 3), (v[:1], 1), (v[:1].expand(1), 1)):
+        assert api._tensor(t).ld == ld
