@@ -277,7 +277,8 @@ rg_status_t rg_attention(const rg_attn_desc_t* d, const rg_tensor_t* Q, const rg
  *
  * rg_rows_t: rows [tokens][heads][dim]; elements of one head are contiguous, the other strides are in elements
  * and free (a slice of a fused product's output will do).  rg_cache_t: [pages][page_size][heads][dim] with any
- * strides for the first three, so both [page][slot][head] and [page][head][slot] memory orders are this type.
+ * strides for the first three, so both [page][slot][head] and [page][head][slot] memory orders are this type; in a
+ * cache that is written no two elements share an address (its dimensions lie inside one another in some order).
  * dim is at most 1024, heads at most 65535. */
 typedef struct {
   void* ptr;

@@ -2,6 +2,7 @@
 // selection, and the host-buffer forms.  Nothing here does arithmetic on data.
 #include <algorithm>
 #include <string.h>
+#include <utility>
 
 #include "rg_internal.h"
 
@@ -482,6 +483,21 @@ rg_status_t check_cache(const rg_cache_t* c) {
   return RG_OK;
 }
 
+// a cache that is written: heads, slots and pages lie inside one another in some order
+rg_status_t check_cache_out(const rg_cache_t* c) {
+  rg_status_t s = check_cache(c);
+  if (s != RG_OK) return s;
+  std::pair<int64_t, int64_t> dims[3] = {{c->page_stride, c->pages}, {c->slot_stride, c->page_size}, {c->head_stride, c->heads}};
+  std::sort(dims, dims + 3);
+  __int128 extent = c->dim;                                // strides and sizes at their limits pass 64 bits
+  for (const auto& d : dims) {
+    if (d.second < 2) continue;
+    if (d.first < extent) return RG_ERR_SHAPE;
+    extent += (__int128)(d.second - 1) * d.first;
+  }
+  return RG_OK;
+}
+
 rg_status_t check_seqs(const rg_paged_seqs_t* q) {
   if (!q) return RG_ERR_NULL;
   if (q->n_seqs < 0 || q->table_cols < 0 || q->table_ld < 0 || q->max_q < 0 || q->max_len < 0) return RG_ERR_SHAPE;
@@ -561,7 +577,7 @@ rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_r
                          const rg_cache_t* k_cache, const rg_cache_t* v_cache, const rg_paged_seqs_t* seqs,
                          const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream) {
   rg_status_t s;
-  if ((s = check_rows(k)) != RG_OK || (s = check_rows(v)) != RG_OK || (s = check_cache(k_cache)) != RG_OK || (s = check_cache(v_cache)) != RG_OK ||
+  if ((s = check_rows(k)) != RG_OK || (s = check_rows(v)) != RG_OK || (s = check_cache_out(k_cache)) != RG_OK || (s = check_cache_out(v_cache)) != RG_OK ||
       (s = check_seqs(seqs)) != RG_OK)
     return s;
   if (!same_shape(k, v) || k->dtype != k_cache->dtype || k->dtype != v_cache->dtype) return RG_ERR_SHAPE;

@@ -6,7 +6,7 @@ import torch
 
 import paper_2609_11356_b200 as rg
 from paper_2609_11356_b200 import _cabi as K, api
-from tests.test_paged_host import SHAPE, WS, append, attend, seqs
+from tests.test_paged_host import SHAPE, WS, append, attend, cache, rows, seqs
 
 I32 = dict(dtype=torch.int32)
 
@@ -80,3 +80,19 @@ def test_matrices_whose_rows_share_memory_are_refused():
     for t, ld in ((a, 64), (a[:1], 64), (torch.zeros(2, 80)[:, :64], 80), (torch.zeros(1, 80)[:, :64], 80), (torch.zeros(4, 64)[::2], 128), (torch.zeros(0, 64), 64),
                   (torch.zeros(3, 1), 1), (v, 1), (torch.zeros(6)[::3], 3), (v[:1], 1), (v[:1].expand(1), 1)):
         assert api._tensor(t).ld == ld
+
+
+@pytest.mark.parametrize("kw", [{"slot_stride": 0}, {"head_stride": 0}, {"page_stride": 0}, {"head_stride": 32}, {"slot_stride": 64}, {"page_stride": 1024}, {"page_stride": 2047},
+                                {"slot_stride": 127}, {"head_stride": 16 * 64 - 1, "slot_stride": 64}, {"pages": 2 ** 31 - 1024, "page_stride": 64, "slot_stride": 2 ** 38, "head_stride": 2 ** 37 - 2 ** 16 - 1},
+                                {"pages": 2 ** 31 - 1024, "page_stride": 2 ** 37, "slot_stride": 64, "head_stride": 2 ** 38}])
+def test_a_cache_whose_elements_share_memory_is_not_written(kw):
+    assert append(kc=cache(**kw), vc=cache(**{k: v for k, v in kw.items() if k == "pages"})) == SHAPE
+    assert append(kc=cache(**{k: v for k, v in kw.items() if k == "pages"}), vc=cache(**kw)) == SHAPE
+
+
+@pytest.mark.parametrize("kw", [{}, {"head_stride": 1024, "slot_stride": 64}, {"page_stride": 4096}, {"page_stride": 128, "slot_stride": 640}, {"page_stride": 64, "slot_stride": 320, "head_stride": 5120},
+                                {"page": 1, "slot_stride": 0, "page_stride": 128}, {"pages": 1, "page_stride": 0}, {"slot_stride": 2 ** 38}, {"page_stride": 2 ** 38, "slot_stride": 2 ** 33}])
+def test_a_cache_of_any_nested_strides_is(kw):
+    assert append(k=rows(0), v=rows(0), kc=cache(**kw), vc=cache(**kw)) == 0    # no tokens: accepted, nothing launched
+    heads = cache(heads=1, head_stride=0)
+    assert append(k=rows(0, heads=1), v=rows(0, heads=1), kc=heads, vc=heads) == 0
