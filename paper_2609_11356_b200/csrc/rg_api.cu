@@ -4,6 +4,7 @@
 #include <string.h>
 #include <utility>
 
+#include "rg_health.h"
 #include "rg_internal.h"
 
 namespace {
@@ -815,18 +816,12 @@ rg_status_t rg_selftest_bounded_wait(uint64_t limit_ns, uint32_t* dev_counter, v
 }
 
 rg_status_t rg_device_status(uint32_t* code) {
-  uint32_t a = 0, b = 0, c = 0;
-  const rg_status_t s1 = rg::read_and_clear_status(&a);          // synchronises the device
-  if (s1 == RG_ERR_CUDA) return s1;
-  const rg_status_t s2 = rg::read_and_clear_reduce_status(&b);
-  if (s2 == RG_ERR_CUDA) return s2;
-  const rg_status_t s3 = rg::read_and_clear_attn_status(&c);
-  if (s3 == RG_ERR_CUDA) return s3;
-  uint32_t e = 0, f = 0;
-  if (rg::read_and_clear_paged_attn_status(&e) == RG_ERR_CUDA || rg::read_and_clear_paged_status(&f) == RG_ERR_CUDA) return RG_ERR_CUDA;
-  const uint32_t waits = a ? a : (b ? b : (c ? c : (e != RG_PAGE_CODE_ATTEND ? e : 0)));   // a wait that gave up goes before a bad page
-  if (code) *code = waits ? waits : (e ? e : f);
-  return waits ? RG_ERR_TIMEOUT : (e || f) ? RG_ERR_PAGE : RG_OK;
+  uint32_t waits[4] = {0, 0, 0, 0}, pages[2] = {0, 0};
+  // the first of them synchronises the device
+  if (rg::read_and_clear_status(&waits[0]) == RG_ERR_CUDA || rg::read_and_clear_reduce_status(&waits[1]) == RG_ERR_CUDA || rg::read_and_clear_attn_status(&waits[2]) == RG_ERR_CUDA ||
+      rg::read_and_clear_paged_attn_status(&waits[3], &pages[0]) == RG_ERR_CUDA || rg::read_and_clear_paged_status(&pages[1]) == RG_ERR_CUDA)
+    return RG_ERR_CUDA;
+  return rg::health_of(waits, 4, pages, 2, code);
 }
 
 const char* rg_status_string(rg_status_t s) {

@@ -115,7 +115,7 @@ struct PagedAttnArgs {
   int32_t causal;
 };
 rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st);
-rg_status_t read_and_clear_paged_attn_status(uint32_t* code);
+rg_status_t read_and_clear_paged_attn_status(uint32_t* wait, uint32_t* page);
 rg_status_t read_and_clear_status(uint32_t* code);
 rg_status_t launch_wait_selftest(uint64_t limit_ns, uint32_t code, unsigned int* left_early, cudaStream_t st);
 // y[i] = FORM(x[i]) by the device functions the kernels use (forms 0-2 and 6; the attention kernel's forms 3-5)

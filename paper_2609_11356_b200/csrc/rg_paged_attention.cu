@@ -38,7 +38,8 @@
 
 namespace rg {
 
-__device__ unsigned int g_paged_attn_status_word = 0;
+__device__ unsigned int g_paged_attn_status_word = 0;      // waits that gave up
+__device__ unsigned int g_paged_attn_page_word = 0;        // pages and lengths outside the cache
 
 namespace {
 
@@ -229,7 +230,7 @@ struct Walk {
     if (s < p.n_seqs) {
       bool bad;
       mine = view_of(p, s, &bad);
-      if (bad) atomicCAS(&g_paged_attn_status_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
+      if (bad) atomicCAS(&g_paged_attn_page_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
     }
   }
   __device__ __forceinline__ void load(const Params& p, int tile_tokens) {
@@ -582,7 +583,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         int32_t page = ahead;
         if (b + 1 < it.b1 && wanted(b + 1)) ahead = entry(b + 1);  // looked up a block ahead of its use
         if (mine && (page < 0 || page >= p.pages)) {               // not a page: the copy from behind the last one fills in zeros
-          if (col == 0) atomicCAS(&g_paged_attn_status_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
+          if (col == 0) atomicCAS(&g_paged_attn_page_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
           page = p.pages;
         }
         const int32_t key = b * BLK + piece * p.box, at = key - key / p.by_page * p.page_size;
@@ -1018,7 +1019,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       auto copy = [&](const CUtensorMap* map, int b, int32_t& id) {
         const bool mine = wanted(b);
         if (mine && (id < 0 || id >= p.pages)) {                   // not a page: the copy from behind the last one fills in zeros
-          if (col == 0) atomicCAS(&g_paged_attn_status_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
+          if (col == 0) atomicCAS(&g_paged_attn_page_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
           id = p.pages;
         }
         const int32_t key = b * BLK + piece * p.box, at = key - key / p.by_page * p.page_size;
@@ -1504,12 +1505,16 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   return RG_OK;
 }
 
-rg_status_t read_and_clear_paged_attn_status(uint32_t* code) {
-  unsigned int v = 0, zero = 0;
-  if (cudaMemcpyFromSymbol(&v, g_paged_attn_status_word, sizeof(v)) != cudaSuccess) return RG_ERR_CUDA;
-  if (v != 0 && cudaMemcpyToSymbol(g_paged_attn_status_word, &zero, sizeof(zero)) != cudaSuccess) return RG_ERR_CUDA;
-  if (code) *code = v;
-  return v ? (v == RG_PAGE_CODE_ATTEND ? RG_ERR_PAGE : RG_ERR_TIMEOUT) : RG_OK;
+rg_status_t read_and_clear_paged_attn_status(uint32_t* wait, uint32_t* page) {
+  unsigned int v[2] = {0, 0}, zero = 0;
+  if (cudaMemcpyFromSymbol(&v[0], g_paged_attn_status_word, sizeof(v[0])) != cudaSuccess || cudaMemcpyFromSymbol(&v[1], g_paged_attn_page_word, sizeof(v[1])) != cudaSuccess)
+    return RG_ERR_CUDA;
+  if ((v[0] != 0 && cudaMemcpyToSymbol(g_paged_attn_status_word, &zero, sizeof(zero)) != cudaSuccess) ||
+      (v[1] != 0 && cudaMemcpyToSymbol(g_paged_attn_page_word, &zero, sizeof(zero)) != cudaSuccess))
+    return RG_ERR_CUDA;
+  *wait = v[0];
+  *page = v[1];
+  return RG_OK;
 }
 
 }  // namespace rg

@@ -44,3 +44,19 @@ def test_append_through_one_table_row():
     place = torch.arange(18, 27, device=DEV)
     assert torch.equal(ks[0][row[0].long()[place // 16], place % 16], k)
     assert torch.equal(ks[0], ks[1]) and torch.equal(vs[0], vs[1])
+
+
+def test_a_wait_that_gave_up_is_told_before_a_bad_page():
+    """Both kinds of news unread: the wait is the answer (here the self-test's, which waits 2 ms for nothing), and both words are cleared."""
+    import ctypes as C
+    from paper_2609_11356_b200 import _cabi
+    from paper_2609_11356_b200.api import rg_selftest_bounded_wait
+    b = Batch([1], [40], hq=2, hkv=2, d=64, page=16, seed=1)
+    b.table[0, 1] = -1
+    attend(b)
+    rg_selftest_bounded_wait(2_000_000, torch.zeros(1, dtype=torch.int32, device=DEV))
+    code = C.c_uint32(0)
+    assert _cabi.load().rg_device_status(C.byref(code)) == 8 and code.value == _cabi.RG_SELFTEST_WAIT_CODE
+    assert rg.rg_device_status() == 0
+    attend(b)
+    assert _cabi.load().rg_device_status(C.byref(code)) == 9 and code.value == rg.RG_PAGE_CODE_ATTEND
