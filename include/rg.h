@@ -360,7 +360,8 @@ rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_r
  * Keys are walked in blocks of 128 places; with s_t = scale * (q . k_t) in fp32 from tensor-core chains over dim,
  *   p_t = exp(s_t - m),   l += sum of the block's p_t,   O += (P . V)_block,   P = p narrowed to the cache's type
  * where m is a running maximum that moves (and O and l are rescaled, in fp32) only when a block's maximum exceeds
- * it by more than 8 / log2(e); the answer is O times 1 / l, rounded once.  exp is the hardware's base-two exponential for some of the
+ * it by more than 8 / log2(e); the answer is O times 1 / l, rounded once.  Weights follow the distances between scores: q . k_t has to be
+ * finite in fp32, s_t need not be (its normaliser is infinite then).  exp is the hardware's base-two exponential for some of the
  * elements and a polynomial of IEEE operations for the others, by the key's place: bits repeat on this architecture.
  * lse (may be NULL): [tokens][query heads] of stride lse_ld, fp32: the natural logarithm of the sum of exp(s_t).  A row that
  * sees no key gives zeros and -inf.  What a row does not see never reaches it, infinities and NaN in masked keys and

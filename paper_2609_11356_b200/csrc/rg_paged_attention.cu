@@ -4,7 +4,7 @@
 // blocks of 128 places.  Per row and block, with c = scale * log2(e):
 //   s_t = q . k_t                             d/16 tcgen05.mma steps from a zero accumulator, ascending
 //   m'  = max_t s_t;  if (m' - m) c > 8:  a = 2^((m - m') c), m = m', l = a l, O = a O      (else m, l and O stay)
-//   p_t = 2^(s_t c - m c);  l += sum of p_t;  O += P V       P = p narrowed, 8 steps on the same accumulator
+//   p_t = 2^(s_t c - m c), or 2^((s_t - m) c) where m c is large;  l += sum of p_t;  O += P V       P = p narrowed, 8 steps on the same accumulator
 // and at the end O * (1 / l).  A running maximum that may lag by 2^8 costs nothing in precision (p is a floating-point number
 // below 2^8) and saves nearly every rescaling of O, which lives in tensor memory.
 //
@@ -385,16 +385,24 @@ __device__ __forceinline__ float quarter_max(const uint32_t* s) {
   return max3(a, b, b);
 }
 
-// The block's maximum mb -> the running maximum; returns the factor that sums and O take (1 nearly always).
+// Whether the block's maximum mb moves the running one (from -inf: any number does; -inf and NaN never), and the factor that sums and O take then.
+__device__ __forceinline__ bool rises(float m, float mb, float c) { return f_mul(f_add(mb, -m), c) > LAG; }
 __device__ __forceinline__ float move_max(float& m, float mb, float c) {
-  float alpha = 1.0f;
-  if (f_mul(f_add(mb, -m), c) > LAG) {                     // from -inf: any number; -inf and NaN: never
-    alpha = pa_ex2(f_mul(f_add(m, -mb), c));
-    m = mb;
-  }
+  const float alpha = pa_ex2(f_mul(f_add(m, -mb), c));
+  m = mb;
   return alpha;
 }
-__device__ __forceinline__ float shift_of(float m, float c) { return m == -INFINITY ? 0.0f : -f_mul(m, c); }
+// What a row's scores take on the way to their exponents: x = (s - off) c + shift.  The product m c is rounded once for all of a row's keys, and what it
+// is off by, up to half its last place, multiplies every weight: nothing while it is below 2^-8, but at 2^31 weights pass fp16's range or
+// vanish, and from 2^128 on there is no product.  Rows that far out take their maximum off first; s - m is exact where it matters.
+constexpr float FAR = 65536.0f;
+__device__ __forceinline__ bool shift_of(float m, float c, float& shift, float& off) {
+  shift = m == -INFINITY ? 0.0f : -f_mul(m, c);
+  off = 0.0f;
+  const bool far = fabsf(shift) >= FAR && m != INFINITY;       // an infinite maximum: the row is NaN
+  if (far) { off = m; shift = 0.0f; }
+  return far;
+}
 
 // The exponentials of two scores.  Which of the two forms a key takes follows from its place alone: the last 4 of every 32 the polynomial,
 // which takes them off the hardware unit (16 results a cycle and SM, where a block of both tiles wants 32768 in 2048 cycles of the tensor core).
@@ -433,16 +441,40 @@ __device__ __forceinline__ float add_quarter(float l, float alpha, float total, 
 }
 __device__ __forceinline__ float join_quarters(float a, float b, float c, float d) { return f_add(f_add(a, b), f_add(c, d)); }
 
-// O = alpha O for one lane's columns
+template <int N>
+__device__ __forceinline__ void pa_ld_cols(uint32_t taddr, uint32_t (&r)[N]);
+template <>
+__device__ __forceinline__ void pa_ld_cols<8>(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+}
+template <>
+__device__ __forceinline__ void pa_ld_cols<16>(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                 "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+template <>
+__device__ __forceinline__ void pa_ld_cols<32>(uint32_t taddr, uint32_t (&r)[32]) { load_quarter(taddr, r); }
+template <int N>
+__device__ __forceinline__ void pa_st_cols(uint32_t taddr, const uint32_t (&r)[N]) {
+  if constexpr (N == 32) pa_st32(taddr, r);
+  else if constexpr (N == 16) pa_st16(taddr, r);
+  else
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr) : "memory");
+}
+
+// O = alpha O for one lane's columns (16 at a time: half of a row's scores are in registers meanwhile, and 32 made the compiler spill some)
 template <int HDP>
 __device__ __forceinline__ void rescale(uint32_t t_o, float alpha) {
 #pragma unroll 1
-  for (int q = 0; q < HDP / QW; ++q) {
-    uint32_t o[QW];
-    load_quarter(t_o + 32u * q, o);
+  for (int q = 0; q < HDP / 16; ++q) {
+    uint32_t o[16];
+    pa_ld_cols<16>(t_o + 16u * q, o);
 #pragma unroll
-    for (int i = 0; i < QW; ++i) o[i] = __float_as_uint(f_mul(__uint_as_float(o[i]), alpha));
-    pa_st32(t_o + 32u * q, o);
+    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(f_mul(__uint_as_float(o[i]), alpha));
+    pa_st16(t_o + 16u * q, o);
   }
 }
 
@@ -709,7 +741,8 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
       const bool tile_live = t * p.tile_tokens < it.n_tok;
       const int32_t place = it.pos + tok;
       const int32_t hi = live ? min(last_seen(p, place, it.len), it.hi) : -1, lo = max(first_seen(p, place), it.lo);
-      float m = -INFINITY, l[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      float m = -INFINITY, l[4] = {0.0f, 0.0f, 0.0f, 0.0f}, shift = 0.0f;
+      bool far = false;
       bool any_masked = masked_block(p, it, it.b0) && it.b1 > it.b0;
       if (it.b1 > it.b0 + 1) any_masked |= masked_block(p, it, it.b1 - 1);      // what is masked lies at the ends
       if (tile_live) {
@@ -729,7 +762,18 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
               for (int i = 0; i < BLK; ++i) s[i] = i >= first && i <= last ? s[i] : 0xff800000u;
             }
             const float mb = max3(max3(quarter_max(s), quarter_max(s + 32), quarter_max(s + 64)), quarter_max(s + 96), -INFINITY);
-            const float alpha = move_max(m, mb, p.c), shift = shift_of(m, p.c);
+            // rare, and in one branch: the maximum moves, or the row is far (as a branch of its own behind the maximum's, the far rows took 3 % of a long chunk)
+            const bool up = rises(m, mb, p.c), moved = __any_sync(0xffffffffu, up || far);
+            float alpha = 1.0f;
+            if (moved) {
+              if (up) alpha = move_max(m, mb, p.c);
+              float off;
+              far = shift_of(m, p.c, shift, off);
+              if (far) {
+#pragma unroll
+                for (int i = 0; i < BLK; ++i) s[i] = __float_as_uint(f_add(__uint_as_float(s[i]), -off));
+              }
+            }
             // probabilities go over scores, which have been read
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -738,7 +782,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
               pa_st16(t_s + 16u * q, packed);
               if (q == 1) {
                 // the scores of this block are complete, so the product of the block before is too: O may be rescaled
-                if (b > it.b0 && __any_sync(0xffffffffu, live && alpha != 1.0f)) rescale<HDP>(t_o, alpha);
+                if (moved && b > it.b0) rescale<HDP>(t_o, alpha);
                 pa_wait_st();
                 pa_fence_before();
                 __syncwarp();
@@ -884,30 +928,6 @@ struct Few {
   static constexpr size_t SMEM = 1024 + LAST;
   static_assert(SMEM <= 115712 && SLOTS / 2 + 1 < FLAGS, "two CTAs fit the SM; the fixer cannot be a whole turn of flags ahead");
 };
-
-template <int N>
-__device__ __forceinline__ void pa_ld_cols(uint32_t taddr, uint32_t (&r)[N]);
-template <>
-__device__ __forceinline__ void pa_ld_cols<8>(uint32_t taddr, uint32_t (&r)[8]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
-}
-template <>
-__device__ __forceinline__ void pa_ld_cols<16>(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-                 "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
-}
-template <>
-__device__ __forceinline__ void pa_ld_cols<32>(uint32_t taddr, uint32_t (&r)[32]) { load_quarter(taddr, r); }
-template <int N>
-__device__ __forceinline__ void pa_st_cols(uint32_t taddr, const uint32_t (&r)[N]) {
-  if constexpr (N == 32) pa_st32(taddr, r);
-  else if constexpr (N == 16) pa_st16(taddr, r);
-  else
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
-                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr) : "memory");
-}
 
 // Butterfly over the warp's lanes for ROWS values a lane, lanes trading halves of what they still hold: lane i ends with the whole value of
 // row i >> (5 - log2 ROWS).  Every level combines lane i's value with lane i ^ x's, x = 16, 8, 4, 2, 1.
@@ -1162,7 +1182,12 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         alive = pa_wait(b_x, block & 1, abort_flag, 0x3640u);
         if (!alive) break;
         const float mb = max3(max3(x[lane], x[32 + lane], x[64 + lane]), x[96 + lane], x[96 + lane]);
-        const float alpha = move_max(m, mb, p.c), shift = shift_of(m, p.c);
+        const float alpha = rises(m, mb, p.c) ? move_max(m, mb, p.c) : 1.0f;
+        float shift, off;
+        if (__any_sync(0xffffffffu, shift_of(m, p.c, shift, off))) {
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) s[i] = __float_as_uint(f_add(__uint_as_float(s[i]), -__shfl_sync(0xffffffffu, off, i << SH)));
+        }
         uint8_t* row = p_row + buf * F::P_BUF;
 #pragma unroll
         for (int i = 0; i < ROWS; i += 2) {

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2609_11356_b200 as rg
-from tests._paged_util import DEV, Batch, attend, check
+from tests._paged_util import DEV, Batch, attend, attention_bounds, check
 
 pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
@@ -60,3 +60,57 @@ def test_a_wait_that_gave_up_is_told_before_a_bad_page():
     assert rg.rg_device_status() == 0
     attend(b)
     assert _cabi.load().rg_device_status(C.byref(code)) == 9 and code.value == rg.RG_PAGE_CODE_ATTEND
+
+
+def _softmax64(q, k, v, scale):
+    """attention64 for scores of any size: the weights from the distances to the maximum.  Output, normaliser, sum of weights times |v|."""
+    n, m, G = q.shape[0], k.shape[0], q.shape[1] // k.shape[1]
+    q, k, v = q.double().permute(1, 0, 2), k.double().repeat_interleave(G, 1).permute(1, 2, 0), v.double().repeat_interleave(G, 1).permute(1, 0, 2)
+    s = (q @ k).masked_fill(torch.arange(m - n, m, device=DEV)[:, None] < torch.arange(m, device=DEV)[None], -float("inf"))
+    top = s.amax(-1, keepdim=True)
+    w = torch.exp((s - top) * scale)
+    total = w.sum(-1, keepdim=True)
+    w = w / total
+    return (w @ v).permute(1, 0, 2), (top * scale + total.log())[..., 0].T, (w @ v.abs()).permute(1, 0, 2)
+
+
+# q = (a, 1, 0, ...), k_t = (b, r_t, 0, ...): the scores a b + r_t are whole numbers that 24 bits hold, so they carry no rounding
+FAR_SCORES = [(BF, 2.0 ** 11, 2.0 ** 11, 1.0), (HF, 2.0 ** 11, -2.0 ** 11, 1.0), (BF, 2.0 ** 11, -2.0 ** 11, 2.0 ** 10), (HF, 2.0 ** 11, 2.0 ** 11, 2.0 ** 8), (BF, 2.0 ** 11, 2.0 ** 11, 2.0 ** 10),
+              (HF, 1.0, 8.0, 1e38), (BF, 1.0, -12.0, 1e38), (HF, -1.0, 12.0, 2e38), (BF, 2.0 ** 63, 2.0 ** 63, 3.0), (BF, 2.0 ** 63, -2.0 ** 63, 3.0)]
+
+
+@pytest.mark.parametrize("split", [0, 128])
+@pytest.mark.parametrize("q_len", [1, 7, 150])
+@pytest.mark.parametrize("dtype,a,b,scale", FAR_SCORES)
+def test_scores_far_from_zero(dtype, a, b, scale, q_len, split):
+    """The weights depend on the distances between scores, however large the scores are: where scale times a score is 2^22 and more, and where that
+    product is beyond fp32.  Rows of one call lie close to zero too: their neighbours' size is nothing to them."""
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    x = Batch([q_len, 2], [700, 300], hq=4, hkv=2, d=64, page=16, dtype=dtype, seed=q_len)
+    x.Q.zero_()
+    x.Q[..., 0], x.Q[..., 1] = a, 1.0
+    g = torch.Generator(device=DEV).manual_seed(5)
+    for i, n in enumerate(x.kv_lens):
+        x.K[i].zero_()
+        x.K[i][..., 0] = b
+        x.K[i][..., 1] = torch.randint(0, 12, (n, 2), generator=g, device=DEV).to(dtype) + torch.arange(n, device=DEV)[:, None].div(100).floor().to(dtype)
+    near = torch.arange(0, q_len, 3, device=DEV)                              # every third row: scores 0 .. 18 times the scale
+    x.Q[near, :, 0] = 0.0
+    if scale != 1.0:
+        x.Q[near, :, 1] = 0.0
+    x.store()
+    out, z = attend(x, scale=scale, split=split)
+    at = 0
+    for i, (n, m) in enumerate(zip(x.q_lens, x.kv_lens)):
+        o, lse, mass = _softmax64(x.Q[at:at + n], x.K[i], x.V[i], scale)
+        # scores exact; an exponent that a weight above 2^-30 has is off by 32 * 2^-22 at most (the scale times log2(e), the distance times that), but in rows near
+        # zero, where scale times maximum (below 32) is rounded: included
+        bound, bound_z = attention_bounds(o, mass, torch.zeros_like(lse), 64, m, dtype, out.dtype)
+        bound = bound + 2.0 ** -17 * mass
+        assert bool(((out[at:at + n].double() - o).abs() <= bound).all())
+        finite = lse.abs() < 3.4e38
+        # normaliser: maximum times scale rounded, the logarithm added, and the logarithm's own rounding
+        off = (z[at:at + n].double() - lse).abs() - (bound_z + 2.0 ** -17 + 2.0 ** -22 * lse.abs())
+        assert bool((off[finite] <= 0).all())
+        assert bool((z[at:at + n][~finite] == lse[~finite].sign() * float("inf")).all())
+        at += n
