@@ -365,7 +365,8 @@ rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_r
  * elements and a polynomial of IEEE operations for the others, by the key's place: bits repeat on this architecture.
  * lse (may be NULL): [tokens][query heads] of stride lse_ld, fp32: the natural logarithm of the sum of exp(s_t).  A row that
  * sees no key gives zeros and -inf.  What a row does not see never reaches it, infinities and NaN in masked keys and
- * values included; where a NaN or infinite value is seen the answer's element is NaN or infinite.
+ * values included; where an infinite value is seen the answer's element is that infinity, and where a NaN or infinities
+ * of both signs are, NaN (NaN also where a part that holds an infinity has no weight next to the others).
  *   split   0, or a multiple of 128: keys [i * split, (i + 1) * split) form a part with a maximum, sum and product of
  *           its own, and the parts are joined in ascending order (by sixteens, and the sixteens then).  It decides bits (rows of one `split` have the same
  *           bits alone and in a chunk) and it spreads few rows with many keys over the GPU: 256 to 512 for single

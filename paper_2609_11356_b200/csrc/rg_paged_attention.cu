@@ -18,8 +18,8 @@
 //   producer                  work items, page numbers, then one TMA box for each page piece (a lane each): K and V blocks into one ring
 //   MMA                       S_t = Q_t K_j^T and O_t += P_t V_j for the CTA's tiles in turn
 //   fixer                     hands each arrived slot to the MMA warp; in blocks where some row is masked it first turns V elements
-//                             that are not finite into zeros (0 * NaN would reach every row of the tile).  Rows that do see such an element
-//                             get it added back when they are stored (rare, from global memory).
+//                             that are not finite into zeros (0 * NaN would reach every row of the tile).  For rows that do see such an element
+//                             the result is put right once they are stored (rare, from global memory).
 //   A chunk of 4096 rows on 16384 keys, 32 heads of 128 on 8 key heads: 0.88-0.90 ms, 1.07-1.10 PFLOP/s.  What bounds it: 512 items on 148 SMs are
 //   four turns of which the last is half empty (0.86), and a tile's chain of product, commit, 112 hardware exponentials a lane and quarter-rate
 //   unit, product (about 3500 cycles for the two tiles' 2048 of the tensor core).  Tried there: all exponentials on the hardware unit 950 us, an eighth
@@ -478,18 +478,23 @@ __device__ __forceinline__ void rescale(uint32_t t_o, float alpha) {
   }
 }
 
+// Which 16-bit elements of two words are not finite, a bit each at 15 and 31.
+template <int DT>
+__device__ __forceinline__ uint32_t not_finite_in(uint32_t x) {
+  constexpr uint32_t EXP = DT == RG_BF16 ? 0x7f807f80u : 0x7c007c00u, ONE = DT == RG_BF16 ? 0x00800080u : 0x04000400u;      // exponent fields, and what makes a full one carry
+  return ((x & EXP) + ONE) & 0x80008000u;
+}
+
 // The fixer's work on a block of V in shared memory (n 16-byte words, 128-byte rows of 64 elements, box after box): elements that are not finite
 // become zero.  Whether one of them belongs to a key of lo .. hi.
 template <int DT>
 __device__ __forceinline__ bool fix_values(uint4* base, uint32_t n, int32_t key0, int32_t lo, int32_t hi) {
-  constexpr uint32_t EXP = DT == RG_BF16 ? 0x7f807f80u : 0x7c007c00u, ONE = DT == RG_BF16 ? 0x00800080u : 0x04000400u;      // exponent fields, and what makes a full one carry
   bool seen = false;
 #pragma unroll 4
   for (uint32_t i = threadIdx.x & 31; i < n; i += 32) {
     uint4 w = base[i];
-    const uint32_t hit = (((w.x & EXP) + ONE) | ((w.y & EXP) + ONE) | ((w.z & EXP) + ONE) | ((w.w & EXP) + ONE)) & 0x80008000u;
-    if (hit) {
-      auto clean = [&](uint32_t x) { const uint32_t h = ((x & EXP) + ONE) & 0x80008000u; return x & ~((h >> 15) * 0xffffu); };
+    if (not_finite_in<DT>(w.x) | not_finite_in<DT>(w.y) | not_finite_in<DT>(w.z) | not_finite_in<DT>(w.w)) {
+      auto clean = [&](uint32_t x) { return x & ~((not_finite_in<DT>(x) >> 15) * 0xffffu); };
       w.x = clean(w.x); w.y = clean(w.y); w.z = clean(w.z); w.w = clean(w.w);
       base[i] = w;
       const int32_t key = key0 + (int32_t)(i / 8 % BLK);
@@ -498,6 +503,73 @@ __device__ __forceinline__ bool fix_values(uint4* base, uint32_t n, int32_t key0
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   return __any_sync(0xffffffffu, seen);
+}
+
+// A key's values for one key head, or null where its page is not in the cache.
+__device__ __forceinline__ const uint16_t* value_row(const Params& p, const Item& it, int32_t key) {
+  const int32_t page = key / p.by_page;
+  const int64_t id = p.table[(int64_t)it.seq * p.table_ld + page];
+  return id < 0 || id >= p.pages ? nullptr : p.v + id * p.v_page + (int64_t)(key - page * p.page_size) * p.v_slot + it.head * p.v_head;
+}
+
+// Elements of O for which a row sees an element of V that is not finite are made anew once the rest is stored, from global memory: the sum of those
+// elements (an infinity, or NaN).  The product does not do: in a block that is masked for its tile the fixer has taken them out, in any other they were
+// multiplied by a weight that may have come out as 0 (NaN for an infinity), and which of the two a block is depends on the rows that came with this one.
+// The warp goes through columns 32 q .. 32 q + 31 of V, 32 keys at a time, in masked blocks only or in `all`.  A lane first holds a key, the kinds of its
+// elements as a bit for each column, then a row, which sees keys lo .. hi (none: lo > hi) and has its results from `at` on in the output or in a part.
+// 0.8 us for 32 keys and 32 columns, 4 where every value is infinite (the 4096-row chunk takes 6 ms with one infinity, 28 with nothing else, 1 with NaN
+// alone); the waits of the other warps, 2 s, allow for four million keys of infinities in a part.
+template <int DT>
+__device__ __forceinline__ void put_odd_values(const Params& p, const Item& it, bool all, int q, int32_t lo, int32_t hi, bool writes, int64_t at) {
+  const int n = min(QW, p.d - 32 * q);
+  const uint32_t full = n == 32 ? 0xffffffffu : (1u << n) - 1;
+  uint32_t up = 0, down = 0, nan = 0;                              // the row's columns that see an infinity, a negative one, a NaN
+#pragma unroll 1
+  for (int32_t k0 = it.lo & ~31; k0 <= it.hi; k0 += 32) {
+    if (!all && !masked_block(p, it, k0 / BLK)) continue;
+    const int32_t key = k0 + (threadIdx.x & 31);
+    const uint16_t* v = key >= it.lo && key <= it.hi ? value_row(p, it, key) : nullptr;
+    uint32_t hit = 0, key_up = 0, key_down = 0, key_nan = 0;
+#pragma unroll
+    for (int w = 0; w < QW / 8; ++w) {
+      const uint4 x = v && w < n / 8 ? *reinterpret_cast<const uint4*>(v + 32 * q + 8 * w) : make_uint4(0u, 0u, 0u, 0u);
+      hit |= not_finite_in<DT>(x.x) | not_finite_in<DT>(x.y) | not_finite_in<DT>(x.z) | not_finite_in<DT>(x.w);
+    }
+#pragma unroll 1
+    for (int w = 0; hit && w < n / 8; ++w) {
+      const uint4 x = *reinterpret_cast<const uint4*>(v + 32 * q + 8 * w);
+      const uint32_t word[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t odd = not_finite_in<DT>(word[i]);
+        if (!odd) continue;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if (!(odd >> (15 + 16 * half) & 1u)) continue;
+          const uint32_t e = word[i] >> (16 * half) & 0xffffu, bit = 1u << (8 * w + 2 * i + half);
+          if (e & (DT == RG_BF16 ? 0x7fu : 0x3ffu)) key_nan |= bit;
+          else if (e >> 15) key_down |= bit;
+          else key_up |= bit;
+        }
+      }
+    }
+#pragma unroll 1
+    for (uint32_t left = __ballot_sync(0xffffffffu, (key_up | key_down | key_nan) != 0); left; left &= left - 1) {
+      const int lane = __ffs(left) - 1;
+      const uint32_t a = __shfl_sync(0xffffffffu, key_up, lane), b = __shfl_sync(0xffffffffu, key_down, lane), c = __shfl_sync(0xffffffffu, key_nan, lane);
+      if (k0 + lane >= lo && k0 + lane <= hi) { up |= a; down |= b; nan |= c; }
+    }
+    if (!__any_sync(0xffffffffu, lo <= hi && (nan | (up & down)) != full)) break;      // NaN everywhere: nothing changes any more
+  }
+  __syncwarp();                                                    // the elements were stored before, by other lanes or as parts of words
+  asm volatile("" ::: "memory");
+  void* base = it.multi ? static_cast<void*>(p.part_o) : p.out;
+  nan |= up & down;
+#pragma unroll 1
+  for (uint32_t left = writes ? up | down | nan : 0u; left; left &= left - 1) {
+    const int i = __ffs(left) - 1;
+    store_scalar(base, it.multi ? (int)RG_F32 : p.o_dtype, at + 32 * q + i, nan >> i & 1u ? __int_as_float(0x7fffffff) : up >> i & 1u ? INFINITY : -INFINITY);
+  }
 }
 
 // A position in a ring of N barriers.
@@ -820,6 +892,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         const bool none = !(sum > 0.0f) && sum == sum;             // no key seen
         const float inv = it.multi ? 1.0f : none ? 0.0f : __frcp_rn(sum);
         float* part = it.multi ? p.part_o + (grow * p.segments + it.seg) * p.d : nullptr;
+        bool odd = false;
 #pragma unroll 1
         for (int q = 0; q < HDP / QW; ++q) {
           if (32 * q >= p.d) break;
@@ -829,23 +902,10 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
           float o[QW];
 #pragma unroll
           for (int i = 0; i < QW; ++i) o[i] = none || !blocks ? 0.0f : f_mul(__uint_as_float(raw[i]), inv);
-          if (add_back && live) {
-            // the elements of V that the fixer took out and this row sees
-            for (int b = it.b0; b < it.b1; ++b) {
-              if (!masked_block(p, it, b)) continue;
-              for (int32_t k = max(lo, b * BLK); k <= min(hi, b * BLK + BLK - 1); ++k) {
-                const int64_t id = p.table[(int64_t)it.seq * p.table_ld + k / p.page_size];
-                if (id < 0 || id >= p.pages) continue;
-                const uint16_t* v = p.v + id * p.v_page + (k % p.page_size) * p.v_slot + it.head * p.v_head;
+          float z = 0.0f;
 #pragma unroll
-                for (int i = 0; i < QW; ++i) {
-                  if (32 * q + i >= p.d) break;
-                  const float x = DT == RG_BF16 ? bf16_bits_to_f32(v[32 * q + i]) : f16_bits_to_f32(v[32 * q + i]);
-                  if (!(f_add(x, -x) == 0.0f)) o[i] = f_add(o[i], x);
-                }
-              }
-            }
-          }
+          for (int i = 0; i < QW; ++i) z = f_fma(o[i], 0.0f, z);
+          odd |= !(z == 0.0f);                                     // O is not finite here
           const int n = live ? min(QW, p.d - 32 * q) : 0;
           if (n == 0) {
           } else if (it.multi) {
@@ -874,6 +934,13 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
               for (int i = 0; i < QW / 2; ++i) if (2 * i < n) { dst[2 * i] = (uint16_t)(w[i] & 0xffffu); dst[2 * i + 1] = (uint16_t)(w[i] >> 16); }
             }
           }
+        }
+        const bool some = live && sum > 0.0f;                      // the row sees keys, and no NaN among its scores
+        odd = __any_sync(0xffffffffu, odd && some);
+        if (odd || add_back) {
+#pragma unroll 1
+          for (int q = 0; 32 * q < p.d; ++q)
+            put_odd_values<DT>(p, it, odd, q, some ? lo : INT32_MAX, hi, some, it.multi ? (grow * p.segments + it.seg) * p.d : token * p.o_tok + head * p.o_head);
         }
         if (live) {
           if (it.multi) p.part_ml[grow * p.segments + it.seg] = make_float2(m, sum);
@@ -1250,23 +1317,11 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
           const float f = __shfl_sync(0xffffffffu, inv, i << SH);
           o[i] = zero ? 0.0f : f_mul(__uint_as_float(raw[i]), f);
         }
-        if (add_back) {
-          // the elements of V that the fixer took out, for the rows that see them
-          for (int b = it.b0; b < it.b1; ++b) {
-            if (!masked_block(p, it, b)) continue;
-            for (int32_t k = max(it.lo, b * BLK); k <= min(it.hi, b * BLK + BLK - 1); ++k) {
-              const int64_t id = p.table[(int64_t)it.seq * p.table_ld + k / p.page_size];
-              const bool there = id >= 0 && id < p.pages && col < p.d;
-              const float x = there ? load_scalar(p.v, DT, id * p.v_page + (int64_t)(k % p.page_size) * p.v_slot + it.head * p.v_head + col) : 0.0f;
-              const bool odd = !(f_add(x, -x) == 0.0f);
+        const bool some = live && sum > 0.0f;                      // lane's row sees keys, and no NaN among its scores
+        const uint32_t some_rows = __ballot_sync(0xffffffffu, some);
+        bool odd = false;                                          // whether O is not finite in one of them
 #pragma unroll
-              for (int i = 0; i < ROWS; ++i) {
-                const int32_t from = __shfl_sync(0xffffffffu, lo, i << SH), to = __shfl_sync(0xffffffffu, hi, i << SH);
-                if (odd && k >= from && k <= to) o[i] = f_add(o[i], x);
-              }
-            }
-          }
-        }
+        for (int i = 0; i < ROWS; ++i) odd |= (some_rows >> (i << SH) & 1u) && !(f_add(o[i], -o[i]) == 0.0f);
         if (col < p.d) {
           int tok = 0, head = 0;
 #pragma unroll
@@ -1279,6 +1334,13 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
               if (++head == p.group) { head = 0; ++tok; }
             }
           }
+        }
+        odd = __any_sync(0xffffffffu, odd);
+        if (odd || add_back) {
+          const int64_t token = (int64_t)it.tok + my_tok;
+          const int h = it.head * p.group + r - my_tok * p.group;
+          put_odd_values<DT>(p, it, odd, warp, some ? lo : INT32_MAX, hi, some && (lane & ((1 << SH) - 1)) == 0,
+                             it.multi ? ((token * p.hq + h) * p.segments + it.seg) * p.d : token * p.o_tok + h * p.o_head);
         }
       }
       if (warp == 0 && live && (lane & ((1 << SH) - 1)) == 0) {

@@ -114,3 +114,67 @@ def test_scores_far_from_zero(dtype, a, b, scale, q_len, split):
         assert bool((off[finite] <= 0).all())
         assert bool((z[at:at + n][~finite] == lse[~finite].sign() * float("inf")).all())
         at += n
+
+
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.mark.parametrize("window", [0, 200])
+@pytest.mark.parametrize("split", [0, 128])
+@pytest.mark.parametrize("dtype,d,hq", [(HF, 64, 4), (BF, 128, 8), (HF, 80, 6)])
+def test_visible_values_that_are_not_finite_do_not_depend_on_the_chunk(dtype, d, hq, split, window):
+    """Scores so far apart that most weights are 0 in the cache's type: a row that sees one infinity gets it, one that sees both or a NaN gets NaN,
+    whether the row comes in a chunk (where the block may be masked for its tile) or alone (where it may not be)."""
+    n, m = 230, 700
+    b = Batch([n], [m], hq=hq, hkv=2, d=d, page=16, dtype=dtype, seed=d, spread=4.0)
+    odd = [(10, 0, 1, INF), (300, 1, 3, INF), (470, 1, 5, -INF), (480, 1, 6, INF), (690, 1, 6, -INF), (520, 0, 7, NAN), (600, 0, d - 1, -INF), (640, 0, d - 1, -INF), (699, 1, 0, INF)]
+    clean, cz = attend(b, split=split, window=window)
+    for key, head, col, value in odd:
+        b.V[0][key, head, col] = value
+    b.store()
+    got, z = attend(b, split=split, window=window)
+    assert torch.equal(z, cz)
+    want = torch.full((n, 2, d), 0.0, device=DEV)
+    place = torch.arange(m - n, m, device=DEV)
+    for key, head, col, value in odd:
+        sees = (place >= key) & (place < key + window if window else True)
+        want[sees, head, col] += value
+    want = want.repeat_interleave(hq // 2, 1)
+    touched = want != 0                                                        # NaN != 0 as well
+    assert torch.equal(got[~touched], clean[~touched]), "an element that sees numbers only changed"
+    if split == 0:                                                             # between parts a weight of 0 may meet an infinity
+        assert torch.equal(torch.nan_to_num(got.float()[touched], 7.0, 8.0, 9.0), torch.nan_to_num(want[touched], 7.0, 8.0, 9.0))
+    else:
+        assert not bool(torch.isfinite(got[touched]).any())
+    for r in (0, 1, 50, 100, 127, 160, 200, n - 1):
+        one = Batch([1], [m - n + r + 1], hq=hq, hkv=2, d=d, page=32, dtype=dtype, seed=1)
+        one.Q, one.K, one.V = b.Q[r:r + 1], [b.K[0][:one.kv_lens[0]]], [b.V[0][:one.kv_lens[0]]]
+        one.store()
+        alone, az = attend(one, split=split, window=window)
+        assert torch.equal(alone[0].view(torch.int16), got[r].view(torch.int16)) and torch.equal(az[0], z[r]), f"row {r} alone"
+
+
+@pytest.mark.parametrize("q_len", [1, 200])
+@pytest.mark.parametrize("what", [NAN, INF])
+def test_values_that_are_all_not_finite(q_len, what):
+    b = Batch([q_len, 3], [3000, 100], hq=8, hkv=2, d=128, page=16, seed=1)
+    ok, okz = attend(b)
+    b.V[0] = torch.full_like(b.V[0], what)
+    b.store()
+    for split in (0, 128):
+        got, z = attend(b, split=split)
+        assert bool((torch.isnan(got[:q_len]) if what != what else got[:q_len] == INF).all())
+        if split == 0:
+            assert torch.equal(got[q_len:], ok[q_len:]) and torch.equal(z, okz)
+
+
+@pytest.mark.parametrize("q_len", [1, 150])
+def test_values_that_sum_beyond_fp32(q_len):
+    """O overflows although every value is finite: nothing is found, and the element stays what the sum made of it; others are not touched."""
+    b = Batch([q_len], [600], hq=4, hkv=2, d=64, page=16, seed=2)
+    ok, okz = attend(b)
+    b.V[0][:, 1, 9] = 3.0e38
+    b.store()
+    got, z = attend(b)
+    assert torch.equal(z, okz) and torch.equal(got[..., :9], ok[..., :9]) and torch.equal(got[..., 10:], ok[..., 10:]) and torch.equal(got[:, :2], ok[:, :2])
+    assert bool((got[:, 2:, 9] == INF).all())
