@@ -1,5 +1,7 @@
 """Paged append and attention at the edges of what their calls allow: tables and positions that sequences or axes share, values and
 scores that are not finite or very large, and results that must not depend on which kernel or tile takes a row."""
+import random
+
 import pytest
 import torch
 
@@ -178,3 +180,52 @@ def test_values_that_sum_beyond_fp32(q_len):
     got, z = attend(b)
     assert torch.equal(z, okz) and torch.equal(got[..., :9], ok[..., :9]) and torch.equal(got[..., 10:], ok[..., 10:]) and torch.equal(got[:, :2], ok[:, :2])
     assert bool((got[:, 2:, 9] == INF).all())
+
+
+@pytest.mark.parametrize("split", [0, 128])
+@pytest.mark.parametrize("window", [0, 150])
+@pytest.mark.parametrize("dtype,d,G", [(HF, 64, 5), (HF, 128, 7), (BF, 80, 7), (HF, 80, 1), (BF, 64, 3), (BF, 24, 8), (HF, 128, 4)])
+def test_bits_do_not_depend_on_the_form_that_takes_a_row(dtype, d, G, window, split):
+    """A row in a long chunk (the form for many rows), alone, and with one to five rows in front of it (the form for few rows at each of its heights)."""
+    n, m = 150, 613
+    b = Batch([n], [m], hq=2 * G, hkv=2, d=d, page=16, dtype=dtype, seed=d + G, spread=1.5)
+    full, z = attend(b, split=split, window=window)
+    check(b, full, z, window=window)
+    for r in (0, 5, 27, 64, 77, 149):
+        for rows in (1, 2, 3, 4, 6):
+            if rows > r + 1:
+                continue
+            end = m - n + r + 1
+            few = Batch([rows], [end], hq=2 * G, hkv=2, d=d, page=24, dtype=dtype, seed=3)
+            few.Q, few.K, few.V = b.Q[r + 1 - rows:r + 1], [b.K[0][:end]], [b.V[0][:end]]
+            few.store()
+            got, gz = attend(few, split=split, window=window)
+            assert torch.equal(got, full[r + 1 - rows:r + 1]) and torch.equal(gz, z[r + 1 - rows:r + 1]), f"{rows} rows up to row {r}"
+
+
+@pytest.mark.parametrize("split", [0, 128])
+@pytest.mark.parametrize("window", [0, 100])
+@pytest.mark.parametrize("form", ["few", "many"])
+def test_news_of_odd_values_keeps_to_its_item(form, window, split):
+    """Twenty items and more for each CTA: short and long sequences, some without new rows, tiles alone and in pairs, parts that a tile does not
+    see.  The odd values of scattered sequences reach those sequences' rows and elements, all of them, and nothing else changes by a bit."""
+    r = random.Random(7)
+    n = 700 if form == "few" else 260
+    q = [r.choice([0, 1, 1, 1]) if form == "few" else r.choice([0, 1, 40, 64, 65, 130, 200]) for _ in range(n)]
+    kv = [x + r.choice([0, r.randint(0, 40), r.randint(0, 400)]) for x in q]
+    b = Batch(q, kv, hq=16, hkv=8, d=64, page=16, dtype=BF, seed=1, tail_rows=3)
+    clean, cz = attend(b, split=split, window=window)
+    want = torch.zeros(b.T, 8, 64, dtype=torch.bool, device=DEV)
+    at = 0
+    for i, (rows, m) in enumerate(zip(q, kv)):
+        if rows and r.random() < 0.3:
+            key, head, col = r.randrange(m), r.randrange(8), r.randrange(64)
+            b.V[i][key, head, col] = r.choice([INF, -INF, NAN])
+            place = torch.arange(m - rows, m, device=DEV)
+            want[at:at + rows, head, col] = (place >= key) & (place < key + (window or 1 << 30))
+        at += rows
+    b.store()
+    got, z = attend(b, split=split, window=window)
+    want = want.repeat_interleave(2, 1)
+    assert int(want.sum()) > 100 and torch.equal(z, cz)
+    assert not bool(torch.isfinite(got[want]).any()) and torch.equal(got[~want], clean[~want])
