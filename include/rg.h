@@ -340,7 +340,7 @@ typedef struct {
 } rg_rope_desc_t;
 
 /* out = x rotated.  x and out: bf16, fp16 or fp32 of one type, same shape, any strides; out may be x itself, else
- * they do not overlap.  pos: RG_I32 or RG_I64, rows = axes, cols = tokens, `ld` elements between axes.  inv_freq:
+ * they do not overlap.  pos: RG_I32 or RG_I64, rows = axes, cols = tokens, `ld` elements between axes (at least tokens, or 0: one row for all).  inv_freq:
  * DEVICE pointer to rot_dim / 2 doubles.  Asynchronous on `cuda_stream`. */
 rg_status_t rg_rope(const rg_rope_desc_t* d, const rg_rows_t* x, const rg_tensor_t* pos, const double* inv_freq,
                     const rg_rows_t* out, void* cuda_stream);

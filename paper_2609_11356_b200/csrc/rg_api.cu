@@ -521,7 +521,7 @@ rg_status_t check_rope_desc(const rg_rope_desc_t* d, int64_t dim) {
 
 rg_status_t check_positions(const rg_rope_desc_t* d, const rg_tensor_t* pos, int64_t tokens) {
   if (pos->dtype != RG_I32 && pos->dtype != RG_I64) return RG_ERR_SHAPE;
-  if (pos->rows != d->n_axes || pos->cols != tokens || (d->n_axes > 1 && pos->ld < tokens)) return RG_ERR_SHAPE;
+  if (pos->rows != d->n_axes || pos->cols != tokens || (d->n_axes > 1 && pos->ld < tokens && pos->ld != 0)) return RG_ERR_SHAPE;      // 0: one row for all axes
   if (tokens > 0 && !pos->ptr) return RG_ERR_NULL;
   if (reinterpret_cast<uintptr_t>(pos->ptr) % (pos->dtype == RG_I64 ? 8 : 4)) return RG_ERR_ALIGNMENT;
   return RG_OK;

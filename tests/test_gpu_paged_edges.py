@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2609_11356_b200 as rg
-from tests._paged_util import DEV, Batch, attend, attention_bounds, check
+from tests._paged_util import DEV, Batch, attend, attention_bounds, check, inv_freq
 
 pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
@@ -229,3 +229,22 @@ def test_news_of_odd_values_keeps_to_its_item(form, window, split):
     want = want.repeat_interleave(2, 1)
     assert int(want.sum()) > 100 and torch.equal(z, cz)
     assert not bool(torch.isfinite(got[want]).any()) and torch.equal(got[~want], clean[~want])
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+def test_axes_that_share_their_positions(dtype):
+    """One row of positions expanded over the axes is what the row repeated is, alone and on the way into the cache."""
+    T = 37
+    x = torch.randn(T, 4, 64, device=DEV)
+    p = torch.randint(0, 9000, (T,), device=DEV).to(dtype)
+    desc, f = rg.rg_rope_desc(rot_dim=64, sections=(8, 12, 12)), inv_freq(64)
+    want = rg.rg_rope(desc, x, p.repeat(3, 1), f, torch.empty_like(x))
+    assert torch.equal(rg.rg_rope(desc, x, p.expand(3, T), f, torch.empty_like(x)), want)
+    assert torch.equal(rg.rg_rope(rg.rg_rope_desc(rot_dim=64), x, p, f, torch.empty_like(x)), want)
+    b = Batch([T], [50], hq=2, hkv=2, d=64, page=16, dtype=BF, garbage=3.0)
+    k, stored = torch.randn(T, 2, 64, device=DEV).to(BF), []
+    for pos in (p.repeat(3, 1), p.expand(3, T)):
+        kc, vc = torch.full_like(b.kc, 3.0), torch.full_like(b.vc, 3.0)
+        rg.rg_kv_append(desc, k, k, f, kc, vc, b.seqs(), pos=pos)
+        stored.append((kc, vc))
+    assert torch.equal(stored[0][0], stored[1][0]) and torch.equal(stored[0][1], stored[1][1])

@@ -6,7 +6,7 @@ import torch
 
 import paper_2609_11356_b200 as rg
 from paper_2609_11356_b200 import _cabi as K, api
-from tests.test_paged_host import SHAPE, WS, append, attend, cache, rows, seqs
+from tests.test_paged_host import SHAPE, WS, append, attend, cache, pos, rope, rows, seqs
 
 I32 = dict(dtype=torch.int32)
 
@@ -96,3 +96,13 @@ def test_a_cache_of_any_nested_strides_is(kw):
     assert append(k=rows(0), v=rows(0), kc=cache(**kw), vc=cache(**kw)) == 0    # no tokens: accepted, nothing launched
     heads = cache(heads=1, head_stride=0)
     assert append(k=rows(0, heads=1), v=rows(0, heads=1), kc=heads, vc=heads) == 0
+
+
+def test_axes_that_share_their_positions():
+    """pos.expand(3, T), text under three axes: one row that all of them read."""
+    d = rg.rg_rope_desc(rot_dim=64, sections=(8, 12, 12))
+    nobody = seqs(n_seqs=0, block_table=None, seq_lens=None, cu_q=None)         # so nothing is launched
+    assert append(d=d, pos=pos(3, ld=0), s=nobody) == 0 and append(d=d, pos=pos(3, ld=4), s=nobody) == 0
+    assert rope(d=d, x=rows(0), out=rows(0), pos=pos(3, cols=0, ld=0)) == 0
+    for ld in (1, 3):
+        assert rope(d=d, pos=pos(3, ld=ld)) == SHAPE and append(d=d, pos=pos(3, ld=ld)) == SHAPE
