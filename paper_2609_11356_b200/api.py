@@ -332,11 +332,16 @@ def _one_device(where: str, *tensors) -> int:
     return device
 
 
+def _fits(bits: int, *values) -> bool:
+    """Whether unsigned fields of so many bits hold the values (ctypes drops what they do not)."""
+    return all(0 <= v < 1 << bits for v in values)
+
+
 def rg_rope_desc(*, rot_dim: int, style: int = K.RG_ROPE_HALF, sections: Sequence[int] = (), inverse: int = 0) -> K.rg_rope_desc_t:
     """Rotary positions (see include/rg.h): `sections` gives the pairs of each axis (default: one axis with all of them)."""
     d = K.rg_rope_desc_t()
     sections = tuple(sections) or (rot_dim // 2,)
-    if len(sections) > 4 or rot_dim < 0 or any(n < 0 for n in sections):
+    if len(sections) > 4 or not _fits(32, rot_dim, *sections) or not _fits(8, style, int(inverse)):
         raise RgError(2, "rg_rope_desc")
     d.size, d.rot_dim, d.style, d.n_axes, d.inverse = C.sizeof(K.rg_rope_desc_t), rot_dim, style, len(sections), int(inverse)
     for i, n in enumerate(sections):
@@ -370,6 +375,8 @@ class rg_paged_seqs:
             raise ValueError(f"{n} sequences need block_table [{n}, pages] and cu_q [{n + 1}], got {tuple(block_table.shape)} and {tuple(cu_q.shape)}")
         if not block_table.device == seq_lens.device == cu_q.device:
             raise ValueError("rg_paged_seqs: tensors on different devices")
+        if not _fits(63, max_q, max_len):
+            raise RgError(4, "rg_paged_seqs")
         cols = block_table.shape[1]
         table_ld = block_table.stride(0) if n > 1 else cols
         if 0 < table_ld < cols:
@@ -392,7 +399,7 @@ def rg_kv_append(d, k, v, inv_freq, k_cache, v_cache, seqs: rg_paged_seqs, *, po
 
 def rg_paged_attn_desc(*, scale: float, split: int = 0, window: int = 0, mask: int = 1) -> K.rg_paged_attn_desc_t:
     """Attention over a paged cache: `split` keys for each part (0: one part), a causal mask (mask=1) of the last `window` keys (0: all)."""
-    if split < 0 or window < 0:
+    if not _fits(32, split, window) or not _fits(8, mask):
         raise RgError(2, "rg_paged_attn_desc")
     return K.rg_paged_attn_desc_t(C.sizeof(K.rg_paged_attn_desc_t), split, window, scale, mask)
 

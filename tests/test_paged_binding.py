@@ -6,7 +6,7 @@ import torch
 
 import paper_2609_11356_b200 as rg
 from paper_2609_11356_b200 import _cabi as K, api
-from tests.test_paged_host import SHAPE, WS, append, attend, cache, pos, rope, rows, seqs
+from tests.test_paged_host import DESC, SHAPE, WS, append, attend, cache, pos, rope, rows, seqs
 
 I32 = dict(dtype=torch.int32)
 
@@ -106,3 +106,24 @@ def test_axes_that_share_their_positions():
     assert rope(d=d, x=rows(0), out=rows(0), pos=pos(3, cols=0, ld=0)) == 0
     for ld in (1, 3):
         assert rope(d=d, pos=pos(3, ld=ld)) == SHAPE and append(d=d, pos=pos(3, ld=ld)) == SHAPE
+
+
+@pytest.mark.parametrize("kw", [{"style": 256}, {"style": -1}, {"inverse": 256}, {"inverse": -256}, {"rot_dim": 2 ** 32 + 64}, {"rot_dim": -64}, {"sections": (2 ** 32 + 32,)}, {"sections": (33, -1)}])
+def test_rope_fields_that_do_not_fit_are_refused(kw):
+    with pytest.raises(rg.RgError) as e:                                      # 256 is 0 in a byte: another rotation, without a word
+        rg.rg_rope_desc(**({"rot_dim": 64} | kw))
+    assert e.value.status == DESC
+
+
+@pytest.mark.parametrize("kw", [{"mask": 256}, {"mask": -1}, {"split": 2 ** 32}, {"split": 2 ** 32 + 128}, {"window": 2 ** 32}, {"window": -1}])
+def test_attention_fields_that_do_not_fit_are_refused(kw):
+    with pytest.raises(rg.RgError) as e:
+        rg.rg_paged_attn_desc(scale=1.0, **kw)
+    assert e.value.status == DESC
+
+
+@pytest.mark.parametrize("kw", [{"max_q": 2 ** 63}, {"max_len": 2 ** 64 + 5}, {"max_q": -1}, {"max_len": -5}])
+def test_bounds_that_do_not_fit_are_refused(kw):
+    with pytest.raises(rg.RgError) as e:
+        rg.rg_paged_seqs(torch.zeros(1, 5, **I32), torch.zeros(1, **I32), torch.zeros(2, **I32), **kw)
+    assert e.value.status == SHAPE
