@@ -1845,7 +1845,6 @@ rg_status_t launch_silu_selftest(const float* x, float* y, int64_t n, cudaStream
   return cudaGetLastError() == cudaSuccess ? RG_OK : RG_ERR_CUDA;
 }
 
-// The same tensor map for other kernels of the library (boxes of 64 columns x box_rows rows, 128-byte swizzle).
 // 4-D tensor map over 16-bit elements (innermost dimension contiguous, strides of the others in elements), 128-byte swizzle, zero fill
 // outside.  The stride of a dimension of one entry is never used and may be anything.
 bool make_tmap_4d(CUtensorMap_st* map, const void* ptr, int dtype, const int64_t (&dims)[4], const int64_t (&strides)[3], const int (&box)[4]) {
@@ -1860,6 +1859,7 @@ bool make_tmap_4d(CUtensorMap_st* map, const void* ptr, int dtype, const int64_t
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same tensor map for other kernels of the library (boxes of 64 columns x box_rows rows, 128-byte swizzle).
 bool make_operand_tmap(CUtensorMap_st* map, const void* ptr, int dtype, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
   return cached_tmap(map, ptr, dtype, rows, cols, ld, box_rows);
 }

@@ -152,7 +152,7 @@ __device__ __forceinline__ int32_t operator/(int32_t n, const Div& v) { return v
 struct Params {
   const int32_t *table, *seq_lens, *cu_q;
   int64_t table_ld, max_len, tokens;
-  int32_t n_seqs, page_size, pages, table_cols;
+  int32_t n_seqs, page_size, pages;
   int32_t hq, hkv, group, d;
   Div by_split, by_hkv, by_hq, by_page, by_group, by_tile;   // by_tile: a CTA's tokens
   int32_t tile_tokens, cta_tokens;       // tokens of one tile: floor(rows of a tile / group); of a CTA: one tile's or two tiles'
@@ -675,7 +675,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
       alive = pa_wait(b_q_empty, q_phase, abort_flag, 0x2100u);
       if (!alive) break;
       q_phase ^= 1u;
-      const int tiles = NT == 2 && it.n_tok > p.tile_tokens ? 2 : 1;
+      const int tiles = it.n_tok > p.tile_tokens ? 2 : 1;
       if (lane == 0) mbar_expect_tx(b_q_full, (uint32_t)(tiles * DB * p.tile_tokens * p.group) * 128u);
       __syncwarp();
       if (lane < tiles * DB) {
@@ -730,7 +730,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
     while (alive && next_item(it, alive)) {
       const int nb = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
       if (nb == 0) continue;
-      const int tiles = NT == 2 && __shfl_sync(0xffffffffu, it.n_tok, 0) > p.tile_tokens ? 2 : 1;
+      const int tiles = __shfl_sync(0xffffffffu, it.n_tok, 0) > p.tile_tokens ? 2 : 1;
       alive = pa_wait(b_q_full, q_phase, abort_flag, 0x2400u);
       q_phase ^= 1u;
       if (!alive) break;
@@ -1547,7 +1547,7 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   const int G = (int)(a.q->heads / hkv), d = (int)a.q->dim, page = (int)a.k->page_size;
   p.table = a.seqs->block_table; p.seq_lens = a.seqs->seq_lens; p.cu_q = a.seqs->cu_q;
   p.table_ld = a.seqs->table_ld; p.max_len = a.max_len; p.tokens = T;
-  p.n_seqs = a.seqs->n_seqs; p.page_size = page; p.pages = (int32_t)a.k->pages; p.table_cols = a.seqs->table_cols;
+  p.n_seqs = a.seqs->n_seqs; p.page_size = page; p.pages = (int32_t)a.k->pages;
   p.hq = (int32_t)a.q->heads; p.hkv = (int32_t)hkv; p.group = G; p.d = d;
   p.split = (int32_t)a.split; p.segments = a.segments; p.causal = a.causal; p.window = (int32_t)a.window;
   p.scale = a.scale; p.c = a.scale * 1.44269504f;
@@ -1560,8 +1560,8 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   p.v = static_cast<const uint16_t*>(a.v->ptr); p.v_page = a.v->page_stride; p.v_slot = a.v->slot_stride; p.v_head = a.v->head_stride;
 
   const int64_t need = a.max_q * G;
-  const int most_rows = d <= 64 ? 32 : 16, FEW_TILES = 1;
-  const int rows = need <= 8 ? 8 : need <= 16 ? 16 : G <= most_rows && need <= FEW_TILES * most_rows ? most_rows : 128;
+  const int most_rows = d <= 64 ? 32 : 16;
+  const int rows = need <= 8 ? 8 : need <= 16 ? 16 : need <= most_rows ? most_rows : 128;
   const bool narrow = rows < 128;
   p.tile_tokens = rows / G;
   int box = page & -page;                                  // the largest power of two that divides the page size: boxes never cross pages
@@ -1578,11 +1578,15 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
 
   p.by_split = Div::by(p.split ? p.split : 1); p.by_hkv = Div::by(p.hkv); p.by_hq = Div::by(p.hq); p.by_page = Div::by(page); p.by_group = Div::by(G);
   // Two tiles share the keys that a CTA reads and the tensor core works for one while the other's softmax runs; but where all tiles find an SM
-  // each, one tile alone is done sooner (about 2600 cycles a block against 3500).
+  // each, one tile alone is done sooner (about 2600 cycles a block against 3500).  128 rows a key head and tile, 1500 keys in front: 16 tiles 31.9 us alone and
+  // 36.1 in twos, 64 tiles 33.3 and 37.3, 128 tiles 32.8 and 36.2; 152 tiles 60.6 and 43.5, 256 tiles 73.9 and 49.0.
   auto items_of = [&](int64_t tokens) { return std::min<int64_t>(T, (T + tokens - 1) / tokens + p.n_seqs) * hkv * a.segments; };
   p.cta_tokens = narrow || items_of(p.tile_tokens) <= current_device().sms ? p.tile_tokens : 2 * p.tile_tokens;
   p.by_tile = Div::by(p.cta_tokens);
-  p.levels = a.split != 0 || p.n_seqs > 128 ? 1 : p.n_seqs > 32 ? 8 : 16;      // a level is a walk over all sequences
+  // A level is a walk over all sequences, so many of them want fewer levels.  Mixed prompts, 1 / 8 / 16 levels, us: 9 sequences of up to 1000 rows 178 / 164 /
+  // 152 and 203 / 190 / 189; 32 of up to 600 rows 268 / 234 / 232; 64 of up to 300 rows 339 / 285 / 294; 128 of up to 200 rows 379 / 346 / 375; 300 of up to
+  // 100 rows 357 / 348 / 424, of up to 4 rows 322 / 344 / 372.  Parts are alike: one level.
+  p.levels = a.split != 0 || p.n_seqs > 128 ? 1 : p.n_seqs > 32 ? 8 : 16;
   // no more CTAs than there can be items
   const int64_t most = items_of(p.cta_tokens);
   if (most >= (int64_t(1) << 31) || T * p.hq >= (int64_t(1) << 31)) return RG_ERR_SHAPE;     // items and rows are counted in 32 bits
