@@ -302,11 +302,12 @@ typedef struct {
  *   max_q    the host's upper bound of new tokens in one sequence (0: the number of rows).  It picks tile
  *            heights and never changes a bit or an answer.
  *   max_len  the host's upper bound of seq_lens (0: table_cols * page_size).  It sizes the workspace.
- * What only the device sees is checked there: a token without a place (seq_lens[s] < its count of new rows), a
- * length beyond max_len or beyond the table, a page outside the cache.  Nothing out of bounds is touched; the
- * health word (rg_device_status) then holds RG_PAGE_CODE_APPEND or RG_PAGE_CODE_ATTEND and the call's answer for
- * that sequence is not meaningful: its key or value is not written, a page outside the cache reads as zeros, a
- * length counts as its bound, a row without a place gives zeros (and -inf).
+ * What only the device sees is checked there: a token without a place (seq_lens[s] < its count of new rows) or with
+ * one beyond the table, a page outside the cache; in rg_paged_attention also a length beyond max_len or the table
+ * (rg_kv_append has no use for max_len).  Nothing out of bounds is touched; the health word (rg_device_status) then
+ * holds RG_PAGE_CODE_APPEND or RG_PAGE_CODE_ATTEND and the call's answer for that sequence is not meaningful: its key
+ * or value is not written, a page outside the cache reads as zeros, a length counts as its bound, a row without a
+ * place gives zeros (and -inf).
  * A page may serve several sequences (a shared prefix) as long as no two tokens of one call write one slot. */
 typedef struct {
   const int32_t* block_table;
@@ -368,9 +369,12 @@ rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_r
  * values included; where an infinite value is seen the answer's element is that infinity, and where a NaN or infinities
  * of both signs are, NaN (NaN also where a part that holds an infinity has no weight next to the others).
  *   split   0, or a multiple of 128: keys [i * split, (i + 1) * split) form a part with a maximum, sum and product of
- *           its own, and the parts are joined in ascending order (by sixteens, and the sixteens then).  It decides bits (rows of one `split` have the same
- *           bits alone and in a chunk) and it spreads few rows with many keys over the GPU: 256 to 512 for single
- *           tokens, 0 for long chunks.
+ *           its own, and the parts are joined in ascending order (by sixteens, and the sixteens then).  It decides bits: rows
+ *           of one `split` have the same bits alone and in a chunk, rows of two have not.  It spreads few rows with many
+ *           keys over the GPU, and every part of every row goes through the workspace.  Single tokens want 256 to 512
+ *           (one on 60001 keys, 32 heads of 128: 55 us with 512, 804 with 0), long chunks 0 (4096 rows on 16384 keys:
+ *           0.85 ms with 0, 1.1 with 2048, 2.4 with 512, 3.7 with 256).  A server whose rows must have the same bits in a
+ *           prompt and as single tokens keeps one `split` for both and pays for it.
  * Pages that lie wholly in front of every new row's window are not read; their table entries may be anything.
  * q, out: [tokens][query heads][dim]; q of the caches' type, bf16 or fp16; out of that type or fp32.  dim is a
  * multiple of 8 up to 128; query heads a multiple of kv heads, at most 128 for each; page_size a multiple of 8;

@@ -6,7 +6,9 @@
 //   m'  = max_t s_t;  if (m' - m) c > 8:  a = 2^((m - m') c), m = m', l = a l, O = a O      (else m, l and O stay)
 //   p_t = 2^(s_t c - m c), or 2^((s_t - m) c) where m c is large;  l += sum of p_t;  O += P V       P = p narrowed, 8 steps on the same accumulator
 // and at the end O * (1 / l).  A running maximum that may lag by 2^8 costs nothing in precision (p is a floating-point number
-// below 2^8) and saves nearly every rescaling of O, which lives in tensor memory.
+// below 2^8) and saves nearly every rescaling of O, which lives in tensor memory.  P is
+// narrowed because the tensor core takes two operands of one 16-bit type: half a step of it on every weight, 0.0023 off in all for bf16 where 32-bit weights
+// are 0.0017 off by the result's own rounding (fp16: 0.00029 and 0.00021); the sum l takes the weights before that.
 //
 // The sum is kept for each quarter of a block's keys (32 of them, added as a butterfly adds them) and the four are joined at the end.  All of it is one
 // fixed order in both kernels below, and neither knows which other rows there are: a block that a row does not see adds exact zeros, so
@@ -20,10 +22,11 @@
 //   fixer                     hands each arrived slot to the MMA warp; in blocks where some row is masked it first turns V elements
 //                             that are not finite into zeros (0 * NaN would reach every row of the tile).  For rows that do see such an element
 //                             the result is put right once they are stored (rare, from global memory).
-//   A chunk of 4096 rows on 16384 keys, 32 heads of 128 on 8 key heads: 0.88-0.90 ms, 1.07-1.10 PFLOP/s.  What bounds it: 512 items on 148 SMs are
+//   A chunk of 4096 rows on 16384 keys, 32 heads of 128 on 8 key heads: 0.95-0.97 ms called on rotating inputs, 1.0 PFLOP/s (0.85 ms, 1.13 PFLOP/s as a graph
+//   of ten on one input).  What bounds it: 512 items on 148 SMs are
 //   four turns of which the last is half empty (0.86), and a tile's chain of product, commit, 112 hardware exponentials a lane and quarter-rate
-//   unit, product (about 3500 cycles for the two tiles' 2048 of the tensor core).  Tried there: all exponentials on the hardware unit 950 us, an eighth
-//   by the polynomial 896, a quarter 906-925, three eighths 985; two threads a row (16 softmax warps) 1070; scores read twice instead of held in
+//   unit, product (about 3500 cycles for the two tiles' 2048 of the tensor core).  Tried there, as graphs: all exponentials on the hardware unit 950 us,
+//   an eighth by the polynomial 896, a quarter 906-925, three eighths 985; two threads a row (16 softmax warps) 1070; scores read twice instead of held in
 //   registers 1090.
 // paged_attention_few_kernel, for single tokens and drafts: further down.
 // The grid is persistent: the work items (sequence, tile, part, key head) are counted out of the sequences' lengths on the device, so
@@ -976,9 +979,9 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
 //   O' += V_j^T P^T    lane = element of the head, column = row of queries; V is read transposed, P from shared memory
 // A softmax thread is one key of the block and holds its score with every row; maxima and sums over the keys go through butterflies
 // in which lanes trade rows (after five steps a lane holds one row's value), and the four warps' maxima through shared memory.
-// What bounds it: the K and V bytes.  64 sequences of up to 8192 keys, 8 key heads of 128 (1.14 GB): 188 us, 6.05 TB/s; 4 of up to 61000 (0.76 GB): 128 us,
-// 5.9 TB/s; one of 8192 (34 MB): 12 us, of which the copies are 5 (launch, item and page look-up, the chain of two blocks and the join are latency).
-// With the queries as the 128 rows instead (the other form, 4 of them filled) the 64 sequences took 234 us, and 278 with each row's keys dealt to
+// What bounds it: the K and V bytes.  64 sequences of up to 8192 keys, 8 key heads of 128 (1.14 GB): 195 us a call, 5.8 TB/s; 4 of up to 61000 (0.76 GB): 131 us,
+// 5.8 TB/s; one of 8192 (34 MB): 13 us, of which the copies are 5 (launch, item and page look-up, the chain of two blocks and the join are latency).
+// With the queries as the 128 rows instead (the other form, 4 of them filled) the 64 sequences took 234 us on the device, and 278 with each row's keys dealt to
 // four warps: the tensor core then reads 128 mostly empty rows from shared memory for every step.
 template <int HDP, int ROWS>
 struct Few {
@@ -1578,8 +1581,8 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
 
   p.by_split = Div::by(p.split ? p.split : 1); p.by_hkv = Div::by(p.hkv); p.by_hq = Div::by(p.hq); p.by_page = Div::by(page); p.by_group = Div::by(G);
   // Two tiles share the keys that a CTA reads and the tensor core works for one while the other's softmax runs; but where all tiles find an SM
-  // each, one tile alone is done sooner (about 2600 cycles a block against 3500).  128 rows a key head and tile, 1500 keys in front: 16 tiles 31.9 us alone and
-  // 36.1 in twos, 64 tiles 33.3 and 37.3, 128 tiles 32.8 and 36.2; 152 tiles 60.6 and 43.5, 256 tiles 73.9 and 49.0.
+  // each, one tile alone is done sooner (about 2600 cycles a block against 3500).  4 query heads a key head, so 32 tokens a tile, on 1500 keys: 16 tiles 31.9 us
+  // alone and 36.1 in twos, 64 tiles 33.3 and 37.3, 128 tiles 32.8 and 36.2; 152 tiles 60.6 and 43.5, 256 tiles 73.9 and 49.0.
   auto items_of = [&](int64_t tokens) { return std::min<int64_t>(T, (T + tokens - 1) / tokens + p.n_seqs) * hkv * a.segments; };
   p.cta_tokens = narrow || items_of(p.tile_tokens) <= current_device().sms ? p.tile_tokens : 2 * p.tile_tokens;
   p.by_tile = Div::by(p.cta_tokens);
