@@ -359,7 +359,7 @@ rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_r
  * Query head h reads key head h / (query heads / kv heads).  A row at place p sees keys t <= p (mask = 1) or all
  * keys of its sequence (mask = 0), and with window > 0 (mask = 1 only) of those the last `window`: t > p - window.
  * Keys are walked in blocks of 128 places; with s_t = scale * (q . k_t) in fp32 from tensor-core chains over dim,
- *   p_t = exp(s_t - m),   l += sum of the block's p_t,   O += (P . V)_block,   P = p narrowed to the cache's type
+ *   p_t = exp(s_t - m),   l += sum of the block's p_t,   O += (P . V)_block,   P = p narrowed to the cache's type (fp16: 2^7 p)
  * where m is a running maximum that moves (and O and l are rescaled, in fp32) only when a block's maximum exceeds
  * it by more than 8 / log2(e); the answer is O times 1 / l, rounded once.  Weights follow the distances between scores: q . k_t has to be
  * finite in fp32, s_t need not be (its normaliser is infinite then).  exp is the hardware's base-two exponential for some of the

@@ -6,9 +6,9 @@
 //   m'  = max_t s_t;  if (m' - m) c > 8:  a = 2^((m - m') c), m = m', l = a l, O = a O      (else m, l and O stay)
 //   p_t = 2^(s_t c - m c), or 2^((s_t - m) c) where m c is large;  l += sum of p_t;  O += P V       P = p narrowed, 8 steps on the same accumulator
 // and at the end O * (1 / l).  A running maximum that may lag by 2^8 costs nothing in precision (p is a floating-point number
-// below 2^8) and saves nearly every rescaling of O, which lives in tensor memory.  P is
-// narrowed because the tensor core takes two operands of one 16-bit type: half a step of it on every weight, 0.0023 off in all for bf16 where 32-bit weights
-// are 0.0017 off by the result's own rounding (fp16: 0.00029 and 0.00021); the sum l takes the weights before that.
+// below 2^8) and saves nearly every rescaling of O, which lives in tensor memory.  P is narrowed because the tensor core takes two
+// operands of one 16-bit type (fp16: 2^7 P, see shift_of): half a step of it on every weight, 0.0023 off in all for bf16 where 32-bit weights are
+// 0.0017 off by the result's own rounding (fp16: 0.00029 and 0.00021); the sum l takes the weights before that.
 //
 // The sum is kept for each quarter of a block's keys (32 of them, added as a butterfly adds them) and the four are joined at the end.  All of it is one
 // fixed order in both kernels below, and neither knows which other rows there are: a block that a row does not see adds exact zeros, so
@@ -339,7 +339,7 @@ __device__ __forceinline__ bool masked_block(const Params& p, const Item& it, in
 }
 
 // ---------------------------------------------------------------- one row, one block
-// 2^x for x <= LAG or NaN by its own steps: the nearest integer by a magic addition, a polynomial of degree 5 for the rest (equal to 1
+// 2^x for x <= LAG + 7 or NaN by its own steps: the nearest integer by a magic addition, a polynomial of degree 5 for the rest (equal to 1
 // at 0; largest relative error 1.7e-7, fitted by iteratively reweighted least squares), the integer added to the exponent; 0 below -125.
 // Two at a time.  The integer sum at the end (and not a multiplication) keeps the assembler from contracting it with the addition that
 // follows.  NaN comes out as some number: a row with a NaN among its scores is marked in its sum.
@@ -398,12 +398,18 @@ __device__ __forceinline__ float move_max(float& m, float mb, float c) {
 // What a row's scores take on the way to their exponents: x = (s - off) c + shift.  The product m c is rounded once for all of a row's keys, and what it
 // is off by, up to half its last place, multiplies every weight: nothing while it is below 2^-8, but at 2^31 weights pass fp16's range or
 // vanish, and from 2^128 on there is no product.  Rows that far out take their maximum off first; s - m is exact where it matters.
+// In fp16 all weights of a row, its sum and O are 2^7 times as large until the end (below 2^15, the maximum's lag included): a weight's half step is then 2^-32
+// of the largest weight or less and not 2^-25, which lost everything below that: 60000 keys of weight 2^-26 next to one of 1 are a thousandth of the result.
 constexpr float FAR = 65536.0f;
+template <int DT> constexpr float UP = DT == RG_F16 ? 7.0f : 0.0f;
+template <int DT> constexpr float DOWN = DT == RG_F16 ? 0x1p-7f : 1.0f;
+template <int DT>
 __device__ __forceinline__ bool shift_of(float m, float c, float& shift, float& off) {
   shift = m == -INFINITY ? 0.0f : -f_mul(m, c);
   off = 0.0f;
   const bool far = fabsf(shift) >= FAR && m != INFINITY;       // an infinite maximum: the row is NaN
   if (far) { off = m; shift = 0.0f; }
+  if (DT == RG_F16) shift = f_add(shift, UP<DT>);
   return far;
 }
 
@@ -843,7 +849,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
             if (moved) {
               if (up) alpha = move_max(m, mb, p.c);
               float off;
-              far = shift_of(m, p.c, shift, off);
+              far = shift_of<DT>(m, p.c, shift, off);
               if (far) {
 #pragma unroll
                 for (int i = 0; i < BLK; ++i) s[i] = __float_as_uint(f_add(__uint_as_float(s[i]), -off));
@@ -893,7 +899,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         const int head = it.head * p.group + my_head;
         const int64_t grow = token * p.hq + head;
         const bool none = !(sum > 0.0f) && sum == sum;             // no key seen
-        const float inv = it.multi ? 1.0f : none ? 0.0f : __frcp_rn(sum);
+        const float inv = it.multi ? DOWN<DT> : none ? 0.0f : __frcp_rn(sum);
         float* part = it.multi ? p.part_o + (grow * p.segments + it.seg) * p.d : nullptr;
         bool odd = false;
 #pragma unroll 1
@@ -946,8 +952,8 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
             put_odd_values<DT>(p, it, odd, q, some ? lo : INT32_MAX, hi, some, it.multi ? (grow * p.segments + it.seg) * p.d : token * p.o_tok + head * p.o_head);
         }
         if (live) {
-          if (it.multi) p.part_ml[grow * p.segments + it.seg] = make_float2(m, sum);
-          else if (p.lse) p.lse[token * p.lse_ld + head] = none ? -INFINITY : f_add(f_mul(m, p.scale), logf(sum));
+          if (it.multi) p.part_ml[grow * p.segments + it.seg] = make_float2(m, f_mul(sum, DOWN<DT>));
+          else if (p.lse) p.lse[token * p.lse_ld + head] = none ? -INFINITY : f_add(f_mul(m, p.scale), logf(f_mul(sum, DOWN<DT>)));
         }
       }
       if (blocks) {
@@ -1254,7 +1260,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         const float mb = max3(max3(x[lane], x[32 + lane], x[64 + lane]), x[96 + lane], x[96 + lane]);
         const float alpha = rises(m, mb, p.c) ? move_max(m, mb, p.c) : 1.0f;
         float shift, off;
-        if (__any_sync(0xffffffffu, shift_of(m, p.c, shift, off))) {
+        if (__any_sync(0xffffffffu, shift_of<DT>(m, p.c, shift, off))) {
 #pragma unroll
           for (int i = 0; i < ROWS; ++i) s[i] = __float_as_uint(f_add(__uint_as_float(s[i]), -__shfl_sync(0xffffffffu, off, i << SH)));
         }
@@ -1307,7 +1313,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         add_back = any_masked && not_finite[slot_flag] != 0;
       }
       const bool none = !(sum > 0.0f) && sum == sum;               // no key seen
-      const float inv = it.multi ? 1.0f : none ? 0.0f : __frcp_rn(sum);
+      const float inv = it.multi ? DOWN<DT> : none ? 0.0f : __frcp_rn(sum);
       const int col = warp * 32 + lane;                            // element of the head
       const int n_rows = it.n_tok * p.group;
       if (warp * 32 < p.d) {
@@ -1349,8 +1355,8 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       if (warp == 0 && live && (lane & ((1 << SH) - 1)) == 0) {
         const int64_t token = (int64_t)it.tok + my_tok;
         const int h = it.head * p.group + r - my_tok * p.group;
-        if (it.multi) p.part_ml[(token * p.hq + h) * p.segments + it.seg] = make_float2(m, sum);
-        else if (p.lse) p.lse[token * p.lse_ld + h] = none ? -INFINITY : f_add(f_mul(m, p.scale), logf(sum));
+        if (it.multi) p.part_ml[(token * p.hq + h) * p.segments + it.seg] = make_float2(m, f_mul(sum, DOWN<DT>));
+        else if (p.lse) p.lse[token * p.lse_ld + h] = none ? -INFINITY : f_add(f_mul(m, p.scale), logf(f_mul(sum, DOWN<DT>)));
       }
       if (blocks) {
         pa_fence_before();

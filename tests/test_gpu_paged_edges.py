@@ -248,3 +248,32 @@ def test_axes_that_share_their_positions(dtype):
         rg.rg_kv_append(desc, k, k, f, kc, vc, b.seqs(), pos=pos)
         stored.append((kc, vc))
     assert torch.equal(stored[0][0], stored[1][0]) and torch.equal(stored[0][1], stored[1][1])
+
+
+@pytest.mark.parametrize("q_len", [1, 40])
+@pytest.mark.parametrize("dtype", [HF, BF])
+def test_many_small_weights_next_to_a_large_one(dtype, q_len):
+    """One key of weight 1 whose value is 0 and 60000 of weight e^-18, 2^-26, whose values are 1 or -2: together a thousandth, and all of the result.
+    In fp16 the narrowed weight is off by half a step of 2^-24, or of its own; scaled by 2^7 that is 2^-32 of the largest weight, which the sum is at
+    least.  (Unscaled, 2^-26 narrows to 0.)  In bf16 the half step is the weight's own."""
+    n = 60000
+    b = Batch([q_len], [n], hq=4, hkv=2, d=64, page=64, dtype=dtype, seed=1)
+    b.Q.zero_()
+    b.Q[..., 0] = 1.0
+    b.K[0].zero_()
+    b.K[0][1:, :, 0] = -18.0
+    b.V[0].fill_(1.0)
+    b.V[0][:, 1, 32:] = -2.0
+    b.V[0][0] = 0.0
+    b.store()
+    for split in (0, 512):
+        out, z = attend(b, scale=1.0, split=split, out_dtype=torch.float32)
+        o, lse, mass = _softmax64(b.Q, b.K[0], b.V[0], 1.0)
+        bound, bound_z = attention_bounds(o, mass, torch.zeros_like(lse), 64, n, dtype, torch.float32)
+        small = 2.0 ** -32 * n * b.V[0].abs().double().amax() if dtype == HF else 0.0
+        # the exponent, 26 in size, is rounded by 2^-20 at most
+        assert bool(((out.double() - o).abs() <= bound + small + 2.0 ** -20 * mass).all()) and bool((o != 0).all())
+        # a quarter's running sum takes n / 128 additions, each rounded by 2^-24 of it
+        assert bool(((z.double() - lse).abs() <= bound_z + 2.0 ** -20 + n / 128 * 2.0 ** -24).all())
+        one, oz = attend(b, scale=1.0, split=split)                            # and in the cache's own type
+        assert torch.equal(one, out.to(dtype)) and torch.equal(oz, z)
