@@ -22,7 +22,7 @@
 //   fixer                     hands each arrived slot to the MMA warp; in blocks where some row is masked it first turns V elements
 //                             that are not finite into zeros (0 * NaN would reach every row of the tile).  For rows that do see such an element
 //                             the result is put right once they are stored (rare, from global memory).
-//   A chunk of 4096 rows on 16384 keys, 32 heads of 128 on 8 key heads: 0.95-0.97 ms called on rotating inputs, 1.0 PFLOP/s (0.85 ms, 1.13 PFLOP/s as a graph
+//   A chunk of 4096 rows on 16384 keys, 32 heads of 128 on 8 key heads: 0.94-0.97 ms called on rotating inputs, 1.0 PFLOP/s (0.85 ms, 1.13 PFLOP/s as a graph
 //   of ten on one input).  What bounds it: 512 items on 148 SMs are
 //   four turns of which the last is half empty (0.86), and a tile's chain of product, commit, 112 hardware exponentials a lane and quarter-rate
 //   unit, product (about 3500 cycles for the two tiles' 2048 of the tensor core).  Tried there, as graphs: all exponentials on the hardware unit 950 us,
@@ -985,7 +985,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
 //   O' += V_j^T P^T    lane = element of the head, column = row of queries; V is read transposed, P from shared memory
 // A softmax thread is one key of the block and holds its score with every row; maxima and sums over the keys go through butterflies
 // in which lanes trade rows (after five steps a lane holds one row's value), and the four warps' maxima through shared memory.
-// What bounds it: the K and V bytes.  64 sequences of up to 8192 keys, 8 key heads of 128 (1.14 GB): 195 us a call, 5.8 TB/s; 4 of up to 61000 (0.76 GB): 131 us,
+// What bounds it: the K and V bytes.  64 sequences of up to 8192 keys, 8 key heads of 128 (1.14 GB): 196 us a call, 5.8 TB/s; 4 of up to 61000 (0.76 GB): 132 us,
 // 5.8 TB/s; one of 8192 (34 MB): 13 us, of which the copies are 5 (launch, item and page look-up, the chain of two blocks and the join are latency).
 // With the queries as the 128 rows instead (the other form, 4 of them filled) the 64 sequences took 234 us on the device, and 278 with each row's keys dealt to
 // four warps: the tensor core then reads 128 mostly empty rows from shared memory for every step.

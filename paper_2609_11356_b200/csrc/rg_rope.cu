@@ -87,7 +87,7 @@ __device__ __forceinline__ bool place_of(const RopeParams& p, int64_t t, int& se
 }
 
 // Units a thread has in flight before the CTA works out its angles.  Alone the rotation gains by four (8192 tokens of 32 heads of 128, 134 MB:
-// 28 -> 24 us on the device, 5.6 TB/s; 25.4 called on rotating inputs).  With the cache (three sets of strides, places to look up) the registers they take cost more than they bring (257 MB: 49 us
+// 28 -> 24 us on the device, 5.6 TB/s; 25.7 called on rotating inputs).  With the cache (three sets of strides, places to look up) the registers they take cost more than they bring (257 MB: 49 us
 // without, 54 with, on the device); there more CTAs at once do it.
 template <bool PAGED> constexpr int BATCH = PAGED ? 1 : 4;
 constexpr int PAGED_UNITS = 8;                         // units of a thread with the cache, one after the other (257 MB: 48 us with four, 46.7 with eight)
