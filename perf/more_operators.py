@@ -1,6 +1,6 @@
-"""The operators of serving in four bits as they are measured: products of a few rows with 4-bit weights (`rg_gemv_w4`), keys and
-values put into a paged cache of 4-bit codes with the rotation on the way and read back (`rg_kv_append4`, `rg_kv_read4`), and attention
-of new tokens over that cache (`rg_paged_attention4`), each beside its plain form in elementary torch operations.
+"""The operators of serving in four bits as they are measured: products of a few rows with 4-bit weights (`rg_gemv_four`), keys and
+values put into a paged cache of 4-bit codes with the rotation on the way and read back (`rg_kv_append_four`, `rg_kv_read_four`), and attention
+of new tokens over that cache (`rg_paged_attention_four`), each beside its plain form in elementary torch operations.
 
 A case's shapes (lengths of the sequences among them) follow from the case alone, its values from the seed.
 """
@@ -323,10 +323,10 @@ def _own(st):
     if "ready" not in st:                                                       # descriptors, handles and workspace are made once
         st["ready"] = True
         if c["op"] == "gemv":
-            st["w"] = rg.rg_w4(st["codes"], st["scales"], zeros=st["zeros"], group=c["group"])
+            st["w"] = rg.rg_weights_four(st["codes"], st["scales"], zeros=st["zeros"], group=c["group"])
         else:
             st["seqs"] = rg.rg_paged_seqs(st["table"], st["seq_lens"], st["cu_q"], max_q=st["max_q"], max_len=st["max_len"])
-            st["kc"], st["vc"] = (rg.rg_cache4(x, page_size=c["page"], dim=c["d"]) for x in (st["k_cache"], st["v_cache"]))
+            st["kc"], st["vc"] = (rg.rg_cache_four(x, page_size=c["page"], dim=c["d"]) for x in (st["k_cache"], st["v_cache"]))
         if c["op"] == "append":
             st["desc"] = rg.rg_rope_desc(rot_dim=c["rot"], style=rg.RG_ROPE_HALF if c["style"] == "half" else rg.RG_ROPE_PAIRS, sections=st["sections"])
         if c["op"] == "attend":
@@ -334,12 +334,12 @@ def _own(st):
             need = rg.rg_paged_attention_workspace_bytes(st["desc"], st["seqs"], st["q"].shape[0], c["hq"], c["d"])
             st["ws"] = torch.empty(need, dtype=torch.uint8, device=DEV) if need else None
     if c["op"] == "gemv":
-        return rg.rg_gemv_w4(st["w"], st["x"], st["out"], bias=st["bias"], act=int(c["act"]), residual=st["residual"])
+        return rg.rg_gemv_four(st["w"], st["x"], st["out"], bias=st["bias"], act=int(c["act"]), residual=st["residual"])
     if c["op"] == "append":
-        rg.rg_kv_append4(st["desc"], st["k"], st["v"], st["inv_freq"], st["kc"], st["vc"], st["seqs"], pos=st["pos"], q=st["q"], q_out=st["out"])
-        rg.rg_kv_read4(st["kc"], st["vc"], st["seqs"], st["k_out"], st["v_out"])
+        rg.rg_kv_append_four(st["desc"], st["k"], st["v"], st["inv_freq"], st["kc"], st["vc"], st["seqs"], pos=st["pos"], q=st["q"], q_out=st["out"])
+        rg.rg_kv_read_four(st["kc"], st["vc"], st["seqs"], st["k_out"], st["v_out"])
         return st["out"], st["k_out"], st["v_out"]
-    rg.rg_paged_attention4(st["desc"], st["q"], st["kc"], st["vc"], st["seqs"], st["out"], lse=st["lse"], ws=st["ws"])
+    rg.rg_paged_attention_four(st["desc"], st["q"], st["kc"], st["vc"], st["seqs"], st["out"], lse=st["lse"], ws=st["ws"])
     return (st["out"], st["lse"]) if c["lse"] else st["out"]
 
 
