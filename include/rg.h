@@ -321,6 +321,7 @@ typedef struct {
 } rg_paged_seqs_t;
 #define RG_PAGE_CODE_APPEND 0x2A00u
 #define RG_PAGE_CODE_ATTEND 0x2B00u
+#define RG_PAGE_CODE_READ 0x2C00u      /* rg_kv_read_four */
 
 /* Rotary positions: pair j (of rot_dim / 2) of every head turns by pos[axis(j)][token] * inv_freq[j] radians,
  * (a, b) -> (a cos - b sin, b cos + a sin); elements from rot_dim on pass through.  RG_ROPE_HALF pairs elements
@@ -395,6 +396,72 @@ size_t rg_paged_attention_workspace_bytes(const rg_paged_attn_desc_t* d, const r
 rg_status_t rg_paged_attention(const rg_paged_attn_desc_t* d, const rg_rows_t* q, const rg_cache_t* k_cache, const rg_cache_t* v_cache,
                                const rg_paged_seqs_t* seqs, const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream);
 
+/* ---- Serving in four bits ---------------------------------------------------------------------------------
+ * Single tokens are bound by the bytes of weights and cache.  These are the forms of the scalar GEMV family, of rg_kv_append and of
+ * rg_paged_attention for operands held in four bits an element.
+ *
+ * rg_weights_four_t: weights [rows][cols], rows being outputs (N) and cols the contracted axis (K).  Code u of element k of a row is the low (k even) or high
+ * (k odd) half of byte k / 2 of the row; w = (u - zero) * scale with one scale, and one zero point in 0..15 (the low four bits of its
+ * byte; all 8 where `zeros` is NULL), for every `group` consecutive k of a row (the last group of a row may be short). */
+typedef struct {
+  const void* codes;      /* [rows][code_ld bytes] */
+  const void* scales;     /* [rows][scale_ld], scale_dtype: bf16, fp16 or fp32 */
+  const void* zeros;      /* [rows][zero_ld] bytes, nullable */
+  int64_t rows, cols;
+  int64_t code_ld;        /* bytes between rows: at least cols / 2, a multiple of 16 */
+  int64_t scale_ld, zero_ld;  /* elements between rows: at least ceil(cols / group) */
+  int32_t group;          /* 32, 64 or 128 */
+  int32_t scale_dtype;
+  int32_t w_static;       /* 1: the caller's promise that no work in flight on the stream writes codes, scales or zeros: the first of them may be read
+                             before the kernels ahead have finished */
+} rg_weights_four_t;
+
+/* C[M][N] = epilogue(A . W^T) with W in four bits.  Per group the products of A with the integers u - zero are summed by a chain of 16-wide
+ * tensor-core steps from zero (fp32; the order of k within a group is fixed by this library), times the group's scale in fp32 and onto a
+ * part's running sum; K has at most eight parts (of whole 256s, as even as that allows), added in ascending order; then the epilogue of rg_gemm and one
+ * rounding.  No weight is narrowed.  A row's bits do not depend on M, strides or the run.  Meant for a few rows: the weights are
+ * read once for every 32 of them (M <= 16: once), and from some hundred rows on weights unpacked once for rg_gemm are faster.
+ *   A: [M][K] bf16 or fp16, 16-byte aligned, ld a multiple of 8; K a multiple of 32; C, bias, residual: bf16, fp16 or fp32, any alignment.
+ *   codes: 16-byte aligned; scales: aligned to their type.  M is at most 2^19.  M == 0 or N == 0: RG_OK, nothing launched.  K == 0: RG_ERR_SHAPE.
+ * Asynchronous on `cuda_stream`; no workspace. */
+rg_status_t rg_gemv_four(const rg_weights_four_t* W, const rg_tensor_t* A, const rg_tensor_t* C, const rg_epilogue_t* epi, void* cuda_stream);
+
+/* rg_cache_four_t: a paged cache in four bits.  A block, one page of one head, is rg_cache_four_block_bytes(page_size, dim) = page_size * dim * 9 / 16
+ * contiguous bytes; page_stride and head_stride are BYTES between blocks, multiples of 16, and so is the address.  In a cache that is written no two
+ * blocks overlap.  page_size is a multiple of 8, dim a multiple of 32 up to 128, heads at most 65535.
+ *   Every 16 consecutive elements of a head form a group with a scale byte b, s = (8 + b % 8) 2^(b / 8 - 22) (integer division), and codes
+ *   c in -8..7; an element's value is c * s, which is a bf16 and an fp16 number exactly.  A block is a row of tiles of 8 slots, each: codes
+ *   [dim / 32][8 slots][4 words of 32 bits], then scale bytes [dim / 32][8 slots][2].  Nibble i of a word is c + 8 of element 2 i (i < 4) or
+ *   2 i - 7 (i >= 4) of its eight.  Every bit pattern is a finite value, so unused slots may hold anything.
+ *   From numbers to codes: s is the smallest scale for which 7.5 s >= the largest magnitude of the group, c the integer nearest to x / s (ties to
+ *   even), at most 7.  The error is at most s / 2, s at most 0.15 of the largest magnitude (where that is between 2^-16 and 57600; groups below
+ *   are held in steps of 2^-19, elements beyond are clipped to -61440 .. 53760, infinities too).  A NaN becomes 0. */
+typedef struct {
+  void* ptr;
+  int64_t pages, page_size, heads, dim;
+  int64_t page_stride, head_stride;   /* bytes */
+} rg_cache_four_t;
+size_t rg_cache_four_block_bytes(int64_t page_size, int64_t dim);   /* 0 for sizes that are refused */
+
+/* rg_kv_append into such caches: the new tokens' keys (rotated) and values go into their pages as codes, and the queries are rotated into q_out with the bits of
+ * rg_rope, in one launch.  The codes are those of the keys rotated in 64 bits, which are not rounded in between.  Everything else is as in rg_kv_append: arguments, checks, health word (RG_PAGE_CODE_APPEND).  k, v, q, q_out: bf16, fp16 or
+ * fp32, one type.  Asynchronous on `cuda_stream`. */
+rg_status_t rg_kv_append_four(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_rows_t* v, const rg_tensor_t* pos, const double* inv_freq,
+                          const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache, const rg_paged_seqs_t* seqs,
+                          const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream);
+
+/* What the caches hold at the places of the new tokens: k_out, v_out [tokens][kv heads][dim], bf16, fp16 or fp32, one type, any strides.  With
+ * cu_q that spans whole sequences (as many new tokens as seq_lens says) it reads whole sequences.  A token without a place reads as zeros and sets
+ * the health word (RG_PAGE_CODE_READ); rows behind the last sequence are left as they were.  Asynchronous on `cuda_stream`. */
+rg_status_t rg_kv_read_four(const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache, const rg_paged_seqs_t* seqs,
+                        const rg_rows_t* k_out, const rg_rows_t* v_out, void* cuda_stream);
+
+/* rg_paged_attention over such caches: the same descriptor, arguments and workspace (rg_paged_attention_workspace_bytes), and the same bits as
+ * rg_paged_attention has over a cache of q's type that holds the values that the codes stand for.  q bf16 or fp16.  Keys and values are always finite, so
+ * nothing that a row does not see can reach it. */
+rg_status_t rg_paged_attention_four(const rg_paged_attn_desc_t* d, const rg_rows_t* q, const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache,
+                                const rg_paged_seqs_t* seqs, const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream);
+
 /* Host-buffer forms of rg_gemm and rg_reduce_rows, for callers whose data lives in host memory.
  * Every tensor / epilogue / args pointer is a HOST pointer (pinned memory makes the copies
  * asynchronous).  `dev_scratch` is a caller-owned DEVICE buffer of at least
@@ -467,7 +534,7 @@ rg_status_t rg_selftest_exp(int32_t form, const float* x, float* y, int64_t n, v
  * wait that gives up records a code here, lets the kernel drain and return, and leaves the
  * context usable.  Copies the word to *code (0 = healthy) and clears it.  Synchronises the
  * device.  Returns RG_ERR_TIMEOUT if the word was non-zero; if all it holds is a code of the paged
- * operators (RG_PAGE_CODE_APPEND, RG_PAGE_CODE_ATTEND), RG_ERR_PAGE. */
+ * operators (RG_PAGE_CODE_APPEND, RG_PAGE_CODE_ATTEND, RG_PAGE_CODE_READ), RG_ERR_PAGE. */
 rg_status_t rg_device_status(uint32_t* code);
 
 const char* rg_status_string(rg_status_t s);

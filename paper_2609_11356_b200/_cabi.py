@@ -18,7 +18,7 @@ STATUS_NAMES = {0: "RG_OK", 1: "RG_ERR_NULL", 2: "RG_ERR_INVALID_DESC", 3: "RG_E
 RG_BF16, RG_F32, RG_F16, RG_F8E4M3 = 0, 1, 2, 3
 RG_I32, RG_I64 = 16, 17
 RG_ROPE_HALF, RG_ROPE_PAIRS = 0, 1
-RG_PAGE_CODE_APPEND, RG_PAGE_CODE_ATTEND = 0x2A00, 0x2B00
+RG_PAGE_CODE_APPEND, RG_PAGE_CODE_ATTEND, RG_PAGE_CODE_READ = 0x2A00, 0x2B00, 0x2C00
 RG_TREE_LEFT, RG_TREE_BALANCED = 0, 1
 RG_ATOM_TC_BF16_K16, RG_ATOM_SCALAR, RG_ATOM_TC_F8_K32 = 0, 1, 2
 RG_COLOP_SUM, RG_COLOP_DOT = 0, 1
@@ -32,7 +32,8 @@ EXPORTS = ["rg_desc_init", "rg_desc_validate", "rg_desc_class", "rg_gemm_workspa
            "rg_reduce_rows", "rg_gemm_host_scratch_bytes", "rg_gemm_host", "rg_reduce_rows_host_scratch_bytes",
            "rg_reduce_rows_host", "rg_device_status", "rg_status_string", "rg_gemm_noalloc",
            "rg_reduce_cols_workspace_bytes", "rg_reduce_cols", "rg_attention", "rg_selftest_bounded_wait", "rg_selftest_exp",
-           "rg_rope", "rg_kv_append", "rg_paged_attention_workspace_bytes", "rg_paged_attention"]
+           "rg_rope", "rg_kv_append", "rg_paged_attention_workspace_bytes", "rg_paged_attention",
+           "rg_gemv_four", "rg_cache_four_block_bytes", "rg_kv_append_four", "rg_kv_read_four", "rg_paged_attention_four"]
 
 
 class rg_attn_desc_t(C.Structure):
@@ -72,6 +73,16 @@ class rg_rows_t(C.Structure):
 class rg_cache_t(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int32), ("pages", C.c_int64), ("page_size", C.c_int64), ("heads", C.c_int64), ("dim", C.c_int64),
                 ("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class rg_weights_four_t(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("zeros", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("code_ld", C.c_int64), ("scale_ld", C.c_int64), ("zero_ld", C.c_int64), ("group", C.c_int32), ("scale_dtype", C.c_int32), ("w_static", C.c_int32)]
+
+
+class rg_cache_four_t(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("pages", C.c_int64), ("page_size", C.c_int64), ("heads", C.c_int64), ("dim", C.c_int64),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 class rg_paged_seqs_t(C.Structure):
@@ -117,11 +128,16 @@ def load():
     L.rg_reduce_cols_workspace_bytes.restype = sz; L.rg_reduce_cols_workspace_bytes.argtypes = [i64, i64]
     L.rg_reduce_cols.restype = C.c_int; L.rg_reduce_cols.argtypes = [D, C.c_int, T, T, T, vp, sz, vp]
     L.rg_attention.restype = C.c_int; L.rg_attention.argtypes = [C.POINTER(rg_attn_desc_t), T, T, T, T, vp]
-    # structures of these four are passed by reference or as packed bytes
+    # structures of these are passed by reference or as packed bytes
     L.rg_rope.restype = C.c_int; L.rg_rope.argtypes = [vp] * 6
     L.rg_kv_append.restype = C.c_int; L.rg_kv_append.argtypes = [vp] * 11
     L.rg_paged_attention_workspace_bytes.restype = sz; L.rg_paged_attention_workspace_bytes.argtypes = [vp, vp, i64, i64, i64, i64]
     L.rg_paged_attention.restype = C.c_int; L.rg_paged_attention.argtypes = [vp] * 7 + [i64, vp, sz, vp]
+    L.rg_gemv_four.restype = C.c_int; L.rg_gemv_four.argtypes = [vp] * 5
+    L.rg_cache_four_block_bytes.restype = sz; L.rg_cache_four_block_bytes.argtypes = [i64, i64]
+    L.rg_kv_append_four.restype = C.c_int; L.rg_kv_append_four.argtypes = [vp] * 11
+    L.rg_kv_read_four.restype = C.c_int; L.rg_kv_read_four.argtypes = [vp] * 6
+    L.rg_paged_attention_four.restype = C.c_int; L.rg_paged_attention_four.argtypes = [vp] * 7 + [i64, vp, sz, vp]
     L.rg_gemm_noalloc.restype = C.c_int; L.rg_gemm_noalloc.argtypes = [D, T, T, T, E, vp]
     L.rg_selftest_bounded_wait.restype = C.c_int; L.rg_selftest_bounded_wait.argtypes = [C.c_uint64, vp, vp]
     L.rg_selftest_exp.restype = C.c_int; L.rg_selftest_exp.argtypes = [C.c_int32, vp, vp, C.c_int64, vp]

@@ -413,18 +413,126 @@ def rg_paged_attention_workspace_bytes(d: K.rg_paged_attn_desc_t, seqs: rg_paged
     return int(K.load().rg_paged_attention_workspace_bytes(C.byref(d), C.byref(seqs.c), page_size, tokens, q_heads, dim))
 
 
+def _normalisers(q, lse):
+    """Address and row stride of the normalisers (none: 0, 0)."""
+    if lse is None:
+        return None, 0
+    import torch
+    if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or (lse.shape[1] > 1 and lse.stride(1) != 1):
+        raise ValueError("lse is float32 [tokens, heads], contiguous along the heads")
+    lse_ld = lse.stride(0) if lse.shape[0] > 1 else lse.shape[1]
+    if lse_ld < lse.shape[1]:
+        raise ValueError(f"rows of lse overlap: {lse.shape[1]} heads, {lse_ld} apart")
+    return lse.data_ptr(), lse_ld
+
+
 def rg_paged_attention(d: K.rg_paged_attn_desc_t, q, k_cache, v_cache, seqs: rg_paged_seqs, out, *, lse=None, ws=None):
     """out = attention of the rows q [tokens, heads, dim] over their sequences' pages; lse: float32 [tokens, heads] or None."""
-    import torch
-    lse_ld = 0
-    if lse is not None:
-        if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or (lse.shape[1] > 1 and lse.stride(1) != 1):
-            raise ValueError("lse is float32 [tokens, heads], contiguous along the heads")
-        lse_ld = lse.stride(0) if lse.shape[0] > 1 else lse.shape[1]
-        if lse_ld < lse.shape[1]:
-            raise ValueError(f"rows of lse overlap: {lse.shape[1]} heads, {lse_ld} apart")
+    lse_ptr, lse_ld = _normalisers(q, lse)
     ws_ptr, ws_bytes = _workspace(ws)
     device = _one_device("rg_paged_attention", q, k_cache, v_cache, seqs, out, lse, ws)
     _call("rg_paged_attention", K.load().rg_paged_attention, device, C.byref(d), _rows(q), _cache(k_cache), _cache(v_cache), C.byref(seqs.c), _rows(out),
-          lse.data_ptr() if lse is not None else None, lse_ld, ws_ptr, ws_bytes)
+          lse_ptr, lse_ld, ws_ptr, ws_bytes)
+    return out
+
+
+# ---------------------------------------------------------------- four bits
+class rg_weights_four:
+    """Weights in four bits (see include/rg.h): codes uint8 [N, K / 2] (element 2 i in the low half of byte i), scales [N, ceil(K / group)] in
+    bfloat16, float16 or float32, zeros uint8 of the scales' shape (None: all 8).  w_static=1: nothing in flight writes them."""
+    __slots__ = ("codes", "scales", "zeros", "device", "c")
+
+    def get_device(self) -> int:
+        return self.device
+
+    def __init__(self, codes, scales, *, zeros=None, group: int = 128, w_static: int = 0):
+        import torch
+        for name, t, types in (("codes", codes, (torch.uint8,)), ("scales", scales, (torch.bfloat16, torch.float16, torch.float32)), ("zeros", zeros, (torch.uint8,))):
+            if t is not None and (t.dtype not in types or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1)):
+                raise ValueError(f"{name} is a {' or '.join(str(x) for x in types)} tensor of 2 dimensions, contiguous along the second")
+        if not _fits(31, group, w_static):
+            raise RgError(2, "rg_weights_four")
+        N, half = codes.shape
+        if group < 1 or scales.shape != (N, -(-2 * half // group)) or (zeros is not None and zeros.shape != scales.shape):
+            raise ValueError(f"codes {tuple(codes.shape)} in groups of {group} do not go with scales {tuple(scales.shape)}" + (f" and zeros {tuple(zeros.shape)}" if zeros is not None else ""))
+        device = codes.get_device()
+        if scales.get_device() != device or (zeros is not None and zeros.get_device() != device):
+            raise ValueError("rg_weights_four: tensors on different devices")
+        # rows that overlap are the library's to refuse
+        ld = lambda t: int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1])  # noqa: E731
+        self.device, self.codes, self.scales, self.zeros = device, codes, scales, zeros
+        code_ld = ld(codes) if N > 1 else -(-half // 16) * 16
+        self.c = K.rg_weights_four_t(codes.data_ptr(), scales.data_ptr(), zeros.data_ptr() if zeros is not None else None, N, 2 * half, code_ld, ld(scales),
+                           ld(zeros) if zeros is not None else 0, group, _code(scales), w_static)
+
+
+def _matrix(t) -> bytes:
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("a matrix has 2 dimensions and contiguous rows")
+    n, c = t.shape
+    return _TENSOR.pack(t.data_ptr(), _code(t), n, c, t.stride(0) if n > 1 else max(t.stride(0), c))
+
+
+def rg_gemv_four(w: rg_weights_four, A, C_out, *, bias=None, act: int = 0, residual=None):
+    """C_out[M, N] = epilogue(A[M, K] @ W[N, K]^T) for a few rows, W in four bits; the epilogue is rg_gemm's."""
+    device = _one_device("rg_gemv_four", A, w, C_out, bias, residual)
+    if bias is not None and (bias.dim() != 1 or bias.shape[0] != C_out.shape[1] or (bias.shape[0] > 1 and bias.stride(0) != 1)):
+        raise ValueError(f"bias is a contiguous tensor of {C_out.shape[1]} elements")
+    if residual is not None and (residual.shape != C_out.shape or (residual.shape[1] > 1 and residual.stride(1) != 1)):
+        raise ValueError("residual has the result's shape and contiguous rows")
+    e = _epilogue(bias, act, residual)
+    if e is not None and residual is not None and residual.shape[0] <= 1:
+        e.ldr = max(e.ldr, C_out.shape[1])
+    _call("rg_gemv_four", K.load().rg_gemv_four, device, C.byref(w.c), _matrix(A), _matrix(C_out), C.byref(e) if e is not None else None)
+    return C_out
+
+
+def rg_cache_four_block_bytes(page_size: int, dim: int) -> int:
+    """Bytes of one page of one head in a cache of four-bit codes."""
+    return int(K.load().rg_cache_four_block_bytes(page_size, dim))
+
+
+class rg_cache_four:
+    """A paged cache of four-bit codes: a uint8 CUDA tensor [pages, heads, rg_cache_four_block_bytes(page_size, dim)], blocks contiguous."""
+    __slots__ = ("tensor", "page_size", "dim", "device", "c")
+
+    def get_device(self) -> int:
+        return self.device
+
+    def __init__(self, tensor, *, page_size: int, dim: int):
+        import torch
+        block = rg_cache_four_block_bytes(page_size, dim)
+        if block == 0:
+            raise RgError(3, "rg_cache_four")
+        if tensor.dtype != torch.uint8 or tensor.dim() != 3 or tensor.stride(2) != 1 or tensor.shape[2] != block:
+            raise ValueError(f"a cache of four-bit codes is a uint8 tensor [pages, heads, {block}], contiguous along the last dimension")
+        n, h, _ = tensor.shape
+        self.tensor, self.page_size, self.dim, self.device = tensor, page_size, dim, tensor.get_device()
+        self.c = K.rg_cache_four_t(tensor.data_ptr(), n, page_size, h, dim, tensor.stride(0) if n > 1 else 0, tensor.stride(1) if h > 1 else 0)
+
+
+def rg_kv_append_four(d, k, v, inv_freq, k_cache: rg_cache_four, v_cache: rg_cache_four, seqs: rg_paged_seqs, *, pos=None, q=None, q_out=None):
+    """rg_kv_append into caches of four-bit codes."""
+    if (q is None) != (q_out is None):
+        raise ValueError("rg_kv_append_four: q and q_out go together")
+    device = _one_device("rg_kv_append_four", k, v, inv_freq, k_cache, v_cache, seqs, pos, q, q_out)
+    _call("rg_kv_append_four", K.load().rg_kv_append_four, device, C.byref(d) if d is not None else None, _rows(k), _rows(v),
+          _positions(pos) if pos is not None else None, None if inv_freq is None else inv_freq.data_ptr() if d is None else _frequencies(inv_freq, d),
+          C.byref(k_cache.c), C.byref(v_cache.c), C.byref(seqs.c), _rows(q) if q is not None else None, _rows(q_out) if q_out is not None else None)
+
+
+def rg_kv_read_four(k_cache: rg_cache_four, v_cache: rg_cache_four, seqs: rg_paged_seqs, k_out, v_out):
+    """k_out, v_out [tokens, heads, dim] = what the caches hold at the places of the batch's new tokens."""
+    device = _one_device("rg_kv_read_four", k_out, v_out, k_cache, v_cache, seqs)
+    _call("rg_kv_read_four", K.load().rg_kv_read_four, device, C.byref(k_cache.c), C.byref(v_cache.c), C.byref(seqs.c), _rows(k_out), _rows(v_out))
+    return k_out, v_out
+
+
+def rg_paged_attention_four(d: K.rg_paged_attn_desc_t, q, k_cache: rg_cache_four, v_cache: rg_cache_four, seqs: rg_paged_seqs, out, *, lse=None, ws=None):
+    """rg_paged_attention over caches of four-bit codes."""
+    lse_ptr, lse_ld = _normalisers(q, lse)
+    ws_ptr, ws_bytes = _workspace(ws)
+    device = _one_device("rg_paged_attention_four", q, k_cache, v_cache, seqs, out, lse, ws)
+    _call("rg_paged_attention_four", K.load().rg_paged_attention_four, device, C.byref(d), _rows(q), C.byref(k_cache.c), C.byref(v_cache.c), C.byref(seqs.c), _rows(out),
+          lse_ptr, lse_ld, ws_ptr, ws_bytes)
     return out

@@ -527,7 +527,9 @@ rg_status_t check_positions(const rg_rope_desc_t* d, const rg_tensor_t* pos, int
   return RG_OK;
 }
 
-void set_rotation(rg::RopeParams* p, const rg_rope_desc_t* d, const rg_tensor_t* pos, const double* inv_freq) {
+extern "C++" {
+template <typename P>
+void set_rotation(P* p, const rg_rope_desc_t* d, const rg_tensor_t* pos, const double* inv_freq) {
   p->rot = (int32_t)d->rot_dim; p->style = d->style; p->inverse = d->inverse;
   uint32_t end = 0;
   for (int a = 0; a < 3; ++a) {
@@ -537,6 +539,13 @@ void set_rotation(rg::RopeParams* p, const rg_rope_desc_t* d, const rg_tensor_t*
   p->inv_freq = inv_freq;
   if (pos) { p->pos = pos->ptr; p->pos64 = pos->dtype == RG_I64; p->pos_ld = pos->ld; }
 }
+
+template <typename P>
+void set_seqs(P* p, const rg_paged_seqs_t* seqs) {
+  p->table = seqs->block_table; p->table_ld = seqs->table_ld; p->table_cols = seqs->table_cols;
+  p->seq_lens = seqs->seq_lens; p->cu_q = seqs->cu_q; p->n_seqs = seqs->n_seqs;
+}
+}  // extern "C++"
 
 bool same_shape(const rg_rows_t* a, const rg_rows_t* b) {
   return a->dtype == b->dtype && a->tokens == b->tokens && a->heads == b->heads && a->dim == b->dim;
@@ -574,17 +583,9 @@ rg_status_t rg_rope(const rg_rope_desc_t* d, const rg_rows_t* x, const rg_tensor
   return rg::launch_rope(p, x->dtype, false, static_cast<cudaStream_t>(cuda_stream));
 }
 
-rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_rows_t* v, const rg_tensor_t* pos, const double* inv_freq,
-                         const rg_cache_t* k_cache, const rg_cache_t* v_cache, const rg_paged_seqs_t* seqs,
-                         const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream) {
+// what rg_kv_append and rg_kv_append_four ask of the rotation and the queries
+static rg_status_t check_append_rotation(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_tensor_t* pos, const double* inv_freq, const rg_rows_t* q, const rg_rows_t* q_out) {
   rg_status_t s;
-  if ((s = check_rows(k)) != RG_OK || (s = check_rows(v)) != RG_OK || (s = check_cache_out(k_cache)) != RG_OK || (s = check_cache_out(v_cache)) != RG_OK ||
-      (s = check_seqs(seqs)) != RG_OK)
-    return s;
-  if (!same_shape(k, v) || k->dtype != k_cache->dtype || k->dtype != v_cache->dtype) return RG_ERR_SHAPE;
-  if (k_cache->pages != v_cache->pages || k_cache->page_size != v_cache->page_size || k_cache->heads != k->heads || v_cache->heads != k->heads ||
-      k_cache->dim != k->dim || v_cache->dim != k->dim || k->dim % 2)
-    return RG_ERR_SHAPE;
   if (!q != !q_out) return RG_ERR_NULL;
   if (d) {
     if ((s = check_rope_desc(d, k->dim)) != RG_OK) return s;
@@ -600,6 +601,21 @@ rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_r
     if ((s = check_rows(q)) != RG_OK || (s = check_rows_out(q_out)) != RG_OK) return s;
     if (!same_shape(q, q_out) || q->tokens != k->tokens || q->dim != k->dim || q->dtype != k->dtype) return RG_ERR_SHAPE;
   }
+  return RG_OK;
+}
+
+rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_rows_t* v, const rg_tensor_t* pos, const double* inv_freq,
+                         const rg_cache_t* k_cache, const rg_cache_t* v_cache, const rg_paged_seqs_t* seqs,
+                         const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream) {
+  rg_status_t s;
+  if ((s = check_rows(k)) != RG_OK || (s = check_rows(v)) != RG_OK || (s = check_cache_out(k_cache)) != RG_OK || (s = check_cache_out(v_cache)) != RG_OK ||
+      (s = check_seqs(seqs)) != RG_OK)
+    return s;
+  if (!same_shape(k, v) || k->dtype != k_cache->dtype || k->dtype != v_cache->dtype) return RG_ERR_SHAPE;
+  if (k_cache->pages != v_cache->pages || k_cache->page_size != v_cache->page_size || k_cache->heads != k->heads || v_cache->heads != k->heads ||
+      k_cache->dim != k->dim || v_cache->dim != k->dim || k->dim % 2)
+    return RG_ERR_SHAPE;
+  if ((s = check_append_rotation(d, k, pos, inv_freq, q, q_out)) != RG_OK) return s;
   if (k->tokens == 0 || seqs->n_seqs == 0) return RG_OK;
   rg::RopeParams p{};
   int n = 0;
@@ -608,8 +624,7 @@ rg_status_t rg_kv_append(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_r
   if (q) p.st[n++] = {q->ptr, q_out->ptr, q->token_stride, q->head_stride, 0, q_out->token_stride, q_out->head_stride, (int32_t)q->heads, 1, 0};
   p.n_streams = n; p.tokens = k->tokens; p.d = (int32_t)k->dim;
   if (d) set_rotation(&p, d, pos, inv_freq);
-  p.table = seqs->block_table; p.table_ld = seqs->table_ld; p.table_cols = seqs->table_cols;
-  p.seq_lens = seqs->seq_lens; p.cu_q = seqs->cu_q; p.n_seqs = seqs->n_seqs;
+  set_seqs(&p, seqs);
   p.pages = k_cache->pages; p.page_size = (int32_t)k_cache->page_size;
   return rg::launch_rope(p, k->dtype, true, static_cast<cudaStream_t>(cuda_stream));
 }
@@ -623,6 +638,36 @@ size_t rg_paged_attention_workspace_bytes(const rg_paged_attn_desc_t* d, const r
   return align_up((size_t)tokens * q_heads * n * (size_t)(dim + 2) * sizeof(float), 256);
 }
 
+// what rg_paged_attention and rg_paged_attention_four have in common, once rows, caches and sequences are checked by themselves
+static rg_status_t attend(const rg_paged_attn_desc_t* d, const rg_rows_t* q, rg::PagedAttnArgs a, rg_status_t caches, int64_t pages, int64_t page_size, int64_t kv_heads, const rg_paged_seqs_t* seqs,
+                          const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream) {
+  if (out->dtype != q->dtype && out->dtype != RG_F32) return RG_ERR_SHAPE;
+  if (out->tokens != q->tokens || out->heads != q->heads || out->dim != q->dim) return RG_ERR_SHAPE;
+  if (q->heads % kv_heads) return RG_ERR_SHAPE;
+  if (q->dim % 8 || q->dim > 128 || page_size % 8 || q->heads / kv_heads > 128) return RG_ERR_UNSUPPORTED;
+  if (lse && (lse_ld < q->heads || reinterpret_cast<uintptr_t>(lse) % 4)) return RG_ERR_SHAPE;
+  if (caches != RG_OK) return caches;                      // their strides and addresses, after the shapes
+  if (q->token_stride % 8 || q->head_stride % 8) return RG_ERR_ALIGNMENT;
+  // a dimension that repeats one address has no tensor map
+  if ((q->token_stride == 0 && q->tokens > 1) || (q->head_stride == 0 && q->heads > 1)) return RG_ERR_UNSUPPORTED;
+  if (reinterpret_cast<uintptr_t>(q->ptr) & 15) return RG_ERR_ALIGNMENT;
+  const int64_t max_len = pages > 0 ? bound_of_len(seqs, page_size) : 0;
+  if (max_len > DIM_LIMIT / 2) return RG_ERR_SHAPE;
+  if (q->tokens == 0 || seqs->n_seqs == 0) return RG_OK;
+  a.q = q; a.seqs = seqs; a.out = out; a.lse = lse; a.lse_ld = lse_ld;
+  a.max_q = seqs->max_q > 0 ? std::min(seqs->max_q, q->tokens) : q->tokens;
+  a.max_len = max_len;
+  a.split = d->split; a.window = d->window; a.scale = d->scale; a.causal = d->mask;
+  a.segments = d->split ? (int32_t)((max_len + d->split - 1) / d->split) : 1;
+  if (a.segments < 1) a.segments = 1;
+  if (a.segments > 1) {
+    if (!ws || ws_bytes < rg_paged_attention_workspace_bytes(d, seqs, page_size, q->tokens, q->heads, q->dim)) return RG_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws) & 15) return RG_ERR_ALIGNMENT;
+    a.ws = ws;
+  }
+  return rg::launch_paged_attention(a, static_cast<cudaStream_t>(cuda_stream));
+}
+
 rg_status_t rg_paged_attention(const rg_paged_attn_desc_t* d, const rg_rows_t* q, const rg_cache_t* k_cache, const rg_cache_t* v_cache,
                                const rg_paged_seqs_t* seqs, const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream) {
   rg_status_t s;
@@ -631,36 +676,137 @@ rg_status_t rg_paged_attention(const rg_paged_attn_desc_t* d, const rg_rows_t* q
       (s = check_seqs(seqs)) != RG_OK)
     return s;
   if (q->dtype == RG_F32) return RG_ERR_UNSUPPORTED;
-  if (k_cache->dtype != q->dtype || v_cache->dtype != q->dtype || (out->dtype != q->dtype && out->dtype != RG_F32)) return RG_ERR_SHAPE;
-  if (out->tokens != q->tokens || out->heads != q->heads || out->dim != q->dim) return RG_ERR_SHAPE;
+  if (k_cache->dtype != q->dtype || v_cache->dtype != q->dtype) return RG_ERR_SHAPE;
   if (k_cache->pages != v_cache->pages || k_cache->page_size != v_cache->page_size || k_cache->heads != v_cache->heads || k_cache->dim != q->dim || v_cache->dim != q->dim)
     return RG_ERR_SHAPE;
-  if (q->heads % k_cache->heads) return RG_ERR_SHAPE;
-  if (q->dim % 8 || q->dim > 128 || k_cache->page_size % 8 || q->heads / k_cache->heads > 128) return RG_ERR_UNSUPPORTED;
-  if (lse && (lse_ld < q->heads || reinterpret_cast<uintptr_t>(lse) % 4)) return RG_ERR_SHAPE;
-  const int64_t strides[] = {q->token_stride, q->head_stride, k_cache->page_stride, k_cache->slot_stride, k_cache->head_stride,
-                             v_cache->page_stride, v_cache->slot_stride, v_cache->head_stride};
-  for (int64_t x : strides) if (x % 8) return RG_ERR_ALIGNMENT;
+  const int64_t strides[] = {k_cache->page_stride, k_cache->slot_stride, k_cache->head_stride, v_cache->page_stride, v_cache->slot_stride, v_cache->head_stride};
   // a dimension that repeats one address has no tensor map
-  const int64_t sizes[] = {q->tokens, q->heads, k_cache->pages, k_cache->page_size, k_cache->heads, v_cache->pages, v_cache->page_size, v_cache->heads};
-  for (int i = 0; i < 8; ++i) if (strides[i] == 0 && sizes[i] > 1) return RG_ERR_UNSUPPORTED;
-  if ((reinterpret_cast<uintptr_t>(q->ptr) | reinterpret_cast<uintptr_t>(k_cache->ptr) | reinterpret_cast<uintptr_t>(v_cache->ptr)) & 15) return RG_ERR_ALIGNMENT;
-  const int64_t max_len = k_cache->pages > 0 ? bound_of_len(seqs, k_cache->page_size) : 0;
-  if (max_len > DIM_LIMIT / 2) return RG_ERR_SHAPE;
-  if (q->tokens == 0 || seqs->n_seqs == 0) return RG_OK;
+  const int64_t sizes[] = {k_cache->pages, k_cache->page_size, k_cache->heads, v_cache->pages, v_cache->page_size, v_cache->heads};
+  rg_status_t caches = RG_OK;
+  for (int64_t x : strides) if (x % 8) caches = RG_ERR_ALIGNMENT;
+  for (int i = 0; i < 6 && caches == RG_OK; ++i) if (strides[i] == 0 && sizes[i] > 1) caches = RG_ERR_UNSUPPORTED;
+  if (caches == RG_OK && ((reinterpret_cast<uintptr_t>(k_cache->ptr) | reinterpret_cast<uintptr_t>(v_cache->ptr)) & 15)) caches = RG_ERR_ALIGNMENT;
   rg::PagedAttnArgs a{};
-  a.q = q; a.k = k_cache; a.v = v_cache; a.seqs = seqs; a.out = out; a.lse = lse; a.lse_ld = lse_ld;
-  a.max_q = seqs->max_q > 0 ? std::min(seqs->max_q, q->tokens) : q->tokens;
-  a.max_len = max_len;
-  a.split = d->split; a.window = d->window; a.scale = d->scale; a.causal = d->mask;
-  a.segments = d->split ? (int32_t)((max_len + d->split - 1) / d->split) : 1;
-  if (a.segments < 1) a.segments = 1;
-  if (a.segments > 1) {
-    if (!ws || ws_bytes < rg_paged_attention_workspace_bytes(d, seqs, k_cache->page_size, q->tokens, q->heads, q->dim)) return RG_ERR_WORKSPACE;
-    if (reinterpret_cast<uintptr_t>(ws) & 15) return RG_ERR_ALIGNMENT;
-    a.ws = ws;
+  a.k = k_cache; a.v = v_cache;
+  return attend(d, q, a, caches, k_cache->pages, k_cache->page_size, k_cache->heads, seqs, out, lse, lse_ld, ws, ws_bytes, cuda_stream);
+}
+
+// ------------------------------------------------------------ four bits
+namespace {
+
+rg_status_t check_cache4(const rg_cache_four_t* c) {
+  if (!c) return RG_ERR_NULL;
+  if (c->pages < 0 || c->pages > DIM_LIMIT || c->page_size < 1 || c->page_size > (1 << 20) || c->heads < 1 || c->heads > 65535 || c->dim < 1 || c->dim > 1024)
+    return RG_ERR_SHAPE;
+  if (c->dim % 32 || c->dim > 128 || c->page_size % 8) return RG_ERR_UNSUPPORTED;
+  if (c->page_stride < 0 || c->head_stride < 0 || c->page_stride > STRIDE_LIMIT || c->head_stride > STRIDE_LIMIT) return RG_ERR_SHAPE;
+  if (c->pages > 0 && !c->ptr) return RG_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(c->ptr) & 15) || c->page_stride % 16 || c->head_stride % 16) return RG_ERR_ALIGNMENT;
+  return RG_OK;
+}
+
+// a cache that is written: its blocks lie beside one another
+rg_status_t check_cache4_out(const rg_cache_four_t* c) {
+  rg_status_t s = check_cache4(c);
+  if (s != RG_OK) return s;
+  std::pair<int64_t, int64_t> dims[2] = {{c->page_stride, c->pages}, {c->head_stride, c->heads}};
+  std::sort(dims, dims + 2);
+  __int128 extent = (__int128)rg_cache_four_block_bytes(c->page_size, c->dim);
+  for (const auto& d : dims) {
+    if (d.second < 2) continue;
+    if (d.first < extent) return RG_ERR_SHAPE;
+    extent += (__int128)(d.second - 1) * d.first;
   }
-  return rg::launch_paged_attention(a, static_cast<cudaStream_t>(cuda_stream));
+  return RG_OK;
+}
+
+rg_status_t check_cache4_pair(const rg_cache_four_t* k, const rg_cache_four_t* v) {
+  return k->pages == v->pages && k->page_size == v->page_size && k->heads == v->heads && k->dim == v->dim ? RG_OK : RG_ERR_SHAPE;
+}
+
+rg_status_t check_w4(const rg_weights_four_t* w) {
+  if (!w) return RG_ERR_NULL;
+  if (w->group != 32 && w->group != 64 && w->group != 128) return RG_ERR_UNSUPPORTED;
+  if (!dtype_ok(w->scale_dtype) || w->w_static < 0 || w->w_static > 1) return RG_ERR_SHAPE;
+  if (w->rows < 0 || w->cols < 1 || w->rows > DIM_LIMIT || w->cols > DIM_LIMIT) return RG_ERR_SHAPE;
+  if (w->cols % 32) return RG_ERR_UNSUPPORTED;
+  const int64_t groups = (w->cols + w->group - 1) / w->group;
+  if (w->code_ld < w->cols / 2 || w->scale_ld < groups || (w->zeros && w->zero_ld < groups)) return RG_ERR_SHAPE;
+  if (w->code_ld > STRIDE_LIMIT || w->scale_ld > STRIDE_LIMIT || (w->zeros && w->zero_ld > STRIDE_LIMIT)) return RG_ERR_SHAPE;
+  if (w->rows > 0 && (!w->codes || !w->scales)) return RG_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(w->codes) & 15) || w->code_ld % 16 || reinterpret_cast<uintptr_t>(w->scales) % esize(w->scale_dtype)) return RG_ERR_ALIGNMENT;
+  return RG_OK;
+}
+
+}  // namespace
+
+size_t rg_cache_four_block_bytes(int64_t page_size, int64_t dim) {
+  if (page_size < 1 || page_size > (1 << 20) || page_size % 8 || dim < 32 || dim > 128 || dim % 32) return 0;
+  return (size_t)(page_size * dim / 16 * 9);
+}
+
+rg_status_t rg_gemv_four(const rg_weights_four_t* W, const rg_tensor_t* A, const rg_tensor_t* C, const rg_epilogue_t* epi, void* cuda_stream) {
+  rg_status_t s;
+  if ((s = check_tensor(A)) != RG_OK || (s = check_tensor(C)) != RG_OK || (s = check_w4(W)) != RG_OK) return s;
+  if (A->dtype == RG_F32) return RG_ERR_UNSUPPORTED;
+  if (A->cols != W->cols || C->rows != A->rows || C->cols != W->rows || A->rows > (1 << 19)) return RG_ERR_SHAPE;
+  if ((s = check_epilogue(epi, W->rows)) != RG_OK) return s;
+  if (A->rows == 0 || W->rows == 0) return RG_OK;
+  if ((reinterpret_cast<uintptr_t>(A->ptr) & 15) || A->ld % 8) return RG_ERR_ALIGNMENT;
+  return rg::launch_gemv_w4(W, A, C, epi, static_cast<cudaStream_t>(cuda_stream));
+}
+
+rg_status_t rg_kv_append_four(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_rows_t* v, const rg_tensor_t* pos, const double* inv_freq,
+                          const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache, const rg_paged_seqs_t* seqs,
+                          const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream) {
+  rg_status_t s;
+  if ((s = check_rows(k)) != RG_OK || (s = check_rows(v)) != RG_OK || (s = check_cache4_out(k_cache)) != RG_OK || (s = check_cache4_out(v_cache)) != RG_OK ||
+      (s = check_seqs(seqs)) != RG_OK)
+    return s;
+  if (!same_shape(k, v) || (s = check_cache4_pair(k_cache, v_cache)) != RG_OK || k_cache->heads != k->heads || k_cache->dim != k->dim) return RG_ERR_SHAPE;
+  if ((s = check_append_rotation(d, k, pos, inv_freq, q, q_out)) != RG_OK) return s;
+  if (k->tokens == 0 || seqs->n_seqs == 0) return RG_OK;
+  rg::Cache4Params p{};
+  int n = 0;
+  p.st[n++] = {k->ptr, k_cache->ptr, k->token_stride, k->head_stride, k_cache->page_stride, 0, k_cache->head_stride, (int32_t)k->heads, 0};
+  p.st[n++] = {v->ptr, v_cache->ptr, v->token_stride, v->head_stride, v_cache->page_stride, 0, v_cache->head_stride, (int32_t)v->heads, 0};
+  if (q) p.st[n++] = {q->ptr, q_out->ptr, q->token_stride, q->head_stride, 0, q_out->token_stride, q_out->head_stride, (int32_t)q->heads, 0};
+  p.n_streams = n; p.tokens = k->tokens; p.d = (int32_t)k->dim;
+  if (d) set_rotation(&p, d, pos, inv_freq);
+  set_seqs(&p, seqs);
+  p.pages = k_cache->pages; p.page_size = (int32_t)k_cache->page_size;
+  return rg::launch_cache4(p, k->dtype, false, static_cast<cudaStream_t>(cuda_stream));
+}
+
+rg_status_t rg_kv_read_four(const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache, const rg_paged_seqs_t* seqs,
+                        const rg_rows_t* k_out, const rg_rows_t* v_out, void* cuda_stream) {
+  rg_status_t s;
+  if ((s = check_cache4(k_cache)) != RG_OK || (s = check_cache4(v_cache)) != RG_OK || (s = check_seqs(seqs)) != RG_OK || (s = check_rows_out(k_out)) != RG_OK ||
+      (s = check_rows_out(v_out)) != RG_OK)
+    return s;
+  if (!same_shape(k_out, v_out) || (s = check_cache4_pair(k_cache, v_cache)) != RG_OK || k_cache->heads != k_out->heads || k_cache->dim != k_out->dim) return RG_ERR_SHAPE;
+  if (k_out->tokens == 0 || seqs->n_seqs == 0) return RG_OK;
+  rg::Cache4Params p{};
+  p.st[0] = {k_cache->ptr, k_out->ptr, 0, k_cache->head_stride, k_cache->page_stride, k_out->token_stride, k_out->head_stride, (int32_t)k_out->heads, 0};
+  p.st[1] = {v_cache->ptr, v_out->ptr, 0, v_cache->head_stride, v_cache->page_stride, v_out->token_stride, v_out->head_stride, (int32_t)v_out->heads, 0};
+  p.n_streams = 2; p.tokens = k_out->tokens; p.d = (int32_t)k_out->dim;
+  set_seqs(&p, seqs);
+  p.pages = k_cache->pages; p.page_size = (int32_t)k_cache->page_size;
+  return rg::launch_cache4(p, k_out->dtype, true, static_cast<cudaStream_t>(cuda_stream));
+}
+
+rg_status_t rg_paged_attention_four(const rg_paged_attn_desc_t* d, const rg_rows_t* q, const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache,
+                                const rg_paged_seqs_t* seqs, const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream) {
+  rg_status_t s;
+  if ((s = check_paged_desc(d)) != RG_OK) return s;
+  if ((s = check_rows(q)) != RG_OK || (s = check_rows_out(out)) != RG_OK || (s = check_cache4(k_cache)) != RG_OK || (s = check_cache4(v_cache)) != RG_OK ||
+      (s = check_seqs(seqs)) != RG_OK)
+    return s;
+  if (q->dtype == RG_F32) return RG_ERR_UNSUPPORTED;
+  if ((s = check_cache4_pair(k_cache, v_cache)) != RG_OK || k_cache->dim != q->dim) return RG_ERR_SHAPE;
+  rg::PagedAttnArgs a{};
+  a.k4 = k_cache; a.v4 = v_cache;
+  return attend(d, q, a, RG_OK, k_cache->pages, k_cache->page_size, k_cache->heads, seqs, out, lse, lse_ld, ws, ws_bytes, cuda_stream);
 }
 
 // ------------------------------------------------------------ host-buffer forms
@@ -816,12 +962,13 @@ rg_status_t rg_selftest_bounded_wait(uint64_t limit_ns, uint32_t* dev_counter, v
 }
 
 rg_status_t rg_device_status(uint32_t* code) {
-  uint32_t waits[4] = {0, 0, 0, 0}, pages[2] = {0, 0};
+  uint32_t waits[4] = {0, 0, 0, 0}, pages[3] = {0, 0, 0};
   // the first of them synchronises the device
   if (rg::read_and_clear_status(&waits[0]) == RG_ERR_CUDA || rg::read_and_clear_reduce_status(&waits[1]) == RG_ERR_CUDA || rg::read_and_clear_attn_status(&waits[2]) == RG_ERR_CUDA ||
-      rg::read_and_clear_paged_attn_status(&waits[3], &pages[0]) == RG_ERR_CUDA || rg::read_and_clear_paged_status(&pages[1]) == RG_ERR_CUDA)
+      rg::read_and_clear_paged_attn_status(&waits[3], &pages[0]) == RG_ERR_CUDA || rg::read_and_clear_paged_status(&pages[1]) == RG_ERR_CUDA ||
+      rg::read_and_clear_cache4_status(&pages[2]) == RG_ERR_CUDA)
     return RG_ERR_CUDA;
-  return rg::health_of(waits, 4, pages, 2, code);
+  return rg::health_of(waits, 4, pages, 3, code);
 }
 
 const char* rg_status_string(rg_status_t s) {

@@ -99,10 +99,45 @@ struct RopeParams {
 rg_status_t launch_rope(RopeParams p, int dtype, bool paged, cudaStream_t st);
 rg_status_t read_and_clear_paged_status(uint32_t* code);
 
+// ---- a paged cache of four-bit codes (rg_cache_four.cu)
+struct Cache4Stream {
+  const void* src;
+  void* dst;
+  int64_t src_tok, src_head;           // rows: elements; blocks of a cache: bytes
+  int64_t dst_page, dst_tok, dst_head; // dst_page: bytes between a cache's pages, whichever side it is
+  int32_t heads;
+  int32_t vec;                         // rows can be moved 16 bytes at a time
+};
+struct Cache4Params {
+  Cache4Stream st[3];                  // keys, values, queries
+  int32_t n_streams, heads_all;
+  int64_t tokens;
+  int32_t d, rot, style, inverse;
+  int32_t axis_end[3];
+  int32_t pos64;
+  const void* pos;
+  int64_t pos_ld;
+  const double* inv_freq;
+  const int32_t* table;
+  int64_t table_ld;
+  const int32_t* seq_lens;
+  const int32_t* cu_q;
+  int64_t pages;
+  int32_t table_cols, n_seqs, page_size;
+  int32_t tile, head_group;
+};
+rg_status_t launch_cache4(Cache4Params p, int dtype, bool read, cudaStream_t st);
+rg_status_t read_and_clear_cache4_status(uint32_t* code);
+
+// ---- products with four-bit weights (rg_gemv_four.cu)
+rg_status_t launch_gemv_w4(const rg_weights_four_t* W, const rg_tensor_t* A, const rg_tensor_t* C, const rg_epilogue_t* epi, cudaStream_t st);
+
 struct PagedAttnArgs {
   const rg_rows_t* q;
   const rg_cache_t* k;
   const rg_cache_t* v;
+  const rg_cache_four_t* k4;               // the caches in four bits, or null
+  const rg_cache_four_t* v4;
   const rg_paged_seqs_t* seqs;
   const rg_rows_t* out;
   float* lse;

@@ -36,6 +36,7 @@
 #include <algorithm>
 
 #include "rg_common.cuh"
+#include "rg_four_bit.cuh"
 #include "rg_internal.h"
 #include "rg_ptx.cuh"
 
@@ -172,6 +173,8 @@ struct Params {
   float2* part_ml;                       // [rows][segments]
   const uint16_t* v;                     // for elements that are not finite
   int64_t v_page, v_slot, v_head;
+  const uint8_t *k4, *v4;                // caches of four-bit codes, strides in bytes
+  int64_t k4_page, k4_head, v4_page, v4_head;
 };
 
 struct alignas(16) Item {
@@ -588,28 +591,111 @@ struct Ring {
   __device__ __forceinline__ void step() { if (++slot == N) { slot = 0; phase ^= 1u; } }
 };
 
-// ---------------------------------------------------------------- the kernel for many rows
+// ---------------------------------------------------------------- four-bit caches
+// The producer copies a block's tiles of codes as they lie (one bulk copy a page piece) into a ring of their own, and the unpacking warps turn them into the
+// 16-bit blocks that the products take: exact values, so the same bits as from a 16-bit cache.  Every byte is a finite value, whatever lies in places
+// that nobody wrote, so nothing needs fixing.
+//
+// What a masked word of two codes plus 8 takes to become two values.  bf16: the mask makes 128 + u of it, and (128 + u) s - 136 s is one fused operation whose
+// addend (17 times four bits) and result (four bits times four) are exact.  fp16 has no room for 1032 s, so the integer comes first.
+template <int DT>
+__device__ __forceinline__ uint32_t two_values(uint32_t w, uint32_t s, uint32_t off) {
+  uint32_t x = (w & 0x000f000fu) | (DT == RG_BF16 ? 0x43004300u : 0x64006400u);
+  if (DT == RG_BF16) {
+    asm("fma.rn.bf16x2 %0, %0, %1, %2;" : "+r"(x) : "r"(s), "r"(off));
+  } else {
+    asm("add.rn.f16x2 %0, %0, %1;" : "+r"(x) : "r"(0xe408e408u));      // -1032
+    asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(x) : "r"(s));
+  }
+  return x;
+}
+// 32 elements of a key: four words of codes, two scale bytes (the first in the low byte); pairs of neighbours in 16 words.
+template <int DT>
+__device__ __forceinline__ void unpack32(const uint4& codes, uint32_t scales, uint32_t (&out)[16]) {
+  const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const uint32_t b = g ? scales >> 8 : scales & 0xffu;
+    uint32_t s, off = 0;
+    if (DT == RG_BF16) {
+      s = b * 0x00100010u + 0x36003600u;                               // exponent b / 8 - 19, mantissa b % 8
+      asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(off) : "r"(s), "r"(0xc308c308u));      // -136 s
+    } else {
+      const __half2 h = __float2half2_rn(scale4(b));                   // a subnormal fp16 number where b < 40, exact all the same
+      s = *reinterpret_cast<const uint32_t*>(&h);
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[8 * g + 4 * q + i] = two_values<DT>(w[2 * g + q] >> (4 * i), s, off);
+  }
+}
+// An unpacking warp's share of a block: keys 32 (first % 4) + lane of chunk first / 4, then each STEP on.
+template <int DT, int STEP>
+__device__ __forceinline__ void unpack_block(const uint8_t* raw, uint8_t* slot, int d, int first) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int i = first; i < d / 8; i += STEP) {
+    const int key = 32 * (i & 3) + lane, chunk = i >> 2;
+    const uint8_t* tile = raw + (key >> 3) * tile4_bytes(d);
+    uint32_t v[16];
+    unpack32<DT>(*reinterpret_cast<const uint4*>(tile + codes4_at(chunk, key & 7)), *reinterpret_cast<const uint16_t*>(tile + scales4_at(d, chunk, key & 7)), v);
+    uint8_t* row = slot + (chunk >> 1) * (BLK * 128) + key * 128;      // boxes of 64 elements, rows of 128 bytes, 16-byte pieces swizzled
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(row + (((4 * (chunk & 1) + q) ^ (key & 7)) << 4)) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+// Heads that do not fill their box: the rest of its rows is zeros for good.
 template <int HDP>
+__device__ __forceinline__ void clear_padding(uint8_t* slots, int n, int d, int first, int step) {
+  const int pieces = (HDP - d) / 8;
+  for (int i = first; i < n * BLK * pieces; i += step) {
+    const int key = i % BLK, x = i / BLK, piece = d / 8 + x % pieces;
+    *reinterpret_cast<uint4*>(slots + (x / pieces) * (HDP / 64 * BLK * 128) + (piece >> 3) * (BLK * 128) + key * 128 + (((piece & 7) ^ (key & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+// A page piece that is not in the cache: zeros.
+__device__ __forceinline__ void fill_zero_codes(uint8_t* raw, uint32_t bytes) {
+  for (uint32_t i = 0; i < bytes; i += 16) *reinterpret_cast<uint4*>(raw + i) = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+// A block's codes into shared memory, a lane with a page piece (`mine`) copies it; the whole warp calls.
+__device__ __forceinline__ void copy_codes(const Params& p, const uint8_t* cache, int64_t page_stride, int64_t head_stride, bool mine, int32_t page, int head, int32_t slot, int piece,
+                                           uint8_t* raw, uint32_t bar) {
+  const uint32_t bytes = (uint32_t)(p.box >> 3) * tile4_bytes(p.d);
+  const bool there = mine && page < p.pages;
+  if (mine && !there) fill_zero_codes(raw + piece * bytes, bytes);
+  const uint32_t all = (uint32_t)__popc(__ballot_sync(0xffffffffu, there)) * bytes;
+  if ((threadIdx.x & 31) == 0) mbar_expect_tx(bar, all);
+  __syncwarp();
+  if (there) bulk_load_1d(smem_u32(raw) + piece * bytes, cache + page * page_stride + head * head_stride + (int64_t)(slot >> 3) * tile4_bytes(p.d), bytes, bar);
+}
+
+// ---------------------------------------------------------------- the kernel for many rows
+template <int HDP, bool FOUR>
 struct Wide {
   static constexpr int DB = HDP / 64;                              // 64-column boxes of a head
   static constexpr int NT = 2, SOFT = 4 * NT;                      // tiles of 128 rows, softmax warps
-  static constexpr int PRODUCER = SOFT, MMA = SOFT + 1, FIXER = SOFT + 2, WARPS = SOFT + 3, THREADS = (SOFT + 4) * 32;   // the last warp does nothing
+  static constexpr int PRODUCER = SOFT, MMA = SOFT + 1, FIXER = SOFT + 2, UNPACK = FOUR ? 2 : 0, WARPS = SOFT + (FOUR ? 4 : 3), THREADS = (SOFT + 4) * 32;   // without unpacking the last warp does nothing
   static constexpr uint32_t Q_BOX = 128 * 128, Q_TILE = DB * Q_BOX;
   static constexpr uint32_t KV_BOX = BLK * 128, SLOT = DB * KV_BOX;
-  static constexpr int SLOTS = HDP == 128 ? 5 : 10;
+  static constexpr int SLOTS = FOUR ? (HDP == 128 ? 4 : 8) : HDP == 128 ? 5 : 10;
+  static constexpr int RAWS = FOUR ? (HDP == 128 ? 3 : 6) : 0;     // blocks of codes
+  static constexpr uint32_t RAW = BLK / 8 * tile4_bytes(HDP);
   static constexpr uint32_t COLS = 512;                            // tensor memory: S_t, and P_t over it, at 128 t, O_t at 128 (2 + t)
-  static constexpr uint32_t KV_AT = NT * Q_TILE, ITEM_AT = KV_AT + SLOTS * SLOT, BAR_AT = ITEM_AT + ITEMS * sizeof(Item), N_BAR = 12 + 3 * SLOTS + 2 * ITEMS,
+  static constexpr uint32_t KV_AT = NT * Q_TILE, RAW_AT = KV_AT + SLOTS * SLOT, ITEM_AT = RAW_AT + RAWS * RAW, BAR_AT = ITEM_AT + ITEMS * sizeof(Item), N_BAR = 12 + 3 * SLOTS + 2 * ITEMS + 2 * RAWS,
                             FLAG_AT = BAR_AT + 8 * N_BAR, LAST = FLAG_AT + 4 * (2 + FLAGS);
   static constexpr size_t SMEM = 1024 + LAST;
   static_assert(SMEM <= 232448 && SLOTS / 2 + 1 < FLAGS, "fits the SM; the fixer cannot be a whole turn of flags ahead");
 };
 
-template <int HDP, int DT>
-__global__ void __launch_bounds__(Wide<HDP>::THREADS, 1)
+template <int HDP, int DT, bool FOUR>
+__global__ void __launch_bounds__(Wide<HDP, FOUR>::THREADS, 1)
 paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                        const __grid_constant__ Params p) {
-  using F = Wide<HDP>;
-  constexpr int DB = F::DB, SLOTS = F::SLOTS, NT = F::NT;
+  using F = Wide<HDP, FOUR>;
+  constexpr int DB = F::DB, SLOTS = F::SLOTS, NT = F::NT, RAWS = FOUR ? F::RAWS : 1;
   constexpr uint32_t IDESC_S = pa_idesc(BLK, DT == RG_BF16, false, false), IDESC_O = pa_idesc(HDP, DT == RG_BF16, false, true);
 
   extern __shared__ uint8_t smem_raw[];
@@ -619,7 +705,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   Item* items = reinterpret_cast<Item*>(smem_gen + F::ITEM_AT);
   const uint32_t bar0 = smem_base + F::BAR_AT;
   const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_s = bar0 + 16, b_o_full = bar0 + 32, b_o_empty = bar0 + 48, b_p = bar0 + 64, b_full = bar0 + 96;   // one a tile from b_s on; b_p: and half of the keys
-  const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS;
+  const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS, b_raw = b_free + 8 * ITEMS, b_raw_empty = b_raw + 8 * RAWS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + F::FLAG_AT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* not_finite = reinterpret_cast<volatile int*>(tmem_slot + 2);          // [FLAGS]
@@ -628,8 +714,9 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   if (threadIdx.x == 0) {
     mbar_init(b_q_full, 1); mbar_init(b_q_empty, 1);
     for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 16 * t, 4); mbar_init(b_p + 16 * t + 8, 4); mbar_init(b_o_full + 8 * t, 1); mbar_init(b_o_empty + 8 * t, 4); }
-    for (int s = 0; s < SLOTS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_ready + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
+    for (int s = 0; s < SLOTS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_ready + 8 * s, FOUR ? F::UNPACK : 1); mbar_init(b_empty + 8 * s, 1); }
     for (int s = 0; s < ITEMS; ++s) { mbar_init(b_item + 8 * s, 1); mbar_init(b_free + 8 * s, F::WARPS - 1); }
+    if (FOUR) for (int s = 0; s < F::RAWS; ++s) { mbar_init(b_raw + 8 * s, 1); mbar_init(b_raw_empty + 8 * s, F::UNPACK); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -665,6 +752,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
     const int pieces = BLK / p.box;                                // TMA boxes along the keys of a block
     const int piece = lane & (pieces - 1), col = lane / pieces;          // col < DB: this lane issues a box
     Ring<SLOTS> kv;
+    Ring<RAWS> raw;
     uint32_t q_phase = 1;
     Walk walk;
     walk.start(p, cta_tokens);
@@ -700,6 +788,17 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
           page = p.pages;
         }
         const int32_t key = b * BLK + piece * p.box, at = key - key / p.by_page * p.page_size;
+        if constexpr (FOUR) {
+#pragma unroll
+          for (int which = 0; which < 2; ++which) {
+            alive = pa_wait(b_raw_empty + 8 * raw.slot, raw.phase ^ 1u, abort_flag, 0x2200u | raw.slot);
+            if (!alive) break;
+            copy_codes(p, which ? p.v4 : p.k4, which ? p.v4_page : p.k4_page, which ? p.v4_head : p.k4_head, mine && col == 0, page, it.head, at, piece,
+                       smem_gen + F::RAW_AT + raw.slot * F::RAW, b_raw + 8 * raw.slot);
+            raw.step();
+          }
+          continue;
+        }
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)p.box * 128u;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
@@ -721,7 +820,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
     auto next_slot = [&](uint32_t& bar) -> uint32_t {
       const uint32_t slot = __shfl_sync(0xffffffffu, kv.slot, 0);
       alive = pa_wait(b_ready + 8 * slot, kv.phase, abort_flag, 0x2300u | slot);
-      if (alive) alive = pa_wait(b_full + 8 * slot, kv.phase, abort_flag, 0x2380u | slot);
+      if (!FOUR && alive) alive = pa_wait(b_full + 8 * slot, kv.phase, abort_flag, 0x2380u | slot);
       pa_fence_after();
       bar = b_empty + 8 * slot;
       kv.step();
@@ -780,6 +879,23 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
           if (more) pa_commit(k_bar);
           if (j + 2 == nb) pa_commit(b_q_empty);
         }
+      }
+    }
+  } else if constexpr (FOUR) {
+    // ------------------------------------------------------------ unpackers
+    Ring<SLOTS> kv;
+    Ring<RAWS> raw;
+    if (p.d < HDP) { clear_padding<HDP>(smem_gen + F::KV_AT, SLOTS, p.d, threadIdx.x - F::FIXER * 32, F::UNPACK * 32); asm volatile("bar.sync 1, %0;" ::"n"(F::UNPACK * 32) : "memory"); }
+    while (alive && next_item(it, alive)) {
+      for (int i = 2 * (it.b1 - it.b0); i > 0; --i) {
+        alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x2600u | kv.slot);
+        if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x2680u | raw.slot);
+        if (!alive) break;
+        unpack_block<DT, F::UNPACK>(smem_gen + F::RAW_AT + raw.slot * F::RAW, smem_gen + F::KV_AT + kv.slot * F::SLOT, p.d, warp - F::FIXER);
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(b_ready + 8 * kv.slot); mbar_arrive(b_raw_empty + 8 * raw.slot); }
+        kv.step();
+        raw.step();
       }
     }
   } else if (warp == F::FIXER) {
@@ -892,7 +1008,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         o_phase ^= 1u;
         if (!alive) break;
         pa_fence_after();
-        add_back = any_masked && not_finite[slot_flag] != 0;
+        if (!FOUR) add_back = any_masked && not_finite[slot_flag] != 0;
       }
       if (warp_live) {
         const int64_t token = (int64_t)it.tok + tok;
@@ -946,7 +1062,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         }
         const bool some = live && sum > 0.0f;                      // the row sees keys, and no NaN among its scores
         odd = __any_sync(0xffffffffu, odd && some);
-        if (odd || add_back) {
+        if (!FOUR && (odd || add_back)) {
 #pragma unroll 1
           for (int q = 0; 32 * q < p.d; ++q)
             put_odd_values<DT>(p, it, odd, q, some ? lo : INT32_MAX, hi, some, it.multi ? (grow * p.segments + it.seg) * p.d : token * p.o_tok + head * p.o_head);
@@ -989,17 +1105,19 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
 // 5.8 TB/s; one of 8192 (34 MB): 13 us, of which the copies are 5 (launch, item and page look-up, the chain of two blocks and the join are latency).
 // With the queries as the 128 rows instead (the other form, 4 of them filled) the 64 sequences took 234 us on the device, and 278 with each row's keys dealt to
 // four warps: the tensor core then reads 128 mostly empty rows from shared memory for every step.
-template <int HDP, int ROWS>
+template <int HDP, int ROWS, bool FOUR>
 struct Few {
   static constexpr int DB = HDP / 64;
-  static constexpr int PRODUCER = 4, MMA = 5, FIXER = 6, WARPS = 7, THREADS = WARPS * 32;
+  static constexpr int PRODUCER = 4, MMA = 5, FIXER = 6, UNPACK = FOUR ? 4 : 0, WARPS = FOUR ? 10 : 7, THREADS = WARPS * 32;
   static constexpr int N = ROWS < 16 ? 16 : ROWS;                  // narrow side of the products
   static constexpr uint32_t Q_BOX = N * 128, P_BOX = N * 128, P_BUF = 2 * P_BOX;      // rows of 64 elements, 64 keys
   static constexpr uint32_t KV_BOX = BLK * 128, SLOT = DB * KV_BOX;
-  static constexpr int SLOTS = HDP == 128 ? 3 : 5;
+  static constexpr int SLOTS = FOUR ? (HDP == 128 ? 2 : 4) : HDP == 128 ? 3 : 5;
+  static constexpr int RAWS = FOUR ? (HDP == 128 ? 3 : 5) : 0;     // blocks of codes
+  static constexpr uint32_t RAW = BLK / 8 * tile4_bytes(HDP);
   static constexpr uint32_t COLS = 128;                            // tensor memory: S' of even and odd blocks at 0 and 32, O' of even and odd items at 64 and 96
-  static constexpr uint32_t Q_AT = SLOTS * SLOT, P_AT = Q_AT + DB * Q_BOX, ITEM_AT = P_AT + 2 * P_BUF, BAR_AT = ITEM_AT + ITEMS * sizeof(Item),
-                            N_BAR = 12 + 3 * SLOTS + 2 * ITEMS, FLAG_AT = BAR_AT + 8 * N_BAR, MAX_AT = (FLAG_AT + 4 * (2 + FLAGS) + 15) & ~15u, SUM_AT = MAX_AT + 2 * 128 * 4,
+  static constexpr uint32_t RAW_AT = SLOTS * SLOT, Q_AT = RAW_AT + (RAWS * RAW + 1023) / 1024 * 1024, P_AT = Q_AT + DB * Q_BOX, ITEM_AT = P_AT + 2 * P_BUF, BAR_AT = ITEM_AT + ITEMS * sizeof(Item),
+                            N_BAR = 12 + 3 * SLOTS + 2 * ITEMS + 2 * RAWS, FLAG_AT = BAR_AT + 8 * N_BAR, MAX_AT = (FLAG_AT + 4 * (2 + FLAGS) + 15) & ~15u, SUM_AT = MAX_AT + 2 * 128 * 4,
                             LAST = SUM_AT + 2 * 128 * 4;
   static constexpr size_t SMEM = 1024 + LAST;
   static_assert(SMEM <= 115712 && SLOTS / 2 + 1 < FLAGS, "two CTAs fit the SM; the fixer cannot be a whole turn of flags ahead");
@@ -1031,12 +1149,12 @@ __device__ __forceinline__ float reduce_rows(float (&v)[ROWS]) {
   return v[0];
 }
 
-template <int HDP, int ROWS, int DT>
-__global__ void __launch_bounds__(Few<HDP, ROWS>::THREADS, 2)
+template <int HDP, int ROWS, int DT, bool FOUR>
+__global__ void __launch_bounds__(Few<HDP, ROWS, FOUR>::THREADS, 2)
 paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                            const __grid_constant__ Params p) {
-  using F = Few<HDP, ROWS>;
-  constexpr int DB = F::DB, SLOTS = F::SLOTS;
+  using F = Few<HDP, ROWS, FOUR>;
+  constexpr int DB = F::DB, SLOTS = F::SLOTS, RAWS = FOUR ? F::RAWS : 1;
   constexpr uint32_t IDESC_S = pa_idesc(F::N, DT == RG_BF16, false, false), IDESC_O = pa_idesc(F::N, DT == RG_BF16, true, false);
 
   extern __shared__ uint8_t smem_raw[];
@@ -1046,7 +1164,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
   Item* items = reinterpret_cast<Item*>(smem_gen + F::ITEM_AT);
   const uint32_t bar0 = smem_base + F::BAR_AT;
   const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_x = bar0 + 16, b_y = bar0 + 24, b_s = bar0 + 32, b_p = bar0 + 48, b_pv = bar0 + 64, b_o_empty = bar0 + 80, b_full = bar0 + 96;   // two each from b_s to b_o_empty
-  const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS;
+  const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS, b_raw = b_free + 8 * ITEMS, b_raw_empty = b_raw + 8 * RAWS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + F::FLAG_AT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* not_finite = reinterpret_cast<volatile int*>(tmem_slot + 2);          // [FLAGS]
@@ -1057,8 +1175,9 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
   if (threadIdx.x == 0) {
     mbar_init(b_q_full, 1); mbar_init(b_q_empty, 1); mbar_init(b_x, 4); mbar_init(b_y, 4);
     for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 8 * t, 4); mbar_init(b_pv + 8 * t, 1); mbar_init(b_o_empty + 8 * t, 4); }
-    for (int s = 0; s < SLOTS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_ready + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
+    for (int s = 0; s < SLOTS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_ready + 8 * s, FOUR ? F::UNPACK : 1); mbar_init(b_empty + 8 * s, 1); }
     for (int s = 0; s < ITEMS; ++s) { mbar_init(b_item + 8 * s, 1); mbar_init(b_free + 8 * s, F::WARPS - 1); }
+    if (FOUR) for (int s = 0; s < F::RAWS; ++s) { mbar_init(b_raw + 8 * s, 1); mbar_init(b_raw_empty + 8 * s, F::UNPACK); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -1090,6 +1209,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     const int pieces = BLK / p.box;
     const int piece = lane & (pieces - 1), col = lane / pieces;
     Ring<SLOTS> kv;
+    Ring<RAWS> raw;
     uint32_t q_phase = 1;
     Walk walk;
     walk.start(p, p.tile_tokens);
@@ -1112,13 +1232,22 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       if (lane == 0) mbar_expect_tx(b_q_full, (uint32_t)(DB * p.tile_tokens * p.group) * 128u);
       __syncwarp();
       if (lane < DB) pa_tma_4d(sQ + lane * F::Q_BOX, &tmap_q, lane * 64, 0, it.tok, it.head, b_q_full);
-      auto copy = [&](const CUtensorMap* map, int b, int32_t& id) {
+      auto copy = [&](bool is_v, int b, int32_t& id) {
+        const CUtensorMap* map = is_v ? &tmap_v : &tmap_k;
         const bool mine = wanted(b);
         if (mine && (id < 0 || id >= p.pages)) {                   // not a page: the copy from behind the last one fills in zeros
           if (col == 0) atomicCAS(&g_paged_attn_page_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
           id = p.pages;
         }
         const int32_t key = b * BLK + piece * p.box, at = key - key / p.by_page * p.page_size;
+        if constexpr (FOUR) {
+          alive = pa_wait(b_raw_empty + 8 * raw.slot, raw.phase ^ 1u, abort_flag, 0x3200u | raw.slot);
+          if (!alive) return;
+          copy_codes(p, is_v ? p.v4 : p.k4, is_v ? p.v4_page : p.k4_page, is_v ? p.v4_head : p.k4_head, mine && col == 0, id, it.head, at, piece,
+                     smem_gen + F::RAW_AT + raw.slot * F::RAW, b_raw + 8 * raw.slot);
+          raw.step();
+          return;
+        }
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)p.box * 128u;
         alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x3200u | kv.slot);
         if (!alive) return;
@@ -1127,11 +1256,11 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         if (mine) pa_tma_4d(sKV + kv.slot * F::SLOT + col * F::KV_BOX + piece * p.box * 128, map, col * 64, at, it.head, id, b_full + 8 * kv.slot);
         kv.step();
       };
-      copy(&tmap_k, it.b0, page);
+      copy(false, it.b0, page);
       for (int b = it.b0; b < it.b1 && alive; ++b) {
         const int32_t later = wanted(b + 2) ? entry(b + 2) : 0;
-        if (b + 1 < it.b1) copy(&tmap_k, b + 1, next);
-        if (alive) copy(&tmap_v, b, page);
+        if (b + 1 < it.b1) copy(false, b + 1, next);
+        if (alive) copy(true, b, page);
         page = next;
         next = later;
       }
@@ -1144,7 +1273,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     auto next_slot = [&](uint32_t& bar) -> uint32_t {
       const uint32_t slot = __shfl_sync(0xffffffffu, kv.slot, 0);
       alive = pa_wait(b_ready + 8 * slot, kv.phase, abort_flag, 0x3300u | slot);
-      if (alive) alive = pa_wait(b_full + 8 * slot, kv.phase, abort_flag, 0x3380u | slot);
+      if (!FOUR && alive) alive = pa_wait(b_full + 8 * slot, kv.phase, abort_flag, 0x3380u | slot);
       pa_fence_after();
       bar = b_empty + 8 * slot;
       kv.step();
@@ -1192,7 +1321,24 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       }
       ++n_item;
     }
-  } else if (warp == F::FIXER) {
+  } else if (FOUR && warp >= F::FIXER) {
+    // ------------------------------------------------------------ unpackers
+    Ring<SLOTS> kv;
+    Ring<RAWS> raw;
+    if (p.d < HDP) { clear_padding<HDP>(smem_gen, SLOTS, p.d, threadIdx.x - F::FIXER * 32, F::UNPACK * 32); asm volatile("bar.sync 1, %0;" ::"n"(F::UNPACK * 32) : "memory"); }
+    while (alive && next_item(it, alive)) {
+      for (int i = 2 * (it.b1 - it.b0); i > 0; --i) {
+        alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x3600u | kv.slot);
+        if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x3680u | raw.slot);
+        if (!alive) break;
+        unpack_block<DT, F::UNPACK>(smem_gen + F::RAW_AT + raw.slot * F::RAW, smem_gen + kv.slot * F::SLOT, p.d, warp - F::FIXER);
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(b_ready + 8 * kv.slot); mbar_arrive(b_raw_empty + 8 * raw.slot); }
+        kv.step();
+        raw.step();
+      }
+    }
+  } else if (!FOUR && warp == F::FIXER) {
     // ------------------------------------------------------------ fixer
     Ring<SLOTS> kv;
     uint32_t flags = 0;
@@ -1310,7 +1456,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         alive = pa_wait(b_pv + 8 * ((block - 1) & 1), ((block - 1) >> 1) & 1, abort_flag, 0x3780u);      // the last block's product
         if (!alive) break;
         pa_fence_after();
-        add_back = any_masked && not_finite[slot_flag] != 0;
+        if (!FOUR) add_back = any_masked && not_finite[slot_flag] != 0;
       }
       const bool none = !(sum > 0.0f) && sum == sum;               // no key seen
       const float inv = it.multi ? DOWN<DT> : none ? 0.0f : __frcp_rn(sum);
@@ -1345,7 +1491,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
           }
         }
         odd = __any_sync(0xffffffffu, odd);
-        if (odd || add_back) {
+        if (!FOUR && (odd || add_back)) {
           const int64_t token = (int64_t)it.tok + my_tok;
           const int h = it.head * p.group + r - my_tok * p.group;
           put_odd_values<DT>(p, it, odd, warp, some ? lo : INT32_MAX, hi, some && (lane & ((1 << SH) - 1)) == 0,
@@ -1520,31 +1666,31 @@ cudaError_t launch_form(Kernel kernel, DeviceOnce& configured, int ctas_per_sm, 
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, q, k, v, p);
 }
-template <int HDP, int DT>
+template <int HDP, int DT, bool FOUR>
 cudaError_t launch_wide(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
   static DeviceOnce configured;
-  return launch_form<Wide<HDP>>(paged_attention_wide_kernel<HDP, DT>, configured, 1, q, k, v, p, most, st);
+  return launch_form<Wide<HDP, FOUR>>(paged_attention_wide_kernel<HDP, DT, FOUR>, configured, 1, q, k, v, p, most, st);
 }
-template <int HDP, int ROWS, int DT>
+template <int HDP, int ROWS, int DT, bool FOUR>
 cudaError_t launch_few(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
   static DeviceOnce configured;
-  return launch_form<Few<HDP, ROWS>>(paged_attention_few_kernel<HDP, ROWS, DT>, configured, 2, q, k, v, p, most, st);
+  return launch_form<Few<HDP, ROWS, FOUR>>(paged_attention_few_kernel<HDP, ROWS, DT, FOUR>, configured, 2, q, k, v, p, most, st);
 }
-template <int DT>
+template <int DT, bool FOUR>
 cudaError_t launch_any(int rows, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
   if (p.d <= 64) {
     switch (rows) {
-      case 8: return launch_few<64, 8, DT>(q, k, v, p, most, st);
-      case 16: return launch_few<64, 16, DT>(q, k, v, p, most, st);
-      case 32: return launch_few<64, 32, DT>(q, k, v, p, most, st);
+      case 8: return launch_few<64, 8, DT, FOUR>(q, k, v, p, most, st);
+      case 16: return launch_few<64, 16, DT, FOUR>(q, k, v, p, most, st);
+      case 32: return launch_few<64, 32, DT, FOUR>(q, k, v, p, most, st);
     }
-    return launch_wide<64, DT>(q, k, v, p, most, st);
+    return launch_wide<64, DT, FOUR>(q, k, v, p, most, st);
   }
   switch (rows) {
-    case 8: return launch_few<128, 8, DT>(q, k, v, p, most, st);
-    case 16: return launch_few<128, 16, DT>(q, k, v, p, most, st);
+    case 8: return launch_few<128, 8, DT, FOUR>(q, k, v, p, most, st);
+    case 16: return launch_few<128, 16, DT, FOUR>(q, k, v, p, most, st);
   }
-  return launch_wide<128, DT>(q, k, v, p, most, st);
+  return launch_wide<128, DT, FOUR>(q, k, v, p, most, st);
 }
 
 }  // namespace
@@ -1552,11 +1698,12 @@ cudaError_t launch_any(int rows, const CUtensorMap& q, const CUtensorMap& k, con
 // All arguments were validated by the caller.
 rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   Params p{};
-  const int64_t T = a.q->tokens, hkv = a.k->heads;
-  const int G = (int)(a.q->heads / hkv), d = (int)a.q->dim, page = (int)a.k->page_size;
+  const bool four = a.k4 != nullptr;
+  const int64_t T = a.q->tokens, hkv = four ? a.k4->heads : a.k->heads;
+  const int G = (int)(a.q->heads / hkv), d = (int)a.q->dim, page = (int)(four ? a.k4->page_size : a.k->page_size);
   p.table = a.seqs->block_table; p.seq_lens = a.seqs->seq_lens; p.cu_q = a.seqs->cu_q;
   p.table_ld = a.seqs->table_ld; p.max_len = a.max_len; p.tokens = T;
-  p.n_seqs = a.seqs->n_seqs; p.page_size = page; p.pages = (int32_t)a.k->pages;
+  p.n_seqs = a.seqs->n_seqs; p.page_size = page; p.pages = (int32_t)(four ? a.k4->pages : a.k->pages);
   p.hq = (int32_t)a.q->heads; p.hkv = (int32_t)hkv; p.group = G; p.d = d;
   p.split = (int32_t)a.split; p.segments = a.segments; p.causal = a.causal; p.window = (int32_t)a.window;
   p.scale = a.scale; p.c = a.scale * 1.44269504f;
@@ -1566,7 +1713,12 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   p.lse = a.lse; p.lse_ld = a.lse_ld;
   p.part_o = static_cast<float*>(a.ws);
   if (a.ws) p.part_ml = reinterpret_cast<float2*>(p.part_o + T * p.hq * (int64_t)a.segments * d);
-  p.v = static_cast<const uint16_t*>(a.v->ptr); p.v_page = a.v->page_stride; p.v_slot = a.v->slot_stride; p.v_head = a.v->head_stride;
+  if (four) {
+    p.k4 = static_cast<const uint8_t*>(a.k4->ptr); p.k4_page = a.k4->page_stride; p.k4_head = a.k4->head_stride;
+    p.v4 = static_cast<const uint8_t*>(a.v4->ptr); p.v4_page = a.v4->page_stride; p.v4_head = a.v4->head_stride;
+  } else {
+    p.v = static_cast<const uint16_t*>(a.v->ptr); p.v_page = a.v->page_stride; p.v_slot = a.v->slot_stride; p.v_head = a.v->head_stride;
+  }
 
   const int64_t need = a.max_q * G;
   const int most_rows = d <= 64 ? 32 : 16;
@@ -1577,13 +1729,17 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   p.box = box = box < BLK ? box : BLK;
 
   CUtensorMap tq, tk, tv;
-  const int64_t pages = p.pages > 0 ? p.pages : 1;
-  const void* kp = p.pages > 0 ? a.k->ptr : a.q->ptr;      // no pages: nothing is read, but a map wants an address
-  const void* vp = p.pages > 0 ? a.v->ptr : a.q->ptr;
-  if (!make_tmap_4d(&tq, a.q->ptr, a.q->dtype, {d, G, T, hkv}, {a.q->head_stride, a.q->token_stride, G * a.q->head_stride}, {64, G, p.tile_tokens, 1}) ||
-      !make_tmap_4d(&tk, kp, a.q->dtype, {d, page, hkv, pages}, {a.k->slot_stride, a.k->head_stride, a.k->page_stride}, {64, box, 1, 1}) ||
-      !make_tmap_4d(&tv, vp, a.q->dtype, {d, page, hkv, pages}, {a.v->slot_stride, a.v->head_stride, a.v->page_stride}, {64, box, 1, 1}))
-    return RG_ERR_CUDA;
+  if (!make_tmap_4d(&tq, a.q->ptr, a.q->dtype, {d, G, T, hkv}, {a.q->head_stride, a.q->token_stride, G * a.q->head_stride}, {64, G, p.tile_tokens, 1})) return RG_ERR_CUDA;
+  if (four) {
+    tk = tv = tq;                                          // codes are copied without maps
+  } else {
+    const int64_t pages = p.pages > 0 ? p.pages : 1;
+    const void* kp = p.pages > 0 ? a.k->ptr : a.q->ptr;    // no pages: nothing is read, but a map wants an address
+    const void* vp = p.pages > 0 ? a.v->ptr : a.q->ptr;
+    if (!make_tmap_4d(&tk, kp, a.q->dtype, {d, page, hkv, pages}, {a.k->slot_stride, a.k->head_stride, a.k->page_stride}, {64, box, 1, 1}) ||
+        !make_tmap_4d(&tv, vp, a.q->dtype, {d, page, hkv, pages}, {a.v->slot_stride, a.v->head_stride, a.v->page_stride}, {64, box, 1, 1}))
+      return RG_ERR_CUDA;
+  }
 
   p.by_split = Div::by(p.split ? p.split : 1); p.by_hkv = Div::by(p.hkv); p.by_hq = Div::by(p.hq); p.by_page = Div::by(page); p.by_group = Div::by(G);
   // Two tiles share the keys that a CTA reads and the tensor core works for one while the other's softmax runs; but where all tiles find an SM
@@ -1599,7 +1755,9 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   // no more CTAs than there can be items
   const int64_t most = items_of(p.cta_tokens);
   if (most >= (int64_t(1) << 31) || T * p.hq >= (int64_t(1) << 31)) return RG_ERR_SHAPE;     // items and rows are counted in 32 bits
-  const cudaError_t e = a.q->dtype == RG_BF16 ? launch_any<RG_BF16>(rows, tq, tk, tv, p, most, st) : launch_any<RG_F16>(rows, tq, tk, tv, p, most, st);
+  const bool bf16 = a.q->dtype == RG_BF16;
+  const cudaError_t e = four ? (bf16 ? launch_any<RG_BF16, true>(rows, tq, tk, tv, p, most, st) : launch_any<RG_F16, true>(rows, tq, tk, tv, p, most, st))
+                             : (bf16 ? launch_any<RG_BF16, false>(rows, tq, tk, tv, p, most, st) : launch_any<RG_F16, false>(rows, tq, tk, tv, p, most, st));
   if (e != cudaSuccess) return RG_ERR_CUDA;
   if (a.segments > 1 && (a.segments <= 16 ? launch_join<1>(p, st) : launch_join<JOIN_THREADS / 32>(p, st)) != cudaSuccess) return RG_ERR_CUDA;
   return RG_OK;

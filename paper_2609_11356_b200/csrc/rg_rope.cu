@@ -16,6 +16,7 @@
 
 #include "rg_common.cuh"
 #include "rg_internal.h"
+#include "rg_place.cuh"
 
 namespace rg {
 
@@ -72,19 +73,6 @@ struct Pack<DT, 4> {
   static __device__ __forceinline__ void put_to(uint4& r, const float (&v)[4]) { uint32_t w[4]; words_put<RG_F32, 4>(w, v); r = make_uint4(w[0], w[1], w[2], w[3]); }
   static __device__ __forceinline__ void put_to(uint2& r, const float (&v)[4]) { uint32_t w[2]; words_put<DT, 2>(w, v); r = make_uint2(w[0], w[1]); }
 };
-
-// Which sequence a row belongs to and its place there; the whole warp calls.  The count of sequences that end at or
-// before the row is its sequence (lengths of zero included), whatever the order of the additions.
-__device__ __forceinline__ bool place_of(const RopeParams& p, int64_t t, int& seq, int64_t& place) {
-  const int lane = threadIdx.x & 31;
-  int before = 0;
-  for (int i = lane; i < p.n_seqs; i += 32) before += p.cu_q[i + 1] <= t ? 1 : 0;
-  seq = __reduce_add_sync(0xffffffffu, before);
-  if (seq >= p.n_seqs) return false;                    // a row behind the last sequence
-  if (t < p.cu_q[seq]) return false;
-  place = (int64_t)p.seq_lens[seq] - ((int64_t)p.cu_q[seq + 1] - t);
-  return true;
-}
 
 // Units a thread has in flight before the CTA works out its angles.  Alone the rotation gains by four (8192 tokens of 32 heads of 128, 134 MB:
 // 28 -> 24 us on the device, 5.6 TB/s; 25.7 called on rotating inputs).  With the cache (three sets of strides, places to look up) the registers they take cost more than they bring (257 MB: 49 us
@@ -157,11 +145,7 @@ __global__ void __launch_bounds__(ROPE_THREADS, PAGED ? 6 : 4) rope_kernel(const
       int seq;
       int64_t place = 0, page = -2;
       if (place_of(p, t0 + w, seq, place)) {
-        page = -1;
-        if (place >= 0 && place < (int64_t)p.table_cols * p.page_size) {
-          const int64_t id = p.table[(int64_t)seq * p.table_ld + place / p.page_size];
-          if (id >= 0 && id < p.pages) page = id;
-        }
+        page = page_of(p, seq, place);
         if (page < 0 && (threadIdx.x & 31) == 0) atomicCAS(&g_paged_status_word, 0u, (unsigned)RG_PAGE_CODE_APPEND);
       }
       if ((threadIdx.x & 31) == 0) { s_page[w] = page; s_slot[w] = (int32_t)(place >= 0 ? place % p.page_size : 0); s_pos[w] = place; }
