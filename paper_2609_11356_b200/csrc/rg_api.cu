@@ -962,13 +962,13 @@ rg_status_t rg_selftest_bounded_wait(uint64_t limit_ns, uint32_t* dev_counter, v
 }
 
 rg_status_t rg_device_status(uint32_t* code) {
-  uint32_t waits[4] = {0, 0, 0, 0}, pages[3] = {0, 0, 0};
+  uint32_t waits[5] = {0, 0, 0, 0, 0}, pages[3] = {0, 0, 0};
   // the first of them synchronises the device
   if (rg::read_and_clear_status(&waits[0]) == RG_ERR_CUDA || rg::read_and_clear_reduce_status(&waits[1]) == RG_ERR_CUDA || rg::read_and_clear_attn_status(&waits[2]) == RG_ERR_CUDA ||
       rg::read_and_clear_paged_attn_status(&waits[3], &pages[0]) == RG_ERR_CUDA || rg::read_and_clear_paged_status(&pages[1]) == RG_ERR_CUDA ||
-      rg::read_and_clear_cache4_status(&pages[2]) == RG_ERR_CUDA)
+      rg::read_and_clear_cache4_status(&pages[2]) == RG_ERR_CUDA || rg::read_and_clear_gemv_four_status(&waits[4]) == RG_ERR_CUDA)
     return RG_ERR_CUDA;
-  return rg::health_of(waits, 4, pages, 3, code);
+  return rg::health_of(waits, 5, pages, 3, code);
 }
 
 const char* rg_status_string(rg_status_t s) {

@@ -131,6 +131,7 @@ rg_status_t read_and_clear_cache4_status(uint32_t* code);
 
 // ---- products with four-bit weights (rg_gemv_four.cu)
 rg_status_t launch_gemv_w4(const rg_weights_four_t* W, const rg_tensor_t* A, const rg_tensor_t* C, const rg_epilogue_t* epi, cudaStream_t st);
+rg_status_t read_and_clear_gemv_four_status(uint32_t* code);
 
 struct PagedAttnArgs {
   const rg_rows_t* q;
