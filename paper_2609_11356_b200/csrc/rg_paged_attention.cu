@@ -456,6 +456,10 @@ __device__ __forceinline__ float join_quarters(float a, float b, float c, float 
 template <int N>
 __device__ __forceinline__ void pa_ld_cols(uint32_t taddr, uint32_t (&r)[N]);
 template <>
+__device__ __forceinline__ void pa_ld_cols<4>(uint32_t taddr, uint32_t (&r)[4]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+template <>
 __device__ __forceinline__ void pa_ld_cols<8>(uint32_t taddr, uint32_t (&r)[8]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
@@ -472,6 +476,7 @@ template <int N>
 __device__ __forceinline__ void pa_st_cols(uint32_t taddr, const uint32_t (&r)[N]) {
   if constexpr (N == 32) pa_st32(taddr, r);
   else if constexpr (N == 16) pa_st16(taddr, r);
+  else if constexpr (N == 4) asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%4], {%0, %1, %2, %3};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(taddr) : "memory");
   else
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
                  ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr) : "memory");
@@ -596,11 +601,17 @@ struct Ring {
 // 16-bit blocks that the products take: exact values, so the same bits as from a 16-bit cache.  Every byte is a finite value, whatever lies in places
 // that nobody wrote, so nothing needs fixing.
 //
-// What a masked word of two codes plus 8 takes to become two values.  bf16: the mask makes 128 + u of it, and (128 + u) s - 136 s is one fused operation whose
-// addend (17 times four bits) and result (four bits times four) are exact.  fp16 has no room for 1032 s, so the integer comes first.
+// A word's nibbles i and i + 4 as two values.  bf16: a mask makes 128 + u of each, and (128 + u) s - 136 s is one fused operation whose addend (17 times four
+// bits) and result (four bits times four) are exact.  fp16 has no room for 1032 s, so the integer comes first.  Mask and magic number are kept in
+// registers, or the compiler takes two operations to use them.
+struct Unpack {
+  uint32_t mask, magic;
+  __device__ __forceinline__ explicit Unpack(int dt) : mask(0x000f000fu), magic(dt == RG_BF16 ? 0x43004300u : 0x64006400u) { asm("" : "+r"(mask), "+r"(magic)); }
+};
 template <int DT>
-__device__ __forceinline__ uint32_t two_values(uint32_t w, uint32_t s, uint32_t off) {
-  uint32_t x = (w & 0x000f000fu) | (DT == RG_BF16 ? 0x43004300u : 0x64006400u);
+__device__ __forceinline__ uint32_t two_values(const Unpack& u, uint32_t w, uint32_t s, uint32_t off) {
+  uint32_t x;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x) : "r"(w), "r"(u.mask), "r"(u.magic));      // (w & mask) | magic
   if (DT == RG_BF16) {
     asm("fma.rn.bf16x2 %0, %0, %1, %2;" : "+r"(x) : "r"(s), "r"(off));
   } else {
@@ -611,7 +622,7 @@ __device__ __forceinline__ uint32_t two_values(uint32_t w, uint32_t s, uint32_t 
 }
 // 32 elements of a key: four words of codes, two scale bytes (the first in the low byte); pairs of neighbours in 16 words.
 template <int DT>
-__device__ __forceinline__ void unpack32(const uint4& codes, uint32_t scales, uint32_t (&out)[16]) {
+__device__ __forceinline__ void unpack32(const Unpack& u, const uint4& codes, uint32_t scales, uint32_t (&out)[16]) {
   const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
@@ -627,23 +638,35 @@ __device__ __forceinline__ void unpack32(const uint4& codes, uint32_t scales, ui
 #pragma unroll
     for (int q = 0; q < 2; ++q)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) out[8 * g + 4 * q + i] = two_values<DT>(w[2 * g + q] >> (4 * i), s, off);
+      for (int i = 0; i < 4; ++i) out[8 * g + 4 * q + i] = two_values<DT>(u, w[2 * g + q] >> (4 * i), s, off);
   }
 }
-// An unpacking warp's share of a block: keys 32 (first % 4) + lane of chunk first / 4, then each STEP on.
-template <int DT, int STEP>
-__device__ __forceinline__ void unpack_block(const uint8_t* raw, uint8_t* slot, int d, int first) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll 1
-  for (int i = first; i < d / 8; i += STEP) {
-    const int key = 32 * (i & 3) + lane, chunk = i >> 2;
-    const uint8_t* tile = raw + (key >> 3) * tile4_bytes(d);
+// A key's elements into its row of a block: boxes of 64 elements, rows of 128 bytes, 16-byte pieces swizzled.  `raw`: the block's codes.
+template <int DT, int HDP>
+__device__ __forceinline__ void unpack_key(const Unpack& u, const uint8_t* raw, uint8_t* slot, int d, int key) {
+  const uint8_t* tile = raw + (key >> 3) * tile4_bytes(d);
+  const uint8_t *codes = tile + codes4_at(0, key & 7), *scales = tile + scales4_at(d, 0, key & 7);
+  uint8_t* const row = slot + key * 128;
+  auto chunk = [&](int c) {
     uint32_t v[16];
-    unpack32<DT>(*reinterpret_cast<const uint4*>(tile + codes4_at(chunk, key & 7)), *reinterpret_cast<const uint16_t*>(tile + scales4_at(d, chunk, key & 7)), v);
-    uint8_t* row = slot + (chunk >> 1) * (BLK * 128) + key * 128;      // boxes of 64 elements, rows of 128 bytes, 16-byte pieces swizzled
+    unpack32<DT>(u, *reinterpret_cast<const uint4*>(codes + codes4_at(c, 0)), *reinterpret_cast<const uint16_t*>(scales + codes4_at(c, 0) / 8), v);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(row + (((4 * (chunk & 1) + q) ^ (key & 7)) << 4)) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<uint4*>(row + (c >> 1) * (BLK * 128) + (((q ^ (key & 7)) << 4) ^ ((c & 1) << 6))) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+  };
+  if (d == HDP) {
+#pragma unroll
+    for (int c = 0; c < HDP / 32; ++c) chunk(c);
+  } else {
+#pragma unroll 1
+    for (int c = 0; c < d / 32; ++c) chunk(c);
   }
+}
+// An unpacking warp's share of a block: a key a lane, 32 of every 32 WARPS.
+template <int DT, int HDP, int WARPS>
+__device__ __forceinline__ void unpack_block(const Unpack& u, const uint8_t* raw, uint8_t* slot, int d, int which) {
+#pragma unroll 1
+  for (int key = 32 * which + (threadIdx.x & 31); key < BLK; key += 32 * WARPS) unpack_key<DT, HDP>(u, raw, slot, d, key);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 // Heads that do not fill their box: the rest of its rows is zeros for good.
@@ -885,13 +908,14 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
     // ------------------------------------------------------------ unpackers
     Ring<SLOTS> kv;
     Ring<RAWS> raw;
+    const Unpack unpack(DT);
     if (p.d < HDP) { clear_padding<HDP>(smem_gen + F::KV_AT, SLOTS, p.d, threadIdx.x - F::FIXER * 32, F::UNPACK * 32); asm volatile("bar.sync 1, %0;" ::"n"(F::UNPACK * 32) : "memory"); }
     while (alive && next_item(it, alive)) {
       for (int i = 2 * (it.b1 - it.b0); i > 0; --i) {
         alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x2600u | kv.slot);
         if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x2680u | raw.slot);
         if (!alive) break;
-        unpack_block<DT, F::UNPACK>(smem_gen + F::RAW_AT + raw.slot * F::RAW, smem_gen + F::KV_AT + kv.slot * F::SLOT, p.d, warp - F::FIXER);
+        unpack_block<DT, HDP, F::UNPACK>(unpack, smem_gen + F::RAW_AT + raw.slot * F::RAW, smem_gen + F::KV_AT + kv.slot * F::SLOT, p.d, warp - F::FIXER);
         __syncwarp();
         if (lane == 0) { mbar_arrive(b_ready + 8 * kv.slot); mbar_arrive(b_raw_empty + 8 * raw.slot); }
         kv.step();
@@ -1325,13 +1349,14 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     // ------------------------------------------------------------ unpackers
     Ring<SLOTS> kv;
     Ring<RAWS> raw;
+    const Unpack unpack(DT);
     if (p.d < HDP) { clear_padding<HDP>(smem_gen, SLOTS, p.d, threadIdx.x - F::FIXER * 32, F::UNPACK * 32); asm volatile("bar.sync 1, %0;" ::"n"(F::UNPACK * 32) : "memory"); }
     while (alive && next_item(it, alive)) {
       for (int i = 2 * (it.b1 - it.b0); i > 0; --i) {
         alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x3600u | kv.slot);
         if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x3680u | raw.slot);
         if (!alive) break;
-        unpack_block<DT, F::UNPACK>(smem_gen + F::RAW_AT + raw.slot * F::RAW, smem_gen + kv.slot * F::SLOT, p.d, warp - F::FIXER);
+        unpack_block<DT, HDP, F::UNPACK>(unpack, smem_gen + F::RAW_AT + raw.slot * F::RAW, smem_gen + kv.slot * F::SLOT, p.d, warp - F::FIXER);
         __syncwarp();
         if (lane == 0) { mbar_arrive(b_ready + 8 * kv.slot); mbar_arrive(b_raw_empty + 8 * raw.slot); }
         kv.step();
@@ -1363,7 +1388,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     }
   } else {
     // ------------------------------------------------------------ softmax and output rows
-    constexpr int SH = ROWS == 8 ? 2 : ROWS == 16 ? 1 : 0;         // lane i looks after row i >> SH
+    constexpr int SH = ROWS == 4 ? 3 : ROWS == 8 ? 2 : ROWS == 16 ? 1 : 0;         // lane i looks after row i >> SH
     const int r = lane >> SH;
     const int my_tok = r / p.by_group;
     const uint32_t t_lane = tmem + (static_cast<uint32_t>(warp * 32) << 16);
@@ -1680,6 +1705,7 @@ template <int DT, bool FOUR>
 cudaError_t launch_any(int rows, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
   if (p.d <= 64) {
     switch (rows) {
+      case 4: if constexpr (FOUR) return launch_few<64, 4, DT, FOUR>(q, k, v, p, most, st);
       case 8: return launch_few<64, 8, DT, FOUR>(q, k, v, p, most, st);
       case 16: return launch_few<64, 16, DT, FOUR>(q, k, v, p, most, st);
       case 32: return launch_few<64, 32, DT, FOUR>(q, k, v, p, most, st);
@@ -1687,6 +1713,7 @@ cudaError_t launch_any(int rows, const CUtensorMap& q, const CUtensorMap& k, con
     return launch_wide<64, DT, FOUR>(q, k, v, p, most, st);
   }
   switch (rows) {
+    case 4: if constexpr (FOUR) return launch_few<128, 4, DT, FOUR>(q, k, v, p, most, st);
     case 8: return launch_few<128, 8, DT, FOUR>(q, k, v, p, most, st);
     case 16: return launch_few<128, 16, DT, FOUR>(q, k, v, p, most, st);
   }
@@ -1722,7 +1749,7 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
 
   const int64_t need = a.max_q * G;
   const int most_rows = d <= 64 ? 32 : 16;
-  const int rows = need <= 8 ? 8 : need <= 16 ? 16 : need <= most_rows ? most_rows : 128;
+  const int rows = four && need <= 4 ? 4 : need <= 8 ? 8 : need <= 16 ? 16 : need <= most_rows ? most_rows : 128;
   const bool narrow = rows < 128;
   p.tile_tokens = rows / G;
   int box = page & -page;                                  // the largest power of two that divides the page size: boxes never cross pages

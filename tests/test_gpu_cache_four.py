@@ -250,6 +250,7 @@ def test_captured_call_follows_the_lengths():
         rg.rg_kv_read_four(c.kh, c.vh, c.seqs, k_out, v_out)
 
     stream = torch.cuda.Stream()
+    torch.cuda.synchronize()                                    # the inputs are another stream's work
     with torch.cuda.stream(stream):
         step()
     torch.cuda.synchronize()

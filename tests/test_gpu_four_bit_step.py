@@ -40,6 +40,7 @@ def test_decode_steps_in_a_graph():
 
     lens.fill_(1)
     stream = torch.cuda.Stream()
+    torch.cuda.synchronize()                                    # the inputs are another stream's work
     with torch.cuda.stream(stream):
         step()
     torch.cuda.synchronize()

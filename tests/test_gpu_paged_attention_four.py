@@ -171,6 +171,7 @@ def test_captured_call_follows_lengths_and_pages():
     need = rg.rg_paged_attention_workspace_bytes(d, s, b.T, b.hq, b.d)
     ws, out = torch.empty(need, dtype=torch.uint8, device=DEV), torch.empty_like(b.Q)
     stream = torch.cuda.Stream()
+    torch.cuda.synchronize()                                    # the inputs are another stream's work
     with torch.cuda.stream(stream):
         rg.rg_paged_attention_four(d, b.Q, *b.c4, s, out, ws=ws)
     torch.cuda.synchronize()
