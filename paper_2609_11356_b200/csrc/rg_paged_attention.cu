@@ -641,32 +641,48 @@ __device__ __forceinline__ void unpack32(const Unpack& u, const uint4& codes, ui
       for (int i = 0; i < 4; ++i) out[8 * g + 4 * q + i] = two_values<DT>(u, w[2 * g + q] >> (4 * i), s, off);
   }
 }
-// A key's elements into its row of a block: boxes of 64 elements, rows of 128 bytes, 16-byte pieces swizzled.  `raw`: the block's codes.
-template <int DT, int HDP>
-__device__ __forceinline__ void unpack_key(const Unpack& u, const uint8_t* raw, uint8_t* slot, int d, int key) {
+// A key's elements, 32 at a time: `put` takes 16 words and the chunk's number.  `raw`: the block's codes.  WHOLE: heads of so many chunks unrolled.  The kernel for many
+// rows, where two warps unpack, has that (4096-row chunk 1067 us, 1120 as a loop); the one for few rows, where thirty warps run five different pieces of
+// code and wait for what does not fit the instruction caches, has a loop (64 single tokens 147 us, 182 unrolled).
+template <int DT, int WHOLE, typename Put>
+__device__ __forceinline__ void unpack_key(const Unpack& u, const uint8_t* raw, int d, int key, Put&& put) {
   const uint8_t* tile = raw + (key >> 3) * tile4_bytes(d);
   const uint8_t *codes = tile + codes4_at(0, key & 7), *scales = tile + scales4_at(d, 0, key & 7);
-  uint8_t* const row = slot + key * 128;
-  auto chunk = [&](int c) {
+  auto chunk = [&](const uint8_t* from, const uint8_t* scale, int c) {
     uint32_t v[16];
-    unpack32<DT>(u, *reinterpret_cast<const uint4*>(codes + codes4_at(c, 0)), *reinterpret_cast<const uint16_t*>(scales + codes4_at(c, 0) / 8), v);
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<uint4*>(row + (c >> 1) * (BLK * 128) + (((q ^ (key & 7)) << 4) ^ ((c & 1) << 6))) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    unpack32<DT>(u, *reinterpret_cast<const uint4*>(from), *reinterpret_cast<const uint16_t*>(scale), v);
+    put(v, c);
   };
-  if (d == HDP) {
+  if (WHOLE && d == 32 * WHOLE) {
 #pragma unroll
-    for (int c = 0; c < HDP / 32; ++c) chunk(c);
+    for (int c = 0; c < WHOLE; ++c) chunk(codes + codes4_at(c, 0), scales + codes4_at(c, 0) / 8, c);
   } else {
 #pragma unroll 1
-    for (int c = 0; c < d / 32; ++c) chunk(c);
+    for (int c = 0; c < d / 32; ++c, codes += codes4_at(1, 0), scales += codes4_at(1, 0) / 8) chunk(codes, scales, c);
   }
 }
+// ... into its row of a block: boxes of 64 elements, rows of 128 bytes, 16-byte pieces swizzled
+template <int DT, int WHOLE>
+__device__ __forceinline__ void unpack_key_to_row(const Unpack& u, const uint8_t* raw, uint8_t* slot, int d, int key) {
+  uint8_t* const row = slot + key * 128;
+  const uint32_t turn = (key & 7) << 4;
+  unpack_key<DT, WHOLE>(u, raw, d, key, [&](const uint32_t (&v)[16], int c) {
+    uint8_t* const box = row + (c >> 1) * (BLK * 128);
+    const uint32_t at = turn ^ ((c & 1) << 6);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(box + (at ^ (q << 4))) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+  });
+}
+// ... into its lane of tensor memory, two a column
+template <int DT>
+__device__ __forceinline__ void unpack_key_to_tmem(const Unpack& u, const uint8_t* raw, uint32_t taddr, int d, int key) {
+  unpack_key<DT, 0>(u, raw, d, key, [&](const uint32_t (&v)[16], int c) { pa_st16(taddr + 16u * c, v); });
+}
 // An unpacking warp's share of a block: a key a lane, 32 of every 32 WARPS.
-template <int DT, int HDP, int WARPS>
+template <int DT, int WHOLE, int WARPS>
 __device__ __forceinline__ void unpack_block(const Unpack& u, const uint8_t* raw, uint8_t* slot, int d, int which) {
 #pragma unroll 1
-  for (int key = 32 * which + (threadIdx.x & 31); key < BLK; key += 32 * WARPS) unpack_key<DT, HDP>(u, raw, slot, d, key);
+  for (int key = 32 * which + (threadIdx.x & 31); key < BLK; key += 32 * WARPS) unpack_key_to_row<DT, WHOLE>(u, raw, slot, d, key);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 // Heads that do not fill their box: the rest of its rows is zeros for good.
@@ -915,7 +931,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x2600u | kv.slot);
         if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x2680u | raw.slot);
         if (!alive) break;
-        unpack_block<DT, HDP, F::UNPACK>(unpack, smem_gen + F::RAW_AT + raw.slot * F::RAW, smem_gen + F::KV_AT + kv.slot * F::SLOT, p.d, warp - F::FIXER);
+        unpack_block<DT, HDP / 32, F::UNPACK>(unpack, smem_gen + F::RAW_AT + raw.slot * F::RAW, smem_gen + F::KV_AT + kv.slot * F::SLOT, p.d, warp - F::FIXER);
         __syncwarp();
         if (lane == 0) { mbar_arrive(b_ready + 8 * kv.slot); mbar_arrive(b_raw_empty + 8 * raw.slot); }
         kv.step();
@@ -1129,22 +1145,26 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
 // 5.8 TB/s; one of 8192 (34 MB): 13 us, of which the copies are 5 (launch, item and page look-up, the chain of two blocks and the join are latency).
 // With the queries as the 128 rows instead (the other form, 4 of them filled) the 64 sequences took 234 us on the device, and 278 with each row's keys dealt to
 // four warps: the tensor core then reads 128 mostly empty rows from shared memory for every step.
+// From a four-bit cache the keys go from registers straight into tensor memory, as the first product's first operand (its lanes are keys, as an unpacking warp's
+// are); only values pass through shared memory a second time.  Small items then fit an SM three times over.
 template <int HDP, int ROWS, bool FOUR>
 struct Few {
   static constexpr int DB = HDP / 64;
   static constexpr int PRODUCER = 4, MMA = 5, FIXER = 6, UNPACK = FOUR ? 4 : 0, WARPS = FOUR ? 10 : 7, THREADS = WARPS * 32;
+  static constexpr int CTAS = FOUR && ROWS == 4 ? 3 : 2;           // of an SM
   static constexpr int N = ROWS < 16 ? 16 : ROWS;                  // narrow side of the products
   static constexpr uint32_t Q_BOX = N * 128, P_BOX = N * 128, P_BUF = 2 * P_BOX;      // rows of 64 elements, 64 keys
   static constexpr uint32_t KV_BOX = BLK * 128, SLOT = DB * KV_BOX;
-  static constexpr int SLOTS = FOUR ? (HDP == 128 ? 2 : 4) : HDP == 128 ? 3 : 5;
+  static constexpr int SLOTS = FOUR ? (HDP == 64 ? 2 : CTAS == 3 ? 1 : 2) : HDP == 128 ? 3 : 5;
   static constexpr int RAWS = FOUR ? (HDP == 128 ? 3 : 5) : 0;     // blocks of codes
   static constexpr uint32_t RAW = BLK / 8 * tile4_bytes(HDP);
-  static constexpr uint32_t COLS = 128;                            // tensor memory: S' of even and odd blocks at 0 and 32, O' of even and odd items at 64 and 96
+  static constexpr uint32_t NC = FOUR ? N : 32;                    // tensor memory: S' of even and odd blocks at 0 and NC, O' of even and odd items at 2 NC and 3 NC, keys at 4 NC
+  static constexpr uint32_t COLS = !FOUR ? 128 : 4 * NC + HDP / 2 > 128 ? 256 : 128;
   static constexpr uint32_t RAW_AT = SLOTS * SLOT, Q_AT = RAW_AT + (RAWS * RAW + 1023) / 1024 * 1024, P_AT = Q_AT + DB * Q_BOX, ITEM_AT = P_AT + 2 * P_BUF, BAR_AT = ITEM_AT + ITEMS * sizeof(Item),
-                            N_BAR = 12 + 3 * SLOTS + 2 * ITEMS + 2 * RAWS, FLAG_AT = BAR_AT + 8 * N_BAR, MAX_AT = (FLAG_AT + 4 * (2 + FLAGS) + 15) & ~15u, SUM_AT = MAX_AT + 2 * 128 * 4,
+                            N_BAR = 12 + 3 * SLOTS + 2 * ITEMS + 2 * RAWS + 2, FLAG_AT = BAR_AT + 8 * N_BAR, MAX_AT = (FLAG_AT + 4 * (2 + FLAGS) + 15) & ~15u, SUM_AT = MAX_AT + 2 * 128 * 4,
                             LAST = SUM_AT + 2 * 128 * 4;
   static constexpr size_t SMEM = 1024 + LAST;
-  static_assert(SMEM <= 115712 && SLOTS / 2 + 1 < FLAGS, "two CTAs fit the SM; the fixer cannot be a whole turn of flags ahead");
+  static_assert(SMEM <= (CTAS == 3 ? 76800 : 115712) && COLS * CTAS <= 512 && SLOTS / 2 + 1 < FLAGS, "CTAS fit the SM; the fixer cannot be a whole turn of flags ahead");
 };
 
 // Butterfly over the warp's lanes for ROWS values a lane, lanes trading halves of what they still hold: lane i ends with the whole value of
@@ -1174,7 +1194,7 @@ __device__ __forceinline__ float reduce_rows(float (&v)[ROWS]) {
 }
 
 template <int HDP, int ROWS, int DT, bool FOUR>
-__global__ void __launch_bounds__(Few<HDP, ROWS, FOUR>::THREADS, 2)
+__global__ void __launch_bounds__(Few<HDP, ROWS, FOUR>::THREADS, Few<HDP, ROWS, FOUR>::CTAS)
 paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                            const __grid_constant__ Params p) {
   using F = Few<HDP, ROWS, FOUR>;
@@ -1188,7 +1208,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
   Item* items = reinterpret_cast<Item*>(smem_gen + F::ITEM_AT);
   const uint32_t bar0 = smem_base + F::BAR_AT;
   const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_x = bar0 + 16, b_y = bar0 + 24, b_s = bar0 + 32, b_p = bar0 + 48, b_pv = bar0 + 64, b_o_empty = bar0 + 80, b_full = bar0 + 96;   // two each from b_s to b_o_empty
-  const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS, b_raw = b_free + 8 * ITEMS, b_raw_empty = b_raw + 8 * RAWS;
+  const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS, b_raw = b_free + 8 * ITEMS, b_raw_empty = b_raw + 8 * RAWS, b_k_ready = b_raw_empty + 8 * RAWS, b_k_free = b_k_ready + 8;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + F::FLAG_AT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* not_finite = reinterpret_cast<volatile int*>(tmem_slot + 2);          // [FLAGS]
@@ -1202,6 +1222,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     for (int s = 0; s < SLOTS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_ready + 8 * s, FOUR ? F::UNPACK : 1); mbar_init(b_empty + 8 * s, 1); }
     for (int s = 0; s < ITEMS; ++s) { mbar_init(b_item + 8 * s, 1); mbar_init(b_free + 8 * s, F::WARPS - 1); }
     if (FOUR) for (int s = 0; s < F::RAWS; ++s) { mbar_init(b_raw + 8 * s, 1); mbar_init(b_raw_empty + 8 * s, F::UNPACK); }
+    if (FOUR) { mbar_init(b_k_ready, F::UNPACK); mbar_init(b_k_free, 1); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -1305,11 +1326,21 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     };
     // The scores of block number c go to columns 32 (c & 1): those of c - 2 have been read, since the product of c - 2 was issued.
     auto scores = [&](uint32_t c, uint32_t sK, uint32_t k_bar) {
+      if constexpr (FOUR) {                                        // keys in tensor memory: 16 elements are 8 columns; only those that the head has
+        alive = pa_wait(b_k_ready, c & 1, abort_flag, 0x3380u);
+        if (!alive) return;
+        pa_fence_after();
+#pragma unroll 1
+        for (int e = 0; e < HDP / 16; ++e)
+          if (leader && 16 * e < p.d) pa_mma_ts(tmem + F::NC * (c & 1), tmem + 4 * F::NC + 8u * e, pa_desc(sQ + (e >> 2) * F::Q_BOX, 16) + 2u * (e & 3), IDESC_S, e ? 1u : 0u);
+        if (leader) { pa_commit(b_s + 8 * (c & 1)); pa_commit(b_k_free); }
+        return;
+      }
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
         const uint64_t k = pa_desc(sK + b * F::KV_BOX, 16), q = pa_desc(sQ + b * F::Q_BOX, 16);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) if (leader) pa_mma_ss(tmem + 32u * (c & 1), k + 2u * e, q + 2u * e, IDESC_S, (b | e) ? 1u : 0u);
+        for (int e = 0; e < 4; ++e) if (leader) pa_mma_ss(tmem + F::NC * (c & 1), k + 2u * e, q + 2u * e, IDESC_S, (b | e) ? 1u : 0u);
       }
       if (leader) { pa_commit(b_s + 8 * (c & 1)); pa_commit(k_bar); }
     };
@@ -1319,16 +1350,19 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       alive = pa_wait(b_q_full, q_phase, abort_flag, 0x3400u);
       q_phase ^= 1u;
       if (!alive) break;
-      uint32_t bar, sK = next_slot(bar);
+      uint32_t bar = 0, sK = 0;
+      if (!FOUR) sK = next_slot(bar);
       if (!alive) break;
       scores(block, sK, bar);
+      if (!alive) break;
       if (nb == 1 && leader) pa_commit(b_q_empty);
-      const uint32_t t_o = tmem + 64u + 32u * (n_item & 1);
+      const uint32_t t_o = tmem + 2 * F::NC + F::NC * (n_item & 1);
       for (int j = 0; j < nb; ++j, ++block) {
         if (j + 1 < nb) {
-          sK = next_slot(bar);
+          if (!FOUR) sK = next_slot(bar);
           if (!alive) break;
           scores(block + 1, sK, bar);
+          if (!alive) break;
           if (j + 2 == nb && leader) pa_commit(b_q_empty);
         }
         const uint32_t sV = next_slot(bar);
@@ -1346,20 +1380,37 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       ++n_item;
     }
   } else if (FOUR && warp >= F::FIXER) {
-    // ------------------------------------------------------------ unpackers
+    // ------------------------------------------------------------ unpackers: K_0, K_1, V_0, K_2, V_1, ..., a key a lane
     Ring<SLOTS> kv;
     Ring<RAWS> raw;
     const Unpack unpack(DT);
-    if (p.d < HDP) { clear_padding<HDP>(smem_gen, SLOTS, p.d, threadIdx.x - F::FIXER * 32, F::UNPACK * 32); asm volatile("bar.sync 1, %0;" ::"n"(F::UNPACK * 32) : "memory"); }
+    const int key = 32 * (warp & 3) + lane;                        // the part of tensor memory that a warp reaches follows from its number
+    uint32_t block = 0;
     while (alive && next_item(it, alive)) {
-      for (int i = 2 * (it.b1 - it.b0); i > 0; --i) {
-        alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x3600u | kv.slot);
-        if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x3680u | raw.slot);
-        if (!alive) break;
-        unpack_block<DT, HDP, F::UNPACK>(unpack, smem_gen + F::RAW_AT + raw.slot * F::RAW, smem_gen + kv.slot * F::SLOT, p.d, warp - F::FIXER);
-        __syncwarp();
-        if (lane == 0) { mbar_arrive(b_ready + 8 * kv.slot); mbar_arrive(b_raw_empty + 8 * raw.slot); }
-        kv.step();
+      const int nb = it.b1 - it.b0;
+      for (int i = 0; i < 2 * nb; ++i) {
+        const uint8_t* const codes = smem_gen + F::RAW_AT + raw.slot * F::RAW;
+        if (i == 2 * nb - 1 || (i >= 2 && !(i & 1))) {
+          alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x3600u | kv.slot);
+          if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x3680u | raw.slot);
+          if (!alive) break;
+          unpack_key_to_row<DT, 0>(unpack, codes, smem_gen + kv.slot * F::SLOT, p.d, key);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) { mbar_arrive(b_ready + 8 * kv.slot); mbar_arrive(b_raw_empty + 8 * raw.slot); }
+          kv.step();
+        } else {
+          alive = pa_wait(b_k_free, (block & 1) ^ 1u, abort_flag, 0x3640u);
+          if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x36c0u | raw.slot);
+          if (!alive) break;
+          pa_fence_after();
+          unpack_key_to_tmem<DT>(unpack, codes, tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 4 * F::NC, p.d, key);
+          pa_wait_st();
+          pa_fence_before();
+          __syncwarp();
+          if (lane == 0) { mbar_arrive(b_k_ready); mbar_arrive(b_raw_empty + 8 * raw.slot); }
+          ++block;
+        }
         raw.step();
       }
     }
@@ -1400,7 +1451,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       const int32_t place = it.pos + my_tok;
       const int32_t hi = live ? min(last_seen(p, place, it.len), it.hi) : -1, lo = max(first_seen(p, place), it.lo);
       const bool blocks = it.b1 > it.b0;
-      const uint32_t t_o = t_lane + 64u + 32u * (n_item & 1);
+      const uint32_t t_o = t_lane + 2 * F::NC + F::NC * (n_item & 1);
       float m = -INFINITY, l = 0.0f;                               // of row r; l over this warp's keys
       bool any_masked = blocks && (masked_block(p, it, it.b0) || masked_block(p, it, it.b1 - 1));       // what is masked lies at the ends
       for (int b = it.b0; b < it.b1; ++b, ++block) {
@@ -1409,7 +1460,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         if (!alive) break;
         pa_fence_after();
         uint32_t s[ROWS];
-        pa_ld_cols<ROWS>(t_lane + 32u * buf, s);
+        pa_ld_cols<ROWS>(t_lane + F::NC * buf, s);
         const bool masked = masked_block(p, it, b);
         const int32_t key = b * BLK + warp * 32 + lane;
         if (masked) {
@@ -1699,7 +1750,7 @@ cudaError_t launch_wide(const CUtensorMap& q, const CUtensorMap& k, const CUtens
 template <int HDP, int ROWS, int DT, bool FOUR>
 cudaError_t launch_few(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
   static DeviceOnce configured;
-  return launch_form<Few<HDP, ROWS, FOUR>>(paged_attention_few_kernel<HDP, ROWS, DT, FOUR>, configured, 2, q, k, v, p, most, st);
+  return launch_form<Few<HDP, ROWS, FOUR>>(paged_attention_few_kernel<HDP, ROWS, DT, FOUR>, configured, Few<HDP, ROWS, FOUR>::CTAS, q, k, v, p, most, st);
 }
 template <int DT, bool FOUR>
 cudaError_t launch_any(int rows, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
