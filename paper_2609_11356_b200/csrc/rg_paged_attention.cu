@@ -716,7 +716,10 @@ template <int HDP, bool FOUR>
 struct Wide {
   static constexpr int DB = HDP / 64;                              // 64-column boxes of a head
   static constexpr int NT = 2, SOFT = 4 * NT;                      // tiles of 128 rows, softmax warps
-  static constexpr int PRODUCER = SOFT, MMA = SOFT + 1, FIXER = SOFT + 2, UNPACK = FOUR ? 2 : 0, WARPS = SOFT + (FOUR ? 4 : 3), THREADS = (SOFT + 4) * 32;   // without unpacking the last warp does nothing
+  static constexpr int PRODUCER = SOFT, MMA = SOFT + 1, FIXER = FOUR ? SOFT + 4 : SOFT + 2, UNPACK = FOUR ? 4 : 0, WARPS = SOFT + (FOUR ? 6 : 3), THREADS = (SOFT + (FOUR ? 8 : 4)) * 32;   // warps without a part do nothing
+  // A softmax thread holds a row's 128 scores: its warps take registers from the others.  At launch a thread has 168 (384 threads) or 128 (512): 2 * 216 + 72 = 3 * 168,
+  // 2 * 208 + 2 * 48 = 4 * 128.
+  static constexpr int SOFT_REGS = FOUR ? 208 : 216, OTHER_REGS = FOUR ? 48 : 72;
   static constexpr uint32_t Q_BOX = 128 * 128, Q_TILE = DB * Q_BOX;
   static constexpr uint32_t KV_BOX = BLK * 128, SLOT = DB * KV_BOX;
   static constexpr int SLOTS = FOUR ? (HDP == 128 ? 4 : 8) : HDP == 128 ? 5 : 10;
@@ -783,9 +786,8 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   };
   Item it;
   bool alive = true;
-  // A softmax thread holds a row's 128 scores: its warps take registers from the other four (168 a thread at launch: 2 * 216 + 72 = 3 * 168).
   if (warp >= F::SOFT) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::OTHER_REGS));
   if (warp == F::PRODUCER) {
     // ------------------------------------------------------------ producer
     const int pieces = BLK / p.box;                                // TMA boxes along the keys of a block
@@ -920,7 +922,8 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         }
       }
     }
-  } else if constexpr (FOUR) {
+  } else if (FOUR && warp >= F::FIXER) {
+    if constexpr (FOUR) {
     // ------------------------------------------------------------ unpackers
     Ring<SLOTS> kv;
     Ring<RAWS> raw;
@@ -938,7 +941,8 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         raw.step();
       }
     }
-  } else if (warp == F::FIXER) {
+    }
+  } else if (!FOUR && warp == F::FIXER) {
     // ------------------------------------------------------------ fixer
     Ring<SLOTS> kv;
     uint32_t flags = 0;
@@ -965,7 +969,7 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   }
   } else {
     // ------------------------------------------------------------ softmax and output rows
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::SOFT_REGS));
     const int t = warp >> 2;                                       // tile
     const int r = (warp & 3) * 32 + lane;                          // row of the tile, and its lane in tensor memory
     const uint32_t t_s = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 128u * t, t_o = t_s + 128u * NT;
