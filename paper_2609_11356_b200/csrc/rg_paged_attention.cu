@@ -1149,26 +1149,20 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
 // 5.8 TB/s; one of 8192 (34 MB): 13 us, of which the copies are 5 (launch, item and page look-up, the chain of two blocks and the join are latency).
 // With the queries as the 128 rows instead (the other form, 4 of them filled) the 64 sequences took 234 us on the device, and 278 with each row's keys dealt to
 // four warps: the tensor core then reads 128 mostly empty rows from shared memory for every step.
-// From a four-bit cache the keys go from registers straight into tensor memory, as the first product's first operand (its lanes are keys, as an unpacking warp's
-// are); only values pass through shared memory a second time.  Small items then fit an SM three times over.
-template <int HDP, int ROWS, bool FOUR>
+template <int HDP, int ROWS>
 struct Few {
   static constexpr int DB = HDP / 64;
-  static constexpr int PRODUCER = 4, MMA = 5, FIXER = 6, UNPACK = FOUR ? 4 : 0, WARPS = FOUR ? 10 : 7, THREADS = WARPS * 32;
-  static constexpr int CTAS = FOUR && ROWS == 4 ? 3 : 2;           // of an SM
+  static constexpr int PRODUCER = 4, MMA = 5, FIXER = 6, WARPS = 7, THREADS = WARPS * 32;
   static constexpr int N = ROWS < 16 ? 16 : ROWS;                  // narrow side of the products
   static constexpr uint32_t Q_BOX = N * 128, P_BOX = N * 128, P_BUF = 2 * P_BOX;      // rows of 64 elements, 64 keys
   static constexpr uint32_t KV_BOX = BLK * 128, SLOT = DB * KV_BOX;
-  static constexpr int SLOTS = FOUR ? (HDP == 64 ? 2 : CTAS == 3 ? 1 : 2) : HDP == 128 ? 3 : 5;
-  static constexpr int RAWS = FOUR ? (HDP == 128 ? 3 : 5) : 0;     // blocks of codes
-  static constexpr uint32_t RAW = BLK / 8 * tile4_bytes(HDP);
-  static constexpr uint32_t NC = FOUR ? N : 32;                    // tensor memory: S' of even and odd blocks at 0 and NC, O' of even and odd items at 2 NC and 3 NC, keys at 4 NC
-  static constexpr uint32_t COLS = !FOUR ? 128 : 4 * NC + HDP / 2 > 128 ? 256 : 128;
-  static constexpr uint32_t RAW_AT = SLOTS * SLOT, Q_AT = RAW_AT + (RAWS * RAW + 1023) / 1024 * 1024, P_AT = Q_AT + DB * Q_BOX, ITEM_AT = P_AT + 2 * P_BUF, BAR_AT = ITEM_AT + ITEMS * sizeof(Item),
-                            N_BAR = 12 + 3 * SLOTS + 2 * ITEMS + 2 * RAWS + 2, FLAG_AT = BAR_AT + 8 * N_BAR, MAX_AT = (FLAG_AT + 4 * (2 + FLAGS) + 15) & ~15u, SUM_AT = MAX_AT + 2 * 128 * 4,
+  static constexpr int SLOTS = HDP == 128 ? 3 : 5;
+  static constexpr uint32_t COLS = 128;                            // tensor memory: S' of even and odd blocks at 0 and 32, O' of even and odd items at 64 and 96
+  static constexpr uint32_t Q_AT = SLOTS * SLOT, P_AT = Q_AT + DB * Q_BOX, ITEM_AT = P_AT + 2 * P_BUF, BAR_AT = ITEM_AT + ITEMS * sizeof(Item),
+                            N_BAR = 12 + 3 * SLOTS + 2 * ITEMS, FLAG_AT = BAR_AT + 8 * N_BAR, MAX_AT = (FLAG_AT + 4 * (2 + FLAGS) + 15) & ~15u, SUM_AT = MAX_AT + 2 * 128 * 4,
                             LAST = SUM_AT + 2 * 128 * 4;
   static constexpr size_t SMEM = 1024 + LAST;
-  static_assert(SMEM <= (CTAS == 3 ? 76800 : 115712) && COLS * CTAS <= 512 && SLOTS / 2 + 1 < FLAGS, "CTAS fit the SM; the fixer cannot be a whole turn of flags ahead");
+  static_assert(SMEM <= 115712 && SLOTS / 2 + 1 < FLAGS, "two CTAs fit the SM; the fixer cannot be a whole turn of flags ahead");
 };
 
 // Butterfly over the warp's lanes for ROWS values a lane, lanes trading halves of what they still hold: lane i ends with the whole value of
@@ -1197,12 +1191,12 @@ __device__ __forceinline__ float reduce_rows(float (&v)[ROWS]) {
   return v[0];
 }
 
-template <int HDP, int ROWS, int DT, bool FOUR>
-__global__ void __launch_bounds__(Few<HDP, ROWS, FOUR>::THREADS, Few<HDP, ROWS, FOUR>::CTAS)
+template <int HDP, int ROWS, int DT>
+__global__ void __launch_bounds__(Few<HDP, ROWS>::THREADS, 2)
 paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                            const __grid_constant__ Params p) {
-  using F = Few<HDP, ROWS, FOUR>;
-  constexpr int DB = F::DB, SLOTS = F::SLOTS, RAWS = FOUR ? F::RAWS : 1;
+  using F = Few<HDP, ROWS>;
+  constexpr int DB = F::DB, SLOTS = F::SLOTS;
   constexpr uint32_t IDESC_S = pa_idesc(F::N, DT == RG_BF16, false, false), IDESC_O = pa_idesc(F::N, DT == RG_BF16, true, false);
 
   extern __shared__ uint8_t smem_raw[];
@@ -1212,7 +1206,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
   Item* items = reinterpret_cast<Item*>(smem_gen + F::ITEM_AT);
   const uint32_t bar0 = smem_base + F::BAR_AT;
   const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_x = bar0 + 16, b_y = bar0 + 24, b_s = bar0 + 32, b_p = bar0 + 48, b_pv = bar0 + 64, b_o_empty = bar0 + 80, b_full = bar0 + 96;   // two each from b_s to b_o_empty
-  const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS, b_raw = b_free + 8 * ITEMS, b_raw_empty = b_raw + 8 * RAWS, b_k_ready = b_raw_empty + 8 * RAWS, b_k_free = b_k_ready + 8;
+  const uint32_t b_ready = b_full + 8 * SLOTS, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + F::FLAG_AT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* not_finite = reinterpret_cast<volatile int*>(tmem_slot + 2);          // [FLAGS]
@@ -1223,10 +1217,8 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
   if (threadIdx.x == 0) {
     mbar_init(b_q_full, 1); mbar_init(b_q_empty, 1); mbar_init(b_x, 4); mbar_init(b_y, 4);
     for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 8 * t, 4); mbar_init(b_pv + 8 * t, 1); mbar_init(b_o_empty + 8 * t, 4); }
-    for (int s = 0; s < SLOTS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_ready + 8 * s, FOUR ? F::UNPACK : 1); mbar_init(b_empty + 8 * s, 1); }
+    for (int s = 0; s < SLOTS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_ready + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
     for (int s = 0; s < ITEMS; ++s) { mbar_init(b_item + 8 * s, 1); mbar_init(b_free + 8 * s, F::WARPS - 1); }
-    if (FOUR) for (int s = 0; s < F::RAWS; ++s) { mbar_init(b_raw + 8 * s, 1); mbar_init(b_raw_empty + 8 * s, F::UNPACK); }
-    if (FOUR) { mbar_init(b_k_ready, F::UNPACK); mbar_init(b_k_free, 1); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -1258,7 +1250,6 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     const int pieces = BLK / p.box;
     const int piece = lane & (pieces - 1), col = lane / pieces;
     Ring<SLOTS> kv;
-    Ring<RAWS> raw;
     uint32_t q_phase = 1;
     Walk walk;
     walk.start(p, p.tile_tokens);
@@ -1281,22 +1272,13 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       if (lane == 0) mbar_expect_tx(b_q_full, (uint32_t)(DB * p.tile_tokens * p.group) * 128u);
       __syncwarp();
       if (lane < DB) pa_tma_4d(sQ + lane * F::Q_BOX, &tmap_q, lane * 64, 0, it.tok, it.head, b_q_full);
-      auto copy = [&](bool is_v, int b, int32_t& id) {
-        const CUtensorMap* map = is_v ? &tmap_v : &tmap_k;
+      auto copy = [&](const CUtensorMap* map, int b, int32_t& id) {
         const bool mine = wanted(b);
         if (mine && (id < 0 || id >= p.pages)) {                   // not a page: the copy from behind the last one fills in zeros
           if (col == 0) atomicCAS(&g_paged_attn_page_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
           id = p.pages;
         }
         const int32_t key = b * BLK + piece * p.box, at = key - key / p.by_page * p.page_size;
-        if constexpr (FOUR) {
-          alive = pa_wait(b_raw_empty + 8 * raw.slot, raw.phase ^ 1u, abort_flag, 0x3200u | raw.slot);
-          if (!alive) return;
-          copy_codes(p, is_v ? p.v4 : p.k4, is_v ? p.v4_page : p.k4_page, is_v ? p.v4_head : p.k4_head, mine && col == 0, id, it.head, at, piece,
-                     smem_gen + F::RAW_AT + raw.slot * F::RAW, b_raw + 8 * raw.slot);
-          raw.step();
-          return;
-        }
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)p.box * 128u;
         alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x3200u | kv.slot);
         if (!alive) return;
@@ -1305,11 +1287,11 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         if (mine) pa_tma_4d(sKV + kv.slot * F::SLOT + col * F::KV_BOX + piece * p.box * 128, map, col * 64, at, it.head, id, b_full + 8 * kv.slot);
         kv.step();
       };
-      copy(false, it.b0, page);
+      copy(&tmap_k, it.b0, page);
       for (int b = it.b0; b < it.b1 && alive; ++b) {
         const int32_t later = wanted(b + 2) ? entry(b + 2) : 0;
-        if (b + 1 < it.b1) copy(false, b + 1, next);
-        if (alive) copy(true, b, page);
+        if (b + 1 < it.b1) copy(&tmap_k, b + 1, next);
+        if (alive) copy(&tmap_v, b, page);
         page = next;
         next = later;
       }
@@ -1322,7 +1304,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     auto next_slot = [&](uint32_t& bar) -> uint32_t {
       const uint32_t slot = __shfl_sync(0xffffffffu, kv.slot, 0);
       alive = pa_wait(b_ready + 8 * slot, kv.phase, abort_flag, 0x3300u | slot);
-      if (!FOUR && alive) alive = pa_wait(b_full + 8 * slot, kv.phase, abort_flag, 0x3380u | slot);
+      if (alive) alive = pa_wait(b_full + 8 * slot, kv.phase, abort_flag, 0x3380u | slot);
       pa_fence_after();
       bar = b_empty + 8 * slot;
       kv.step();
@@ -1330,21 +1312,11 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     };
     // The scores of block number c go to columns 32 (c & 1): those of c - 2 have been read, since the product of c - 2 was issued.
     auto scores = [&](uint32_t c, uint32_t sK, uint32_t k_bar) {
-      if constexpr (FOUR) {                                        // keys in tensor memory: 16 elements are 8 columns; only those that the head has
-        alive = pa_wait(b_k_ready, c & 1, abort_flag, 0x3380u);
-        if (!alive) return;
-        pa_fence_after();
-#pragma unroll 1
-        for (int e = 0; e < HDP / 16; ++e)
-          if (leader && 16 * e < p.d) pa_mma_ts(tmem + F::NC * (c & 1), tmem + 4 * F::NC + 8u * e, pa_desc(sQ + (e >> 2) * F::Q_BOX, 16) + 2u * (e & 3), IDESC_S, e ? 1u : 0u);
-        if (leader) { pa_commit(b_s + 8 * (c & 1)); pa_commit(b_k_free); }
-        return;
-      }
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
         const uint64_t k = pa_desc(sK + b * F::KV_BOX, 16), q = pa_desc(sQ + b * F::Q_BOX, 16);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) if (leader) pa_mma_ss(tmem + F::NC * (c & 1), k + 2u * e, q + 2u * e, IDESC_S, (b | e) ? 1u : 0u);
+        for (int e = 0; e < 4; ++e) if (leader) pa_mma_ss(tmem + 32u * (c & 1), k + 2u * e, q + 2u * e, IDESC_S, (b | e) ? 1u : 0u);
       }
       if (leader) { pa_commit(b_s + 8 * (c & 1)); pa_commit(k_bar); }
     };
@@ -1354,19 +1326,16 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       alive = pa_wait(b_q_full, q_phase, abort_flag, 0x3400u);
       q_phase ^= 1u;
       if (!alive) break;
-      uint32_t bar = 0, sK = 0;
-      if (!FOUR) sK = next_slot(bar);
+      uint32_t bar, sK = next_slot(bar);
       if (!alive) break;
       scores(block, sK, bar);
-      if (!alive) break;
       if (nb == 1 && leader) pa_commit(b_q_empty);
-      const uint32_t t_o = tmem + 2 * F::NC + F::NC * (n_item & 1);
+      const uint32_t t_o = tmem + 64u + 32u * (n_item & 1);
       for (int j = 0; j < nb; ++j, ++block) {
         if (j + 1 < nb) {
-          if (!FOUR) sK = next_slot(bar);
+          sK = next_slot(bar);
           if (!alive) break;
           scores(block + 1, sK, bar);
-          if (!alive) break;
           if (j + 2 == nb && leader) pa_commit(b_q_empty);
         }
         const uint32_t sV = next_slot(bar);
@@ -1383,42 +1352,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       }
       ++n_item;
     }
-  } else if (FOUR && warp >= F::FIXER) {
-    // ------------------------------------------------------------ unpackers: K_0, K_1, V_0, K_2, V_1, ..., a key a lane
-    Ring<SLOTS> kv;
-    Ring<RAWS> raw;
-    const Unpack unpack(DT);
-    const int key = 32 * (warp & 3) + lane;                        // the part of tensor memory that a warp reaches follows from its number
-    uint32_t block = 0;
-    while (alive && next_item(it, alive)) {
-      const int nb = it.b1 - it.b0;
-      for (int i = 0; i < 2 * nb; ++i) {
-        const uint8_t* const codes = smem_gen + F::RAW_AT + raw.slot * F::RAW;
-        if (i == 2 * nb - 1 || (i >= 2 && !(i & 1))) {
-          alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x3600u | kv.slot);
-          if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x3680u | raw.slot);
-          if (!alive) break;
-          unpack_key_to_row<DT, 0>(unpack, codes, smem_gen + kv.slot * F::SLOT, p.d, key);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) { mbar_arrive(b_ready + 8 * kv.slot); mbar_arrive(b_raw_empty + 8 * raw.slot); }
-          kv.step();
-        } else {
-          alive = pa_wait(b_k_free, (block & 1) ^ 1u, abort_flag, 0x3640u);
-          if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x36c0u | raw.slot);
-          if (!alive) break;
-          pa_fence_after();
-          unpack_key_to_tmem<DT>(unpack, codes, tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + 4 * F::NC, p.d, key);
-          pa_wait_st();
-          pa_fence_before();
-          __syncwarp();
-          if (lane == 0) { mbar_arrive(b_k_ready); mbar_arrive(b_raw_empty + 8 * raw.slot); }
-          ++block;
-        }
-        raw.step();
-      }
-    }
-  } else if (!FOUR && warp == F::FIXER) {
+  } else if (warp == F::FIXER) {
     // ------------------------------------------------------------ fixer
     Ring<SLOTS> kv;
     uint32_t flags = 0;
@@ -1443,7 +1377,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
     }
   } else {
     // ------------------------------------------------------------ softmax and output rows
-    constexpr int SH = ROWS == 4 ? 3 : ROWS == 8 ? 2 : ROWS == 16 ? 1 : 0;         // lane i looks after row i >> SH
+    constexpr int SH = ROWS == 8 ? 2 : ROWS == 16 ? 1 : 0;         // lane i looks after row i >> SH
     const int r = lane >> SH;
     const int my_tok = r / p.by_group;
     const uint32_t t_lane = tmem + (static_cast<uint32_t>(warp * 32) << 16);
@@ -1455,7 +1389,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
       const int32_t place = it.pos + my_tok;
       const int32_t hi = live ? min(last_seen(p, place, it.len), it.hi) : -1, lo = max(first_seen(p, place), it.lo);
       const bool blocks = it.b1 > it.b0;
-      const uint32_t t_o = t_lane + 2 * F::NC + F::NC * (n_item & 1);
+      const uint32_t t_o = t_lane + 64u + 32u * (n_item & 1);
       float m = -INFINITY, l = 0.0f;                               // of row r; l over this warp's keys
       bool any_masked = blocks && (masked_block(p, it, it.b0) || masked_block(p, it, it.b1 - 1));       // what is masked lies at the ends
       for (int b = it.b0; b < it.b1; ++b, ++block) {
@@ -1464,7 +1398,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         if (!alive) break;
         pa_fence_after();
         uint32_t s[ROWS];
-        pa_ld_cols<ROWS>(t_lane + F::NC * buf, s);
+        pa_ld_cols<ROWS>(t_lane + 32u * buf, s);
         const bool masked = masked_block(p, it, b);
         const int32_t key = b * BLK + warp * 32 + lane;
         if (masked) {
@@ -1536,7 +1470,7 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
         alive = pa_wait(b_pv + 8 * ((block - 1) & 1), ((block - 1) >> 1) & 1, abort_flag, 0x3780u);      // the last block's product
         if (!alive) break;
         pa_fence_after();
-        if (!FOUR) add_back = any_masked && not_finite[slot_flag] != 0;
+        add_back = any_masked && not_finite[slot_flag] != 0;
       }
       const bool none = !(sum > 0.0f) && sum == sum;               // no key seen
       const float inv = it.multi ? DOWN<DT> : none ? 0.0f : __frcp_rn(sum);
@@ -1571,11 +1505,370 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
           }
         }
         odd = __any_sync(0xffffffffu, odd);
-        if (!FOUR && (odd || add_back)) {
+        if (odd || add_back) {
           const int64_t token = (int64_t)it.tok + my_tok;
           const int h = it.head * p.group + r - my_tok * p.group;
           put_odd_values<DT>(p, it, odd, warp, some ? lo : INT32_MAX, hi, some && (lane & ((1 << SH) - 1)) == 0,
                              it.multi ? ((token * p.hq + h) * p.segments + it.seg) * p.d : token * p.o_tok + h * p.o_head);
+        }
+      }
+      if (warp == 0 && live && (lane & ((1 << SH) - 1)) == 0) {
+        const int64_t token = (int64_t)it.tok + my_tok;
+        const int h = it.head * p.group + r - my_tok * p.group;
+        if (it.multi) p.part_ml[(token * p.hq + h) * p.segments + it.seg] = make_float2(m, f_mul(sum, DOWN<DT>));
+        else if (p.lse) p.lse[token * p.lse_ld + h] = none ? -INFINITY : f_add(f_mul(m, p.scale), logf(f_mul(sum, DOWN<DT>)));
+      }
+      if (blocks) {
+        pa_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_o_empty + 8 * (n_item & 1));
+        ++n_item;
+      }
+    }
+  }
+
+  // ---------------------------------------------------------------- teardown
+  __syncthreads();
+  if (*abort_flag) {                                               // a wait gave up: let copies and products in flight end
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == F::MMA) {
+    pa_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(F::COLS) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------- few rows, four-bit caches
+// The same products and the same order of sums, so the same bits.  Keys go from the unpacking warps' registers straight into tensor memory, as the first
+// product's first operand (its lanes are keys, as those warps' lanes are): only values pass through shared memory a second time, and a CTA with up to four
+// rows fits an SM three times.
+// 64 sequences of up to 8192 keys, 8 key heads of 128 (0.32 GB): 145 us a call; with keys through shared memory too, so two CTAs an SM, 152.  What bounds it: instruction
+// issue (0.58 of the slots; half of the instructions unpack) and, of the rest, the chain of a block in a CTA.  Tried there: two blocks a turn for the
+// softmax warps 184 us (parts of four blocks leave too little to run ahead of), the next item's queries fetched ahead 153, unpacking unrolled 167-182.
+template <int HDP, int ROWS>
+struct Few4 {
+  static constexpr int DB = HDP / 64;
+  static constexpr int PRODUCER = 4, MMA = 5, UNPACK = 6, UNPACKERS = 4, WARPS = 10, THREADS = WARPS * 32;
+  static constexpr int CTAS = ROWS == 4 ? 3 : 2;                   // of an SM
+  static constexpr int N = ROWS < 16 ? 16 : ROWS;                  // narrow side of the products
+  // rows of 64 elements: where there are at most 8 the other eight that the product reads are the next box's, and nobody looks at what they give
+  static constexpr uint32_t BOX = ROWS <= 8 ? 1024 : N * 128, P_BUF = 2 * BOX;
+  static constexpr uint32_t V_BOX = BLK * 128, SLOT = DB * V_BOX;
+  static constexpr int SLOTS = HDP == 128 && CTAS == 3 ? 1 : 2;    // blocks of values
+  static constexpr int RAWS = HDP == 128 ? 3 : 5;                  // blocks of codes
+  static constexpr uint32_t RAW = BLK / 8 * tile4_bytes(HDP);
+  static constexpr uint32_t S_AT = 0, O_AT = 2 * N, K_AT = 4 * N, COLS = K_AT + HDP / 2 > 128 ? 256 : 128;      // tensor memory: two blocks' S', even and odd items' O', a block's keys
+  static constexpr uint32_t RAW_AT = SLOTS * SLOT, Q_AT = RAW_AT + (RAWS * RAW + 1023) / 1024 * 1024, P_AT = Q_AT + DB * BOX, ITEM_AT = P_AT + 2 * P_BUF + (ROWS <= 8 ? 1024 : 0),
+                            BAR_AT = ITEM_AT + ITEMS * sizeof(Item), N_BAR = 14 + 2 * SLOTS + 2 * ITEMS + 2 * RAWS, FLAG_AT = BAR_AT + 8 * N_BAR, MAX_AT = (FLAG_AT + 8 + 15) & ~15u,
+                            SUM_AT = MAX_AT + 2 * 128 * 4, LAST = SUM_AT + 2 * 128 * 4;
+  static constexpr size_t SMEM = 1024 + LAST;
+  static_assert(SMEM <= (CTAS == 3 ? 76800 : 115712) && COLS * CTAS <= 512, "CTAS of them fit the SM");
+};
+
+template <int HDP, int ROWS, int DT>
+__global__ void __launch_bounds__(Few4<HDP, ROWS>::THREADS, Few4<HDP, ROWS>::CTAS)
+paged_attention_few4_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ Params p) {
+  using F = Few4<HDP, ROWS>;
+  constexpr int DB = F::DB, SLOTS = F::SLOTS, RAWS = F::RAWS;
+  constexpr uint32_t IDESC_S = pa_idesc(F::N, DT == RG_BF16, false, false), IDESC_O = pa_idesc(F::N, DT == RG_BF16, true, false);
+
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
+  const uint32_t sV = smem_base, sQ = smem_base + F::Q_AT, sP = smem_base + F::P_AT;
+  Item* items = reinterpret_cast<Item*>(smem_gen + F::ITEM_AT);
+  const uint32_t bar0 = smem_base + F::BAR_AT;
+  const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_x = bar0 + 16, b_y = bar0 + 24, b_k_ready = bar0 + 32, b_k_free = bar0 + 40;
+  const uint32_t b_s = bar0 + 48, b_p = bar0 + 64, b_pv = bar0 + 80, b_o_empty = bar0 + 96;      // two each
+  const uint32_t b_ready = bar0 + 112, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS, b_raw = b_free + 8 * ITEMS, b_raw_empty = b_raw + 8 * RAWS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + F::FLAG_AT);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* xm = reinterpret_cast<float*>(smem_gen + F::MAX_AT);                          // [2][4][32]: the warps' maxima of a block, by its parity
+  float* xl = reinterpret_cast<float*>(smem_gen + F::SUM_AT);                          // [2][4][32]: their sums, by the item's parity
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(b_q_full, 1); mbar_init(b_q_empty, 1); mbar_init(b_x, 4); mbar_init(b_y, 4); mbar_init(b_k_ready, F::UNPACKERS); mbar_init(b_k_free, 1);
+    for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 8 * t, 4); mbar_init(b_pv + 8 * t, 1); mbar_init(b_o_empty + 8 * t, 4); }
+    for (int s = 0; s < SLOTS; ++s) { mbar_init(b_ready + 8 * s, F::UNPACKERS); mbar_init(b_empty + 8 * s, 1); }
+    for (int s = 0; s < ITEMS; ++s) { mbar_init(b_item + 8 * s, 1); mbar_init(b_free + 8 * s, F::WARPS - 1); }
+    for (int s = 0; s < RAWS; ++s) { mbar_init(b_raw + 8 * s, 1); mbar_init(b_raw_empty + 8 * s, F::UNPACKERS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == F::MMA) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(F::COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pa_fence_before();
+  __syncthreads();
+  pa_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");               // the set-up ran under the tail of the kernel in front; from here on its results are read
+  if (p.segments > 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  Ring<ITEMS> ir;
+  auto next_item = [&](Item& it, bool& alive) -> bool {
+    if (!pa_wait(b_item + 8 * ir.slot, ir.phase, abort_flag, 0x5000u)) { alive = false; return false; }
+    it = items[ir.slot];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(b_free + 8 * ir.slot);
+    ir.step();
+    return it.n_tok > 0;
+  };
+  Item it;
+  bool alive = true;
+
+  if (warp == F::PRODUCER) {
+    // ------------------------------------------------------------ producer: K_0, K_1, V_0, K_2, V_1, ..., as they are used
+    const int pieces = BLK / p.box, piece = lane & (pieces - 1);
+    Ring<RAWS> raw;
+    uint32_t q_phase = 1;
+    Walk walk;
+    walk.start(p, p.tile_tokens);
+    while (alive) {
+      const bool more = walk.get(p, p.tile_tokens, it);
+      if (!more) it.n_tok = 0;
+      alive = pa_wait(b_free + 8 * ir.slot, ir.phase ^ 1u, abort_flag, 0x5080u);
+      if (!alive) break;
+      if (lane == 0) { items[ir.slot] = it; mbar_arrive(b_item + 8 * ir.slot); }
+      ir.step();
+      if (!more) break;
+      if (it.b1 == it.b0) continue;
+      const int32_t* row = p.table + (int64_t)it.seq * p.table_ld;
+      // a lane's page of block b, looked up a block ahead of its first use and kept for its second
+      auto wanted = [&](int b) -> bool { const int32_t k = b * BLK + piece * p.box; return lane < pieces && b < it.b1 && k <= it.hi && k + p.box > it.lo; };
+      auto entry = [&](int b) -> int32_t { return wanted(b) ? row[(b * BLK + piece * p.box) / p.by_page] : 0; };
+      int32_t page = entry(it.b0), next = entry(it.b0 + 1);
+      alive = pa_wait(b_q_empty, q_phase, abort_flag, 0x5100u);
+      if (!alive) break;
+      q_phase ^= 1u;
+      if (lane == 0) mbar_expect_tx(b_q_full, (uint32_t)(DB * p.tile_tokens * p.group) * 128u);
+      __syncwarp();
+      if (lane < DB) pa_tma_4d(sQ + lane * F::BOX, &tmap_q, lane * 64, 0, it.tok, it.head, b_q_full);
+      auto copy = [&](bool is_v, int b, int32_t& id) {
+        const bool mine = wanted(b);
+        if (mine && (id < 0 || id >= p.pages)) {                   // not a page: zeros
+          atomicCAS(&g_paged_attn_page_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
+          id = p.pages;
+        }
+        const int32_t key = b * BLK + piece * p.box, at = key - key / p.by_page * p.page_size;
+        alive = pa_wait(b_raw_empty + 8 * raw.slot, raw.phase ^ 1u, abort_flag, 0x5200u | raw.slot);
+        if (!alive) return;
+        copy_codes(p, is_v ? p.v4 : p.k4, is_v ? p.v4_page : p.k4_page, is_v ? p.v4_head : p.k4_head, mine, id, it.head, at, piece, smem_gen + F::RAW_AT + raw.slot * F::RAW, b_raw + 8 * raw.slot);
+        raw.step();
+      };
+      copy(false, it.b0, page);
+      for (int b = it.b0; b < it.b1 && alive; ++b) {
+        const int32_t later = entry(b + 2);
+        if (b + 1 < it.b1) copy(false, b + 1, next);
+        if (alive) copy(true, b, page);
+        page = next;
+        next = later;
+      }
+    }
+  } else if (warp == F::MMA) {
+    // ------------------------------------------------------------ MMA issuer
+    const bool leader = elect_one();
+    Ring<SLOTS> kv;
+    uint32_t q_phase = 0, block = 0, n_item = 0;
+    // The scores of block number c go to columns N (c & 1): those of c - 2 have been read, since the product of c - 2 was issued.
+    auto scores = [&](uint32_t c) {
+      alive = pa_wait(b_k_ready, c & 1, abort_flag, 0x5340u);
+      if (!alive) return;
+      pa_fence_after();
+      // 16 elements of the keys are 8 columns; only those that the head has
+#pragma unroll 1
+      for (int e = 0; 16 * e < p.d; ++e)
+        if (leader) pa_mma_ts(tmem + F::S_AT + F::N * (c & 1), tmem + F::K_AT + 8u * e, pa_desc(sQ + (e >> 2) * F::BOX, 16) + 2u * (e & 3), IDESC_S, e ? 1u : 0u);
+      if (leader) { pa_commit(b_s + 8 * (c & 1)); pa_commit(b_k_free); }
+    };
+    while (alive && next_item(it, alive)) {
+      const int nb = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
+      if (nb == 0) continue;
+      alive = pa_wait(b_q_full, q_phase, abort_flag, 0x5400u);
+      q_phase ^= 1u;
+      if (!alive) break;
+      scores(block);
+      if (!alive) break;
+      if (nb == 1 && leader) pa_commit(b_q_empty);
+      const uint32_t t_o = tmem + F::O_AT + F::N * (n_item & 1);
+      for (int j = 0; j < nb; ++j, ++block) {
+        if (j + 1 < nb) {
+          scores(block + 1);
+          if (!alive) break;
+          if (j + 2 == nb && leader) pa_commit(b_q_empty);
+        }
+        const uint32_t slot = __shfl_sync(0xffffffffu, kv.slot, 0);
+        alive = pa_wait(b_ready + 8 * slot, kv.phase, abort_flag, 0x5380u | slot);
+        kv.step();
+        if (alive) alive = pa_wait(b_p + 8 * (block & 1), (block >> 1) & 1, abort_flag, 0x5500u);
+        if (alive && j == 0) alive = pa_wait(b_o_empty + 8 * (n_item & 1), ((n_item >> 1) & 1) ^ 1u, abort_flag, 0x5580u);
+        if (!alive) break;
+        pa_fence_after();
+        // heads of up to 64 elements: the upper 64 lanes repeat the lower ones (distance 0 between the column groups), nobody reads them
+        const uint64_t v = pa_desc(__shfl_sync(0xffffffffu, sV + slot * F::SLOT, 0), HDP == 128 ? F::V_BOX : 0);
+        const uint64_t pr = pa_desc(__shfl_sync(0xffffffffu, sP + (block & 1) * F::P_BUF, 0), 16);
+#pragma unroll 1
+        for (int e = 0; e < BLK / 16; ++e)
+          if (leader) pa_mma_ss(t_o, v + (uint64_t)(e * (2048 >> 4)), pr + (uint64_t)((e >> 2) * (F::BOX >> 4) + 2 * (e & 3)), IDESC_O, (j | e) ? 1u : 0u);
+        if (leader) { pa_commit(b_pv + 8 * (block & 1)); pa_commit(b_empty + 8 * slot); }
+      }
+      ++n_item;
+    }
+  } else if (warp >= F::UNPACK) {
+    // ------------------------------------------------------------ unpackers, in the producer's order; a key a lane
+    Ring<SLOTS> kv;
+    Ring<RAWS> raw;
+    const Unpack unpack(DT);
+    const int key = 32 * (warp & 3) + lane;                        // the part of tensor memory that a warp reaches follows from its number
+    const uint32_t t_k = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + F::K_AT;
+    uint32_t block = 0;
+    while (alive && next_item(it, alive)) {
+      const int nb = it.b1 - it.b0;
+#pragma unroll 1
+      for (int i = 0; i < 2 * nb; ++i) {
+        const bool is_v = i == 2 * nb - 1 || (i >= 2 && !(i & 1));
+        if (is_v) alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x5600u | kv.slot);
+        else alive = pa_wait(b_k_free, (block & 1) ^ 1u, abort_flag, 0x5640u);
+        if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x5680u | raw.slot);
+        if (!alive) break;
+        const uint8_t* const codes = smem_gen + F::RAW_AT + raw.slot * F::RAW;
+        if (is_v) {
+          unpack_key_to_row<DT, 0>(unpack, codes, smem_gen + kv.slot * F::SLOT, p.d, key);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        } else {
+          pa_fence_after();
+          unpack_key_to_tmem<DT>(unpack, codes, t_k, p.d, key);
+          pa_wait_st();
+          pa_fence_before();
+          ++block;
+        }
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(is_v ? b_ready + 8 * kv.slot : b_k_ready); mbar_arrive(b_raw_empty + 8 * raw.slot); }
+        if (is_v) kv.step();
+        raw.step();
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ softmax and output rows
+    constexpr int SH = ROWS == 4 ? 3 : ROWS == 8 ? 2 : ROWS == 16 ? 1 : 0;         // lane i looks after row i >> SH
+    const int r = lane >> SH;
+    const int my_tok = r / p.by_group;
+    const uint32_t t_lane = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+    uint32_t block = 0, n_item = 0;
+    uint8_t* const p_row = smem_gen + F::P_AT + (warp >> 1) * F::BOX + (lane & 7) * 2;     // this key's place in the rows of P: 16-byte pieces of 8 keys, swizzled
+    const int p_piece = (warp & 1) * 4 + (lane >> 3);
+    while (alive && next_item(it, alive)) {
+      const bool live = my_tok < it.n_tok && my_tok < p.tile_tokens;
+      const int32_t place = it.pos + my_tok;
+      const int32_t hi = live ? min(last_seen(p, place, it.len), it.hi) : -1, lo = max(first_seen(p, place), it.lo);
+      const bool blocks = it.b1 > it.b0;
+      const uint32_t t_o = t_lane + F::O_AT + F::N * (n_item & 1);
+      float m = -INFINITY, l = 0.0f;                               // of row r; l over this warp's keys
+      for (int b = it.b0; b < it.b1; ++b, ++block) {
+        const uint32_t buf = block & 1, phase = (block >> 1) & 1;
+        alive = pa_wait(b_s + 8 * buf, phase, abort_flag, 0x5700u);
+        if (!alive) break;
+        pa_fence_after();
+        uint32_t s[ROWS];
+        pa_ld_cols<ROWS>(t_lane + F::S_AT + F::N * buf, s);
+        if (masked_block(p, it, b)) {
+          const int32_t at = b * BLK + warp * 32 + lane;
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) {
+            const int32_t from = __shfl_sync(0xffffffffu, lo, i << SH), to = __shfl_sync(0xffffffffu, hi, i << SH);
+            s[i] = at >= from && at <= to ? s[i] : 0xff800000u;
+          }
+        }
+        float v[ROWS];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) v[i] = __uint_as_float(s[i]);
+        float* x = xm + buf * 128;                                 // a warp is at most one block ahead of another
+        x[warp * 32 + lane] = reduce_rows<ROWS, true>(v);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_x);
+        alive = pa_wait(b_x, block & 1, abort_flag, 0x5740u);
+        if (!alive) break;
+        const float mb = max3(max3(x[lane], x[32 + lane], x[64 + lane]), x[96 + lane], x[96 + lane]);
+        const float alpha = rises(m, mb, p.c) ? move_max(m, mb, p.c) : 1.0f;
+        float shift, off;
+        if (__any_sync(0xffffffffu, shift_of<DT>(m, p.c, shift, off))) {
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) s[i] = __float_as_uint(f_add(__uint_as_float(s[i]), -__shfl_sync(0xffffffffu, off, i << SH)));
+        }
+        uint8_t* const row = p_row + buf * F::P_BUF;
+#pragma unroll
+        for (int i = 0; i < ROWS; i += 2) {
+          const float s0 = __shfl_sync(0xffffffffu, shift, i << SH), s1 = __shfl_sync(0xffffffffu, shift, (i + 1) << SH);
+          const float2 sc = make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+          const float2 eh = prob2<false>(sc, p.c, s0, s1), ep = prob2<true>(sc, p.c, s0, s1);
+          const float2 e = lane >= POLY_FROM ? ep : eh;
+          v[i] = e.x; v[i + 1] = e.y;
+          const uint32_t w = pack_16x2(e.x, e.y, DT);
+          *reinterpret_cast<uint16_t*>(row + i * 128 + ((p_piece ^ (i & 7)) << 4)) = (uint16_t)(w & 0xffffu);
+          *reinterpret_cast<uint16_t*>(row + (i + 1) * 128 + ((p_piece ^ ((i + 1) & 7)) << 4)) = (uint16_t)(w >> 16);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        if (b > it.b0 && __any_sync(0xffffffffu, live && alpha != 1.0f)) {
+          // O' takes the factor once the product of the block before is complete; the one of this block waits for this warp
+          alive = pa_wait(b_pv + 8 * (buf ^ 1), ((block - 1) >> 1) & 1, abort_flag, 0x5780u);
+          if (!alive) break;
+          pa_fence_after();
+          uint32_t o[ROWS];
+          pa_ld_cols<ROWS>(t_o, o);
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) o[i] = __float_as_uint(f_mul(__uint_as_float(o[i]), __shfl_sync(0xffffffffu, alpha, i << SH)));
+          pa_st_cols<ROWS>(t_o, o);
+          pa_wait_st();
+        }
+        pa_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_p + 8 * buf);
+        l = add_quarter(l, alpha, reduce_rows<ROWS, false>(v), m, mb);
+      }
+      if (!alive) break;
+      float sum = 0.0f;
+      if (blocks) {
+        float* x = xl + (n_item & 1) * 128;
+        x[warp * 32 + lane] = l;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_y);
+        alive = pa_wait(b_y, n_item & 1, abort_flag, 0x57c0u);
+        if (!alive) break;
+        sum = join_quarters(x[lane], x[32 + lane], x[64 + lane], x[96 + lane]);
+        alive = pa_wait(b_pv + 8 * ((block - 1) & 1), ((block - 1) >> 1) & 1, abort_flag, 0x5800u);      // the last block's product
+        if (!alive) break;
+        pa_fence_after();
+      }
+      const bool none = !(sum > 0.0f) && sum == sum;               // no key seen
+      const float inv = it.multi ? DOWN<DT> : none ? 0.0f : __frcp_rn(sum);
+      const int col = warp * 32 + lane;                            // element of the head
+      const int n_rows = it.n_tok * p.group;
+      if (warp * 32 < p.d) {
+        uint32_t raw[ROWS];
+        if (blocks) pa_ld_cols<ROWS>(t_o, raw);
+        float o[ROWS];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+          const bool zero = __shfl_sync(0xffffffffu, (int)none, i << SH) || !blocks;
+          const float f = __shfl_sync(0xffffffffu, inv, i << SH);
+          o[i] = zero ? 0.0f : f_mul(__uint_as_float(raw[i]), f);
+        }
+        if (col < p.d) {
+          int tok = 0, head = 0;
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) {
+            if (i < n_rows) {
+              const int64_t token = (int64_t)it.tok + tok;
+              const int h = it.head * p.group + head;
+              if (it.multi) p.part_o[((token * p.hq + h) * p.segments + it.seg) * p.d + col] = o[i];
+              else store_scalar(p.out, p.o_dtype, token * p.o_tok + h * p.o_head + col, o[i]);
+              if (++head == p.group) { head = 0; ++tok; }
+            }
+          }
         }
       }
       if (warp == 0 && live && (lane & ((1 << SH) - 1)) == 0) {
@@ -1725,9 +2018,8 @@ cudaError_t launch_join(const Params& p, cudaStream_t st) {
 }
 
 // ---------------------------------------------------------------- host
-template <typename F, typename Kernel>
-cudaError_t launch_form(Kernel kernel, DeviceOnce& configured, int ctas_per_sm, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most,
-                        cudaStream_t st) {
+template <typename F, typename Kernel, typename... Args>
+cudaError_t launch_form(Kernel kernel, DeviceOnce& configured, int ctas_per_sm, int64_t most, cudaStream_t st, const Args&... args) {
   const DeviceInfo dev = current_device();
   if (!configured.has(dev.dev)) {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::SMEM);
@@ -1744,35 +2036,30 @@ cudaError_t launch_form(Kernel kernel, DeviceOnce& configured, int ctas_per_sm, 
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, q, k, v, p);
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 template <int HDP, int DT, bool FOUR>
 cudaError_t launch_wide(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
   static DeviceOnce configured;
-  return launch_form<Wide<HDP, FOUR>>(paged_attention_wide_kernel<HDP, DT, FOUR>, configured, 1, q, k, v, p, most, st);
+  return launch_form<Wide<HDP, FOUR>>(paged_attention_wide_kernel<HDP, DT, FOUR>, configured, 1, most, st, q, k, v, p);
 }
 template <int HDP, int ROWS, int DT, bool FOUR>
 cudaError_t launch_few(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
   static DeviceOnce configured;
-  return launch_form<Few<HDP, ROWS, FOUR>>(paged_attention_few_kernel<HDP, ROWS, DT, FOUR>, configured, Few<HDP, ROWS, FOUR>::CTAS, q, k, v, p, most, st);
+  if constexpr (FOUR) return launch_form<Few4<HDP, ROWS>>(paged_attention_few4_kernel<HDP, ROWS, DT>, configured, Few4<HDP, ROWS>::CTAS, most, st, q, p);
+  else return launch_form<Few<HDP, ROWS>>(paged_attention_few_kernel<HDP, ROWS, DT>, configured, 2, most, st, q, k, v, p);
+}
+template <int HDP, int DT, bool FOUR>
+cudaError_t launch_head(int rows, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
+  if constexpr (FOUR) { if (rows == 4) return launch_few<HDP, 4, DT, FOUR>(q, k, v, p, most, st); }
+  if constexpr (HDP == 64) { if (rows == 32) return launch_few<64, 32, DT, FOUR>(q, k, v, p, most, st); }
+  if (rows == 8) return launch_few<HDP, 8, DT, FOUR>(q, k, v, p, most, st);
+  if (rows == 16) return launch_few<HDP, 16, DT, FOUR>(q, k, v, p, most, st);
+  return launch_wide<HDP, DT, FOUR>(q, k, v, p, most, st);
 }
 template <int DT, bool FOUR>
 cudaError_t launch_any(int rows, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
-  if (p.d <= 64) {
-    switch (rows) {
-      case 4: if constexpr (FOUR) return launch_few<64, 4, DT, FOUR>(q, k, v, p, most, st);
-      case 8: return launch_few<64, 8, DT, FOUR>(q, k, v, p, most, st);
-      case 16: return launch_few<64, 16, DT, FOUR>(q, k, v, p, most, st);
-      case 32: return launch_few<64, 32, DT, FOUR>(q, k, v, p, most, st);
-    }
-    return launch_wide<64, DT, FOUR>(q, k, v, p, most, st);
-  }
-  switch (rows) {
-    case 4: if constexpr (FOUR) return launch_few<128, 4, DT, FOUR>(q, k, v, p, most, st);
-    case 8: return launch_few<128, 8, DT, FOUR>(q, k, v, p, most, st);
-    case 16: return launch_few<128, 16, DT, FOUR>(q, k, v, p, most, st);
-  }
-  return launch_wide<128, DT, FOUR>(q, k, v, p, most, st);
+  return p.d <= 64 ? launch_head<64, DT, FOUR>(rows, q, k, v, p, most, st) : launch_head<128, DT, FOUR>(rows, q, k, v, p, most, st);
 }
 
 }  // namespace
