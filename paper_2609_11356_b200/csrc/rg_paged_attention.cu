@@ -661,28 +661,18 @@ __device__ __forceinline__ void unpack_key(const Unpack& u, const uint8_t* raw, 
     for (int c = 0; c < d / 32; ++c, codes += codes4_at(1, 0), scales += codes4_at(1, 0) / 8) chunk(codes, scales, c);
   }
 }
-// ... into its row of a block: boxes of 64 elements, rows of 128 bytes, 16-byte pieces swizzled
-template <int DT, int WHOLE>
-__device__ __forceinline__ void unpack_key_to_row(const Unpack& u, const uint8_t* raw, uint8_t* slot, int d, int key) {
-  uint8_t* const row = slot + key * 128;
-  const uint32_t turn = (key & 7) << 4;
-  unpack_key<DT, WHOLE>(u, raw, d, key, [&](const uint32_t (&v)[16], int c) {
-    uint8_t* const box = row + (c >> 1) * (BLK * 128);
-    const uint32_t at = turn ^ ((c & 1) << 6);
+// A chunk's place in a key's row of a block: boxes of 64 elements, rows of 128 bytes, 16-byte pieces swizzled.
+__device__ __forceinline__ void store_to_row(const uint32_t (&v)[16], uint8_t* slot, int key, int c) {
+  uint8_t* const box = slot + (c >> 1) * (BLK * 128) + key * 128;
+  const uint32_t at = ((key & 7) << 4) ^ ((c & 1) << 6);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(box + (at ^ (q << 4))) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-  });
-}
-// ... into its lane of tensor memory, two a column
-template <int DT>
-__device__ __forceinline__ void unpack_key_to_tmem(const Unpack& u, const uint8_t* raw, uint32_t taddr, int d, int key) {
-  unpack_key<DT, 0>(u, raw, d, key, [&](const uint32_t (&v)[16], int c) { pa_st16(taddr + 16u * c, v); });
+  for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(box + (at ^ (q << 4))) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
 }
 // An unpacking warp's share of a block: a key a lane, 32 of every 32 WARPS.
 template <int DT, int WHOLE, int WARPS>
 __device__ __forceinline__ void unpack_block(const Unpack& u, const uint8_t* raw, uint8_t* slot, int d, int which) {
 #pragma unroll 1
-  for (int key = 32 * which + (threadIdx.x & 31); key < BLK; key += 32 * WARPS) unpack_key_to_row<DT, WHOLE>(u, raw, slot, d, key);
+  for (int key = 32 * which + (threadIdx.x & 31); key < BLK; key += 32 * WARPS) unpack_key<DT, WHOLE>(u, raw, d, key, [&](const uint32_t (&v)[16], int c) { store_to_row(v, slot, key, c); });
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 // Heads that do not fill their box: the rest of its rows is zeros for good.
@@ -1736,12 +1726,15 @@ paged_attention_few4_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x5680u | raw.slot);
         if (!alive) break;
         const uint8_t* const codes = smem_gen + F::RAW_AT + raw.slot * F::RAW;
+        if (!is_v) pa_fence_after();
+        uint8_t* const to = smem_gen + kv.slot * F::SLOT;
+        unpack_key<DT, 0>(unpack, codes, p.d, key, [&](const uint32_t (&v)[16], int c) {
+          if (is_v) store_to_row(v, to, key, c);
+          else pa_st16(t_k + 16u * c, v);                          // two elements a column
+        });
         if (is_v) {
-          unpack_key_to_row<DT, 0>(unpack, codes, smem_gen + kv.slot * F::SLOT, p.d, key);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         } else {
-          pa_fence_after();
-          unpack_key_to_tmem<DT>(unpack, codes, t_k, p.d, key);
           pa_wait_st();
           pa_fence_before();
           ++block;
