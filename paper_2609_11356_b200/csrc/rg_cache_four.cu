@@ -3,7 +3,7 @@
 //
 // Keys are rotated in 64 bits (the pair's sine and cosine as well): a code is a step function, and an fp32 rotation, whose result is off by 2^-22 or
 // so, would put one key in some hundred thousand on the other side of a border between codes; even a 64-bit one rounded to fp32 does so for one in ten
-// million.  Codes are chosen in fp32; a group in which that is close (one in 30000) is done again in 64 bits.  Queries are rotated as rg_rope does it, with its bits.
+// million.  Codes are chosen in fp32; a group in which that is close (one in 4000) is done again in 64 bits.  Queries are rotated as rg_rope does it, with its bits.
 //
 // What bounds it: bytes for prompts, latency for single tokens.  A thread takes one group of 16 elements of one row (query, key or value) and the group
 // that the rotation pairs with it: 32-byte loads, no exchange between threads, and a key's 8 code bytes and its scale byte are a thread's own.
@@ -28,27 +28,33 @@ constexpr int TOKENS = THREADS / 32;                   // most tokens of a CTA: 
 template <int DT>
 using Elem = typename std::conditional<DT == RG_F32, float, uint16_t>::type;
 
-// 16 elements from `src` on as fp32
+// Eight elements as they lie in memory, and as fp32.
 template <int DT>
-__device__ __forceinline__ void load16(const Elem<DT>* src, bool vec, float (&v)[16]) {
+struct Eight { uint4 w[DT == RG_F32 ? 2 : 1]; };
+template <int DT>
+__device__ __forceinline__ Eight<DT> load8(const Elem<DT>* src, bool vec) {
+  Eight<DT> r;
   if (vec) {
-    constexpr int WORDS = DT == RG_F32 ? 16 : 8;
-    uint32_t w[WORDS];
 #pragma unroll
-    for (int i = 0; i < WORDS / 4; ++i) {
-      const uint4 x = *(reinterpret_cast<const uint4*>(src) + i);
-      w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if constexpr (DT == RG_F32) v[i] = __uint_as_float(w[i]);
-      else { const uint32_t h = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu; v[i] = DT == RG_F16 ? f16_bits_to_f32(h) : bf16_bits_to_f32(h); }
-    }
+    for (int i = 0; i < (DT == RG_F32 ? 2 : 1); ++i) r.w[i] = *(reinterpret_cast<const uint4*>(src) + i);
   } else {
+    Elem<DT>* const to = reinterpret_cast<Elem<DT>*>(&r);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if constexpr (DT == RG_F32) v[i] = src[i];
-      else v[i] = DT == RG_F16 ? f16_bits_to_f32(src[i]) : bf16_bits_to_f32(src[i]);
+    for (int i = 0; i < 8; ++i) to[i] = src[i];
+  }
+  return r;
+}
+template <int DT>
+__device__ __forceinline__ void widen8(const Eight<DT>& r, float* v) {
+  if constexpr (DT == RG_F32) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) { v[4 * i] = __uint_as_float(r.w[i].x); v[4 * i + 1] = __uint_as_float(r.w[i].y); v[4 * i + 2] = __uint_as_float(r.w[i].z); v[4 * i + 3] = __uint_as_float(r.w[i].w); }
+  } else {
+    const uint32_t w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = DT == RG_F16 ? f16_bits_to_f32(w[i] & 0xffffu) : bf16_bits_to_f32(w[i]);          // bf16: the upper half leaves by the shift
+      v[2 * i + 1] = DT == RG_F16 ? f16_bits_to_f32(w[i] >> 16) : __uint_as_float(w[i] & 0xffff0000u);
     }
   }
 }
@@ -79,6 +85,22 @@ struct Places {
   }
 };
 
+// A thread's token, chunk of 32 elements, half of it (its group) and first head, and how many heads further its next one is.  Threads run over the halves, the
+// tokens, the chunks and the heads; what is left of the CTA has nothing to do.
+struct Spot {
+  int t, chunk, g, head, heads;
+  bool active;
+  __device__ __forceinline__ Spot(const Cache4Params& p, int n_tok) {
+    const int per_head = p.d / 32 * 2 * p.tile, r = threadIdx.x % per_head;
+    head = threadIdx.x / per_head;
+    heads = THREADS / per_head;
+    g = r & 1;
+    t = (r >> 1) & (p.tile - 1);
+    chunk = (r >> 1) / p.tile;
+    active = head < heads && t < n_tok;
+  }
+};
+
 // A pair's place in the CTA's tables of sines: threads that hold neighbouring groups, or one group of neighbouring tokens, read different banks (rows are
 // 2 modulo 16 apart, a group's pairs one more than their count).
 __device__ __forceinline__ int pair_at(int row, int t, int j, int per_group) { return t * row + j + (per_group == 16 ? j >> 4 : j >> 3); }
@@ -87,68 +109,56 @@ __host__ __device__ constexpr int pair_row(int half) { const int n = half + (hal
 // A query's 16 elements: pairs 8 u .. 8 u + 7 whole (another thread's stores must not reach them: the result may lie where the queries do), what is not
 // rotated as it lies.  Element c of this order, as an element of the head.
 __device__ __forceinline__ int paired(const Cache4Params& p, int c) { return c >= p.rot || p.style == RG_ROPE_PAIRS ? c : (c >> 1) + (c & 1) * (p.rot >> 1); }
-template <int DT>
-__device__ __forceinline__ void rotate_query(const Cache4Params& p, const Elem<DT>* src, Elem<DT>* dst, bool vec, int u, const float2* cs, int row, int t) {
-  const int half = p.rot >> 1;
-  const bool halves = p.style == RG_ROPE_HALF && 16 * u < p.rot, wide = vec && p.rot % 16 == 0;
-  constexpr int EIGHT = DT == RG_F32 ? 2 : 1;                          // 16-byte words of 8 elements
-  const int first = halves ? 8 * u : 16 * u, second = halves ? half + 8 * u : first + 8;
-  float v[16];                                                         // pairs side by side
-  if (wide) {
-    uint32_t w[8 * EIGHT];
-#pragma unroll
-    for (int i = 0; i < 2 * EIGHT; ++i) {
-      const uint4 x = *(reinterpret_cast<const uint4*>(src + (i < EIGHT ? first : second)) + i % EIGHT);
-      w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
-    }
-    float x[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if constexpr (DT == RG_F32) x[i] = __uint_as_float(w[i]);
-      else { const uint32_t h = i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu; x[i] = DT == RG_F16 ? f16_bits_to_f32(h) : bf16_bits_to_f32(h); }
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = halves ? x[(i >> 1) + 8 * (i & 1)] : x[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = load_scalar(src, DT, paired(p, 16 * u + i));
-  }
+// HALVES: pair e is elements e of the two eights, else neighbours.
+template <int DT, bool HALVES>
+__device__ __forceinline__ void rotate16(Eight<DT>& a, Eight<DT>& b, const float2* cs) {
+  float v[16];
+  widen8<DT>(a, v);
+  widen8<DT>(b, v + 8);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    if (16 * u + 2 * e >= p.rot) break;
-    const float2 w = cs[pair_at(row, t, 8 * u + e, 8)];
-    const float x = v[2 * e], y = v[2 * e + 1];
-    v[2 * e] = f_fma(-y, w.y, f_mul(x, w.x));
-    v[2 * e + 1] = f_fma(x, w.y, f_mul(y, w.x));
+    const float2 w = cs[e];
+    float &x = v[HALVES ? e : 2 * e], &y = v[HALVES ? 8 + e : 2 * e + 1];
+    const float x0 = x;
+    x = f_fma(-y, w.y, f_mul(x0, w.x));
+    y = f_fma(x0, w.y, f_mul(y, w.x));
   }
-  if (wide) {
-    float x[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = halves ? v[2 * (i & 7) + (i >> 3)] : v[i];
-    store8<DT>(dst + first, x);
-    store8<DT>(dst + second, x + 8);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) store_scalar(dst, DT, paired(p, 16 * u + i), v[i]);
+  store8<DT>(reinterpret_cast<Elem<DT>*>(&a), v);
+  store8<DT>(reinterpret_cast<Elem<DT>*>(&b), v + 8);
+}
+// Heads that no whole eights are rotated in, or rows that no 16-byte access reaches: element by element.
+template <int DT>
+__device__ __noinline__ void rotate_query_slowly(const Cache4Params& p, const Elem<DT>* src, Elem<DT>* dst, int u, const float2* cs) {
+  for (int e = 0; e < 8; ++e) {
+    const int i = paired(p, 16 * u + 2 * e), j = paired(p, 16 * u + 2 * e + 1);
+    float x = load_scalar(src, DT, i), y = load_scalar(src, DT, j);
+    if (16 * u + 2 * e < p.rot) {
+      const float2 w = cs[e];
+      const float x0 = x;
+      x = f_fma(-y, w.y, f_mul(x0, w.x));
+      y = f_fma(x0, w.y, f_mul(y, w.x));
+    }
+    store_scalar(dst, DT, i, x);
+    store_scalar(dst, DT, j, y);
   }
 }
 
-// An element of a key, rotated in 64 bits.
+// An element of a key, rotated in 64 bits; or, not rotated, of a value.
 template <int DT>
-__device__ __forceinline__ double rotated_key(const Cache4Params& p, const Elem<DT>* src, int i, const double2* cs, int row, int t) {
+__device__ __forceinline__ double element(const Cache4Params& p, const Elem<DT>* src, bool rotate, int i, const double2* cs, int row, int t) {
   const double x = (double)load_scalar(src, DT, i);
-  if (i >= p.rot) return x;
+  if (!rotate || i >= p.rot) return x;
   const int half = p.rot >> 1;
   const bool pairs = p.style == RG_ROPE_PAIRS, second = pairs ? i & 1 : i >= half;
   const double y = (double)load_scalar(src, DT, pairs ? i ^ 1 : second ? i - half : i + half);
   const double2 w = cs[pair_at(row, t, pairs ? i >> 1 : second ? i - half : i, pairs ? 8 : 16)];
   return __fma_rn(second ? y : -y, w.y, __dmul_rn(x, w.x));
 }
-// A group's codes and scale byte from there.
+// A group's codes and scale byte by the definition: for those with numbers next to a border, too large, infinite or NaN.
 template <int DT>
-__device__ __noinline__ uint3 quantise_in_64_bits(const Cache4Params& p, const Elem<DT>* src, int e0, const double2* cs, int row, int t) {
+__device__ __noinline__ uint3 quantise_in_64_bits(const Cache4Params& p, const Elem<DT>* src, bool rotate, int e0, const double2* cs, int row, int t) {
   double amax = 0.0;
-  for (int e = 0; e < 16; ++e) amax = fmax(amax, fabs(rotated_key<DT>(p, src, e0 + e, cs, row, t)));
+  for (int e = 0; e < 16; ++e) amax = fmax(amax, fabs(element<DT>(p, src, rotate, e0 + e, cs, row, t)));       // passes over NaN
   uint32_t b = scale4_byte(__double2float_rn(amax));
   while (b > 0 && 7.5 * (double)scale4(b - 1) >= amax) --b;
   while (b < 255 && 7.5 * (double)scale4(b) < amax) ++b;
@@ -157,7 +167,7 @@ __device__ __noinline__ uint3 quantise_in_64_bits(const Cache4Params& p, const E
 #pragma unroll
   for (int q = 0; q < 2; ++q)
     for (int e = 0; e < 8; ++e) {
-      const double x = rotated_key<DT>(p, src, e0 + 8 * q + e, cs, row, t);
+      const double x = element<DT>(p, src, rotate, e0 + 8 * q + e, cs, row, t);
       const int c = x == x ? (int)fmin(fmax(rint(x / s), -8.0), 7.0) : 0;
       w[q] |= (uint32_t)(c + 8) << (4 * (e >> 1) + 16 * (e & 1));
     }
@@ -165,7 +175,7 @@ __device__ __noinline__ uint3 quantise_in_64_bits(const Cache4Params& p, const E
 }
 
 template <int DT>
-__global__ void __launch_bounds__(THREADS) append4_kernel(const __grid_constant__ Cache4Params p) {
+__global__ void __launch_bounds__(THREADS, 3) append4_kernel(const __grid_constant__ Cache4Params p) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ Places at;
   const int64_t t0 = (int64_t)blockIdx.x * p.tile;
@@ -174,6 +184,9 @@ __global__ void __launch_bounds__(THREADS) append4_kernel(const __grid_constant_
   double2* cs64 = reinterpret_cast<double2*>(smem);                    // [tokens][row] (cos, sin)
   float2* cs32 = reinterpret_cast<float2*>(cs64 + p.tile * row);
   const int h0 = blockIdx.y * p.head_group, n_heads = min(p.head_group, p.heads_all - h0);
+  // a thread's token and group are the same for all its heads
+  const Spot spot(p, n_tok);
+  const int t = spot.t, chunk = spot.chunk, g = spot.g, e0 = 32 * chunk + 16 * g;      // first element of the group
   // what the kernel in front wrote is read from here on; the one behind may be set up meanwhile (it waits in the same way)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -206,70 +219,95 @@ __global__ void __launch_bounds__(THREADS) append4_kernel(const __grid_constant_
   }
   __syncthreads();
 
-  const int chunks = p.d / 32, per_chunk = 2 * n_tok, per_head = chunks * per_chunk, all = n_heads * per_head;
-  for (int i = threadIdx.x; i < all; i += THREADS) {
-    int h = h0 + i / per_head, r = i % per_head;
-    const int chunk = r / per_chunk;
-    r -= chunk * per_chunk;
-    const int t = r >> 1, e0 = 32 * chunk + 16 * (r & 1);              // first element of the thread's group
-    int k = 0;
-    if (h >= p.st[0].heads) { h -= p.st[0].heads; k = 1; }
-    if (k == 1 && h >= p.st[1].heads) { h -= p.st[1].heads; k = 2; }
+  if (!spot.active) return;
+  const int64_t page = at.page[t];
+  if (page == -2) return;
+  const int hk = p.st[0].heads, hv = hk + p.st[1].heads, end = h0 + n_heads;
+  int i = h0 + spot.head;
+  if (page < 0) while (i < hv) i += spot.heads;                        // no place for key and value
+  // keys and values
+  const int slot = at.slot[t], code_at = codes4_at(chunk, slot & 7) + 8 * g, scale_at = scales4_at(p.d, chunk, slot & 7) + g;
+  const int64_t in_page = (int64_t)(slot >> 3) * tile4_bytes(p.d);
+  for (; i < min(end, hv); i += spot.heads) {
+    const int k = i >= hk ? 1 : 0, h = i - (k ? hk : 0);
     const Cache4Stream& st = p.st[k];
-    const int64_t page = at.page[t];
-    if (page == -2 || (k < 2 && page < 0)) continue;
     const Elem<DT>* src = static_cast<const Elem<DT>*>(st.src) + (t0 + t) * st.src_tok + (int64_t)h * st.src_head;
-    if (k == 2) {
-      rotate_query<DT>(p, src, static_cast<Elem<DT>*>(st.dst) + (t0 + t) * st.dst_tok + (int64_t)h * st.dst_head, st.vec, e0 >> 4, cs32, row, t);
-      continue;
-    }
+    const bool rotated = k == 0 && e0 < p.rot;
     float v[16];
-    load16<DT>(src + e0, st.vec, v);
-    if (k == 0 && e0 < p.rot) {
-      float y[16];                                                     // each element's partner
-      if (p.style == RG_ROPE_PAIRS) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) y[e] = v[e ^ 1];
-      } else if (half % 16 == 0) {
-        load16<DT>(src + (e0 < half ? e0 + half : e0 - half), st.vec, y);
-      } else {
+    {
+      const Eight<DT> a = load8<DT>(src + e0, st.vec), b = load8<DT>(src + e0 + 8, st.vec);
+      if (rotated && p.style == RG_ROPE_HALF && half % 16 == 0) {
+        const bool second = e0 >= half;
+        const int other = second ? e0 - half : e0 + half;
+        const Eight<DT> c = load8<DT>(src + other, st.vec), d = load8<DT>(src + other + 8, st.vec);
+        const double2* const cs = cs64 + pair_at(row, t, second ? e0 - half : e0, 16);
+        float y[16];
+        widen8<DT>(a, v); widen8<DT>(b, v + 8); widen8<DT>(c, y); widen8<DT>(d, y + 8);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int i = e0 + e;
-          y[e] = i < p.rot ? load_scalar(src, DT, i < half ? i + half : i - half) : 0.0f;
+          const double2 w = cs[e];
+          v[e] = __double2float_rn(__fma_rn((double)(second ? y[e] : -y[e]), w.y, __dmul_rn((double)v[e], w.x)));
+        }
+      } else {
+        widen8<DT>(a, v); widen8<DT>(b, v + 8);
+        if (rotated) {
+#pragma unroll 1
+          for (int e = 0; e < 16; ++e) {
+            const float x = (float)element<DT>(p, src, true, e0 + e, cs64, row, t);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) v[q] = q == e ? x : v[q];
+          }
         }
       }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int i = e0 + e;
-        if (i >= p.rot) break;
-        const bool second = p.style == RG_ROPE_PAIRS ? e & 1 : i >= half;
-        const int j = p.style == RG_ROPE_PAIRS ? i >> 1 : second ? i - half : i;
-        const double2 w = cs64[pair_at(row, t, j, per_group)];
-        v[e] = __double2float_rn(__fma_rn((double)(second ? y[e] : -y[e]), w.y, __dmul_rn((double)v[e], w.x)));
-      }
     }
-    float amax = 0.0f;
+    float amax = 0.0f;                                                 // NaN if one is
 #pragma unroll
-    for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(v[e]));
-    uint32_t b = scale4_byte(amax);
-    const float s = scale4(b), inv = __frcp_rn(s);
-    uint32_t w[2];
-    bool near = scale4_near(amax);
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      w[q] = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[q] |= code4(v[8 * q + e], s, inv, near) << (4 * (e >> 1) + 16 * (e & 1));
-    }
-    if (near && k == 0 && e0 < p.rot) {
-      const uint3 exact = quantise_in_64_bits<DT>(p, src, e0, cs64, row, t);
+    for (int e = 0; e < 16; e += 2) amax = absmax3_nan(amax, v[e], v[e + 1]);
+    uint32_t b = scale4_byte(amax), w[2];
+    bool near = !(amax <= 57600.0f) || ((DT == RG_F32 || rotated) && scale4_near(amax));
+    codes4(v, __frcp_rn(scale4(b)), w, near, DT == RG_F32 || rotated);
+    if (near) {
+      const uint3 exact = quantise_in_64_bits<DT>(p, src, rotated, e0, cs64, row, t);
       w[0] = exact.x; w[1] = exact.y; b = exact.z;
     }
-    const int slot = at.slot[t];
-    uint8_t* tile = static_cast<uint8_t*>(st.dst) + page * st.dst_page + (int64_t)h * st.dst_head + (int64_t)(slot >> 3) * tile4_bytes(p.d);
-    *reinterpret_cast<uint2*>(tile + codes4_at(chunk, slot & 7) + 8 * (r & 1)) = make_uint2(w[0], w[1]);
-    tile[scales4_at(p.d, chunk, slot & 7) + (r & 1)] = (uint8_t)b;
+    uint8_t* to = static_cast<uint8_t*>(st.dst) + page * st.dst_page + in_page + (int64_t)h * st.dst_head;
+    *reinterpret_cast<uint2*>(to + code_at) = make_uint2(w[0], w[1]);
+    to[scale_at] = (uint8_t)b;
+  }
+  // queries, two heads at a time
+  if (i >= end) return;
+  const Cache4Stream& st = p.st[2];
+  const Elem<DT>* src = static_cast<const Elem<DT>*>(st.src) + (t0 + t) * st.src_tok + (int64_t)(i - hv) * st.src_head;
+  Elem<DT>* dst = static_cast<Elem<DT>*>(st.dst) + (t0 + t) * st.dst_tok + (int64_t)(i - hv) * st.dst_head;
+  const int64_t src_step = (int64_t)spot.heads * st.src_head, dst_step = (int64_t)spot.heads * st.dst_head;
+  const int u = 2 * chunk + g;
+  const float2* const cs = cs32 + pair_at(row, t, 8 * u, 8);
+  const bool turned = 16 * u < p.rot;
+  if (!st.vec || p.rot % 16) {
+    for (; i < end; i += spot.heads, src += src_step, dst += dst_step) rotate_query_slowly<DT>(p, src, dst, u, cs);
+    return;
+  }
+  const bool halves = turned && p.style == RG_ROPE_HALF;
+  const int first = halves ? 8 * u : 16 * u, second = halves ? half + 8 * u : first + 8;
+  auto turn = [&](Eight<DT>& a, Eight<DT>& b) {
+    if (halves) rotate16<DT, true>(a, b, cs);
+    else if (turned) rotate16<DT, false>(a, b, cs);
+  };
+  auto put = [&](Elem<DT>* to, const Eight<DT>& r) {
+#pragma unroll
+    for (int q = 0; q < (DT == RG_F32 ? 2 : 1); ++q) *(reinterpret_cast<uint4*>(to) + q) = r.w[q];
+  };
+  for (; i + spot.heads < end; i += 2 * spot.heads, src += 2 * src_step, dst += 2 * dst_step) {
+    Eight<DT> a0 = load8<DT>(src + first, true), b0 = load8<DT>(src + second, true), a1 = load8<DT>(src + src_step + first, true), b1 = load8<DT>(src + src_step + second, true);
+    turn(a0, b0);
+    put(dst + first, a0); put(dst + second, b0);
+    turn(a1, b1);
+    put(dst + dst_step + first, a1); put(dst + dst_step + second, b1);
+  }
+  if (i < end) {
+    Eight<DT> a = load8<DT>(src + first, true), b = load8<DT>(src + second, true);
+    turn(a, b);
+    put(dst + first, a); put(dst + second, b);
   }
 }
 
@@ -284,29 +322,27 @@ __global__ void __launch_bounds__(THREADS) read4_kernel(const __grid_constant__ 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   at.look_up(p, t0, n_tok, true);
   __syncthreads();
-  const int chunks = p.d / 32, per_chunk = 2 * n_tok, per_head = chunks * per_chunk, all = n_heads * per_head;
-  for (int i = threadIdx.x; i < all; i += THREADS) {
-    int h = h0 + i / per_head, r = i % per_head;
-    const int chunk = r / per_chunk;
-    r -= chunk * per_chunk;
-    const int t = r >> 1, k = h >= p.st[0].heads ? 1 : 0;
-    h -= k ? p.st[0].heads : 0;
+  const Spot spot(p, n_tok);
+  const int t = spot.t, chunk = spot.chunk, g = spot.g;
+  if (!spot.active) return;
+  const int64_t page = at.page[t];
+  if (page == -2) return;
+  const int slot = at.slot[t], code_at = codes4_at(chunk, slot & 7) + 8 * g, scale_at = scales4_at(p.d, chunk, slot & 7) + g;
+  for (int i = h0 + spot.head; i < h0 + n_heads; i += spot.heads) {
+    const int k = i >= p.st[0].heads ? 1 : 0, h = i - (k ? p.st[0].heads : 0);
     const Cache4Stream& st = p.st[k];
-    const int64_t page = at.page[t];
-    if (page == -2) continue;
     uint2 w = make_uint2(0x88888888u, 0x88888888u);                    // a row without a place: zeros
     uint32_t b = 0;
     if (page >= 0) {
-      const int slot = at.slot[t];
       const uint8_t* tile = static_cast<const uint8_t*>(st.src) + page * st.dst_page + (int64_t)h * st.src_head + (int64_t)(slot >> 3) * tile4_bytes(p.d);
-      w = *reinterpret_cast<const uint2*>(tile + codes4_at(chunk, slot & 7) + 8 * (r & 1));
-      b = tile[scales4_at(p.d, chunk, slot & 7) + (r & 1)];
+      w = *reinterpret_cast<const uint2*>(tile + code_at);
+      b = tile[scale_at];
     }
     const float s = scale4(b);
     float v[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) v[e] = f_mul((float)((int)((e < 8 ? w.x : w.y) >> (4 * ((e & 7) >> 1) + 16 * (e & 1)) & 15u) - 8), s);
-    Elem<DT>* dst = static_cast<Elem<DT>*>(st.dst) + (t0 + t) * st.dst_tok + (int64_t)h * st.dst_head + 32 * chunk + 16 * (r & 1);
+    Elem<DT>* dst = static_cast<Elem<DT>*>(st.dst) + (t0 + t) * st.dst_tok + (int64_t)h * st.dst_head + 32 * chunk + 16 * g;
     if (st.vec) {
       store8<DT>(dst, v);
       store8<DT>(dst + 8, v + 8);

@@ -33,19 +33,28 @@ __device__ __forceinline__ uint32_t scale4_byte(float amax) {
   return (uint32_t)b;
 }
 
-// The code of x, plus 8: the integer nearest to x / s, ties to even, kept within -8..7; inv = 1 / s.  The product x inv may land on the wrong side of a
-// border; the remainder x - q s is exact and tells.  NaN becomes 0.  `near`: x is so close to a border that half a unit of its last place, or a few, decide.
-__device__ __forceinline__ uint32_t code4(float x, float s, float inv, bool& near) {
-  x = x == x ? x : 0.0f;
-  const float q = rintf(fminf(fmaxf(f_mul(x, inv), -8.0f), 8.0f)), rem = f_fma(-q, s, x), half = f_mul(0.5f, s);
-  near |= fabsf(f_add(fabsf(rem), -half)) <= f_mul(fabsf(x), 0x1p-22f);
-  int c = (int)q;
-  const bool odd = c & 1;
-  if (rem > half || (odd && rem == half)) ++c;
-  if (rem < -half || (odd && rem == -half)) --c;
-  return (uint32_t)(min(max(c, -8), 7) + 8);
-}
 // Whether the scale of a group with this largest magnitude hangs on its last few bits.
 __device__ __forceinline__ bool scale4_near(float amax) { return ((__float_as_uint(f_mul(amax, 0x1.111112p-3f)) + 16u) & 0xfffffu) <= 32u; }
+
+// Sixteen codes, as they lie in two words, for a scale that reaches the largest magnitude; inv = 1 / s.  x inv is off by 2^-22 at most, so it may miss a
+// border between two codes; it is rounded to a multiple of 2^-16 first, which puts what is next to a border exactly there, and then to an integer, ties to even.
+// For 16-bit inputs that is all: x / s is a border or 2^-12 from one (the products 2 x and (2 k + 1) s are multiples of 2^-11 of x).  For others (`look`) `near` tells
+// that a border decided, and the caller looks again.  The integer stands in the low bits of a float above 2^23 (the 8 is added there), which is
+// multiplied to its nibble; what stands above the integers adds up to a constant.  Codes of 8 become 7 by a minimum in front.
+__device__ __forceinline__ void codes4(const float (&x)[16], float inv, uint32_t (&w)[2], bool& near, bool look) {
+  bool border = false;
+  constexpr uint32_t ABOVE = 0x4b400000u * 0x11111111u;            // 0x4b400000 in every nibble's place
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    w[q] = 0u - ABOVE;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float t = f_add(f_add(f_mul(x[8 * q + e], inv), 192.0f), -192.0f), m = f_add(fminf(t, 7.25f), 12582920.0f);
+      border |= fabsf(f_add(t, -f_add(m, -12582920.0f))) == 0.5f;
+      w[q] += __float_as_uint(m) << (4 * (e >> 1) + 16 * (e & 1));
+    }
+  }
+  near |= look && border;
+}
 
 }  // namespace rg
