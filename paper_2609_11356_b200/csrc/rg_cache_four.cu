@@ -1,13 +1,14 @@
 // Rows into a paged cache of four-bit codes (rg_kv_append_four), with the rotation on the way, and back out of it (rg_kv_read_four).  The format is
 // rg_four_bit.cuh's.
 //
-// Keys are rotated in 64 bits (the pair's sine and cosine as well): a code is a step function, and an fp32 rotation, whose result is off by 2^-22 or
-// so, would put one key in some hundred thousand on the other side of a border between codes; even a 64-bit one rounded to fp32 does so for one in ten
-// million.  Codes are chosen in fp32; a group in which that is close (one in 4000) is done again in 64 bits.  Queries are rotated as rg_rope does it, with its bits.
+// Keys are rotated and quantised in 64 bits (the pair's sine and cosine as well): a code is a step function, and an fp32 rotation, whose result is off by
+// 2^-22 or so, would put one key in some hundred thousand on the other side of a border between codes, so that two caches of one text would differ.  (Doing only
+// the close ones in 64 bits costs more: their code is never in the instruction cache, 3 us in a call of 64 tokens.)  Queries are rotated as rg_rope does it,
+// with its bits.
 //
-// What bounds it: bytes for prompts, latency for single tokens.  A thread takes one group of 16 elements of one row (query, key or value) and the group
-// that the rotation pairs with it: 32-byte loads, no exchange between threads, and a key's 8 code bytes and its scale byte are a thread's own.
-// Threads run over two groups, then the CTA's tokens, then the chunks of the head: neighbours write the neighbouring slots of a tile.
+// What bounds it: bytes for prompts, latency for single tokens.  A thread takes one group of 16 elements of one row (a query, or a key and a value) and the group
+// that the rotation pairs with it: 16-byte loads, several of them in flight, no exchange between threads, and a key's 8 code bytes and its scale byte are
+// a thread's own.  Threads run over two groups, then the CTA's tokens, then the chunks of the head: neighbours write the neighbouring slots of a tile.
 #include <algorithm>
 #include <type_traits>
 
@@ -101,30 +102,27 @@ struct Spot {
   }
 };
 
-// A pair's place in the CTA's tables of sines: threads that hold neighbouring groups, or one group of neighbouring tokens, read different banks (rows are
-// 2 modulo 16 apart, a group's pairs one more than their count).
-__device__ __forceinline__ int pair_at(int row, int t, int j, int per_group) { return t * row + j + (per_group == 16 ? j >> 4 : j >> 3); }
+// A pair's place in the CTA's tables of sines: eight pairs are a thread's, and threads that hold neighbouring eights, or one of neighbouring tokens, read different
+// banks (eights are 9 apart, rows 2 modulo 16).
+__device__ __forceinline__ int pair_at(int row, int t, int j) { return t * row + j + (j >> 3); }
 __host__ __device__ constexpr int pair_row(int half) { const int n = half + (half >> 3) + 1; return n + (18 - n % 16) % 16; }
 
 // A query's 16 elements: pairs 8 u .. 8 u + 7 whole (another thread's stores must not reach them: the result may lie where the queries do), what is not
 // rotated as it lies.  Element c of this order, as an element of the head.
 __device__ __forceinline__ int paired(const Cache4Params& p, int c) { return c >= p.rot || p.style == RG_ROPE_PAIRS ? c : (c >> 1) + (c & 1) * (p.rot >> 1); }
 // HALVES: pair e is elements e of the two eights, else neighbours.
-template <int DT, bool HALVES>
-__device__ __forceinline__ void rotate16(Eight<DT>& a, Eight<DT>& b, const float2* cs) {
-  float v[16];
-  widen8<DT>(a, v);
-  widen8<DT>(b, v + 8);
+__device__ __forceinline__ float turn_one(float a, float b, float s, float c) { return f_fma(b, s, f_mul(a, c)); }
+__device__ __forceinline__ double turn_one(double a, double b, double s, double c) { return __fma_rn(b, s, __dmul_rn(a, c)); }
+template <bool HALVES, typename T, typename T2>
+__device__ __forceinline__ void rotate16(T (&v)[16], const T2* cs) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float2 w = cs[e];
-    float &x = v[HALVES ? e : 2 * e], &y = v[HALVES ? 8 + e : 2 * e + 1];
-    const float x0 = x;
-    x = f_fma(-y, w.y, f_mul(x0, w.x));
-    y = f_fma(x0, w.y, f_mul(y, w.x));
+    const T2 w = cs[e];
+    T &x = v[HALVES ? e : 2 * e], &y = v[HALVES ? 8 + e : 2 * e + 1];
+    const T x0 = x;
+    x = turn_one(x0, -y, w.y, w.x);
+    y = turn_one(y, x0, w.y, w.x);
   }
-  store8<DT>(reinterpret_cast<Elem<DT>*>(&a), v);
-  store8<DT>(reinterpret_cast<Elem<DT>*>(&b), v + 8);
 }
 // Heads that no whole eights are rotated in, or rows that no 16-byte access reaches: element by element.
 template <int DT>
@@ -143,78 +141,91 @@ __device__ __noinline__ void rotate_query_slowly(const Cache4Params& p, const El
   }
 }
 
+// Pair j's angle for a token, as a fraction of a turn.
+__device__ __forceinline__ double turn_of(const Cache4Params& p, int64_t token, int64_t place, int j) {
+  int64_t pos = place;
+  if (p.pos) {
+    const int axis = (j >= p.axis_end[0]) + (j >= p.axis_end[1]) + (j >= p.axis_end[2]);
+    const int64_t k = (int64_t)axis * p.pos_ld + token;
+    pos = p.pos64 ? static_cast<const int64_t*>(p.pos)[k] : (int64_t)static_cast<const int32_t*>(p.pos)[k];
+  }
+  const double turns = __dmul_rn(__dmul_rn((double)pos, p.inv_freq[j]), 0x1.45f306dc9c883p-3);      // 1 / (2 pi)
+  return turns - rint(turns);
+}
+// An element's pair, the other element of it, and whether it is the second of the two.
+__device__ __forceinline__ int pair_of(const Cache4Params& p, int i, int& other, bool& second) {
+  const int half = p.rot >> 1;
+  const bool pairs = p.style == RG_ROPE_PAIRS;
+  second = pairs ? i & 1 : i >= half;
+  other = pairs ? i ^ 1 : second ? i - half : i + half;
+  return pairs ? i >> 1 : second ? other : i;
+}
 // An element of a key, rotated in 64 bits; or, not rotated, of a value.
 template <int DT>
 __device__ __forceinline__ double element(const Cache4Params& p, const Elem<DT>* src, bool rotate, int i, const double2* cs, int row, int t) {
   const double x = (double)load_scalar(src, DT, i);
   if (!rotate || i >= p.rot) return x;
-  const int half = p.rot >> 1;
-  const bool pairs = p.style == RG_ROPE_PAIRS, second = pairs ? i & 1 : i >= half;
-  const double y = (double)load_scalar(src, DT, pairs ? i ^ 1 : second ? i - half : i + half);
-  const double2 w = cs[pair_at(row, t, pairs ? i >> 1 : second ? i - half : i, pairs ? 8 : 16)];
+  int other;
+  bool second;
+  const int j = pair_of(p, i, other, second);
+  const double y = (double)load_scalar(src, DT, other);
+  const double2 w = cs[pair_at(row, t, j)];
   return __fma_rn(second ? y : -y, w.y, __dmul_rn(x, w.x));
 }
-// A group's codes and scale byte by the definition: for those with numbers next to a border, too large, infinite or NaN.
+// Codes and scale byte of a group with numbers that are too large, infinite or NaN (which becomes 0): elements e0 .. e0 + n - 1, n = 16, or n = 8 where the neighbouring
+// lane has the other eight and calls too.
+struct Codes { uint32_t w[2], b; };
 template <int DT>
-__device__ __noinline__ uint3 quantise_in_64_bits(const Cache4Params& p, const Elem<DT>* src, bool rotate, int e0, const double2* cs, int row, int t) {
+__device__ __noinline__ Codes quantise_slowly(const Cache4Params& p, const Elem<DT>* src, bool rotate, int e0, int n, const double2* cs, int row, int t) {
   double amax = 0.0;
-  for (int e = 0; e < 16; ++e) amax = fmax(amax, fabs(element<DT>(p, src, rotate, e0 + e, cs, row, t)));       // passes over NaN
-  uint32_t b = scale4_byte(__double2float_rn(amax));
-  while (b > 0 && 7.5 * (double)scale4(b - 1) >= amax) --b;
-  while (b < 255 && 7.5 * (double)scale4(b) < amax) ++b;
-  const double s = (double)scale4(b);
-  uint32_t w[2] = {0u, 0u};
-#pragma unroll
-  for (int q = 0; q < 2; ++q)
-    for (int e = 0; e < 8; ++e) {
-      const double x = element<DT>(p, src, rotate, e0 + 8 * q + e, cs, row, t);
-      const int c = x == x ? (int)fmin(fmax(rint(x / s), -8.0), 7.0) : 0;
-      w[q] |= (uint32_t)(c + 8) << (4 * (e >> 1) + 16 * (e & 1));
-    }
-  return make_uint3(w[0], w[1], b);
+#pragma unroll 1
+  for (int e = 0; e < n; ++e) amax = fmax(amax, fabs(element<DT>(p, src, rotate, e0 + e, cs, row, t)));       // passes over NaN
+  if (n == 8) amax = fmax(amax, __shfl_xor_sync(3u << (threadIdx.x & 30), amax, 1));
+  Codes r = {{0u, 0u}, scale4_byte(magnitude4_value(((uint32_t)__double2hiint(amax) & 0x7fffffffu) | min((uint32_t)__double2loint(amax), 1u)))};
+  const double inv = inverse4(scale4(r.b));
+#pragma unroll 1
+  for (int e = 0; e < n; ++e) {
+    double x = element<DT>(p, src, rotate, e0 + e, cs, row, t);
+    x = x == x ? fmin(fmax(x, -61440.0), 57600.0) : 0.0;
+    const double t = __dadd_rn(__dadd_rn(__dmul_rn(x, inv), 6144.0), -6144.0);
+    r.w[e >> 3] |= (uint32_t)((int)rint(fmin(fmax(t, -8.0), 7.25)) + 8) << (4 * ((e & 7) >> 1) + 16 * (e & 1));
+  }
+  return r;
 }
 
 template <int DT>
-__global__ void __launch_bounds__(THREADS, 3) append4_kernel(const __grid_constant__ Cache4Params p) {
+__global__ void __launch_bounds__(THREADS, 4) append4_kernel(const __grid_constant__ Cache4Params p) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ Places at;
   const int64_t t0 = (int64_t)blockIdx.x * p.tile;
   const int n_tok = (int)min((int64_t)p.tile, p.tokens - t0);
-  const int half = p.rot >> 1, row = pair_row(half), per_group = p.style == RG_ROPE_HALF ? 16 : 8;      // pairs that 16 neighbouring elements belong to
-  double2* cs64 = reinterpret_cast<double2*>(smem);                    // [tokens][row] (cos, sin)
-  float2* cs32 = reinterpret_cast<float2*>(cs64 + p.tile * row);
+  const int half = p.rot >> 1, row = pair_row(half);
+  double2* const cs64 = reinterpret_cast<double2*>(smem);              // [tokens][row] (cos, sin) for keys, and for queries
+  float2* const csq = reinterpret_cast<float2*>(cs64 + p.tile * row);
   const int h0 = blockIdx.y * p.head_group, n_heads = min(p.head_group, p.heads_all - h0);
   // a thread's token and group are the same for all its heads
   const Spot spot(p, n_tok);
-  const int t = spot.t, chunk = spot.chunk, g = spot.g, e0 = 32 * chunk + 16 * g;      // first element of the group
+  const int t = spot.t, chunk = spot.chunk, g = spot.g;
   // what the kernel in front wrote is read from here on; the one behind may be set up meanwhile (it waits in the same way)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   at.look_up(p, t0, n_tok, false);
   __syncthreads();
-  // streams: keys, values, queries
-  const bool keys = p.rot && h0 < p.st[0].heads, queries = h0 + n_heads > p.st[0].heads + p.st[1].heads;
+  // heads: pairs of a key and a value, then queries
+  const int hk = p.st[0].heads, end = h0 + n_heads;
+  const bool keys = p.rot && h0 < hk, queries = end > hk;
   for (int i = threadIdx.x; i < n_tok * half; i += THREADS) {
-    const int t = i / half, j = i - t * half;
-    int64_t pos;
-    if (p.pos) {
-      const int axis = (j >= p.axis_end[0]) + (j >= p.axis_end[1]) + (j >= p.axis_end[2]);
-      const int64_t k = (int64_t)axis * p.pos_ld + t0 + t;
-      pos = p.pos64 ? static_cast<const int64_t*>(p.pos)[k] : (int64_t)static_cast<const int32_t*>(p.pos)[k];
-    } else {
-      pos = at.place[t];
-    }
-    const double turns = __dmul_rn(__dmul_rn((double)pos, p.inv_freq[j]), 0x1.45f306dc9c883p-3);      // 1 / (2 pi)
-    const double part = turns - rint(turns);
+    const int tok = i / half, j = i - tok * half;
+    const double turn = turn_of(p, t0 + tok, at.place[tok], j);
     if (keys) {
       double s, c;
-      sincospi(2.0 * part, &s, &c);
-      cs64[pair_at(row, t, j, per_group)] = make_double2(c, s);
+      sincospi(2.0 * turn, &s, &c);
+      cs64[pair_at(row, tok, j)] = make_double2(c, s);
     }
     if (queries) {
       float s, c;
-      sincospif(2.0f * (float)part, &s, &c);
-      cs32[pair_at(row, t, j, 8)] = make_float2(c, s);
+      sincospif(2.0f * (float)turn, &s, &c);
+      csq[pair_at(row, tok, j)] = make_float2(c, s);
     }
   }
   __syncthreads();
@@ -222,93 +233,130 @@ __global__ void __launch_bounds__(THREADS, 3) append4_kernel(const __grid_consta
   if (!spot.active) return;
   const int64_t page = at.page[t];
   if (page == -2) return;
-  const int hk = p.st[0].heads, hv = hk + p.st[1].heads, end = h0 + n_heads;
   int i = h0 + spot.head;
-  if (page < 0) while (i < hv) i += spot.heads;                        // no place for key and value
-  // keys and values
-  const int slot = at.slot[t], code_at = codes4_at(chunk, slot & 7) + 8 * g, scale_at = scales4_at(p.d, chunk, slot & 7) + g;
-  const int64_t in_page = (int64_t)(slot >> 3) * tile4_bytes(p.d);
-  for (; i < min(end, hv); i += spot.heads) {
-    const int k = i >= hk ? 1 : 0, h = i - (k ? hk : 0);
-    const Cache4Stream& st = p.st[k];
-    const Elem<DT>* src = static_cast<const Elem<DT>*>(st.src) + (t0 + t) * st.src_tok + (int64_t)h * st.src_head;
-    const bool rotated = k == 0 && e0 < p.rot;
+  // Sixteen elements that a thread rotates: pairs 8 u .. 8 u + 7, or, behind the rotated ones, elements 16 u .. 16 u + 15.
+  const int u = 2 * chunk + g;
+  const bool turned = 16 * u < p.rot, halves = turned && p.style == RG_ROPE_HALF;
+  const int first = halves ? 8 * u : 16 * u, second = halves ? half + 8 * u : first + 8;
+
+  // ---- keys and values
+  const int slot = at.slot[t];
+  const int64_t in_page = page * p.st[0].dst_page + (int64_t)(slot >> 3) * tile4_bytes(p.d), in_page_v = page * p.st[1].dst_page + (int64_t)(slot >> 3) * tile4_bytes(p.d);
+  // the eight elements (a word) from e on in a tile, and the scale of its group
+  auto word_at = [&](int e) -> int { return codes4_at(e >> 5, slot & 7) + (e >> 3 & 3) * 4; };
+  auto scale_at = [&](int e) -> int { return scales4_at(p.d, e >> 5, slot & 7) + (e >> 4 & 1); };
+  auto max8 = [](const float* v) -> float {                            // NaN if one is
+    float m = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) m = absmax3_nan(m, v[e], v[e + 1]);
+    return m;
+  };
+  // a whole group: elements 16 u ..
+  auto put_group = [&](uint8_t* tile, const Elem<DT>* src, const auto* v, bool rotated) {
+    uint32_t b;
+    uint2 w;
+    float amax;
+    if constexpr (sizeof(*v) == 8) {
+      amax = magnitude4_value(max(magnitude4(v), magnitude4(v + 8)));
+      b = scale4_byte(amax);
+      const double inv = inverse4(scale4(b));
+      w = make_uint2(codes4(v, inv), codes4(v + 8, inv));
+    } else {
+      amax = absmax3_nan(0.0f, max8(v), max8(v + 8));
+      b = scale4_byte(amax);
+      const float inv = __frcp_rn(scale4(b));
+      w = make_uint2(codes4(v, inv), codes4(v + 8, inv));
+    }
+    if (!(amax <= 57600.0f)) {
+      const Codes c = quantise_slowly<DT>(p, src, rotated, 16 * u, 16, cs64, row, t);
+      w = make_uint2(c.w[0], c.w[1]);
+      b = c.b;
+    }
+    *reinterpret_cast<uint2*>(tile + word_at(16 * u)) = w;
+    tile[scale_at(16 * u)] = (uint8_t)b;
+  };
+  // half a group, elements e .. e + 7; the neighbouring lane has the other half
+  auto put_half = [&](uint8_t* tile, const Elem<DT>* src, const double* v, int e) {
+    const uint32_t mine = magnitude4(v);
+    const float amax = magnitude4_value(max(mine, __shfl_xor_sync(3u << (threadIdx.x & 30), mine, 1)));
+    uint32_t b = scale4_byte(amax), w = codes4(v, inverse4(scale4(b)));
+    if (!(amax <= 57600.0f)) {
+      const Codes c = quantise_slowly<DT>(p, src, true, e, 8, cs64, row, t);
+      w = c.w[0];
+      b = c.b;
+    }
+    *reinterpret_cast<uint32_t*>(tile + word_at(e)) = w;
+    if (!(e & 8)) tile[scale_at(e)] = (uint8_t)b;
+  };
+  const bool whole_eights = p.style == RG_ROPE_HALF ? p.rot % 32 == 0 : p.rot % 16 == 0;      // of the rotated elements' groups
+  const int k_first = whole_eights ? first : 16 * u, k_second = whole_eights ? second : 16 * u + 8;      // 16-byte accesses reach them
+  const double2* const csk = cs64 + pair_at(row, t, 8 * u);
+  for (; i < min(end, hk); i += spot.heads) {
+    if (page < 0) continue;                                            // no place for key and value
+    const Elem<DT>* k_src = static_cast<const Elem<DT>*>(p.st[0].src) + (t0 + t) * p.st[0].src_tok + (int64_t)i * p.st[0].src_head;
+    const Elem<DT>* v_src = static_cast<const Elem<DT>*>(p.st[1].src) + (t0 + t) * p.st[1].src_tok + (int64_t)i * p.st[1].src_head;
+    uint8_t* const k_tile = static_cast<uint8_t*>(p.st[0].dst) + in_page + (int64_t)i * p.st[0].dst_head;
+    uint8_t* const v_tile = static_cast<uint8_t*>(p.st[1].dst) + in_page_v + (int64_t)i * p.st[1].dst_head;
+    const Eight<DT> ka = load8<DT>(k_src + k_first, p.st[0].vec), kb = load8<DT>(k_src + k_second, p.st[0].vec);
+    const Eight<DT> va = load8<DT>(v_src + 16 * u, p.st[1].vec), vb = load8<DT>(v_src + 16 * u + 8, p.st[1].vec);
     float v[16];
-    {
-      const Eight<DT> a = load8<DT>(src + e0, st.vec), b = load8<DT>(src + e0 + 8, st.vec);
-      if (rotated && p.style == RG_ROPE_HALF && half % 16 == 0) {
-        const bool second = e0 >= half;
-        const int other = second ? e0 - half : e0 + half;
-        const Eight<DT> c = load8<DT>(src + other, st.vec), d = load8<DT>(src + other + 8, st.vec);
-        const double2* const cs = cs64 + pair_at(row, t, second ? e0 - half : e0, 16);
-        float y[16];
-        widen8<DT>(a, v); widen8<DT>(b, v + 8); widen8<DT>(c, y); widen8<DT>(d, y + 8);
+    widen8<DT>(ka, v); widen8<DT>(kb, v + 8);
+    if (turned || DT == RG_F32) {
+      double x[16];
+      if (!whole_eights && turned) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const double2 w = cs[e];
-          v[e] = __double2float_rn(__fma_rn((double)(second ? y[e] : -y[e]), w.y, __dmul_rn((double)v[e], w.x)));
-        }
+        for (int e = 0; e < 16; ++e) x[e] = element<DT>(p, k_src, true, 16 * u + e, cs64, row, t);
       } else {
-        widen8<DT>(a, v); widen8<DT>(b, v + 8);
-        if (rotated) {
-#pragma unroll 1
-          for (int e = 0; e < 16; ++e) {
-            const float x = (float)element<DT>(p, src, true, e0 + e, cs64, row, t);
 #pragma unroll
-            for (int q = 0; q < 16; ++q) v[q] = q == e ? x : v[q];
-          }
-        }
+        for (int e = 0; e < 16; ++e) x[e] = (double)v[e];
+        if (halves) rotate16<true>(x, csk);
+        else if (turned) rotate16<false>(x, csk);
       }
+      if (halves && whole_eights) {
+        put_half(k_tile, k_src, x, first);
+        put_half(k_tile, k_src, x + 8, second);
+      } else {
+        put_group(k_tile, k_src, x, turned);
+      }
+    } else {
+      put_group(k_tile, k_src, v, false);
     }
-    float amax = 0.0f;                                                 // NaN if one is
+    widen8<DT>(va, v); widen8<DT>(vb, v + 8);
+    if constexpr (DT == RG_F32) {
+      double x[16];
 #pragma unroll
-    for (int e = 0; e < 16; e += 2) amax = absmax3_nan(amax, v[e], v[e + 1]);
-    uint32_t b = scale4_byte(amax), w[2];
-    bool near = !(amax <= 57600.0f) || ((DT == RG_F32 || rotated) && scale4_near(amax));
-    codes4(v, __frcp_rn(scale4(b)), w, near, DT == RG_F32 || rotated);
-    if (near) {
-      const uint3 exact = quantise_in_64_bits<DT>(p, src, rotated, e0, cs64, row, t);
-      w[0] = exact.x; w[1] = exact.y; b = exact.z;
+      for (int e = 0; e < 16; ++e) x[e] = (double)v[e];
+      put_group(v_tile, v_src, x, false);
+    } else {
+      put_group(v_tile, v_src, v, false);
     }
-    uint8_t* to = static_cast<uint8_t*>(st.dst) + page * st.dst_page + in_page + (int64_t)h * st.dst_head;
-    *reinterpret_cast<uint2*>(to + code_at) = make_uint2(w[0], w[1]);
-    to[scale_at] = (uint8_t)b;
   }
-  // queries, two heads at a time
+
+  // ---- queries, two heads at a time
   if (i >= end) return;
   const Cache4Stream& st = p.st[2];
-  const Elem<DT>* src = static_cast<const Elem<DT>*>(st.src) + (t0 + t) * st.src_tok + (int64_t)(i - hv) * st.src_head;
-  Elem<DT>* dst = static_cast<Elem<DT>*>(st.dst) + (t0 + t) * st.dst_tok + (int64_t)(i - hv) * st.dst_head;
+  const Elem<DT>* src = static_cast<const Elem<DT>*>(st.src) + (t0 + t) * st.src_tok + (int64_t)(i - hk) * st.src_head;
+  Elem<DT>* dst = static_cast<Elem<DT>*>(st.dst) + (t0 + t) * st.dst_tok + (int64_t)(i - hk) * st.dst_head;
   const int64_t src_step = (int64_t)spot.heads * st.src_head, dst_step = (int64_t)spot.heads * st.dst_head;
-  const int u = 2 * chunk + g;
-  const float2* const cs = cs32 + pair_at(row, t, 8 * u, 8);
-  const bool turned = 16 * u < p.rot;
+  const float2* const cs = csq + pair_at(row, t, 8 * u);
   if (!st.vec || p.rot % 16) {
     for (; i < end; i += spot.heads, src += src_step, dst += dst_step) rotate_query_slowly<DT>(p, src, dst, u, cs);
     return;
   }
-  const bool halves = turned && p.style == RG_ROPE_HALF;
-  const int first = halves ? 8 * u : 16 * u, second = halves ? half + 8 * u : first + 8;
-  auto turn = [&](Eight<DT>& a, Eight<DT>& b) {
-    if (halves) rotate16<DT, true>(a, b, cs);
-    else if (turned) rotate16<DT, false>(a, b, cs);
-  };
-  auto put = [&](Elem<DT>* to, const Eight<DT>& r) {
-#pragma unroll
-    for (int q = 0; q < (DT == RG_F32 ? 2 : 1); ++q) *(reinterpret_cast<uint4*>(to) + q) = r.w[q];
+  auto turn_and_put = [&](Elem<DT>* to, const Eight<DT>& a, const Eight<DT>& b) {
+    float v[16];
+    widen8<DT>(a, v); widen8<DT>(b, v + 8);
+    if (halves) rotate16<true>(v, cs);
+    else if (turned) rotate16<false>(v, cs);
+    store8<DT>(to + first, v);
+    store8<DT>(to + second, v + 8);
   };
   for (; i + spot.heads < end; i += 2 * spot.heads, src += 2 * src_step, dst += 2 * dst_step) {
-    Eight<DT> a0 = load8<DT>(src + first, true), b0 = load8<DT>(src + second, true), a1 = load8<DT>(src + src_step + first, true), b1 = load8<DT>(src + src_step + second, true);
-    turn(a0, b0);
-    put(dst + first, a0); put(dst + second, b0);
-    turn(a1, b1);
-    put(dst + dst_step + first, a1); put(dst + dst_step + second, b1);
+    const Eight<DT> a0 = load8<DT>(src + first, true), b0 = load8<DT>(src + second, true), a1 = load8<DT>(src + src_step + first, true), b1 = load8<DT>(src + src_step + second, true);
+    turn_and_put(dst, a0, b0);
+    turn_and_put(dst + dst_step, a1, b1);
   }
-  if (i < end) {
-    Eight<DT> a = load8<DT>(src + first, true), b = load8<DT>(src + second, true);
-    turn(a, b);
-    put(dst + first, a); put(dst + second, b);
-  }
+  if (i < end) turn_and_put(dst, load8<DT>(src + first, true), load8<DT>(src + second, true));
 }
 
 // The other way: a thread takes a group's codes and stores 16 elements.
@@ -376,7 +424,7 @@ rg_status_t launch_cache4(Cache4Params p, int dtype, bool read, cudaStream_t st)
   p.heads_all = 0;
   for (int k = 0; k < p.n_streams; ++k) {
     Cache4Stream& s = p.st[k];
-    p.heads_all += s.heads;
+    if (read || k != 1) p.heads_all += s.heads;                          // written, a key and its value go together
     // the sides that are rows
     const bool src = !read, dst = read || k == 2;
     s.vec = (!src || (reinterpret_cast<uintptr_t>(s.src) % 16 == 0 && s.src_tok * es % 16 == 0 && s.src_head * es % 16 == 0)) &&

@@ -33,28 +33,42 @@ __device__ __forceinline__ uint32_t scale4_byte(float amax) {
   return (uint32_t)b;
 }
 
-// Whether the scale of a group with this largest magnitude hangs on its last few bits.
-__device__ __forceinline__ bool scale4_near(float amax) { return ((__float_as_uint(f_mul(amax, 0x1.111112p-3f)) + 16u) & 0xfffffu) <= 32u; }
-
-// Sixteen codes, as they lie in two words, for a scale that reaches the largest magnitude; inv = 1 / s.  x inv is off by 2^-22 at most, so it may miss a
-// border between two codes; it is rounded to a multiple of 2^-16 first, which puts what is next to a border exactly there, and then to an integer, ties to even.
-// For 16-bit inputs that is all: x / s is a border or 2^-12 from one (the products 2 x and (2 k + 1) s are multiples of 2^-11 of x).  For others (`look`) `near` tells
-// that a border decided, and the caller looks again.  The integer stands in the low bits of a float above 2^23 (the 8 is added there), which is
-// multiplied to its nibble; what stands above the integers adds up to a constant.  Codes of 8 become 7 by a minimum in front.
-__device__ __forceinline__ void codes4(const float (&x)[16], float inv, uint32_t (&w)[2], bool& near, bool look) {
-  bool border = false;
-  constexpr uint32_t ABOVE = 0x4b400000u * 0x11111111u;            // 0x4b400000 in every nibble's place
+// Eight codes of 16-bit numbers, as they lie in a word, for a scale that reaches their largest magnitude; inv = 1 / s.  x inv is off by 2^-21 at most, so it
+// may miss a border between two codes; it is rounded to a multiple of 2^-15 first, which puts what is next to a border exactly there, and then to an integer, ties to
+// even.  That is exact: x / s is a border or 2^-13 from one (2 x and (2 k + 1) s differ by 2^-8 of the last place of s or more).  The integer stands in the
+// low bits of a float above 2^23 (the 8 is added there), which is multiplied to its nibble; what stands above the codes adds up to a constant.  Codes of 8
+// become 7 by a minimum in front.
+__device__ __forceinline__ uint32_t codes4(const float* x, float inv) {
+  uint32_t w = 0u - 0x4b400000u * 0x11111111u;                     // 0x4b400000 in every nibble's place
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    w[q] = 0u - ABOVE;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float t = f_add(f_add(f_mul(x[8 * q + e], inv), 192.0f), -192.0f), m = f_add(fminf(t, 7.25f), 12582920.0f);
-      border |= fabsf(f_add(t, -f_add(m, -12582920.0f))) == 0.5f;
-      w[q] += __float_as_uint(m) << (4 * (e >> 1) + 16 * (e & 1));
-    }
+  for (int e = 0; e < 8; ++e) {
+    const float t = f_add(f_add(f_mul(x[e], inv), 384.0f), -384.0f);
+    w += __float_as_uint(f_add(fminf(t, 7.25f), 12582920.0f)) << (4 * (e >> 1) + 16 * (e & 1));
   }
-  near |= look && border;
+  return w;
 }
+// The same for numbers in 64 bits.  x inv is off by 2^-48 or so and rounded to a multiple of 2^-40.
+__device__ __forceinline__ uint32_t codes4(const double* x, double inv) {
+  uint32_t w = 0u;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const double t = __dadd_rn(__dadd_rn(__dmul_rn(x[e], inv), 6144.0), -6144.0);
+    w |= min((uint32_t)__double2loint(__dadd_rn(t, 6755399441055752.0)), 15u) << (4 * (e >> 1) + 16 * (e & 1));      // 1.5 2^52 + 8
+  }
+  return w;
+}
+__device__ __forceinline__ double inverse4(float s) {              // 1 / s to 2^-47
+  const double d = (double)s, r = (double)__frcp_rn(s);
+  return __fma_rn(r, __fma_rn(-d, r, 1.0), r);
+}
+// The largest magnitude of eight numbers in 64 bits, as far as scale4_byte goes by it: 20 bits, the last of which stands for all that follow (7.5 s has eight
+// bits).  Upper halves of doubles, which order as they do.
+__device__ __forceinline__ uint32_t magnitude4(const double* x) {
+  uint32_t m = 0u;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, ((uint32_t)__double2hiint(x[e]) & 0x7fffffffu) | min((uint32_t)__double2loint(x[e]), 1u));
+  return m;
+}
+__device__ __forceinline__ float magnitude4_value(uint32_t m) { return __double2float_rn(__hiloint2double((int)m, 0)); }
 
 }  // namespace rg
