@@ -3,8 +3,8 @@
 //
 // The inner sum is a chain of 16-wide tensor-core steps from a zero accumulator: u - z is an integer of at most four bits and a sign, exact in bf16 and
 // fp16, so nothing is rounded before the products' fp32 sum.  The scale multiplies a finished group once, in fp32 (fused, onto the running sum of a part of
-// K): no weight is ever narrowed, whatever the scales' type.  A part is a run of whole 256-wide stages, at most eight of them over K; parts are added in
-// ascending order.  The cut follows from K alone and an accumulator's column is one row of A, so a row's bits do not depend on M.
+// K): no weight is ever narrowed, whatever the scales' type.  A part is a run of whole 256-wide stages, at most eight of them over K; parts are added as a
+// balanced tree of eight adds them.  The cut follows from K alone and an accumulator's column is one row of A, so a row's bits do not depend on M.
 //
 // What bounds it: the bytes of the codes, and next the instructions that unpack them (1.4 a code and lane: a mask that makes a float's mantissa of the nibble,
 // and one subtraction, for two codes).  Weights are the 16 rows of mma.sync's first operand, read straight from the natural order of the codes: a warp's
@@ -81,7 +81,7 @@ struct Shape4 {
   static constexpr int SLOT = MT * STAGE, SCALES = PER<GROUP> * COLS * 8;           // (scale, less) pairs of a stage
   static constexpr int PART = ROWS * (COLS + 1) * 4;   // a part's sums, of all the rows there can be
   static constexpr int SCALE_AT = WARPS * DEPTH * SLOT, BAR_AT = SCALE_AT + WARPS * SCALES, FLAG_AT = BAR_AT + WARPS * DEPTH * 8, PART_AT = FLAG_AT + 16, SMEM = 1024 + PART_AT;
-  static constexpr int MOST = SMEM + (WARPS == 8 ? 1 : 2) * PARTS * PART;      // eight warps share one tile, of four two at least
+  static constexpr int MOST = SMEM + (WARPS == 8 ? 1 : 4) * PARTS * PART;      // eight warps share one tile, four have up to four
   static_assert(MOST <= 232448 && BAR_AT % 8 == 0, "fits the SM");
 };
 
@@ -90,8 +90,43 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(0), "r"(bar) : "memory");
 }
 
+// The scales and zero points of a warp's stages, PER * 16 MT of each a stage, fetched one stage ahead: a lane's share is one group of rows lane / PER, STEP further, ...
+template <int GROUP, int MT>
+struct Scales {
+  static constexpr int G = PER<GROUP>, SHARE = G * 16 * MT / 32, STEP = 32 / G;
+  float scale[SHARE];
+  uint32_t zero[SHARE];
+  int64_t s_from, z_from, s_step, z_step;
+  int group, left;
+  __device__ __forceinline__ Scales(const W4Params& p, int64_t row, int first_group)
+      : s_from(row * p.scale_ld + first_group), z_from(row * p.zero_ld + first_group), s_step(STEP * p.scale_ld), z_step(STEP * p.zero_ld), group(first_group), left((int)max(p.N - row, (int64_t)0)) {}
+  __device__ __forceinline__ void fetch(const W4Params& p) {
+    const int n = group < p.groups ? left : 0;
+    auto load = [&](auto get) {
+#pragma unroll
+      for (int q = 0; q < SHARE; ++q) scale[q] = STEP * q < n ? get(s_from + q * s_step) : 0.0f;
+    };
+    if (p.scale_dtype == RG_BF16) load([&](int64_t i) { return bf16_bits_to_f32(__ldg(static_cast<const uint16_t*>(p.scales) + i)); });
+    else if (p.scale_dtype == RG_F16) load([&](int64_t i) { return f16_bits_to_f32(__ldg(static_cast<const uint16_t*>(p.scales) + i)); });
+    else load([&](int64_t i) { return __ldg(static_cast<const float*>(p.scales) + i); });
+#pragma unroll
+    for (int q = 0; q < SHARE; ++q) zero[q] = p.zeros && STEP * q < n ? __ldg(p.zeros + z_from + q * z_step) : 8u;
+    s_from += G; z_from += G; group += G;
+  }
+  // as (scale, -(128 + z) or -(1024 + z) twice) pairs [MT][G][16]
+  __device__ __forceinline__ void put(float2* sz, bool f16) const {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int q = 0; q < SHARE; ++q) {
+      const int row = lane / G + STEP * q;
+      const uint32_t less = (zero[q] & 15u) * 0x10001u + (f16 ? 0xe400e400u : 0xc300c300u);
+      sz[((row >> 4) * G + lane % G) * 16 + (row & 15)] = make_float2(scale[q], __uint_as_float(less));
+    }
+  }
+};
+
 template <bool F16, int GROUP, int MT, int NT, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32, NT <= 2 ? 16 / WARPS : 8 / WARPS) gemv_w4_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constant__ W4Params p) {
+__global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constant__ W4Params p) {
   using S = Shape4<GROUP, MT, NT, WARPS>;
   constexpr int G = PER<GROUP>, WORDS = GROUP / 32;    // words of eight codes that a lane takes of each row and group
   constexpr int COLS = S::COLS, DEPTH = S::DEPTH;
@@ -125,43 +160,14 @@ __global__ void __launch_bounds__(WARPS * 32, NT <= 2 ? 16 / WARPS : 8 / WARPS) 
     }
     ++r_i;
   };
-  // The scales and zero points of a stage, G * COLS of each, one stage ahead: a lane's share is one group of rows lane / G, STEP further, ...
-  constexpr int SHARE = G * COLS / 32, STEP = 32 / G;
-  float scale[SHARE];
-  uint32_t zero[SHARE];
-  const int64_t n_first = (int64_t)tile * COLS + lane / G;
-  int s_group = s0 * G + lane % G;
-  const int s_left = (int)(p.N - n_first);
-  int64_t s_from = n_first * p.scale_ld + s_group, z_from = n_first * p.zero_ld + s_group;
-  const int64_t s_step = STEP * p.scale_ld, z_step = STEP * p.zero_ld;
-  auto fetch = [&] {
-    const int left = s_group < p.groups ? s_left : 0;
-    auto load = [&](auto get) {
-#pragma unroll
-      for (int q = 0; q < SHARE; ++q) scale[q] = STEP * q < left ? get(s_from + q * s_step) : 0.0f;
-    };
-    if (p.scale_dtype == RG_BF16) load([&](int64_t i) { return bf16_bits_to_f32(__ldg(static_cast<const uint16_t*>(p.scales) + i)); });
-    else if (p.scale_dtype == RG_F16) load([&](int64_t i) { return f16_bits_to_f32(__ldg(static_cast<const uint16_t*>(p.scales) + i)); });
-    else load([&](int64_t i) { return __ldg(static_cast<const float*>(p.scales) + i); });
-#pragma unroll
-    for (int q = 0; q < SHARE; ++q) zero[q] = p.zeros && STEP * q < left ? __ldg(p.zeros + z_from + q * z_step) : 8u;
-    s_from += G; z_from += G; s_group += G;
-  };
-  auto put = [&] {
-#pragma unroll
-    for (int q = 0; q < SHARE; ++q) {
-      const int row = lane / G + STEP * q;
-      const uint32_t less = (zero[q] & 15u) * 0x10001u + (F16 ? 0xe400e400u : 0xc300c300u);       // -(1024 + z), -(128 + z)
-      sz[((row >> 4) * G + lane % G) * 16 + (row & 15)] = make_float2(scale[q], __uint_as_float(less));
-    }
-  };
+  Scales<GROUP, MT> scales(p, (int64_t)tile * COLS + lane / G, s0 * G + lane % G);
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // with the promise that nothing in flight writes the weights their first stages are on their way before the kernels ahead have finished
   if (!p.w_static) asm volatile("griddepcontrol.wait;" ::: "memory");
 #pragma unroll
   for (int i = 0; i < DEPTH - 1; ++i) request();
-  if (n_st > 0) fetch();
+  if (n_st > 0) scales.fetch(p);
   if (p.w_static) asm volatile("griddepcontrol.wait;" ::: "memory");
 
   const int t = lane & 3, rr = lane >> 2;
@@ -241,8 +247,8 @@ __global__ void __launch_bounds__(WARPS * 32, NT <= 2 ? 16 / WARPS : 8 / WARPS) 
 #pragma unroll
       for (int g = 0; g < G; ++g) load_x(g, left, tail);
     }
-    put();
-    if (i + 1 < n_st) fetch();
+    scales.put(sz, F16);
+    if (i + 1 < n_st) scales.fetch(p);
     request();
     const uint32_t slot = i % DEPTH;
     warp_mbar_wait(bars + 8 * slot, (i / DEPTH) & 1, abort_flag, &g_gemv_four_status_word, 0x4000u | slot);      // one that gives up lets the kernel run out
@@ -262,9 +268,8 @@ __global__ void __launch_bounds__(WARPS * 32, NT <= 2 ? 16 / WARPS : 8 / WARPS) 
     if (left >= SPAN) stage(i, left, std::false_type{});
     else stage(i, left, std::true_type{});
     if (++in_part == p.part || i + 1 == n_st) {
-      // A part is done.  The parts are joined in ascending order: by the tile's only warp as it goes, into the place of the first, or by all warps at the end.
-      float* const to = reinterpret_cast<float*>(smem + S::PART_AT) + ((p.wpt == 1 ? own : own * PARTS + part) * rows + 2 * t) * (COLS + 1) + r;       // [rows][COLS + 1]
-      const bool onto = p.wpt == 1 && part > 0;
+      // a part is done; all are joined at the end
+      float* const to = reinterpret_cast<float*>(smem + S::PART_AT) + ((own * PARTS + part) * rows + 2 * t) * (COLS + 1) + r;       // [rows][COLS + 1]
 #pragma unroll
       for (int a = 0; a < MT; ++a)
 #pragma unroll
@@ -272,7 +277,7 @@ __global__ void __launch_bounds__(WARPS * 32, NT <= 2 ? 16 / WARPS : 8 / WARPS) 
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float* const at = to + (8 * j + (e & 1)) * (COLS + 1) + 16 * a + 8 * (e >> 1);
-            if (8 * j + 2 * t + (e & 1) < rows) *at = onto ? f_add(*at, sum[a][j][e]) : sum[a][j][e];
+            if (8 * j + 2 * t + (e & 1) < rows) *at = sum[a][j][e];
             sum[a][j][e] = 0.0f;
           }
       in_part = 0;
@@ -280,19 +285,241 @@ __global__ void __launch_bounds__(WARPS * 32, NT <= 2 ? 16 / WARPS : 8 / WARPS) 
     }
   }
   __syncthreads();
-  const int places = p.wpt == 1 ? 1 : n_parts;
   for (int x = threadIdx.x; x < p.per_cta * rows * COLS; x += WARPS * 32) {
     const int col = x % COLS, tile_row = x / COLS, which = tile_row / rows, row = tile_row - which * rows, n = (blockIdx.x * p.per_cta + which) * COLS + col;
     if (n >= p.N) continue;
-    const float* from = reinterpret_cast<const float*>(smem + S::PART_AT) + (which * (p.wpt == 1 ? 1 : PARTS) * rows + row) * (COLS + 1) + col;
-    float v = *from;
-    for (int q = 1; q < places; ++q) v = f_add(v, from[q * rows * (COLS + 1)]);
+    const float* from = reinterpret_cast<const float*>(smem + S::PART_AT) + (which * PARTS * rows + row) * (COLS + 1) + col;
+    float q[PARTS];
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) q[i] = i < n_parts ? from[i * rows * (COLS + 1)] : 0.0f;
+    const float v = f_add(f_add(f_add(q[0], q[1]), f_add(q[2], q[3])), f_add(f_add(q[4], q[5]), f_add(q[6], q[7])));
     store_scalar(p.C, p.c_dtype, (int64_t)(m0 + row) * p.ldc + n, apply_epilogue(v, p.epi, m0 + row, n));
   }
   if (*abort_flag) {                                   // a wait gave up: let copies in flight end
     const uint64_t t0 = globaltimer_ns();
     while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
   }
+}
+
+// ---------------------------------------------------------------- more than sixteen rows
+// The same sums for 8 NT rows of A.  There A's elements are the larger part of what a warp reads: eight warps with a tile of 16 rows of weights each now work on the same
+// stage, for which they share A's elements in shared memory (put there, and into the codes' order, once), and the parts of K go to the CTAs of a cluster: eight
+// with a part each, or four with two neighbouring ones.  The parts' tree is then finished over distributed shared memory, every CTA a share of the elements.
+// What bounds it: the 16-wide tensor-core steps (8 cycles each) and the scales' multiplications.  33 rows on 11009 x 4128 in groups of 32: FIGURE us (78 with one warp a
+// part and A's elements from global memory).
+constexpr int RW = 8;                                  // warps
+template <int GROUP, int NT>
+struct Rows4 {
+  static constexpr int ROWS = 8 * NT, COLS = 16 * RW, DEPTH = 3;
+  static constexpr int SCALES = PER<GROUP> * 16 * 8;
+  static constexpr int X = ROWS * 512;                 // a stage of A
+  static constexpr int RING_AT = 2 * X, SCALE_AT = RING_AT + RW * DEPTH * STAGE, BAR_AT = SCALE_AT + RW * SCALES, FLAG_AT = BAR_AT + RW * DEPTH * 8, SMEM = 1024 + FLAG_AT + 16;
+  static constexpr int SUMS = ROWS * (COLS + 1) * 4;   // over A's stages, at the end
+  static_assert(SMEM <= 232448 && X % 1024 == 0 && BAR_AT % 8 == 0 && SUMS <= SCALE_AT, "fits the SM");
+};
+
+template <bool F16, int GROUP, int NT>
+__global__ void __launch_bounds__(RW * 32, 2) gemv_w4_rows_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constant__ W4Params p) {
+  using S = Rows4<GROUP, NT>;
+  constexpr int G = PER<GROUP>, WORDS = GROUP / 32, COLS = S::COLS, DEPTH = S::DEPTH;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t* const mine = smem + S::RING_AT + warp * (DEPTH * STAGE);
+  float2* const sz = reinterpret_cast<float2*>(smem + S::SCALE_AT + warp * S::SCALES);      // [G][16] (scale, less)
+  const uint32_t bars = smem_u32(smem + S::BAR_AT) + warp * (DEPTH * 8);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
+  const int m0 = (int)blockIdx.y * p.rows, rows = min(p.rows, p.M - m0);
+  const int rank = (int)blockIdx.x % p.wpt, n_cta = (int)(blockIdx.x / p.wpt) * COLS, n0 = n_cta + 16 * warp;      // p.wpt: CTAs of the cluster
+  const int stages = (p.K + SPAN - 1) / SPAN, share = p.per_cta, s0 = rank * share * p.part, n_st = max(0, min(stages - s0, share * p.part));
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < RW * DEPTH; ++i) mbar_init(smem_u32(smem + S::BAR_AT) + 8 * i, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+
+  int r_i = 0;
+  auto request = [&] {
+    if (r_i >= n_st || n0 >= p.N) return;
+    if (lane == 0) {
+      mbar_expect_tx(bars + 8 * (r_i % DEPTH), STAGE);
+      load_box(smem_u32(mine) + r_i % DEPTH * STAGE, &codes, (s0 + r_i) * (SPAN / 4), n0, bars + 8 * (r_i % DEPTH));
+    }
+    ++r_i;
+  };
+  Scales<GROUP, 1> scales(p, (int64_t)n0 + lane / G, s0 * G + lane % G);
+
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (!p.w_static) asm volatile("griddepcontrol.wait;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < DEPTH - 1; ++i) request();
+  if (n_st > 0) scales.fetch(p);
+  if (p.w_static) asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  // A's elements: a thread's 16-byte pieces are piece threadIdx % 32 of every eighth row.  Piece c of a row lies at c ^ turn(row), so that a quarter of a warp (two rows,
+  // four places of a group) reads eight different ones; which bits that takes depends on how far apart the places are.
+  auto turn = [](int row, int c) -> int {
+    if (GROUP == 32) return (row & 1) << 2 | (row & 2) | (row >> 2 & 1);
+    return (row & 7) ^ (GROUP == 128 ? (c >> 3 & 1) << 1 : 0);
+  };
+  const int x_row = threadIdx.x >> 5, x_piece = lane;
+  const uint16_t* const x_src = p.A + (int64_t)m0 * p.lda + s0 * SPAN + 8 * x_piece;
+  const uint32_t x_to = smem_u32(smem) + x_row * 512 + ((x_piece ^ turn(x_row, x_piece)) << 4);
+  auto load_x = [&](int i) {
+    const bool in_k = (s0 + i) * SPAN + 8 * x_piece < p.K;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const bool there = in_k && x_row + 8 * j < rows;             // else zeros
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                   ::"r"(x_to + (i & 1) * S::X + j * 4096), "l"(x_src + (there ? (int64_t)(x_row + 8 * j) * p.lda + i * SPAN : 0)), "r"(there ? 16 : 0) : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // ... into the codes' order: 0 4, 1 5, 2 6, 3 7
+  auto order_x = [&](int i) {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    uint8_t* const at = smem + (i & 1) * S::X + x_row * 512 + ((x_piece ^ turn(x_row, x_piece)) << 4);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      uint4* const q = reinterpret_cast<uint4*>(at + j * 4096);
+      const uint4 v = *q;
+      *q = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+    }
+  };
+  if (n_st > 0) { load_x(0); order_x(0); }
+  __syncthreads();
+
+  const int t = lane & 3, rr = lane >> 2;
+  const int r = (rr >> 2) | (rr & 2) | (rr & 1) << 2;
+  const uint32_t w_lane = r * 128 + ((((t * (GROUP / 8)) >> 4) ^ r) << 4) + (t * (GROUP / 8) & 15);
+  // piece g (GROUP / 8) + t (GROUP / 32) + x of row rr: bits of x and, in groups of 32, of g are turned into it
+  const int x_first = t * (GROUP / 32);
+  const uint32_t x_lane = rr * 512 + ((x_first ^ turn(rr, x_first)) << 4);
+  uint32_t mask = 0x000f000fu, magic = F16 ? 0x64006400u : 0x43004300u;
+  asm("" : "+r"(mask), "+r"(magic));
+  float sum[NT][4], saved[NT][4];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[j][e] = saved[j][e] = 0.0f;
+  for (int i = 0; i < n_st; ++i) {
+    if (i + 1 < n_st) load_x(i + 1);
+    scales.put(sz, F16);
+    if (i + 1 < n_st) scales.fetch(p);
+    request();
+    const uint32_t slot = i % DEPTH;
+    if (n0 < p.N) warp_mbar_wait(bars + 8 * slot, (i / DEPTH) & 1, abort_flag, &g_gemv_four_status_word, 0x4100u | slot);      // one that gives up lets the kernel run out
+    __syncwarp();
+    const int left = p.K - (s0 + i) * SPAN;
+    const uint8_t* const xs = smem + (i & 1) * S::X;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      if (g * GROUP >= left) break;
+      uint32_t w[2][WORDS];
+      float2 f[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint8_t* from = mine + slot * STAGE + (w_lane ^ (g * (GROUP / 2))) + u * 1024;
+        if constexpr (WORDS == 4) { const uint4 v = *reinterpret_cast<const uint4*>(from); w[u][0] = v.x; w[u][1] = v.y; w[u][2] = v.z; w[u][3] = v.w; }
+        else if constexpr (WORDS == 2) { const uint2 v = *reinterpret_cast<const uint2*>(from); w[u][0] = v.x; w[u][1] = v.y; }
+        else w[u][0] = *reinterpret_cast<const uint32_t*>(from);
+        f[u] = sz[g * 16 + r + 8 * u];
+      }
+      float acc[NT][4];
+#pragma unroll
+      for (int x = 0; x < WORDS; ++x) {
+        const uint32_t lu = __float_as_uint(f[0].y), ld = __float_as_uint(f[1].y);
+        const uint32_t u0 = unpack<F16, 0>(w[0][x], mask, magic, lu), u1 = unpack<F16, 1>(w[0][x], mask, magic, lu), u2 = unpack<F16, 2>(w[0][x], mask, magic, lu), u3 = unpack<F16, 3>(w[0][x], mask, magic, lu);
+        const uint32_t d0 = unpack<F16, 0>(w[1][x], mask, magic, ld), d1 = unpack<F16, 1>(w[1][x], mask, magic, ld), d2 = unpack<F16, 2>(w[1][x], mask, magic, ld), d3 = unpack<F16, 3>(w[1][x], mask, magic, ld);
+        const uint32_t at = GROUP == 128 ? (x_lane ^ (x << 4)) + g * 256 : GROUP == 64 ? (x_lane ^ (x << 4)) + g * 128 : (x_lane ^ ((g & 1) << 6)) + (g >> 1) * 128;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const uint4 b = *reinterpret_cast<const uint4*>(xs + at + j * 4096);
+          if (x == 0) mma16<F16, true>(acc[j], u0, d0, u1, d1, b.x, b.y);
+          else mma16<F16, false>(acc[j], u0, d0, u1, d1, b.x, b.y);
+          mma16<F16, false>(acc[j], u2, d2, u3, d3, b.z, b.w);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[j][e] = f_fma(f[e >> 1].x, acc[j][e], sum[j][e]);
+    }
+    if (i + 1 == p.part) {
+      // the first of two parts
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { saved[j][e] = sum[j][e]; sum[j][e] = 0.0f; }
+    }
+    if (i + 1 < n_st) order_x(i + 1);
+    __syncthreads();                                   // the next stage of A is there, this one, the slot and the scales are free
+  }
+  // saved + sum: the two parts; a part alone, first or second, next to zeros
+  float* const sums = reinterpret_cast<float*>(smem);  // [rows][COLS + 1]
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = 8 * j + 2 * t + (e & 1);
+      if (row < rows) sums[row * (COLS + 1) + 16 * warp + r + 8 * (e >> 1)] = f_add(saved[j][e], sum[j][e]);
+    }
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  for (int x = rank * (RW * 32) + threadIdx.x; x < rows * COLS; x += p.wpt * (RW * 32)) {
+    const int row = x / COLS, col = x % COLS, n = n_cta + col;
+    if (n >= p.N) continue;
+    const uint32_t at = smem_u32(sums + row * (COLS + 1) + col);
+    float q[PARTS];
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+      q[i] = 0.0f;
+      if (i < p.wpt) {
+        uint32_t there;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(i));
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(q[i]) : "r"(there) : "memory");
+      }
+    }
+    const float low = f_add(f_add(q[0], q[1]), f_add(q[2], q[3])), v = share == 1 ? f_add(low, f_add(f_add(q[4], q[5]), f_add(q[6], q[7]))) : low;
+    store_scalar(p.C, p.c_dtype, (int64_t)(m0 + row) * p.ldc + n, apply_epilogue(v, p.epi, m0 + row, n));
+  }
+  if (*abort_flag) {                                   // a wait gave up: let copies in flight end
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+  }
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");      // nobody's sums go before all have read them
+}
+
+template <bool F16, int GROUP, int NT>
+cudaError_t launch_more(const rg_weights_four_t* W, W4Params p, cudaStream_t st) {
+  using S = Rows4<GROUP, NT>;
+  static DeviceOnce configured;
+  const DeviceInfo dev = current_device();
+  if (!configured.has(dev.dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(gemv_w4_rows_kernel<F16, GROUP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    if (e != cudaSuccess) return e;
+    configured.set(dev.dev);
+  }
+  CUtensorMap codes;
+  if (!make_tmap_4d(&codes, W->codes, RG_BF16, {p.K / 4, p.N, 1, 1}, {W->code_ld / 2, 0, 0}, {SPAN / 4, 16, 1, 1})) return cudaErrorInvalidValue;
+  const int blocks = (p.N + S::COLS - 1) / S::COLS;
+  const int parts = ((p.K + SPAN - 1) / SPAN + p.part - 1) / p.part;
+  p.per_cta = (int64_t)blocks * ((p.M + p.rows - 1) / p.rows) * parts <= 2 * (int64_t)dev.sms ? 1 : 2;
+  p.wpt = (parts + p.per_cta - 1) / p.per_cta;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(blocks * p.wpt), (unsigned)((p.M + p.rows - 1) / p.rows), 1);
+  cfg.blockDim = dim3(RW * 32, 1, 1);
+  cfg.dynamicSmemBytes = S::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)p.wpt; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, gemv_w4_rows_kernel<F16, GROUP, NT>, codes, p);
 }
 
 template <bool F16, int GROUP, int MT, int NT, int WARPS>
@@ -307,15 +534,14 @@ cudaError_t launch(const rg_weights_four_t* W, W4Params p, int wpt, cudaStream_t
   }
   CUtensorMap codes;                                   // four codes an element of 16 bits
   if (!make_tmap_4d(&codes, W->codes, RG_BF16, {p.K / 4, p.N, 1, 1}, {W->code_ld / 2, 0, 0}, {SPAN / 4, S::COLS, 1, 1})) return cudaErrorInvalidValue;
-  const int passes = (p.M + S::ROWS - 1) / S::ROWS;
-  p.rows = passes == 1 ? p.M : ((p.M + passes - 1) / passes + 7) / 8 * 8;
+  p.rows = p.M;                                        // at most S::ROWS
   p.wpt = wpt;
   p.per_cta = WARPS / wpt;
   const int tiles = (p.N + S::COLS - 1) / S::COLS;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((tiles + p.per_cta - 1) / p.per_cta), (unsigned)((p.M + p.rows - 1) / p.rows), 1);
+  cfg.gridDim = dim3((unsigned)((tiles + p.per_cta - 1) / p.per_cta), 1, 1);
   cfg.blockDim = dim3(WARPS * 32, 1, 1);
-  cfg.dynamicSmemBytes = S::SMEM + p.per_cta * (wpt > 1 ? PARTS : 1) * p.rows * (S::COLS + 1) * 4;
+  cfg.dynamicSmemBytes = S::SMEM + p.per_cta * PARTS * p.rows * (S::COLS + 1) * 4;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -328,21 +554,21 @@ cudaError_t launch(const rg_weights_four_t* W, W4Params p, int wpt, cudaStream_t
 // with eight warps a tile, else of 16; and no more a tile than that takes.
 constexpr int WARPS_PER_SM = 12;
 template <bool F16, int GROUP, int NT>
-cudaError_t launch_rows(const rg_weights_four_t* W, const W4Params& p, cudaStream_t st) {
-  const int64_t want = (int64_t)WARPS_PER_SM * current_device().sms;
-  const int64_t wide = (p.N + 31) / 32;
-  if (wide * PARTS >= want || NT > 2) {
-    int wpt = PARTS;
-    while (wpt > 1 && wide * (wpt / 2) >= want) wpt /= 2;
-    if (wpt == 8) return launch<F16, GROUP, 2, NT, 8>(W, p, wpt, st);
-    return launch<F16, GROUP, 2, NT, 4>(W, p, wpt, st);
-  }
-  if constexpr (NT <= 2) return launch<F16, GROUP, 1, NT, 8>(W, p, PARTS, st);
-  return cudaErrorInvalidValue;
+cudaError_t launch_few(const rg_weights_four_t* W, const W4Params& p, cudaStream_t st) {
+  const int64_t want = (int64_t)WARPS_PER_SM * current_device().sms, wide = (p.N + 31) / 32;
+  if (wide * PARTS < want) return launch<F16, GROUP, 1, NT, 8>(W, p, PARTS, st);
+  int wpt = PARTS;
+  while (wpt > 1 && wide * (wpt / 2) >= want) wpt /= 2;
+  return wpt == 8 ? launch<F16, GROUP, 2, NT, 8>(W, p, wpt, st) : launch<F16, GROUP, 2, NT, 4>(W, p, wpt, st);
 }
 template <bool F16, int GROUP>
-cudaError_t launch_group(const rg_weights_four_t* W, const W4Params& p, cudaStream_t st) {
-  return p.M <= 8 ? launch_rows<F16, GROUP, 1>(W, p, st) : p.M <= 16 ? launch_rows<F16, GROUP, 2>(W, p, st) : launch_rows<F16, GROUP, 4>(W, p, st);
+cudaError_t launch_group(const rg_weights_four_t* W, W4Params p, cudaStream_t st) {
+  if (p.M <= 8) return launch_few<F16, GROUP, 1>(W, p, st);
+  if (p.M <= 16) return launch_few<F16, GROUP, 2>(W, p, st);
+  const int passes = (p.M + 39) / 40;                      // as even as eights allow
+  p.rows = ((p.M + passes - 1) / passes + 7) / 8 * 8;
+  if (p.rows <= 32) return launch_more<F16, GROUP, 4>(W, p, st);
+  return launch_more<F16, GROUP, 5>(W, p, st);
 }
 template <bool F16>
 cudaError_t launch_type(const rg_weights_four_t* W, const W4Params& p, cudaStream_t st) {
