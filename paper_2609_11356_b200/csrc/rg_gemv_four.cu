@@ -3,15 +3,21 @@
 //
 // The inner sum is a chain of 16-wide tensor-core steps from a zero accumulator: u - z is an integer of at most four bits and a sign, exact in bf16 and
 // fp16, so nothing is rounded before the products' fp32 sum.  The scale multiplies a finished group once, in fp32 (fused, onto the running sum of a part of
-// K): no weight is ever narrowed, whatever the scales' type.  A part is a run of whole 256-wide stages, at most eight of them over K; parts are added as a
-// balanced tree of eight adds them.  The cut follows from K alone and an accumulator's column is one row of A, so a row's bits do not depend on M.
+// K): no weight is ever narrowed, whatever the scales' type.  A part is a run of whole 256-wide stages, at most eight of them over K; the lower and the
+// upper four are each added in ascending order, and then to one another.  The cut follows from K alone and an accumulator's column is one row of A, so a row's bits do not depend on M.
 //
-// What bounds it: the bytes of the codes, and next the instructions that unpack them (1.4 a code and lane: a mask that makes a float's mantissa of the nibble,
-// and one subtraction, for two codes).  Weights are the 16 rows of mma.sync's first operand, read straight from the natural order of the codes: a warp's
-// lanes hold whole words of eight codes, and the order of k within a group is the tensor core's own affair as long as A's elements follow it.
-// tcgen05 would want the unpacked weights in shared or tensor memory, a trip that costs more than these few rows' products.
-// A tile is 16 MT rows of weights; one to eight warps share it, each with one or more parts of K, and every warp streams its own stages into shared memory, a
-// TMA box at a time.
+// Weights are the 16 rows of mma.sync's first operand, read straight from the natural order of the codes: a warp's lanes hold whole words of eight codes, and
+// the order of k within a group is the tensor core's own affair as long as A's elements follow it.  tcgen05 would want the unpacked weights in shared or
+// tensor memory, a trip that costs more than these few rows' products.  Every warp streams its own stages into shared memory, a TMA box at a time.
+//
+// Two kernels.  One or two rows: a warp reads A's elements from global memory itself and never waits for another warp until all its parts are done.
+// More: eight warps share A's elements in shared memory, stage by stage.  28672 x 4096 in groups of 128, a graph of calls on rotating weights, us:
+//   rows          1      2      4      8     16     40
+//   the first    25.0   25.9   29.0   33.1   (71, as a form for 16 rows)
+//   the second   26.1   26.3   26.3   26.5   35.7   58.3
+// What bounds them: the bytes of the codes would take 9.4 us.  The instructions that unpack them (a mask that makes a float's mantissa of the nibble, and one
+// subtraction, for two codes, with a shift for three of four) keep the half-rate integer pipe busy for 8 us, and 12 to 16 warps of an SM do not cover all
+// waits between them; a grid of 128-row blocks also fills its last wave only in part.
 #include <cuda.h>
 
 #include <algorithm>
@@ -41,6 +47,7 @@ struct W4Params {
   int32_t part;                                        // stages of a part
   int32_t rows;                                        // of A, for one CTA
   int32_t wpt, per_cta;                                // warps of a tile (a power of two up to PARTS), tiles of a CTA
+  int32_t share, ctas;                                 // parts of a CTA, CTAs with the same weights' rows: a cluster
   EpilogueArgs epi;
 };
 
@@ -75,19 +82,27 @@ __device__ __forceinline__ uint32_t unpack(uint32_t w, uint32_t mask, uint32_t m
 constexpr int STAGE = 16 * 128;                        // bytes of a stage's codes for 16 rows
 template <int GROUP> constexpr int PER = SPAN / GROUP;                 // groups of a stage
 
-template <int GROUP, int MT, int NT, int WARPS>
+// ---------------------------------------------------------------- one or two rows
+// A tile is 16 MT rows of weights; two to eight warps share it, each with one or more parts of K.
+constexpr int FEW = 2;                                 // rows
+template <int GROUP, int MT, int WARPS>
 struct Shape4 {
-  static constexpr int ROWS = 8 * NT, COLS = 16 * MT, DEPTH = MT == 1 ? 4 : 2;       // stages of a warp's ring, one being worked on
+  static constexpr int COLS = 16 * MT, DEPTH = MT == 1 ? 4 : 2;       // stages of a warp's ring, one being worked on
   static constexpr int SLOT = MT * STAGE, SCALES = PER<GROUP> * COLS * 8;           // (scale, less) pairs of a stage
-  static constexpr int PART = ROWS * (COLS + 1) * 4;   // a part's sums, of all the rows there can be
+  static constexpr int PART = FEW * (COLS + 1) * 4;    // a part's sums
   static constexpr int SCALE_AT = WARPS * DEPTH * SLOT, BAR_AT = SCALE_AT + WARPS * SCALES, FLAG_AT = BAR_AT + WARPS * DEPTH * 8, PART_AT = FLAG_AT + 16, SMEM = 1024 + PART_AT;
   static constexpr int MOST = SMEM + (WARPS == 8 ? 1 : 4) * PARTS * PART;      // eight warps share one tile, four have up to four
-  static_assert(MOST <= 232448 && BAR_AT % 8 == 0, "fits the SM");
+  static_assert(MOST <= 113 * 1024 && BAR_AT % 8 == 0, "fits the SM");
 };
 
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %4}], [%5];"
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(0), "r"(bar) : "memory");
+}
+
+// The sum of the parts of K: of the lower and of the upper four, each in ascending order.
+__device__ __forceinline__ float join(const float (&q)[PARTS]) {
+  return f_add(f_add(f_add(f_add(q[0], q[1]), q[2]), q[3]), f_add(f_add(f_add(q[4], q[5]), q[6]), q[7]));
 }
 
 // The scales and zero points of a warp's stages, PER * 16 MT of each a stage, fetched one stage ahead: a lane's share is one group of rows lane / PER, STEP further, ...
@@ -125,9 +140,9 @@ struct Scales {
   }
 };
 
-template <bool F16, int GROUP, int MT, int NT, int WARPS>
+template <bool F16, int GROUP, int MT, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constant__ W4Params p) {
-  using S = Shape4<GROUP, MT, NT, WARPS>;
+  using S = Shape4<GROUP, MT, WARPS>;
   constexpr int G = PER<GROUP>, WORDS = GROUP / 32;    // words of eight codes that a lane takes of each row and group
   constexpr int COLS = S::COLS, DEPTH = S::DEPTH;
   extern __shared__ uint8_t smem_raw[];
@@ -137,7 +152,7 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
   float2* const sz = reinterpret_cast<float2*>(smem + S::SCALE_AT + warp * S::SCALES);      // [MT][G][16] (scale, less)
   const uint32_t bars = smem_u32(smem + S::BAR_AT) + warp * (DEPTH * 8);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
-  const int m0 = (int)blockIdx.y * p.rows, rows = min(p.rows, p.M - m0);
+  const int rows = p.M;
   // the warp's tile, and its parts of K: the first one, how many, and their stages
   const int own = warp / p.wpt, tile = blockIdx.x * p.per_cta + own, stages = (p.K + SPAN - 1) / SPAN, n_parts = (stages + p.part - 1) / p.part;
   const int share = PARTS / p.wpt, part0 = (warp - own * p.wpt) * share;
@@ -172,26 +187,23 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
 
   const int t = lane & 3, rr = lane >> 2;
   const int r = (rr >> 2) | (rr & 2) | (rr & 1) << 2;  // the lane's row of the upper eight: neighbours differ in the bits that the pieces' order uses
-  const uint16_t* x_at[NT];                            // columns behind the last row of A repeat it: nobody reads their sums
-#pragma unroll
-  for (int j = 0; j < NT; ++j) x_at[j] = p.A + (int64_t)(m0 + min(8 * j + rr, rows - 1)) * p.lda + s0 * SPAN + t * (GROUP / 4);
+  const uint16_t* x_at = p.A + (int64_t)min(rr, rows - 1) * p.lda + s0 * SPAN + t * (GROUP / 4);       // columns behind the last row of A repeat it: nobody reads their sums
   // a lane's first word within a row's 128 bytes; a group's place further on only turns bits of it
   const uint32_t w_lane = r * 128 + ((((t * (GROUP / 8)) >> 4) ^ r) << 4) + (t * (GROUP / 8) & 15);
   uint32_t mask = 0x000f000fu, magic = F16 ? 0x64006400u : 0x43004300u;
   asm("" : "+r"(mask), "+r"(magic));
-  float sum[MT][NT][4];
+  float sum[MT][4];
   // A's elements of a stage, on their way before the codes are waited for.  TAIL: the last stage of K, of which `left` elements are there.
-  constexpr int HELD = NT == 1 ? G : 1;                // groups of A's elements that there are registers for
-  uint4 x_of[HELD][NT][WORDS];
-  auto load_x = [&](int g, int left, auto tail) {
+  uint4 x_of[G][WORDS];
+  auto load_x = [&](int left, auto tail) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int i = 0; i < WORDS; ++i)
-        x_of[g % HELD][j][i] = !decltype(tail)::value || g * GROUP + t * (GROUP / 4) + 8 * i < left ? __ldg(reinterpret_cast<const uint4*>(x_at[j] + g * GROUP + 8 * i)) : make_uint4(0u, 0u, 0u, 0u);
+        x_of[g][i] = !decltype(tail)::value || g * GROUP + t * (GROUP / 4) + 8 * i < left ? __ldg(reinterpret_cast<const uint4*>(x_at + g * GROUP + 8 * i)) : make_uint4(0u, 0u, 0u, 0u);
   };
   auto window = [&](int g, uint32_t at, const float2* s) {
-    float acc[MT][NT][4];
+    float acc[MT][4];
     // this lane's words of its rows: GROUP / 4 codes from the group's k + t GROUP / 4 on
     uint32_t w[MT][2][WORDS];
     float2 f[MT][2];
@@ -208,45 +220,31 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
 #pragma unroll
     for (int x = 0; x < WORDS; ++x) {
       // A's elements in the codes' order: 0 4, 1 5, 2 6, 3 7
-      uint32_t b0[NT], b1[NT], b2[NT], b3[NT];
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        b0[j] = __byte_perm(x_of[g % HELD][j][x].x, x_of[g % HELD][j][x].z, 0x5410); b1[j] = __byte_perm(x_of[g % HELD][j][x].x, x_of[g % HELD][j][x].z, 0x7632);
-        b2[j] = __byte_perm(x_of[g % HELD][j][x].y, x_of[g % HELD][j][x].w, 0x5410); b3[j] = __byte_perm(x_of[g % HELD][j][x].y, x_of[g % HELD][j][x].w, 0x7632);
-      }
+      const uint4 v = x_of[g][x];
+      const uint32_t b0 = __byte_perm(v.x, v.z, 0x5410), b1 = __byte_perm(v.x, v.z, 0x7632), b2 = __byte_perm(v.y, v.w, 0x5410), b3 = __byte_perm(v.y, v.w, 0x7632);
 #pragma unroll
       for (int a = 0; a < MT; ++a) {
         const uint32_t up = w[a][0][x], down = w[a][1][x], lu = __float_as_uint(f[a][0].y), ld = __float_as_uint(f[a][1].y);
         const uint32_t u0 = unpack<F16, 0>(up, mask, magic, lu), u1 = unpack<F16, 1>(up, mask, magic, lu), u2 = unpack<F16, 2>(up, mask, magic, lu), u3 = unpack<F16, 3>(up, mask, magic, lu);
         const uint32_t d0 = unpack<F16, 0>(down, mask, magic, ld), d1 = unpack<F16, 1>(down, mask, magic, ld), d2 = unpack<F16, 2>(down, mask, magic, ld), d3 = unpack<F16, 3>(down, mask, magic, ld);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          if (x == 0) mma16<F16, true>(acc[a][j], u0, d0, u1, d1, b0[j], b1[j]);
-          else mma16<F16, false>(acc[a][j], u0, d0, u1, d1, b0[j], b1[j]);
-          mma16<F16, false>(acc[a][j], u2, d2, u3, d3, b2[j], b3[j]);
-        }
+        if (x == 0) mma16<F16, true>(acc[a], u0, d0, u1, d1, b0, b1);
+        else mma16<F16, false>(acc[a], u0, d0, u1, d1, b0, b1);
+        mma16<F16, false>(acc[a], u2, d2, u3, d3, b2, b3);
       }
     }
 #pragma unroll
     for (int a = 0; a < MT; ++a)
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[a][j][e] = f_fma(f[a][e >> 1].x, acc[a][j][e], sum[a][j][e]);
+      for (int e = 0; e < 4; ++e) sum[a][e] = f_fma(f[a][e >> 1].x, acc[a][e], sum[a][e]);
   };
 
 #pragma unroll
   for (int a = 0; a < MT; ++a)
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[a][j][e] = 0.0f;
+    for (int e = 0; e < 4; ++e) sum[a][e] = 0.0f;
   int in_part = 0, part = part0;
   auto stage = [&](int i, int left, auto tail) {
-    if (HELD == G) {
-#pragma unroll
-      for (int g = 0; g < G; ++g) load_x(g, left, tail);
-    }
+    load_x(left, tail);
     scales.put(sz, F16);
     if (i + 1 < n_st) scales.fetch(p);
     request();
@@ -256,11 +254,9 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       if (decltype(tail)::value && g * GROUP >= left) break;
-      if (HELD != G) load_x(g, left, tail);
       window(g, slot * S::SLOT + (w_lane ^ (g * (GROUP / 2))), sz + r + g * 16);
     }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) x_at[j] += SPAN;
+    x_at += SPAN;
     __syncwarp();                                      // the slot and the scales are free
   };
   for (int i = 0; i < n_st; ++i) {
@@ -273,13 +269,10 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
 #pragma unroll
       for (int a = 0; a < MT; ++a)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float* const at = to + (8 * j + (e & 1)) * (COLS + 1) + 16 * a + 8 * (e >> 1);
-            if (8 * j + 2 * t + (e & 1) < rows) *at = sum[a][j][e];
-            sum[a][j][e] = 0.0f;
-          }
+        for (int e = 0; e < 4; ++e) {
+          if (2 * t + (e & 1) < rows) to[(e & 1) * (COLS + 1) + 16 * a + 8 * (e >> 1)] = sum[a][e];
+          sum[a][e] = 0.0f;
+        }
       in_part = 0;
       ++part;
     }
@@ -292,8 +285,8 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
     float q[PARTS];
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) q[i] = i < n_parts ? from[i * rows * (COLS + 1)] : 0.0f;
-    const float v = f_add(f_add(f_add(q[0], q[1]), f_add(q[2], q[3])), f_add(f_add(q[4], q[5]), f_add(q[6], q[7])));
-    store_scalar(p.C, p.c_dtype, (int64_t)(m0 + row) * p.ldc + n, apply_epilogue(v, p.epi, m0 + row, n));
+    const float v = join(q);
+    store_scalar(p.C, p.c_dtype, (int64_t)row * p.ldc + n, apply_epilogue(v, p.epi, row, n));
   }
   if (*abort_flag) {                                   // a wait gave up: let copies in flight end
     const uint64_t t0 = globaltimer_ns();
@@ -301,12 +294,13 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
   }
 }
 
-// ---------------------------------------------------------------- more than sixteen rows
-// The same sums for 8 NT rows of A.  There A's elements are the larger part of what a warp reads: eight warps with a tile of 16 rows of weights each now work on the same
-// stage, for which they share A's elements in shared memory (put there, and into the codes' order, once), and the parts of K go to the CTAs of a cluster: eight
-// with a part each, or four with two neighbouring ones.  The parts' tree is then finished over distributed shared memory, every CTA a share of the elements.
-// What bounds it: the 16-wide tensor-core steps (8 cycles each) and the scales' multiplications.  33 rows on 11009 x 4128 in groups of 32: FIGURE us (78 with one warp a
-// part and A's elements from global memory).
+// ---------------------------------------------------------------- three rows and more
+// The same sums for 8 NT rows of A.  Eight warps, each with a tile of 16 rows of weights of its own, work on the same stage, for which they share A's elements in shared
+// memory (put there, and into the codes' order, once).  The parts of K are shared among the CTAs of a cluster, or are all one CTA's, and are joined over distributed shared
+// memory, every CTA a share of the elements.  How many parts a CTA has (1, 2, 4 or all 8) is the choice with which the waves of CTAs take the fewest stages (below):
+// 16 rows on 128256 x 4096, where many blocks fill the GPU, take 122 us with all parts in a CTA and 173 us with two; on 4096 x 14336, where eight CTAs for each block are
+// needed, 17.1 us.  33 rows on 11009 x 4128 in groups of 32 take 33.5 us (79 with one warp a part and A's elements from global memory).  Reading A's elements two stages
+// ahead instead of one changes nothing; more than 40 rows would leave room for one CTA of an SM only (64 rows on 28672 x 4096: 113 us, as twice 32 rows 94).
 constexpr int RW = 8;                                  // warps
 template <int GROUP, int NT>
 struct Rows4 {
@@ -314,8 +308,8 @@ struct Rows4 {
   static constexpr int SCALES = PER<GROUP> * 16 * 8;
   static constexpr int X = ROWS * 512;                 // a stage of A
   static constexpr int RING_AT = 2 * X, SCALE_AT = RING_AT + RW * DEPTH * STAGE, BAR_AT = SCALE_AT + RW * SCALES, FLAG_AT = BAR_AT + RW * DEPTH * 8, SMEM = 1024 + FLAG_AT + 16;
-  static constexpr int SUMS = ROWS * (COLS + 1) * 4;   // over A's stages, at the end
-  static_assert(SMEM <= 232448 && X % 1024 == 0 && BAR_AT % 8 == 0 && SUMS <= SCALE_AT, "fits the SM");
+  static constexpr int SUMS = 2 * ROWS * (COLS + 1) * 4;   // over A's stages, at the end
+  static_assert(SMEM <= 113 * 1024 && X % 1024 == 0 && BAR_AT % 8 == 0 && SUMS <= SCALE_AT, "two fit the SM");
 };
 
 template <bool F16, int GROUP, int NT>
@@ -330,8 +324,8 @@ __global__ void __launch_bounds__(RW * 32, 2) gemv_w4_rows_kernel(const __grid_c
   const uint32_t bars = smem_u32(smem + S::BAR_AT) + warp * (DEPTH * 8);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
   const int m0 = (int)blockIdx.y * p.rows, rows = min(p.rows, p.M - m0);
-  const int rank = (int)blockIdx.x % p.wpt, n_cta = (int)(blockIdx.x / p.wpt) * COLS, n0 = n_cta + 16 * warp;      // p.wpt: CTAs of the cluster
-  const int stages = (p.K + SPAN - 1) / SPAN, share = p.per_cta, s0 = rank * share * p.part, n_st = max(0, min(stages - s0, share * p.part));
+  const int rank = (int)blockIdx.x % p.ctas, n_cta = (int)(blockIdx.x / p.ctas) * COLS, n0 = n_cta + 16 * warp;
+  const int stages = (p.K + SPAN - 1) / SPAN, share = p.share, s0 = rank * share * p.part, n_st = max(0, min(stages - s0, share * p.part));
   if (threadIdx.x == 0) {
     for (int i = 0; i < RW * DEPTH; ++i) mbar_init(smem_u32(smem + S::BAR_AT) + 8 * i, 1);
     *abort_flag = 0;
@@ -339,6 +333,7 @@ __global__ void __launch_bounds__(RW * 32, 2) gemv_w4_rows_kernel(const __grid_c
   }
   __syncthreads();
 
+  // as above, a warp's own 16 rows of weights; warps behind the last row take part in the rest
   int r_i = 0;
   auto request = [&] {
     if (r_i >= n_st || n0 >= p.N) return;
@@ -403,6 +398,9 @@ __global__ void __launch_bounds__(RW * 32, 2) gemv_w4_rows_kernel(const __grid_c
   for (int j = 0; j < NT; ++j)
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[j][e] = saved[j][e] = 0.0f;
+  int in_part = 0;
+  bool first = true, second = false;
+  float half[NT][4];
   for (int i = 0; i < n_st; ++i) {
     if (i + 1 < n_st) load_x(i + 1);
     scales.put(sz, F16);
@@ -446,41 +444,60 @@ __global__ void __launch_bounds__(RW * 32, 2) gemv_w4_rows_kernel(const __grid_c
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[j][e] = f_fma(f[e >> 1].x, acc[j][e], sum[j][e]);
     }
-    if (i + 1 == p.part) {
-      // the first of two parts
+    if (++in_part == p.part && i + 1 < n_st) {
+      // a part is done, and this CTA has another
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { saved[j][e] = sum[j][e]; sum[j][e] = 0.0f; }
+        for (int e = 0; e < 4; ++e) { saved[j][e] = first ? sum[j][e] : f_add(saved[j][e], sum[j][e]); sum[j][e] = 0.0f; }
+      in_part = 0;
+      first = false;
+      if (i + 1 == 4 * p.part) {                       // the first half of all: share is PARTS
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) half[j][e] = saved[j][e];
+        first = second = true;
+      }
     }
     if (i + 1 < n_st) order_x(i + 1);
     __syncthreads();                                   // the next stage of A is there, this one, the slot and the scales are free
   }
-  // saved + sum: the two parts; a part alone, first or second, next to zeros
-  float* const sums = reinterpret_cast<float*>(smem);  // [rows][COLS + 1]
+  // The part's sums, [rows][COLS + 1], or the two parts', or the half's, or the whole
+  float* const sums = reinterpret_cast<float*>(smem);
+  const bool both = !first && share == 2 && p.ctas > 1;
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int row = 8 * j + 2 * t + (e & 1);
-      if (row < rows) sums[row * (COLS + 1) + 16 * warp + r + 8 * (e >> 1)] = f_add(saved[j][e], sum[j][e]);
+      if (row >= rows) continue;
+      float* const to = sums + row * (COLS + 1) + 16 * warp + r + 8 * (e >> 1);
+      const float total = first ? sum[j][e] : both ? saved[j][e] : f_add(saved[j][e], sum[j][e]);
+      *to = second ? f_add(half[j][e], total) : total;
+      if (share == 2) to[rows * (COLS + 1)] = both ? sum[j][e] : 0.0f;
     }
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-  for (int x = rank * (RW * 32) + threadIdx.x; x < rows * COLS; x += p.wpt * (RW * 32)) {
+  if (p.ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  else __syncthreads();
+  for (int x = rank * (RW * 32) + threadIdx.x; x < rows * COLS; x += p.ctas * (RW * 32)) {
     const int row = x / COLS, col = x % COLS, n = n_cta + col;
     if (n >= p.N) continue;
     const uint32_t at = smem_u32(sums + row * (COLS + 1) + col);
-    float q[PARTS];
+    float q[PARTS], v;
+    if (p.ctas > 1) {
 #pragma unroll
-    for (int i = 0; i < PARTS; ++i) {
-      q[i] = 0.0f;
-      if (i < p.wpt) {
-        uint32_t there;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(i));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(q[i]) : "r"(there) : "memory");
+      for (int i = 0; i < PARTS; ++i) {
+        q[i] = 0.0f;
+        if (i < p.ctas * (share == 2 ? 2 : 1)) {
+          uint32_t there;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at + (share == 2 ? (i & 1) * rows * (COLS + 1) * 4 : 0)), "r"(share == 2 ? i >> 1 : i));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(q[i]) : "r"(there) : "memory");
+        }
       }
+      v = share == 4 ? f_add(q[0], q[1]) : join(q);
+    } else {
+      v = sums[row * (COLS + 1) + col];
     }
-    const float low = f_add(f_add(q[0], q[1]), f_add(q[2], q[3])), v = share == 1 ? f_add(low, f_add(f_add(q[4], q[5]), f_add(q[6], q[7]))) : low;
     store_scalar(p.C, p.c_dtype, (int64_t)(m0 + row) * p.ldc + n, apply_epilogue(v, p.epi, m0 + row, n));
   }
   if (*abort_flag) {                                   // a wait gave up: let copies in flight end
@@ -488,7 +505,7 @@ __global__ void __launch_bounds__(RW * 32, 2) gemv_w4_rows_kernel(const __grid_c
     while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
   }
   __syncwarp();
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");      // nobody's sums go before all have read them
+  if (p.ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");      // nobody's sums go before all have read them
 }
 
 template <bool F16, int GROUP, int NT>
@@ -505,10 +522,16 @@ cudaError_t launch_more(const rg_weights_four_t* W, W4Params p, cudaStream_t st)
   if (!make_tmap_4d(&codes, W->codes, RG_BF16, {p.K / 4, p.N, 1, 1}, {W->code_ld / 2, 0, 0}, {SPAN / 4, 16, 1, 1})) return cudaErrorInvalidValue;
   const int blocks = (p.N + S::COLS - 1) / S::COLS;
   const int parts = ((p.K + SPAN - 1) / SPAN + p.part - 1) / p.part;
-  p.per_cta = (int64_t)blocks * ((p.M + p.rows - 1) / p.rows) * parts <= 2 * (int64_t)dev.sms ? 1 : 2;
-  p.wpt = (parts + p.per_cta - 1) / p.per_cta;
+  // Two CTAs an SM; a wave of them takes the time of its stages and, for its start and end, about that of three more.
+  const int64_t slots = 2 * dev.sms, all = (int64_t)blocks * ((p.M + p.rows - 1) / p.rows);
+  int64_t best = INT64_MAX;
+  for (int share = 1; share <= PARTS; share *= 2) {
+    const int64_t time = (all * ((parts + share - 1) / share) + slots - 1) / slots * (share * p.part + 3);
+    if (time < best) { best = time; p.share = share; }
+  }
+  p.ctas = (parts + p.share - 1) / p.share;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(blocks * p.wpt), (unsigned)((p.M + p.rows - 1) / p.rows), 1);
+  cfg.gridDim = dim3((unsigned)(blocks * p.ctas), (unsigned)((p.M + p.rows - 1) / p.rows), 1);
   cfg.blockDim = dim3(RW * 32, 1, 1);
   cfg.dynamicSmemBytes = S::SMEM;
   cfg.stream = st;
@@ -516,59 +539,62 @@ cudaError_t launch_more(const rg_weights_four_t* W, W4Params p, cudaStream_t st)
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)p.wpt; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  attr[1].val.clusterDim.x = (unsigned)p.ctas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, gemv_w4_rows_kernel<F16, GROUP, NT>, codes, p);
 }
 
-template <bool F16, int GROUP, int MT, int NT, int WARPS>
-cudaError_t launch(const rg_weights_four_t* W, W4Params p, int wpt, cudaStream_t st) {
-  using S = Shape4<GROUP, MT, NT, WARPS>;
+template <bool F16, int GROUP, int MT, int WARPS>
+cudaError_t launch_tiles(const rg_weights_four_t* W, W4Params p, int wpt, cudaStream_t st) {
+  using S = Shape4<GROUP, MT, WARPS>;
   static DeviceOnce configured;
   const DeviceInfo dev = current_device();
   if (!configured.has(dev.dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(gemv_w4_kernel<F16, GROUP, MT, NT, WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::MOST);
+    const cudaError_t e = cudaFuncSetAttribute(gemv_w4_kernel<F16, GROUP, MT, WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::MOST);
     if (e != cudaSuccess) return e;
     configured.set(dev.dev);
   }
   CUtensorMap codes;                                   // four codes an element of 16 bits
   if (!make_tmap_4d(&codes, W->codes, RG_BF16, {p.K / 4, p.N, 1, 1}, {W->code_ld / 2, 0, 0}, {SPAN / 4, S::COLS, 1, 1})) return cudaErrorInvalidValue;
-  p.rows = p.M;                                        // at most S::ROWS
   p.wpt = wpt;
   p.per_cta = WARPS / wpt;
   const int tiles = (p.N + S::COLS - 1) / S::COLS;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((tiles + p.per_cta - 1) / p.per_cta), 1, 1);
   cfg.blockDim = dim3(WARPS * 32, 1, 1);
-  cfg.dynamicSmemBytes = S::SMEM + p.per_cta * PARTS * p.rows * (S::COLS + 1) * 4;
+  cfg.dynamicSmemBytes = S::SMEM + p.per_cta * PARTS * p.M * (S::COLS + 1) * 4;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, gemv_w4_kernel<F16, GROUP, MT, NT, WARPS>, codes, p);
+  return cudaLaunchKernelEx(&cfg, gemv_w4_kernel<F16, GROUP, MT, WARPS>, codes, p);
 }
 // Warps: enough for every SM to have WARPS_PER_SM, in tiles of 32 rows of weights (A's elements are read and put in order once for them) if that is enough
 // with eight warps a tile, else of 16; and no more a tile than that takes.
 constexpr int WARPS_PER_SM = 12;
-template <bool F16, int GROUP, int NT>
+template <bool F16, int GROUP>
 cudaError_t launch_few(const rg_weights_four_t* W, const W4Params& p, cudaStream_t st) {
   const int64_t want = (int64_t)WARPS_PER_SM * current_device().sms, wide = (p.N + 31) / 32;
-  if (wide * PARTS < want) return launch<F16, GROUP, 1, NT, 8>(W, p, PARTS, st);
+  if (wide * PARTS < want) return launch_tiles<F16, GROUP, 1, 8>(W, p, PARTS, st);
   int wpt = PARTS;
   while (wpt > 1 && wide * (wpt / 2) >= want) wpt /= 2;
-  return wpt == 8 ? launch<F16, GROUP, 2, NT, 8>(W, p, wpt, st) : launch<F16, GROUP, 2, NT, 4>(W, p, wpt, st);
+  return wpt == 8 ? launch_tiles<F16, GROUP, 2, 8>(W, p, wpt, st) : launch_tiles<F16, GROUP, 2, 4>(W, p, wpt, st);
 }
 template <bool F16, int GROUP>
 cudaError_t launch_group(const rg_weights_four_t* W, W4Params p, cudaStream_t st) {
-  if (p.M <= 8) return launch_few<F16, GROUP, 1>(W, p, st);
-  if (p.M <= 16) return launch_few<F16, GROUP, 2>(W, p, st);
-  const int passes = (p.M + 39) / 40;                      // as even as eights allow
+  if (p.M <= FEW) return launch_few<F16, GROUP>(W, p, st);
+  const int passes = (p.M + 39) / 40;                  // over the rows, as even as eights allow
   p.rows = ((p.M + passes - 1) / passes + 7) / 8 * 8;
-  if (p.rows <= 32) return launch_more<F16, GROUP, 4>(W, p, st);
-  return launch_more<F16, GROUP, 5>(W, p, st);
+  switch (p.rows / 8) {
+    case 1: return launch_more<F16, GROUP, 1>(W, p, st);
+    case 2: return launch_more<F16, GROUP, 2>(W, p, st);
+    case 3: return launch_more<F16, GROUP, 3>(W, p, st);
+    case 4: return launch_more<F16, GROUP, 4>(W, p, st);
+    default: return launch_more<F16, GROUP, 5>(W, p, st);
+  }
 }
 template <bool F16>
 cudaError_t launch_type(const rg_weights_four_t* W, const W4Params& p, cudaStream_t st) {
