@@ -111,6 +111,17 @@ def test_bits_do_not_depend_on_the_other_rows(N, K, group, dtype):
     assert torch.equal(product(A, *w, group, F32, w_static=1), whole)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N,K", [(30011, 2112), (15000, 4096), (7001, 4128), (250, 1056), (129, 544)])
+def test_bits_do_not_depend_on_how_many_ctas_share_k(N, K, group):
+    """Numbers of rows with 1, 2, 4 and all 8 parts of K a CTA, in one pass over the rows and in two, the last CTA's weights cut."""
+    codes, s, z = weights(N, K, group, seed=N)
+    A = torch.randn(81, K, generator=generator(5), device=DEV).to(BF)
+    full = check(A, codes, s, z, group, F32)
+    for M in (1, 2, 3, 8, 9, 16, 17, 24, 25, 32, 33, 40, 41, 72):
+        assert torch.equal(product(A[:M].contiguous(), codes, s, z, group, F32), full[:M]), M
+
+
 def test_strides():
     K, N, M = 544, 90, 11
     codes, s, z = weights(N, K, 32, pad=16, seed=9)
