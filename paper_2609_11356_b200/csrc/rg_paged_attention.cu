@@ -643,7 +643,7 @@ __device__ __forceinline__ void unpack32(const Unpack& u, const uint4& codes, ui
 }
 // A key's elements, 32 at a time: `put` takes 16 words and the chunk's number.  `raw`: the block's codes.  WHOLE: heads of so many chunks unrolled.  The kernel for many
 // rows, where two warps unpack, has that (4096-row chunk 1067 us, 1120 as a loop); the one for few rows, where thirty warps run five different pieces of
-// code and wait for what does not fit the instruction caches, has a loop (64 single tokens 147 us, 182 unrolled).
+// code and wait for what does not fit the instruction caches, has a loop (64 single tokens 131 us, 153 unrolled by two, 161 wholly).
 template <int DT, int WHOLE, typename Put>
 __device__ __forceinline__ void unpack_key(const Unpack& u, const uint8_t* raw, int d, int key, Put&& put) {
   const uint8_t* tile = raw + (key >> 3) * tile4_bytes(d);
@@ -1532,36 +1532,40 @@ paged_attention_few_kernel(const __grid_constant__ CUtensorMap tmap_q, const __g
 
 // ---------------------------------------------------------------- few rows, four-bit caches
 // The same products and the same order of sums, so the same bits.  Keys go from the unpacking warps' registers straight into tensor memory, as the first
-// product's first operand (its lanes are keys, as those warps' lanes are): only values pass through shared memory a second time, and a CTA with up to four
-// rows fits an SM three times.
-// 64 sequences of up to 8192 keys, 8 key heads of 128 (0.32 GB): 145 us a call; with keys through shared memory too, so two CTAs an SM, 152.  What bounds it: instruction
-// issue (0.58 of the slots; half of the instructions unpack) and, of the rest, the chain of a block in a CTA.  Tried there: two blocks a turn for the
-// softmax warps 184 us (parts of four blocks leave too little to run ahead of), the next item's queries fetched ahead 153, unpacking unrolled 167-182.
+// product's first operand (its lanes are keys, as those warps' lanes are): only values pass through shared memory a second time.  There is room for two blocks
+// of each.  Keys' and values' codes have a copying warp each (a bulk copy is some twenty instructions for every lane that makes one) and, for up to four rows, where a
+// thread has few registers, four unpacking warps each.
+// 64 sequences of up to 8192 keys, 8 key heads of 128 (0.32 GB), 4 query heads each: 131 us a call; with one copying warp and four unpacking ones, two CTAs an SM and
+// a block of keys 156, three CTAs and a block of values 135.  8 query heads: 153 us (178 before), 16: 191 (226).  What bounds it: instruction issue (0.67 of the slots; half
+// of the instructions unpack, a quarter of the time goes without them) and, of the rest, the chain of a block in the softmax warps, 1900 cycles, with a drain for
+// every item.  Tried there: two blocks a turn for the softmax warps 184 us (parts of four blocks leave too little to run ahead of), an item's output behind the first block of
+// the next 143, the next item's queries fetched ahead 153, unpacking unrolled by two 153 and wholly 161.
 template <int HDP, int ROWS>
 struct Few4 {
   static constexpr int DB = HDP / 64;
-  static constexpr int PRODUCER = 4, MMA = 5, UNPACK = 6, UNPACKERS = 4, WARPS = 10, THREADS = WARPS * 32;
-  static constexpr int CTAS = ROWS == 4 ? 3 : 2;                   // of an SM
-  static constexpr int N = ROWS < 16 ? 16 : ROWS;                  // narrow side of the products
+  static constexpr bool SPLIT = ROWS == 4;                         // keys and values have unpacking warps of their own
+  static constexpr int PRODUCER = 4, MMA = 5, V_PRODUCER = 6, UNPACK = 7, UNPACKERS = 4, WARPS = UNPACK + (SPLIT ? 2 : 1) * UNPACKERS, THREADS = WARPS * 32;
+  static constexpr int CTAS = 2;                                   // of an SM
+  static constexpr int N = 16;                                     // narrow side of the products
   // rows of 64 elements: where there are at most 8 the other eight that the product reads are the next box's, and nobody looks at what they give
   static constexpr uint32_t BOX = ROWS <= 8 ? 1024 : N * 128, P_BUF = 2 * BOX;
   static constexpr uint32_t V_BOX = BLK * 128, SLOT = DB * V_BOX;
-  static constexpr int SLOTS = HDP == 128 && CTAS == 3 ? 1 : 2;    // blocks of values
-  static constexpr int RAWS = HDP == 128 ? 3 : 5;                  // blocks of codes
+  static constexpr int SLOTS = 2;                                  // blocks of values
+  static constexpr int RAWS_K = 2, RAWS_V = HDP == 128 && ROWS > 8 ? 1 : 2, RAWS = RAWS_K + RAWS_V;      // blocks of codes, of keys and of values
   static constexpr uint32_t RAW = BLK / 8 * tile4_bytes(HDP);
-  static constexpr uint32_t S_AT = 0, O_AT = 2 * N, K_AT = 4 * N, COLS = K_AT + HDP / 2 > 128 ? 256 : 128;      // tensor memory: two blocks' S', even and odd items' O', a block's keys
+  static constexpr uint32_t S_AT = 0, O_AT = 2 * N, K_AT = 4 * N, COLS = K_AT + HDP > 128 ? 256 : 128;      // tensor memory: two blocks' S', even and odd items' O', two blocks' keys
   static constexpr uint32_t RAW_AT = SLOTS * SLOT, Q_AT = RAW_AT + (RAWS * RAW + 1023) / 1024 * 1024, P_AT = Q_AT + DB * BOX, ITEM_AT = P_AT + 2 * P_BUF + (ROWS <= 8 ? 1024 : 0),
-                            BAR_AT = ITEM_AT + ITEMS * sizeof(Item), N_BAR = 14 + 2 * SLOTS + 2 * ITEMS + 2 * RAWS, FLAG_AT = BAR_AT + 8 * N_BAR, MAX_AT = (FLAG_AT + 8 + 15) & ~15u,
+                            BAR_AT = ITEM_AT + ITEMS * sizeof(Item), N_BAR = 16 + 2 * SLOTS + 2 * ITEMS + 2 * RAWS, FLAG_AT = BAR_AT + 8 * N_BAR, MAX_AT = (FLAG_AT + 8 + 15) & ~15u,
                             SUM_AT = MAX_AT + 2 * 128 * 4, LAST = SUM_AT + 2 * 128 * 4;
   static constexpr size_t SMEM = 1024 + LAST;
-  static_assert(SMEM <= (CTAS == 3 ? 76800 : 115712) && COLS * CTAS <= 512, "CTAS of them fit the SM");
+  static_assert(SMEM <= 115712 && COLS * CTAS <= 512, "CTAS of them fit the SM");
 };
 
 template <int HDP, int ROWS, int DT>
 __global__ void __launch_bounds__(Few4<HDP, ROWS>::THREADS, Few4<HDP, ROWS>::CTAS)
 paged_attention_few4_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ Params p) {
   using F = Few4<HDP, ROWS>;
-  constexpr int DB = F::DB, SLOTS = F::SLOTS, RAWS = F::RAWS;
+  constexpr int DB = F::DB, SLOTS = F::SLOTS, RAWS = F::RAWS, RAWS_K = F::RAWS_K, RAWS_V = F::RAWS_V;
   constexpr uint32_t IDESC_S = pa_idesc(F::N, DT == RG_BF16, false, false), IDESC_O = pa_idesc(F::N, DT == RG_BF16, true, false);
 
   extern __shared__ uint8_t smem_raw[];
@@ -1570,9 +1574,9 @@ paged_attention_few4_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   const uint32_t sV = smem_base, sQ = smem_base + F::Q_AT, sP = smem_base + F::P_AT;
   Item* items = reinterpret_cast<Item*>(smem_gen + F::ITEM_AT);
   const uint32_t bar0 = smem_base + F::BAR_AT;
-  const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_x = bar0 + 16, b_y = bar0 + 24, b_k_ready = bar0 + 32, b_k_free = bar0 + 40;
-  const uint32_t b_s = bar0 + 48, b_p = bar0 + 64, b_pv = bar0 + 80, b_o_empty = bar0 + 96;      // two each
-  const uint32_t b_ready = bar0 + 112, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS, b_raw = b_free + 8 * ITEMS, b_raw_empty = b_raw + 8 * RAWS;
+  const uint32_t b_q_full = bar0, b_q_empty = bar0 + 8, b_x = bar0 + 16, b_y = bar0 + 24;
+  const uint32_t b_s = bar0 + 32, b_p = bar0 + 48, b_pv = bar0 + 64, b_o_empty = bar0 + 80, b_k_ready = bar0 + 96, b_k_free = bar0 + 112;      // two each
+  const uint32_t b_ready = bar0 + 128, b_empty = b_ready + 8 * SLOTS, b_item = b_empty + 8 * SLOTS, b_free = b_item + 8 * ITEMS, b_raw = b_free + 8 * ITEMS, b_raw_empty = b_raw + 8 * RAWS;      // of keys, then of values
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + F::FLAG_AT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* xm = reinterpret_cast<float*>(smem_gen + F::MAX_AT);                          // [2][4][32]: the warps' maxima of a block, by its parity
@@ -1580,8 +1584,8 @@ paged_attention_few4_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    mbar_init(b_q_full, 1); mbar_init(b_q_empty, 1); mbar_init(b_x, 4); mbar_init(b_y, 4); mbar_init(b_k_ready, F::UNPACKERS); mbar_init(b_k_free, 1);
-    for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 8 * t, 4); mbar_init(b_pv + 8 * t, 1); mbar_init(b_o_empty + 8 * t, 4); }
+    mbar_init(b_q_full, 1); mbar_init(b_q_empty, 1); mbar_init(b_x, 4); mbar_init(b_y, 4);
+    for (int t = 0; t < 2; ++t) { mbar_init(b_s + 8 * t, 1); mbar_init(b_p + 8 * t, 4); mbar_init(b_pv + 8 * t, 1); mbar_init(b_o_empty + 8 * t, 4); mbar_init(b_k_ready + 8 * t, F::UNPACKERS); mbar_init(b_k_free + 8 * t, 1); }
     for (int s = 0; s < SLOTS; ++s) { mbar_init(b_ready + 8 * s, F::UNPACKERS); mbar_init(b_empty + 8 * s, 1); }
     for (int s = 0; s < ITEMS; ++s) { mbar_init(b_item + 8 * s, 1); mbar_init(b_free + 8 * s, F::WARPS - 1); }
     for (int s = 0; s < RAWS; ++s) { mbar_init(b_raw + 8 * s, 1); mbar_init(b_raw_empty + 8 * s, F::UNPACKERS); }
@@ -1611,52 +1615,58 @@ paged_attention_few4_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
   Item it;
   bool alive = true;
 
-  if (warp == F::PRODUCER) {
-    // ------------------------------------------------------------ producer: K_0, K_1, V_0, K_2, V_1, ..., as they are used
+  if (warp == F::PRODUCER || warp == F::V_PRODUCER) {
+    // ------------------------------------------------------------ producers, of items, queries and keys, and of values
+    const bool is_v = warp == F::V_PRODUCER;
     const int pieces = BLK / p.box, piece = lane & (pieces - 1);
-    Ring<RAWS> raw;
+    const uint8_t* const cache = is_v ? p.v4 : p.k4;
+    const int64_t page_stride = is_v ? p.v4_page : p.k4_page, head_stride = is_v ? p.v4_head : p.k4_head;
+    const uint32_t first = is_v ? RAWS_K : 0, slots = is_v ? RAWS_V : RAWS_K;
+    uint32_t raw = 0, raw_phase = 0;
     uint32_t q_phase = 1;
     Walk walk;
-    walk.start(p, p.tile_tokens);
+    if (!is_v) walk.start(p, p.tile_tokens);
     while (alive) {
-      const bool more = walk.get(p, p.tile_tokens, it);
-      if (!more) it.n_tok = 0;
-      alive = pa_wait(b_free + 8 * ir.slot, ir.phase ^ 1u, abort_flag, 0x5080u);
-      if (!alive) break;
-      if (lane == 0) { items[ir.slot] = it; mbar_arrive(b_item + 8 * ir.slot); }
-      ir.step();
-      if (!more) break;
+      if (is_v) {
+        if (!next_item(it, alive)) break;
+      } else {
+        const bool more = walk.get(p, p.tile_tokens, it);
+        if (!more) it.n_tok = 0;
+        alive = pa_wait(b_free + 8 * ir.slot, ir.phase ^ 1u, abort_flag, 0x5080u);
+        if (!alive) break;
+        if (lane == 0) { items[ir.slot] = it; mbar_arrive(b_item + 8 * ir.slot); }
+        ir.step();
+        if (!more) break;
+      }
       if (it.b1 == it.b0) continue;
       const int32_t* row = p.table + (int64_t)it.seq * p.table_ld;
-      // a lane's page of block b, looked up a block ahead of its first use and kept for its second
+      // a lane's page of block b, looked up a block ahead
       auto wanted = [&](int b) -> bool { const int32_t k = b * BLK + piece * p.box; return lane < pieces && b < it.b1 && k <= it.hi && k + p.box > it.lo; };
       auto entry = [&](int b) -> int32_t { return wanted(b) ? row[(b * BLK + piece * p.box) / p.by_page] : 0; };
-      int32_t page = entry(it.b0), next = entry(it.b0 + 1);
-      alive = pa_wait(b_q_empty, q_phase, abort_flag, 0x5100u);
-      if (!alive) break;
-      q_phase ^= 1u;
-      if (lane == 0) mbar_expect_tx(b_q_full, (uint32_t)(DB * p.tile_tokens * p.group) * 128u);
-      __syncwarp();
-      if (lane < DB) pa_tma_4d(sQ + lane * F::BOX, &tmap_q, lane * 64, 0, it.tok, it.head, b_q_full);
-      auto copy = [&](bool is_v, int b, int32_t& id) {
+      int32_t page = entry(it.b0);
+      if (!is_v) {
+        alive = pa_wait(b_q_empty, q_phase, abort_flag, 0x5100u);
+        if (!alive) break;
+        q_phase ^= 1u;
+        if (lane == 0) mbar_expect_tx(b_q_full, (uint32_t)(DB * p.tile_tokens * p.group) * 128u);
+        __syncwarp();
+        if (lane < DB) pa_tma_4d(sQ + lane * F::BOX, &tmap_q, lane * 64, 0, it.tok, it.head, b_q_full);
+      }
+#pragma unroll 1
+      for (int b = it.b0; b < it.b1; ++b) {
+        const int32_t next = entry(b + 1);
         const bool mine = wanted(b);
-        if (mine && (id < 0 || id >= p.pages)) {                   // not a page: zeros
+        if (mine && (page < 0 || page >= p.pages)) {               // not a page: zeros
           atomicCAS(&g_paged_attn_page_word, 0u, (unsigned)RG_PAGE_CODE_ATTEND);
-          id = p.pages;
+          page = p.pages;
         }
         const int32_t key = b * BLK + piece * p.box, at = key - key / p.by_page * p.page_size;
-        alive = pa_wait(b_raw_empty + 8 * raw.slot, raw.phase ^ 1u, abort_flag, 0x5200u | raw.slot);
-        if (!alive) return;
-        copy_codes(p, is_v ? p.v4 : p.k4, is_v ? p.v4_page : p.k4_page, is_v ? p.v4_head : p.k4_head, mine, id, it.head, at, piece, smem_gen + F::RAW_AT + raw.slot * F::RAW, b_raw + 8 * raw.slot);
-        raw.step();
-      };
-      copy(false, it.b0, page);
-      for (int b = it.b0; b < it.b1 && alive; ++b) {
-        const int32_t later = entry(b + 2);
-        if (b + 1 < it.b1) copy(false, b + 1, next);
-        if (alive) copy(true, b, page);
+        const uint32_t slot = first + raw;
+        alive = pa_wait(b_raw_empty + 8 * slot, raw_phase ^ 1u, abort_flag, 0x5200u | slot);
+        if (!alive) break;
+        copy_codes(p, cache, page_stride, head_stride, mine, page, it.head, at, piece, smem_gen + F::RAW_AT + slot * F::RAW, b_raw + 8 * slot);
+        if (++raw == slots) { raw = 0; raw_phase ^= 1u; }
         page = next;
-        next = later;
       }
     }
   } else if (warp == F::MMA) {
@@ -1664,16 +1674,21 @@ paged_attention_few4_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
     const bool leader = elect_one();
     Ring<SLOTS> kv;
     uint32_t q_phase = 0, block = 0, n_item = 0;
+    const uint64_t q_desc = pa_desc(sQ, 16);
     // The scores of block number c go to columns N (c & 1): those of c - 2 have been read, since the product of c - 2 was issued.
     auto scores = [&](uint32_t c) {
-      alive = pa_wait(b_k_ready, c & 1, abort_flag, 0x5340u);
+      alive = pa_wait(b_k_ready + 8 * (c & 1), (c >> 1) & 1, abort_flag, 0x5340u);
       if (!alive) return;
       pa_fence_after();
       // 16 elements of the keys are 8 columns; only those that the head has
-#pragma unroll 1
-      for (int e = 0; 16 * e < p.d; ++e)
-        if (leader) pa_mma_ts(tmem + F::S_AT + F::N * (c & 1), tmem + F::K_AT + 8u * e, pa_desc(sQ + (e >> 2) * F::BOX, 16) + 2u * (e & 3), IDESC_S, e ? 1u : 0u);
-      if (leader) { pa_commit(b_s + 8 * (c & 1)); pa_commit(b_k_free); }
+      if (leader) {
+        const uint32_t t_s = tmem + F::S_AT + F::N * (c & 1), t_k = tmem + F::K_AT + HDP / 2 * (c & 1);
+#pragma unroll
+        for (int e = 0; e < HDP / 16; ++e)
+          if (16 * e < p.d) pa_mma_ts(t_s, t_k + 8u * e, q_desc + (uint64_t)((e >> 2) * (F::BOX >> 4) + 2 * (e & 3)), IDESC_S, e ? 1u : 0u);
+        pa_commit(b_s + 8 * (c & 1));
+        pa_commit(b_k_free + 8 * (c & 1));
+      }
     };
     while (alive && next_item(it, alive)) {
       const int nb = __shfl_sync(0xffffffffu, it.b1 - it.b0, 0);
@@ -1701,17 +1716,22 @@ paged_attention_few4_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
         // heads of up to 64 elements: the upper 64 lanes repeat the lower ones (distance 0 between the column groups), nobody reads them
         const uint64_t v = pa_desc(__shfl_sync(0xffffffffu, sV + slot * F::SLOT, 0), HDP == 128 ? F::V_BOX : 0);
         const uint64_t pr = pa_desc(__shfl_sync(0xffffffffu, sP + (block & 1) * F::P_BUF, 0), 16);
-#pragma unroll 1
-        for (int e = 0; e < BLK / 16; ++e)
-          if (leader) pa_mma_ss(t_o, v + (uint64_t)(e * (2048 >> 4)), pr + (uint64_t)((e >> 2) * (F::BOX >> 4) + 2 * (e & 3)), IDESC_O, (j | e) ? 1u : 0u);
-        if (leader) { pa_commit(b_pv + 8 * (block & 1)); pa_commit(b_empty + 8 * slot); }
+        if (leader) {
+#pragma unroll
+          for (int e = 0; e < BLK / 16; ++e)
+            pa_mma_ss(t_o, v + (uint64_t)(e * (2048 >> 4)), pr + (uint64_t)((e >> 2) * (F::BOX >> 4) + 2 * (e & 3)), IDESC_O, (j | e) ? 1u : 0u);
+          pa_commit(b_pv + 8 * (block & 1));
+          pa_commit(b_empty + 8 * slot);
+        }
       }
       ++n_item;
     }
   } else if (warp >= F::UNPACK) {
-    // ------------------------------------------------------------ unpackers, in the producer's order; a key a lane
+    // ------------------------------------------------------------ unpackers, a key a lane: of keys, of values, or of K_0, K_1, V_0, K_2, V_1, ..., as they are used
+    const bool keys = !F::SPLIT || warp < F::UNPACK + F::UNPACKERS, values = !F::SPLIT || !keys;
     Ring<SLOTS> kv;
-    Ring<RAWS> raw;
+    Ring<RAWS_K> raw_k;
+    Ring<RAWS_V> raw_v;
     const Unpack unpack(DT);
     const int key = 32 * (warp & 3) + lane;                        // the part of tensor memory that a warp reaches follows from its number
     const uint32_t t_k = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + F::K_AT;
@@ -1719,30 +1739,31 @@ paged_attention_few4_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
     while (alive && next_item(it, alive)) {
       const int nb = it.b1 - it.b0;
 #pragma unroll 1
-      for (int i = 0; i < 2 * nb; ++i) {
-        const bool is_v = i == 2 * nb - 1 || (i >= 2 && !(i & 1));
+      for (int i = 0; i < (F::SPLIT ? nb : 2 * nb); ++i) {
+        const bool is_v = F::SPLIT ? values : i == 2 * nb - 1 || (i >= 2 && !(i & 1));
+        const uint32_t slot = is_v ? RAWS_K + raw_v.slot : raw_k.slot;
         if (is_v) alive = pa_wait(b_empty + 8 * kv.slot, kv.phase ^ 1u, abort_flag, 0x5600u | kv.slot);
-        else alive = pa_wait(b_k_free, (block & 1) ^ 1u, abort_flag, 0x5640u);
-        if (alive) alive = pa_wait(b_raw + 8 * raw.slot, raw.phase, abort_flag, 0x5680u | raw.slot);
+        else alive = pa_wait(b_k_free + 8 * (block & 1), ((block >> 1) & 1) ^ 1u, abort_flag, 0x5640u);
+        if (alive) alive = pa_wait(b_raw + 8 * slot, is_v ? raw_v.phase : raw_k.phase, abort_flag, 0x5680u | slot);
         if (!alive) break;
-        const uint8_t* const codes = smem_gen + F::RAW_AT + raw.slot * F::RAW;
+        const uint8_t* const codes = smem_gen + F::RAW_AT + slot * F::RAW;
         if (!is_v) pa_fence_after();
         uint8_t* const to = smem_gen + kv.slot * F::SLOT;
+        const uint32_t t_to = t_k + HDP / 2 * (block & 1);
         unpack_key<DT, 0>(unpack, codes, p.d, key, [&](const uint32_t (&v)[16], int c) {
           if (is_v) store_to_row(v, to, key, c);
-          else pa_st16(t_k + 16u * c, v);                          // two elements a column
+          else pa_st16(t_to + 16u * c, v);                         // two elements a column
         });
         if (is_v) {
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         } else {
           pa_wait_st();
           pa_fence_before();
-          ++block;
         }
         __syncwarp();
-        if (lane == 0) { mbar_arrive(is_v ? b_ready + 8 * kv.slot : b_k_ready); mbar_arrive(b_raw_empty + 8 * raw.slot); }
-        if (is_v) kv.step();
-        raw.step();
+        if (lane == 0) { mbar_arrive(is_v ? b_ready + 8 * kv.slot : b_k_ready + 8 * (block & 1)); mbar_arrive(b_raw_empty + 8 * slot); }
+        if (is_v) { kv.step(); raw_v.step(); }
+        else { ++block; raw_k.step(); }
       }
     }
   } else {
@@ -1851,15 +1872,18 @@ paged_attention_few4_kernel(const __grid_constant__ CUtensorMap tmap_q, const __
           o[i] = zero ? 0.0f : f_mul(__uint_as_float(raw[i]), f);
         }
         if (col < p.d) {
-          int tok = 0, head = 0;
+          // from one row to the next: a head on, or a token on
+          const int64_t per_head = it.multi ? (int64_t)p.segments * p.d : p.o_head, per_token = it.multi ? p.hq * per_head : p.o_tok, turn = per_token - (p.group - 1) * per_head;
+          int64_t at = it.tok * per_token + it.head * p.group * per_head + col + (it.multi ? it.seg * p.d : 0);
+          const int type = it.multi ? (int)RG_F32 : p.o_dtype;
+          void* const base = it.multi ? static_cast<void*>(p.part_o) : p.out;
+          int head = 0;
 #pragma unroll
           for (int i = 0; i < ROWS; ++i) {
             if (i < n_rows) {
-              const int64_t token = (int64_t)it.tok + tok;
-              const int h = it.head * p.group + head;
-              if (it.multi) p.part_o[((token * p.hq + h) * p.segments + it.seg) * p.d + col] = o[i];
-              else store_scalar(p.out, p.o_dtype, token * p.o_tok + h * p.o_head + col, o[i]);
-              if (++head == p.group) { head = 0; ++tok; }
+              store_scalar(base, type, at, o[i]);
+              at += ++head == p.group ? turn : per_head;
+              head = head == p.group ? 0 : head;
             }
           }
         }
@@ -2045,7 +2069,7 @@ cudaError_t launch_few(const CUtensorMap& q, const CUtensorMap& k, const CUtenso
 template <int HDP, int DT, bool FOUR>
 cudaError_t launch_head(int rows, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Params& p, int64_t most, cudaStream_t st) {
   if constexpr (FOUR) { if (rows == 4) return launch_few<HDP, 4, DT, FOUR>(q, k, v, p, most, st); }
-  if constexpr (HDP == 64) { if (rows == 32) return launch_few<64, 32, DT, FOUR>(q, k, v, p, most, st); }
+  if constexpr (HDP == 64 && !FOUR) { if (rows == 32) return launch_few<64, 32, DT, FOUR>(q, k, v, p, most, st); }
   if (rows == 8) return launch_few<HDP, 8, DT, FOUR>(q, k, v, p, most, st);
   if (rows == 16) return launch_few<HDP, 16, DT, FOUR>(q, k, v, p, most, st);
   return launch_wide<HDP, DT, FOUR>(q, k, v, p, most, st);
@@ -2083,8 +2107,10 @@ rg_status_t launch_paged_attention(const PagedAttnArgs& a, cudaStream_t st) {
   }
 
   const int64_t need = a.max_q * G;
-  const int most_rows = d <= 64 ? 32 : 16;
-  const int rows = four && need <= 4 ? 4 : need <= 8 ? 8 : need <= 16 ? 16 : need <= most_rows ? most_rows : 128;
+  const int most_rows = d <= 64 && !four ? 32 : 16;
+  // Codes are cheap to read twice: up to 32 rows are two tiles of 16 (64 sequences with up to 20 rows 231 us against 309 in the kernel for many rows, 8
+  // sequences 32 and 50; up to 32 rows 274 and 299; three tiles for 40 rows with heads of 64 27.7 and 25.6).
+  const int rows = four && need <= 4 ? 4 : need <= 8 ? 8 : need <= 16 || (four && need <= 32 && G <= 16) ? 16 : need <= most_rows ? most_rows : 128;
   const bool narrow = rows < 128;
   p.tile_tokens = rows / G;
   int box = page & -page;                                  // the largest power of two that divides the page size: boxes never cross pages

@@ -73,6 +73,19 @@ def test_sliding_window(window, split):
     check4(b, *both(b, window=window, split=split), window=window)
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("hq,hkv,most", [(8, 2, 8), (8, 2, 5), (16, 2, 3), (6, 2, 7), (16, 1, 2), (2, 2, 20), (40, 2, 1), (8, 2, 9)])
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_a_few_tokens_each(d, hq, hkv, most, dtype):
+    """Up to 32 rows a key head, and just more: one tile of rows, two, or the form for many; sequences of every length below, none, and many blocks of keys."""
+    q = [most, 1, 0, max(most - 1, 0), most, 1]
+    kv = [5000, 1, 700, 128 + most, most, 2300]
+    b = Batch4(q, kv, hq=hq, hkv=hkv, d=d, page=16, dtype=dtype, seed=hq + most)
+    check4(b, *both(b))
+    check4(b, *both(b, split=256))
+    check4(b, *both(b, window=300), window=300)
+
+
 @pytest.mark.parametrize("split", [0, 128])
 def test_no_mask(split):
     b = Batch4([1, 130, 40], [500, 130, 257], hq=4, hkv=4, d=128, page=16, seed=3)
