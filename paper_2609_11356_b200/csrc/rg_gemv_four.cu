@@ -10,10 +10,10 @@
 // the order of k within a group is the tensor core's own affair as long as A's elements follow it.  tcgen05 would want the unpacked weights in shared or
 // tensor memory, a trip that costs more than these few rows' products.  Every warp streams its own stages into shared memory, a TMA box at a time.
 //
-// Two kernels.  One or two rows: a warp reads A's elements from global memory itself and never waits for another warp until all its parts are done.
+// Two kernels.  One or two rows: a warp copies A's elements along with its codes and never waits for another warp until all its parts are done.
 // More: eight warps share A's elements in shared memory, stage by stage.  28672 x 4096 in groups of 128, a graph of calls on rotating weights, us:
 //   rows          1      2      4      8     16     40
-//   the first    25.0   25.9   29.0   33.1   (71, as a form for 16 rows)
+//   the first    22.9   23.4   (29.0   33.1   71, as forms for up to 16 rows that read A's elements from global memory; so 25.0 and 25.9 for 1 and 2)
 //   the second   26.1   26.3   26.3   26.5   35.7   58.3
 // What bounds them: the bytes of the codes would take 9.4 us.  The instructions that unpack them (a mask that makes a float's mantissa of the nibble, and one
 // subtraction, for two codes, with a shift for three of four) keep the half-rate integer pipe busy for 8 us, and 12 to 16 warps of an SM do not cover all
@@ -90,7 +90,8 @@ struct Shape4 {
   static constexpr int COLS = 16 * MT, DEPTH = MT == 1 ? 4 : 2;       // stages of a warp's ring, one being worked on
   static constexpr int SLOT = MT * STAGE, SCALES = PER<GROUP> * COLS * 8;           // (scale, less) pairs of a stage
   static constexpr int PART = FEW * (COLS + 1) * 4;    // a part's sums
-  static constexpr int SCALE_AT = WARPS * DEPTH * SLOT, BAR_AT = SCALE_AT + WARPS * SCALES, FLAG_AT = BAR_AT + WARPS * DEPTH * 8, PART_AT = FLAG_AT + 16, SMEM = 1024 + PART_AT;
+  static constexpr int X_ROW = SPAN * 2 + 16, X = FEW * X_ROW;      // a stage of A; rows begin in different banks
+  static constexpr int X_AT = WARPS * DEPTH * SLOT, SCALE_AT = X_AT + WARPS * DEPTH * X, BAR_AT = SCALE_AT + WARPS * SCALES, FLAG_AT = BAR_AT + WARPS * DEPTH * 8, PART_AT = FLAG_AT + 16, SMEM = 1024 + PART_AT;
   static constexpr int MOST = SMEM + (WARPS == 8 ? 1 : 4) * PARTS * PART;      // eight warps share one tile, four have up to four
   static_assert(MOST <= 113 * 1024 && BAR_AT % 8 == 0, "fits the SM");
 };
@@ -149,6 +150,7 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint8_t* const mine = smem + warp * (DEPTH * S::SLOT);
+  uint8_t* const x_mine = smem + S::X_AT + warp * (DEPTH * S::X);
   float2* const sz = reinterpret_cast<float2*>(smem + S::SCALE_AT + warp * S::SCALES);      // [MT][G][16] (scale, less)
   const uint32_t bars = smem_u32(smem + S::BAR_AT) + warp * (DEPTH * 8);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
@@ -166,14 +168,15 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
 
   // Requests run ahead of the arithmetic.  A box is COLS rows of 128 bytes, 16-byte piece c at c ^ (row & 7), zeros behind the last row and behind K (A
   // has zeros there too, and the rows' sums are dropped).
-  int r_i = 0;
-  auto request = [&] {
-    if (r_i >= n_st) return;
-    if (lane == 0) {
-      mbar_expect_tx(bars + 8 * (r_i % DEPTH), S::SLOT);
-      load_box(smem_u32(mine) + r_i % DEPTH * S::SLOT, &codes, (s0 + r_i) * (SPAN / 4), tile * COLS, bars + 8 * (r_i % DEPTH));
+  auto request_codes = [&](int i) {
+    if (i < n_st && lane == 0) {
+      mbar_expect_tx(bars + 8 * (i % DEPTH), S::SLOT + rows * 2 * min(SPAN, p.K - (s0 + i) * SPAN));
+      load_box(smem_u32(mine) + i % DEPTH * S::SLOT, &codes, (s0 + i) * (SPAN / 4), tile * COLS, bars + 8 * (i % DEPTH));
     }
-    ++r_i;
+  };
+  auto request_x = [&](int i) {
+    if (i < n_st && lane < rows)
+      bulk_load_1d(smem_u32(x_mine) + i % DEPTH * S::X + lane * S::X_ROW, p.A + lane * p.lda + (s0 + i) * SPAN, 2 * min(SPAN, p.K - (s0 + i) * SPAN), bars + 8 * (i % DEPTH));
   };
   Scales<GROUP, MT> scales(p, (int64_t)tile * COLS + lane / G, s0 * G + lane % G);
 
@@ -181,28 +184,23 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
   // with the promise that nothing in flight writes the weights their first stages are on their way before the kernels ahead have finished
   if (!p.w_static) asm volatile("griddepcontrol.wait;" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < DEPTH - 1; ++i) request();
+  for (int i = 0; i < DEPTH - 1; ++i) request_codes(i);
   if (n_st > 0) scales.fetch(p);
   if (p.w_static) asm volatile("griddepcontrol.wait;" ::: "memory");
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < DEPTH - 1; ++i) request_x(i);
 
   const int t = lane & 3, rr = lane >> 2;
   const int r = (rr >> 2) | (rr & 2) | (rr & 1) << 2;  // the lane's row of the upper eight: neighbours differ in the bits that the pieces' order uses
-  const uint16_t* x_at = p.A + (int64_t)min(rr, rows - 1) * p.lda + s0 * SPAN + t * (GROUP / 4);       // columns behind the last row of A repeat it: nobody reads their sums
+  const uint8_t* const x_at = x_mine + min(rr, rows - 1) * S::X_ROW + t * (GROUP / 2);       // columns behind the last row of A repeat it: nobody reads their sums
   // a lane's first word within a row's 128 bytes; a group's place further on only turns bits of it
   const uint32_t w_lane = r * 128 + ((((t * (GROUP / 8)) >> 4) ^ r) << 4) + (t * (GROUP / 8) & 15);
   uint32_t mask = 0x000f000fu, magic = F16 ? 0x64006400u : 0x43004300u;
   asm("" : "+r"(mask), "+r"(magic));
   float sum[MT][4];
-  // A's elements of a stage, on their way before the codes are waited for.  TAIL: the last stage of K, of which `left` elements are there.
-  uint4 x_of[G][WORDS];
-  auto load_x = [&](int left, auto tail) {
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-      for (int i = 0; i < WORDS; ++i)
-        x_of[g][i] = !decltype(tail)::value || g * GROUP + t * (GROUP / 4) + 8 * i < left ? __ldg(reinterpret_cast<const uint4*>(x_at + g * GROUP + 8 * i)) : make_uint4(0u, 0u, 0u, 0u);
-  };
-  auto window = [&](int g, uint32_t at, const float2* s) {
+  // TAIL: the last stage of K, of which `left` elements are there
+  auto window = [&](int g, uint32_t at, const uint8_t* xs, const float2* s, int left, auto tail) {
     float acc[MT][4];
     // this lane's words of its rows: GROUP / 4 codes from the group's k + t GROUP / 4 on
     uint32_t w[MT][2][WORDS];
@@ -220,7 +218,8 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
 #pragma unroll
     for (int x = 0; x < WORDS; ++x) {
       // A's elements in the codes' order: 0 4, 1 5, 2 6, 3 7
-      const uint4 v = x_of[g][x];
+      uint4 v = *reinterpret_cast<const uint4*>(xs + g * (GROUP * 2) + 16 * x);
+      if (decltype(tail)::value && g * GROUP + t * (GROUP / 4) + 8 * x >= left) v = make_uint4(0u, 0u, 0u, 0u);
       const uint32_t b0 = __byte_perm(v.x, v.z, 0x5410), b1 = __byte_perm(v.x, v.z, 0x7632), b2 = __byte_perm(v.y, v.w, 0x5410), b3 = __byte_perm(v.y, v.w, 0x7632);
 #pragma unroll
       for (int a = 0; a < MT; ++a) {
@@ -244,19 +243,19 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
     for (int e = 0; e < 4; ++e) sum[a][e] = 0.0f;
   int in_part = 0, part = part0;
   auto stage = [&](int i, int left, auto tail) {
-    load_x(left, tail);
     scales.put(sz, F16);
     if (i + 1 < n_st) scales.fetch(p);
-    request();
+    request_codes(i + DEPTH - 1);
+    __syncwarp();
+    request_x(i + DEPTH - 1);
     const uint32_t slot = i % DEPTH;
     warp_mbar_wait(bars + 8 * slot, (i / DEPTH) & 1, abort_flag, &g_gemv_four_status_word, 0x4000u | slot);      // one that gives up lets the kernel run out
     __syncwarp();                                      // and every lane's scales are there
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       if (decltype(tail)::value && g * GROUP >= left) break;
-      window(g, slot * S::SLOT + (w_lane ^ (g * (GROUP / 2))), sz + r + g * 16);
+      window(g, slot * S::SLOT + (w_lane ^ (g * (GROUP / 2))), x_at + slot * S::X, sz + r + g * 16, left, tail);
     }
-    x_at += SPAN;
     __syncwarp();                                      // the slot and the scales are free
   };
   for (int i = 0; i < n_st; ++i) {
