@@ -444,23 +444,24 @@ typedef struct {
 size_t rg_cache_four_block_bytes(int64_t page_size, int64_t dim);   /* 0 for sizes that are refused */
 
 /* rg_kv_append into such caches: the new tokens' keys (rotated) and values go into their pages as codes, and the queries are rotated into q_out with the bits of
- * rg_rope, in one launch.  The codes are those of the keys rotated in 64 bits, which are not rounded in between.  Everything else is as in rg_kv_append: arguments, checks, health word (RG_PAGE_CODE_APPEND).  k, v, q, q_out: bf16, fp16 or
+ * rg_rope, in one launch.  The codes are those of the keys rotated in 64 bits, which are not rounded in between.  Everything else is as in
+ * rg_kv_append: arguments, checks, health word (RG_PAGE_CODE_APPEND).  k, v, q, q_out: bf16, fp16 or
  * fp32, one type.  Asynchronous on `cuda_stream`. */
 rg_status_t rg_kv_append_four(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_rows_t* v, const rg_tensor_t* pos, const double* inv_freq,
-                          const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache, const rg_paged_seqs_t* seqs,
-                          const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream);
+                              const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache, const rg_paged_seqs_t* seqs,
+                              const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream);
 
 /* What the caches hold at the places of the new tokens: k_out, v_out [tokens][kv heads][dim], bf16, fp16 or fp32, one type, any strides.  With
  * cu_q that spans whole sequences (as many new tokens as seq_lens says) it reads whole sequences.  A token without a place reads as zeros and sets
  * the health word (RG_PAGE_CODE_READ); rows behind the last sequence are left as they were.  Asynchronous on `cuda_stream`. */
 rg_status_t rg_kv_read_four(const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache, const rg_paged_seqs_t* seqs,
-                        const rg_rows_t* k_out, const rg_rows_t* v_out, void* cuda_stream);
+                            const rg_rows_t* k_out, const rg_rows_t* v_out, void* cuda_stream);
 
 /* rg_paged_attention over such caches: the same descriptor, arguments and workspace (rg_paged_attention_workspace_bytes), and the same bits as
  * rg_paged_attention has over a cache of q's type that holds the values that the codes stand for.  q bf16 or fp16.  Keys and values are always finite, so
  * nothing that a row does not see can reach it. */
 rg_status_t rg_paged_attention_four(const rg_paged_attn_desc_t* d, const rg_rows_t* q, const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache,
-                                const rg_paged_seqs_t* seqs, const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream);
+                                    const rg_paged_seqs_t* seqs, const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream);
 
 /* Host-buffer forms of rg_gemm and rg_reduce_rows, for callers whose data lives in host memory.
  * Every tensor / epilogue / args pointer is a HOST pointer (pinned memory makes the copies

@@ -757,8 +757,8 @@ rg_status_t rg_gemv_four(const rg_weights_four_t* W, const rg_tensor_t* A, const
 }
 
 rg_status_t rg_kv_append_four(const rg_rope_desc_t* d, const rg_rows_t* k, const rg_rows_t* v, const rg_tensor_t* pos, const double* inv_freq,
-                          const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache, const rg_paged_seqs_t* seqs,
-                          const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream) {
+                              const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache, const rg_paged_seqs_t* seqs,
+                              const rg_rows_t* q, const rg_rows_t* q_out, void* cuda_stream) {
   rg_status_t s;
   if ((s = check_rows(k)) != RG_OK || (s = check_rows(v)) != RG_OK || (s = check_cache4_out(k_cache)) != RG_OK || (s = check_cache4_out(v_cache)) != RG_OK ||
       (s = check_seqs(seqs)) != RG_OK)
@@ -779,7 +779,7 @@ rg_status_t rg_kv_append_four(const rg_rope_desc_t* d, const rg_rows_t* k, const
 }
 
 rg_status_t rg_kv_read_four(const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache, const rg_paged_seqs_t* seqs,
-                        const rg_rows_t* k_out, const rg_rows_t* v_out, void* cuda_stream) {
+                            const rg_rows_t* k_out, const rg_rows_t* v_out, void* cuda_stream) {
   rg_status_t s;
   if ((s = check_cache4(k_cache)) != RG_OK || (s = check_cache4(v_cache)) != RG_OK || (s = check_seqs(seqs)) != RG_OK || (s = check_rows_out(k_out)) != RG_OK ||
       (s = check_rows_out(v_out)) != RG_OK)
@@ -796,7 +796,7 @@ rg_status_t rg_kv_read_four(const rg_cache_four_t* k_cache, const rg_cache_four_
 }
 
 rg_status_t rg_paged_attention_four(const rg_paged_attn_desc_t* d, const rg_rows_t* q, const rg_cache_four_t* k_cache, const rg_cache_four_t* v_cache,
-                                const rg_paged_seqs_t* seqs, const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream) {
+                                    const rg_paged_seqs_t* seqs, const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream) {
   rg_status_t s;
   if ((s = check_paged_desc(d)) != RG_OK) return s;
   if ((s = check_rows(q)) != RG_OK || (s = check_rows_out(out)) != RG_OK || (s = check_cache4(k_cache)) != RG_OK || (s = check_cache4(v_cache)) != RG_OK ||

@@ -9,6 +9,8 @@
 // What bounds it: bytes for prompts, latency for single tokens.  A thread takes one group of 16 elements of one row (a query, or a key and a value) and the group
 // that the rotation pairs with it: 16-byte loads, several of them in flight, no exchange between threads, and a key's 8 code bytes and its scale byte are
 // a thread's own.  Threads run over two groups, then the CTA's tokens, then the chunks of the head: neighbours write the neighbouring slots of a tile.
+// 8 key heads and 32 query heads of 128 in bf16: 10.5 k tokens of 5 prompts 63 us (3.6 TB/s; 99.8 with remainders instead of magic sums, 67.5 with a second look at
+// close codes; 60 with fp32 sines), 64 single tokens 5.3 us.  Reading those tokens back: 17.2 us (4.9 TB/s) and 3.1; two heads of a thread in flight 18.1.
 #include <algorithm>
 #include <type_traits>
 

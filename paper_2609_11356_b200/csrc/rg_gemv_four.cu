@@ -504,7 +504,7 @@ __global__ void __launch_bounds__(RW * 32, 2) gemv_w4_rows_kernel(const __grid_c
     while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
   }
   __syncwarp();
-  if (p.ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");      // nobody's sums go before all have read them
+  if (p.ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");      // nobody's sums go before all have read (and stored) them
 }
 
 template <bool F16, int GROUP, int NT>

@@ -695,6 +695,7 @@ __device__ __forceinline__ void copy_codes(const Params& p, const uint8_t* cache
   const uint32_t bytes = (uint32_t)(p.box >> 3) * tile4_bytes(p.d);
   const bool there = mine && page < p.pages;
   if (mine && !there) fill_zero_codes(raw + piece * bytes, bytes);
+  __syncwarp();
   const uint32_t all = (uint32_t)__popc(__ballot_sync(0xffffffffu, there)) * bytes;
   if ((threadIdx.x & 31) == 0) mbar_expect_tx(bar, all);
   __syncwarp();

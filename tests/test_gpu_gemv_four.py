@@ -187,6 +187,41 @@ def test_back_to_back_on_two_streams_and_in_a_graph():
     assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("M,K", [(5, 1024), (40, 1024), (12, 2560), (70, 544)])
+def test_chains_of_several_rows(M, K):
+    """The same with the form for more rows, whose CTAs share K in clusters of several sizes: on two streams at a time, and captured twice."""
+    w = [rg.rg_weights_four(*weights(K, K, 128, seed=i)[:2], group=128, w_static=1) for i in range(6)]
+    x0 = torch.randn(M, K, generator=generator(3), device=DEV).to(BF)
+
+    def chain(x):
+        for m in w:
+            x = rg.rg_gemv_four(m, x, torch.empty(M, K, dtype=BF, device=DEV))
+        return x
+
+    want = x0
+    for m in w:
+        want = rg.rg_gemv_four(m, want, torch.empty(M, K, dtype=BF, device=DEV))
+        torch.cuda.synchronize()
+    assert bool(want.isfinite().all()) and float(want.abs().max()) > 0
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs, graphs = [], []
+    for i in range(8):
+        with torch.cuda.stream(streams[i % 2]):
+            outs.append(chain(x0))
+    torch.cuda.synchronize()
+    for stream in streams:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            outs.append(chain(x0))
+    for _ in range(3):
+        for stream, graph in zip(streams, graphs):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
 def test_codes_beyond_32_bits():
     """Rows of weights more than 2^32 bytes apart from the first."""
     K, N = 64, 40
