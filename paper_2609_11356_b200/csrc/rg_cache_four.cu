@@ -9,8 +9,8 @@
 // What bounds it: bytes for prompts, latency for single tokens.  A thread takes one group of 16 elements of one row (a query, or a key and a value) and the group
 // that the rotation pairs with it: 16-byte loads, several of them in flight, no exchange between threads, and a key's 8 code bytes and its scale byte are
 // a thread's own.  Threads run over two groups, then the CTA's tokens, then the chunks of the head: neighbours write the neighbouring slots of a tile.
-// 8 key heads and 32 query heads of 128 in bf16: 10.5 k tokens of 5 prompts 63 us (3.6 TB/s; 99.8 with remainders instead of magic sums, 67.5 with a second look at
-// close codes; 60 with fp32 sines), 64 single tokens 5.3 us.  Reading those tokens back: 17.2 us (4.9 TB/s) and 3.1; two heads of a thread in flight 18.1.
+// 8 key heads and 32 query heads of 128 in bf16: 10.5 k tokens of 5 prompts 56 us (4 TB/s; 99.8 with remainders instead of magic sums, 67.5 with a second look at
+// close codes, 63 with queries dealt out as keys are), 64 single tokens 5.3 us.  Reading those tokens back: 17.2 us (4.9 TB/s) and 3.1; two heads of a thread in flight 18.1.
 #include <algorithm>
 #include <type_traits>
 
@@ -105,9 +105,10 @@ struct Spot {
 };
 
 // A pair's place in the CTA's tables of sines: eight pairs are a thread's, and threads that hold neighbouring eights, or one of neighbouring tokens, read different
-// banks (eights are 9 apart, rows 2 modulo 16).
+// banks (eights are 9 apart; rows of keys 2, of queries 8 modulo 16).
 __device__ __forceinline__ int pair_at(int row, int t, int j) { return t * row + j + (j >> 3); }
 __host__ __device__ constexpr int pair_row(int half) { const int n = half + (half >> 3) + 1; return n + (18 - n % 16) % 16; }
+__host__ __device__ constexpr int query_row(int half) { const int n = half + (half >> 3) + 1; return n + (24 - n % 16) % 16; }
 
 // A query's 16 elements: pairs 8 u .. 8 u + 7 whole (another thread's stores must not reach them: the result may lie where the queries do), what is not
 // rotated as it lies.  Element c of this order, as an element of the head.
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(THREADS, 4) append4_kernel(const __grid_consta
   __shared__ Places at;
   const int64_t t0 = (int64_t)blockIdx.x * p.tile;
   const int n_tok = (int)min((int64_t)p.tile, p.tokens - t0);
-  const int half = p.rot >> 1, row = pair_row(half);
+  const int half = p.rot >> 1, row = pair_row(half), row_q = query_row(half);
   double2* const cs64 = reinterpret_cast<double2*>(smem);              // [tokens][row] (cos, sin) for keys, and for queries
   float2* const csq = reinterpret_cast<float2*>(cs64 + p.tile * row);
   const int h0 = blockIdx.y * p.head_group, n_heads = min(p.head_group, p.heads_all - h0);
@@ -227,21 +228,27 @@ __global__ void __launch_bounds__(THREADS, 4) append4_kernel(const __grid_consta
     if (queries) {
       float s, c;
       sincospif(2.0f * (float)turn, &s, &c);
-      csq[pair_at(row, tok, j)] = make_float2(c, s);
+      csq[pair_at(row_q, tok, j)] = make_float2(c, s);
     }
   }
   __syncthreads();
 
-  if (!spot.active) return;
-  const int64_t page = at.page[t];
-  if (page == -2) return;
   int i = h0 + spot.head;
+  if (spot.head >= spot.heads) return;
   // Sixteen elements that a thread rotates: pairs 8 u .. 8 u + 7, or, behind the rotated ones, elements 16 u .. 16 u + 15.
-  const int u = 2 * chunk + g;
-  const bool turned = 16 * u < p.rot, halves = turned && p.style == RG_ROPE_HALF;
-  const int first = halves ? 8 * u : 16 * u, second = halves ? half + 8 * u : first + 8;
-
+  struct Sixteen {
+    int u, first, second;
+    bool turned, halves;
+    __device__ __forceinline__ Sixteen(const Cache4Params& p, int u) : u(u), turned(16 * u < p.rot), halves(turned && p.style == RG_ROPE_HALF) {
+      first = halves ? 8 * u : 16 * u;
+      second = halves ? (p.rot >> 1) + 8 * u : first + 8;
+    }
+  };
   // ---- keys and values
+  const int64_t page = spot.active ? at.page[t] : -2;
+  const Sixteen mine(p, 2 * chunk + g);
+  const int u = mine.u, first = mine.first, second = mine.second;
+  const bool turned = mine.turned, halves = mine.halves;
   const int slot = at.slot[t];
   const int64_t in_page = page * p.st[0].dst_page + (int64_t)(slot >> 3) * tile4_bytes(p.d), in_page_v = page * p.st[1].dst_page + (int64_t)(slot >> 3) * tile4_bytes(p.d);
   // the eight elements (a word) from e on in a tile, and the scale of its group
@@ -334,31 +341,35 @@ __global__ void __launch_bounds__(THREADS, 4) append4_kernel(const __grid_consta
     }
   }
 
-  // ---- queries, two heads at a time
+  // ---- queries, two heads at a time.  Here a head's threads run over its groups first, then over the tokens: neighbours read and write neighbouring pieces of a row
+  // (10.5 k tokens with 32 heads of queries: 56 us, 63 in the keys' order).
   if (i >= end) return;
+  const int r = threadIdx.x % (p.d / 16 * p.tile), tq = r / (p.d / 16);
+  if (tq >= n_tok || at.page[tq] == -2) return;
+  const Sixteen own(p, r % (p.d / 16));
   const Cache4Stream& st = p.st[2];
-  const Elem<DT>* src = static_cast<const Elem<DT>*>(st.src) + (t0 + t) * st.src_tok + (int64_t)(i - hk) * st.src_head;
-  Elem<DT>* dst = static_cast<Elem<DT>*>(st.dst) + (t0 + t) * st.dst_tok + (int64_t)(i - hk) * st.dst_head;
+  const Elem<DT>* src = static_cast<const Elem<DT>*>(st.src) + (t0 + tq) * st.src_tok + (int64_t)(i - hk) * st.src_head;
+  Elem<DT>* dst = static_cast<Elem<DT>*>(st.dst) + (t0 + tq) * st.dst_tok + (int64_t)(i - hk) * st.dst_head;
   const int64_t src_step = (int64_t)spot.heads * st.src_head, dst_step = (int64_t)spot.heads * st.dst_head;
-  const float2* const cs = csq + pair_at(row, t, 8 * u);
+  const float2* const cs = csq + pair_at(row_q, tq, 8 * own.u);
   if (!st.vec || p.rot % 16) {
-    for (; i < end; i += spot.heads, src += src_step, dst += dst_step) rotate_query_slowly<DT>(p, src, dst, u, cs);
+    for (; i < end; i += spot.heads, src += src_step, dst += dst_step) rotate_query_slowly<DT>(p, src, dst, own.u, cs);
     return;
   }
   auto turn_and_put = [&](Elem<DT>* to, const Eight<DT>& a, const Eight<DT>& b) {
     float v[16];
     widen8<DT>(a, v); widen8<DT>(b, v + 8);
-    if (halves) rotate16<true>(v, cs);
-    else if (turned) rotate16<false>(v, cs);
-    store8<DT>(to + first, v);
-    store8<DT>(to + second, v + 8);
+    if (own.halves) rotate16<true>(v, cs);
+    else if (own.turned) rotate16<false>(v, cs);
+    store8<DT>(to + own.first, v);
+    store8<DT>(to + own.second, v + 8);
   };
   for (; i + spot.heads < end; i += 2 * spot.heads, src += 2 * src_step, dst += 2 * dst_step) {
-    const Eight<DT> a0 = load8<DT>(src + first, true), b0 = load8<DT>(src + second, true), a1 = load8<DT>(src + src_step + first, true), b1 = load8<DT>(src + src_step + second, true);
+    const Eight<DT> a0 = load8<DT>(src + own.first, true), b0 = load8<DT>(src + own.second, true), a1 = load8<DT>(src + src_step + own.first, true), b1 = load8<DT>(src + src_step + own.second, true);
     turn_and_put(dst, a0, b0);
     turn_and_put(dst + dst_step, a1, b1);
   }
-  if (i < end) turn_and_put(dst, load8<DT>(src + first, true), load8<DT>(src + second, true));
+  if (i < end) turn_and_put(dst, load8<DT>(src + own.first, true), load8<DT>(src + own.second, true));
 }
 
 // The other way: a thread takes a group's codes and stores 16 elements.
@@ -444,7 +455,7 @@ rg_status_t launch_cache4(Cache4Params p, int dtype, bool read, cudaStream_t st)
   p.head_group = (p.heads_all + groups - 1) / groups;
   groups = (p.heads_all + p.head_group - 1) / p.head_group;
   const dim3 grid((unsigned)tiles, (unsigned)groups, 1);
-  const size_t smem = read || !p.rot ? 0 : (size_t)tile * pair_row(p.rot / 2) * (sizeof(double2) + sizeof(float2));
+  const size_t smem = read || !p.rot ? 0 : (size_t)tile * (pair_row(p.rot / 2) * sizeof(double2) + query_row(p.rot / 2) * sizeof(float2));
   cudaError_t e;
   if (read) e = dtype == RG_F32 ? launch(read4_kernel<RG_F32>, p, grid, 0, st) : dtype == RG_F16 ? launch(read4_kernel<RG_F16>, p, grid, 0, st) : launch(read4_kernel<RG_BF16>, p, grid, 0, st);
   else e = dtype == RG_F32 ? launch(append4_kernel<RG_F32>, p, grid, smem, st) : dtype == RG_F16 ? launch(append4_kernel<RG_F16>, p, grid, smem, st) : launch(append4_kernel<RG_BF16>, p, grid, smem, st);
