@@ -13,7 +13,7 @@
 // Two kernels.  One or two rows: a warp copies A's elements along with its codes and never waits for another warp until all its parts are done.
 // More: eight warps share A's elements in shared memory, stage by stage.  28672 x 4096 in groups of 128, a graph of calls on rotating weights, us:
 //   rows          1      2      4      8     16     40
-//   the first    22.9   23.4   (29.0   33.1   71, as forms for up to 16 rows that read A's elements from global memory; so 25.0 and 25.9 for 1 and 2)
+//   the first    21.1   21.6   (29.0   33.1   71, as forms for up to 16 rows that read A's elements from global memory; so 25.0 and 25.9 for 1 and 2)
 //   the second   26.1   26.3   26.3   26.5   35.7   58.3
 // What bounds them: the bytes of the codes would take 9.4 us.  The instructions that unpack them (a mask that makes a float's mantissa of the nibble, and one
 // subtraction, for two codes, with a shift for three of four) keep the half-rate integer pipe busy for 8 us, and 12 to 16 warps of an SM do not cover all
@@ -46,7 +46,6 @@ struct W4Params {
   int32_t scale_dtype, c_dtype, w_static;
   int32_t part;                                        // stages of a part
   int32_t rows;                                        // of A, for one CTA
-  int32_t wpt, per_cta;                                // warps of a tile (a power of two up to PARTS), tiles of a CTA
   int32_t share, ctas;                                 // parts of a CTA, CTAs with the same weights' rows: a cluster
   EpilogueArgs epi;
 };
@@ -83,7 +82,7 @@ constexpr int STAGE = 16 * 128;                        // bytes of a stage's cod
 template <int GROUP> constexpr int PER = SPAN / GROUP;                 // groups of a stage
 
 // ---------------------------------------------------------------- one or two rows
-// A tile is 16 MT rows of weights; two to eight warps share it, each with one or more parts of K.
+// A CTA's tile is 16 MT rows of weights; its four or eight warps share it, each with one or two parts of K.
 constexpr int FEW = 2;                                 // rows
 template <int GROUP, int MT, int WARPS>
 struct Shape4 {
@@ -92,7 +91,7 @@ struct Shape4 {
   static constexpr int PART = FEW * (COLS + 1) * 4;    // a part's sums
   static constexpr int X_ROW = SPAN * 2 + 16, X = FEW * X_ROW;      // a stage of A; rows begin in different banks
   static constexpr int X_AT = WARPS * DEPTH * SLOT, SCALE_AT = X_AT + WARPS * DEPTH * X, BAR_AT = SCALE_AT + WARPS * SCALES, FLAG_AT = BAR_AT + WARPS * DEPTH * 8, PART_AT = FLAG_AT + 16, SMEM = 1024 + PART_AT;
-  static constexpr int MOST = SMEM + (WARPS == 8 ? 1 : 4) * PARTS * PART;      // eight warps share one tile, four have up to four
+  static constexpr int MOST = SMEM + PARTS * PART;
   static_assert(MOST <= 113 * 1024 && BAR_AT % 8 == 0, "fits the SM");
 };
 
@@ -155,10 +154,10 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
   const uint32_t bars = smem_u32(smem + S::BAR_AT) + warp * (DEPTH * 8);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
   const int rows = p.M;
-  // the warp's tile, and its parts of K: the first one, how many, and their stages
-  const int own = warp / p.wpt, tile = blockIdx.x * p.per_cta + own, stages = (p.K + SPAN - 1) / SPAN, n_parts = (stages + p.part - 1) / p.part;
-  const int share = PARTS / p.wpt, part0 = (warp - own * p.wpt) * share;
-  const int s0 = part0 * p.part, n_st = tile * COLS < p.N ? max(0, min(stages - s0, share * p.part)) : 0;
+  // the warp's parts of K: the first one, how many, and their stages
+  const int tile = blockIdx.x, stages = (p.K + SPAN - 1) / SPAN, n_parts = (stages + p.part - 1) / p.part;
+  constexpr int SHARE = PARTS / WARPS;
+  const int part0 = warp * SHARE, s0 = part0 * p.part, n_st = max(0, min(stages - s0, SHARE * p.part));
   if (threadIdx.x == 0) {
     for (int i = 0; i < WARPS * DEPTH; ++i) mbar_init(smem_u32(smem + S::BAR_AT) + 8 * i, 1);
     *abort_flag = 0;
@@ -264,7 +263,7 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
     else stage(i, left, std::true_type{});
     if (++in_part == p.part || i + 1 == n_st) {
       // a part is done; all are joined at the end
-      float* const to = reinterpret_cast<float*>(smem + S::PART_AT) + ((own * PARTS + part) * rows + 2 * t) * (COLS + 1) + r;       // [rows][COLS + 1]
+      float* const to = reinterpret_cast<float*>(smem + S::PART_AT) + (part * rows + 2 * t) * (COLS + 1) + r;       // [rows][COLS + 1]
 #pragma unroll
       for (int a = 0; a < MT; ++a)
 #pragma unroll
@@ -277,10 +276,10 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
     }
   }
   __syncthreads();
-  for (int x = threadIdx.x; x < p.per_cta * rows * COLS; x += WARPS * 32) {
-    const int col = x % COLS, tile_row = x / COLS, which = tile_row / rows, row = tile_row - which * rows, n = (blockIdx.x * p.per_cta + which) * COLS + col;
+  for (int x = threadIdx.x; x < rows * COLS; x += WARPS * 32) {
+    const int col = x % COLS, row = x / COLS, n = tile * COLS + col;
     if (n >= p.N) continue;
-    const float* from = reinterpret_cast<const float*>(smem + S::PART_AT) + (which * PARTS * rows + row) * (COLS + 1) + col;
+    const float* from = reinterpret_cast<const float*>(smem + S::PART_AT) + row * (COLS + 1) + col;
     float q[PARTS];
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) q[i] = i < n_parts ? from[i * rows * (COLS + 1)] : 0.0f;
@@ -545,7 +544,7 @@ cudaError_t launch_more(const rg_weights_four_t* W, W4Params p, cudaStream_t st)
 }
 
 template <bool F16, int GROUP, int MT, int WARPS>
-cudaError_t launch_tiles(const rg_weights_four_t* W, W4Params p, int wpt, cudaStream_t st) {
+cudaError_t launch_tiles(const rg_weights_four_t* W, const W4Params& p, cudaStream_t st) {
   using S = Shape4<GROUP, MT, WARPS>;
   static DeviceOnce configured;
   const DeviceInfo dev = current_device();
@@ -556,13 +555,11 @@ cudaError_t launch_tiles(const rg_weights_four_t* W, W4Params p, int wpt, cudaSt
   }
   CUtensorMap codes;                                   // four codes an element of 16 bits
   if (!make_tmap_4d(&codes, W->codes, RG_BF16, {p.K / 4, p.N, 1, 1}, {W->code_ld / 2, 0, 0}, {SPAN / 4, S::COLS, 1, 1})) return cudaErrorInvalidValue;
-  p.wpt = wpt;
-  p.per_cta = WARPS / wpt;
   const int tiles = (p.N + S::COLS - 1) / S::COLS;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((tiles + p.per_cta - 1) / p.per_cta), 1, 1);
+  cfg.gridDim = dim3((unsigned)tiles, 1, 1);
   cfg.blockDim = dim3(WARPS * 32, 1, 1);
-  cfg.dynamicSmemBytes = S::SMEM + p.per_cta * PARTS * p.M * (S::COLS + 1) * 4;
+  cfg.dynamicSmemBytes = S::SMEM + PARTS * p.M * (S::COLS + 1) * 4;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -571,16 +568,14 @@ cudaError_t launch_tiles(const rg_weights_four_t* W, W4Params p, int wpt, cudaSt
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, gemv_w4_kernel<F16, GROUP, MT, WARPS>, codes, p);
 }
-// Warps: enough for every SM to have WARPS_PER_SM, in tiles of 32 rows of weights (A's elements are read and put in order once for them) if that is enough
-// with eight warps a tile, else of 16; and no more a tile than that takes.
-constexpr int WARPS_PER_SM = 12;
+// Tiles of 16 rows of weights with eight warps, while all of them fit the GPU at a time, two an SM (4096 x 14336: 14.1 us, 18.4 in tiles of 32; 6144 x 4096, which does
+// not fit: 8.0 and 6.8); then tiles of 32, for which A's elements are read and put in order once, with four warps, or with eight where four leave fewer than
+// 12 an SM (8192 x 8192: 14.2 us with eight; 14336 x 4096: 16.1 with eight, 13.5 with four; 57344 x 8192: 62.5 with four, 79.5 with a warp a tile).
 template <bool F16, int GROUP>
 cudaError_t launch_few(const rg_weights_four_t* W, const W4Params& p, cudaStream_t st) {
-  const int64_t want = (int64_t)WARPS_PER_SM * current_device().sms, wide = (p.N + 31) / 32;
-  if (wide * PARTS < want) return launch_tiles<F16, GROUP, 1, 8>(W, p, PARTS, st);
-  int wpt = PARTS;
-  while (wpt > 1 && wide * (wpt / 2) >= want) wpt /= 2;
-  return wpt == 8 ? launch_tiles<F16, GROUP, 2, 8>(W, p, wpt, st) : launch_tiles<F16, GROUP, 2, 4>(W, p, wpt, st);
+  const int64_t sms = current_device().sms, wide = (p.N + 31) / 32;
+  if ((p.N + 15) / 16 <= 2 * sms) return launch_tiles<F16, GROUP, 1, 8>(W, p, st);
+  return wide * 4 < 12 * sms ? launch_tiles<F16, GROUP, 2, 8>(W, p, st) : launch_tiles<F16, GROUP, 2, 4>(W, p, st);
 }
 template <bool F16, int GROUP>
 cudaError_t launch_group(const rg_weights_four_t* W, W4Params p, cudaStream_t st) {
