@@ -10,11 +10,11 @@
 // the order of k within a group is the tensor core's own affair as long as A's elements follow it.  tcgen05 would want the unpacked weights in shared or
 // tensor memory, a trip that costs more than these few rows' products.  Every warp streams its own stages into shared memory, a TMA box at a time.
 //
-// Two kernels.  One or two rows: a warp copies A's elements along with its codes and never waits for another warp until all its parts are done.
+// Two kernels.  One to four rows: a warp copies A's elements along with its codes and never waits for another warp until all its parts are done.
 // More: eight warps share A's elements in shared memory, stage by stage.  28672 x 4096 in groups of 128, a graph of calls on rotating weights, us:
 //   rows          1      2      4      8     16     40
-//   the first    21.1   21.6   (29.0   33.1   71, as forms for up to 16 rows that read A's elements from global memory; so 25.0 and 25.9 for 1 and 2)
-//   the second   26.1   26.3   26.3   26.5   35.7   58.3
+//   the first    21.3   21.7   22.5   29.7   (71, as a form for 16 rows that reads A's elements from global memory)
+//   the second   26.1   26.2   26.2   26.5   35.7   58.3
 // What bounds them: the bytes of the codes would take 9.4 us.  The instructions that unpack them (a mask that makes a float's mantissa of the nibble, and one
 // subtraction, for two codes, with a shift for three of four) keep the half-rate integer pipe busy for 8 us, and 12 to 16 warps of an SM do not cover all
 // waits between them; a grid of 128-row blocks also fills its last wave only in part.
@@ -81,18 +81,18 @@ __device__ __forceinline__ uint32_t unpack(uint32_t w, uint32_t mask, uint32_t m
 constexpr int STAGE = 16 * 128;                        // bytes of a stage's codes for 16 rows
 template <int GROUP> constexpr int PER = SPAN / GROUP;                 // groups of a stage
 
-// ---------------------------------------------------------------- one or two rows
+// ---------------------------------------------------------------- one to four rows
 // A CTA's tile is 16 MT rows of weights; its four or eight warps share it, each with one or two parts of K.
-constexpr int FEW = 2;                                 // rows
+constexpr int FEW = 4;                                 // rows
 template <int GROUP, int MT, int WARPS>
 struct Shape4 {
-  static constexpr int COLS = 16 * MT, DEPTH = MT == 1 ? 4 : 2;       // stages of a warp's ring, one being worked on
+  static constexpr int COLS = 16 * MT, DEPTH = MT == 1 ? 3 : 2;       // stages of a warp's ring, one being worked on
   static constexpr int SLOT = MT * STAGE, SCALES = PER<GROUP> * COLS * 8;           // (scale, less) pairs of a stage
-  static constexpr int PART = FEW * (COLS + 1) * 4;    // a part's sums
-  static constexpr int X_ROW = SPAN * 2 + 16, X = FEW * X_ROW;      // a stage of A; rows begin in different banks
-  static constexpr int X_AT = WARPS * DEPTH * SLOT, SCALE_AT = X_AT + WARPS * DEPTH * X, BAR_AT = SCALE_AT + WARPS * SCALES, FLAG_AT = BAR_AT + WARPS * DEPTH * 8, PART_AT = FLAG_AT + 16, SMEM = 1024 + PART_AT;
-  static constexpr int MOST = SMEM + PARTS * PART;
-  static_assert(MOST <= 113 * 1024 && BAR_AT % 8 == 0, "fits the SM");
+  static constexpr int X_ROW = SPAN * 2 + 16;          // a row of a stage of A; rows begin in different banks
+  static constexpr int SCALE_AT = WARPS * DEPTH * SLOT, BAR_AT = SCALE_AT + WARPS * SCALES, FLAG_AT = BAR_AT + WARPS * DEPTH * 8, PART_AT = FLAG_AT + 16, SMEM = 1024 + PART_AT;
+  static constexpr int ROW = PARTS * (COLS + 1) * 4 + WARPS * DEPTH * X_ROW;         // for every row of A: its parts' sums and, behind them all, its stages
+  static constexpr int MOST = SMEM + FEW * ROW;
+  static_assert(MOST <= 120 * 1024 && BAR_AT % 8 == 0, "fits the SM, but for four rows of eight warps in groups of 32 twice");
 };
 
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
@@ -149,11 +149,11 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint8_t* const mine = smem + warp * (DEPTH * S::SLOT);
-  uint8_t* const x_mine = smem + S::X_AT + warp * (DEPTH * S::X);
   float2* const sz = reinterpret_cast<float2*>(smem + S::SCALE_AT + warp * S::SCALES);      // [MT][G][16] (scale, less)
   const uint32_t bars = smem_u32(smem + S::BAR_AT) + warp * (DEPTH * 8);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + S::FLAG_AT);
-  const int rows = p.M;
+  const int rows = p.M, x_slot = rows * S::X_ROW;
+  uint8_t* const x_mine = smem + S::PART_AT + PARTS * rows * (COLS + 1) * 4 + warp * (DEPTH * x_slot);
   // the warp's parts of K: the first one, how many, and their stages
   const int tile = blockIdx.x, stages = (p.K + SPAN - 1) / SPAN, n_parts = (stages + p.part - 1) / p.part;
   constexpr int SHARE = PARTS / WARPS;
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
   };
   auto request_x = [&](int i) {
     if (i < n_st && lane < rows)
-      bulk_load_1d(smem_u32(x_mine) + i % DEPTH * S::X + lane * S::X_ROW, p.A + lane * p.lda + (s0 + i) * SPAN, 2 * min(SPAN, p.K - (s0 + i) * SPAN), bars + 8 * (i % DEPTH));
+      bulk_load_1d(smem_u32(x_mine) + i % DEPTH * x_slot + lane * S::X_ROW, p.A + lane * p.lda + (s0 + i) * SPAN, 2 * min(SPAN, p.K - (s0 + i) * SPAN), bars + 8 * (i % DEPTH));
   };
   Scales<GROUP, MT> scales(p, (int64_t)tile * COLS + lane / G, s0 * G + lane % G);
 
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       if (decltype(tail)::value && g * GROUP >= left) break;
-      window(g, slot * S::SLOT + (w_lane ^ (g * (GROUP / 2))), x_at + slot * S::X, sz + r + g * 16, left, tail);
+      window(g, slot * S::SLOT + (w_lane ^ (g * (GROUP / 2))), x_at + slot * x_slot, sz + r + g * 16, left, tail);
     }
     __syncwarp();                                      // the slot and the scales are free
   };
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
   }
 }
 
-// ---------------------------------------------------------------- three rows and more
+// ---------------------------------------------------------------- five rows and more
 // The same sums for 8 NT rows of A.  Eight warps, each with a tile of 16 rows of weights of its own, work on the same stage, for which they share A's elements in shared
 // memory (put there, and into the codes' order, once).  The parts of K are shared among the CTAs of a cluster, or are all one CTA's, and are joined over distributed shared
 // memory, every CTA a share of the elements.  How many parts a CTA has (1, 2, 4 or all 8) is the choice with which the waves of CTAs take the fewest stages (below):
@@ -559,7 +559,7 @@ cudaError_t launch_tiles(const rg_weights_four_t* W, const W4Params& p, cudaStre
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)tiles, 1, 1);
   cfg.blockDim = dim3(WARPS * 32, 1, 1);
-  cfg.dynamicSmemBytes = S::SMEM + PARTS * p.M * (S::COLS + 1) * 4;
+  cfg.dynamicSmemBytes = S::SMEM + p.M * S::ROW;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
