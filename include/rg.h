@@ -191,7 +191,7 @@ size_t rg_gemm_workspace_bytes(const rg_desc_t* d, int64_t M, int64_t N);
  *
  *   A: [M,K], B: [N,K] (both K-contiguous) at d->in_dtype (bf16 or fp16); C: [M,N] bf16, fp16 or fp32;
  *   bias and residual likewise bf16, fp16 or fp32.
- *   A.ptr, B.ptr 16-byte aligned; A.ld, B.ld multiples of 8.  C, bias, residual: any alignment.
+ *   A.ptr, B.ptr 16-byte aligned; A.ld, B.ld multiples of 8.  C, bias, residual: aligned to their type.
  *   epi: nullable.  ws: device, 16-byte aligned, >= rg_gemm_workspace_bytes; contents undefined
  *   afterwards (it may not be touched at all when the library merges in-cluster); may be NULL when
  *   there are no cuts or when the descriptor sets split_merge = 2.
@@ -421,7 +421,7 @@ typedef struct {
  * part's running sum; K has at most eight parts (of whole 256s, each but the last of equal length), the first four and the rest added in ascending order each,
  * then to one another; then the epilogue of rg_gemm and one rounding.  No weight is narrowed.  A row's bits do not depend on M, strides or
  * the run.  Meant for a few rows: the weights are read once for every 40 of them, and from some hundred rows on weights unpacked once for rg_gemm are faster.
- *   A: [M][K] bf16 or fp16, 16-byte aligned, ld a multiple of 8; K a multiple of 32; C, bias, residual: bf16, fp16 or fp32, any alignment.
+ *   A: [M][K] bf16 or fp16, 16-byte aligned, ld a multiple of 8; K a multiple of 32; C, bias, residual: bf16, fp16 or fp32, aligned to their type.
  *   codes: 16-byte aligned; scales: aligned to their type.  M is at most 2^19.  M == 0 or N == 0: RG_OK, nothing launched.  K == 0: RG_ERR_SHAPE.
  * Asynchronous on `cuda_stream`; no workspace. */
 rg_status_t rg_gemv_four(const rg_weights_four_t* W, const rg_tensor_t* A, const rg_tensor_t* C, const rg_epilogue_t* epi, void* cuda_stream);

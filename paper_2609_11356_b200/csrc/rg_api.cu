@@ -95,6 +95,14 @@ rg_status_t check_epilogue(const rg_epilogue_t* e, int64_t N) {
   return RG_OK;
 }
 
+// Results, bias and residual are read and written element by element: any place that their type can have.
+rg_status_t check_element_alignment(const rg_tensor_t* C, const rg_epilogue_t* e) {
+  auto off = [](const void* p, int32_t dtype) { return reinterpret_cast<uintptr_t>(p) % esize(dtype) != 0; };
+  if (off(C->ptr, C->dtype)) return RG_ERR_ALIGNMENT;
+  if (e && ((e->bias && off(e->bias, e->bias_dtype)) || (e->residual && off(e->residual, e->residual_dtype)))) return RG_ERR_ALIGNMENT;
+  return RG_OK;
+}
+
 rg_status_t check_gemm_shapes(const rg_tensor_t* A, const rg_tensor_t* B, const rg_tensor_t* C) {
   rg_status_t s;
   if ((s = check_tensor(A, true)) != RG_OK || (s = check_tensor(B, true)) != RG_OK || (s = check_tensor(C)) != RG_OK) return s;
@@ -357,6 +365,7 @@ rg_status_t rg_gemm(const rg_desc_t* d, const rg_tensor_t* A, const rg_tensor_t*
   if ((reinterpret_cast<uintptr_t>(A->ptr) & 15) || (reinterpret_cast<uintptr_t>(B->ptr) & 15) ||
       (A->ld % ld_mult) || (B->ld % ld_mult))
     return RG_ERR_ALIGNMENT;
+  if ((s = check_element_alignment(C, epi)) != RG_OK) return s;
   if (A->dtype == RG_F8E4M3 && (K & 1)) return RG_ERR_SHAPE;   // rows of 8-bit operands are whole byte pairs
   if (d->n_cuts && d->split_merge != 2) {                    // the in-cluster merge keeps the parts in shared memory
     if (!ws || ws_bytes < rg_gemm_workspace_bytes(d, M, N)) return RG_ERR_WORKSPACE;
@@ -753,6 +762,7 @@ rg_status_t rg_gemv_four(const rg_weights_four_t* W, const rg_tensor_t* A, const
   if ((s = check_epilogue(epi, W->rows)) != RG_OK) return s;
   if (A->rows == 0 || W->rows == 0) return RG_OK;
   if ((reinterpret_cast<uintptr_t>(A->ptr) & 15) || A->ld % 8) return RG_ERR_ALIGNMENT;
+  if ((s = check_element_alignment(C, epi)) != RG_OK) return s;
   return rg::launch_gemv_w4(W, A, C, epi, static_cast<cudaStream_t>(cuda_stream));
 }
 

@@ -237,6 +237,23 @@ def test_argument_errors_are_reported_before_any_launch():
     assert L.rg_reduce_cols_workspace_bytes(65537, 10) == (257 + 2) * 10 * 4
 
 
+@pytest.mark.parametrize("atom", [K.RG_ATOM_TC_BF16_K16, K.RG_ATOM_SCALAR])
+@pytest.mark.parametrize("dtype,off", [(K.RG_BF16, 1), (K.RG_F16, 1), (K.RG_F32, 1), (K.RG_F32, 2)])
+def test_results_and_epilogues_off_their_type_are_refused(dtype, off, atom):
+    fake = 1 << 20
+    d, A, B = rg.rg_desc(atom=atom), K.rg_tensor_t(fake, K.RG_BF16, 4, 64, 64), K.rg_tensor_t(fake, K.RG_BF16, 8, 64, 64)
+
+    def gemm(c=fake, **kw):
+        e = K.rg_epilogue_t()
+        for k, v in kw.items():
+            setattr(e, k, v)
+        return K.load().rg_gemm(C.byref(d), C.byref(A), C.byref(B), C.byref(K.rg_tensor_t(c, dtype, 4, 8, 8)), C.byref(e), None, 0, None)
+
+    assert gemm(fake + off) == 5                              # RG_ERR_ALIGNMENT
+    assert gemm(bias=fake + off, bias_dtype=dtype) == 5
+    assert gemm(residual=fake + off, residual_dtype=dtype, ldr=8) == 5
+
+
 def test_status_strings():
     for s in range(9):
         assert len(rg.rg_status_string(s)) > 1

@@ -80,6 +80,16 @@ def test_gemv_refusals(status, kw):
     assert gemv(**kw) == status
 
 
+@pytest.mark.parametrize("dtype,off", [(K.RG_BF16, 1), (K.RG_F16, 1), (K.RG_F32, 1), (K.RG_F32, 2)])
+def test_gemv_refuses_results_and_epilogues_off_their_type(dtype, off):
+    """Elements are accessed one by one, each where its type can lie."""
+    assert gemv(C=matrix(3, 32, dtype=dtype, ptr=FAKE + off)) == ALIGN
+    assert gemv(epi=epilogue(bias=FAKE + off, bias_dtype=dtype)) == ALIGN
+    assert gemv(epi=epilogue(residual=FAKE + off, residual_dtype=dtype, ldr=32)) == ALIGN
+    # nothing to compute, nothing to access
+    assert gemv(A=matrix(0), C=matrix(0, 32, dtype=dtype, ptr=FAKE + off)) == OK
+
+
 CACHES = [
     (NULL, None), (NULL, cache(ptr=None)), (SHAPE, cache(pages=-1)), (SHAPE, cache(page=0)), (SHAPE, cache(heads=0)), (SHAPE, cache(heads=65536)), (SHAPE, cache(dim=2048)),
     (UNSUPPORTED, cache(dim=48)), (UNSUPPORTED, cache(dim=160)), (UNSUPPORTED, cache(page=12)), (ALIGN, cache(ptr=FAKE + 8)), (ALIGN, cache(head_stride=16 * 36 + 8)),
