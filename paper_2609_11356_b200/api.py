@@ -470,7 +470,7 @@ def _matrix(t) -> bytes:
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError("a matrix has 2 dimensions and contiguous rows")
     n, c = t.shape
-    return _TENSOR.pack(t.data_ptr(), _code(t), n, c, t.stride(0) if n > 1 else max(t.stride(0), c))
+    return _TENSOR.pack(t.data_ptr(), _code(t), n, c, t.stride(0) if n > 1 else c)       # one row: nothing lies a stride further
 
 
 def rg_gemv_four(w: rg_weights_four, A, C_out, *, bias=None, act: int = 0, residual=None):

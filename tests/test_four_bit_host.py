@@ -6,6 +6,7 @@ import torch
 
 import paper_2609_11356_b200 as rg
 from paper_2609_11356_b200 import _cabi as K
+from paper_2609_11356_b200 import api
 
 FAKE = 1 << 20                                               # an address that no refused call may touch
 OK, NULL, DESC, UNSUPPORTED, SHAPE, ALIGN, WS = 0, 1, 2, 3, 4, 5, 6
@@ -146,6 +147,13 @@ def test_block_bytes():
     assert rg.rg_cache_four_block_bytes(16, 128) == 1152 and rg.rg_cache_four_block_bytes(8, 32) == 144
     for page, dim in ((0, 64), (12, 64), (-8, 64), (16, 48), (16, 160), (16, 0), ((1 << 20) + 8, 64)):
         assert rg.rg_cache_four_block_bytes(page, dim) == 0
+
+
+def test_one_row_has_no_stride():
+    """Nothing lies a stride behind a single row, so a view into a wider buffer of any pitch is described as a dense row; several rows keep theirs."""
+    buf = torch.zeros(3, 259, dtype=torch.bfloat16)
+    for t, ld in ((buf[:1, :256], 256), (buf[2:, 1:257], 256), (buf[:0, :256], 256), (buf[:2, :256], 259), (buf[:1, :256].expand(2, 256), 0)):
+        assert api._TENSOR.unpack(api._matrix(t)) == (t.data_ptr(), K.RG_BF16, t.shape[0], 256, ld)
 
 
 def test_handles_describe_their_tensors():

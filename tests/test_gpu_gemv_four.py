@@ -232,3 +232,16 @@ def test_codes_beyond_32_bits():
     codes.copy_(c)
     A = torch.randn(3, K, generator=generator(2), device=DEV).to(BF)
     assert torch.equal(product(A, codes, s, z, 32, F32), product(A, c, s, z, 32, F32))
+
+
+@pytest.mark.parametrize("pitch", [513, 515, 524])
+def test_one_row_of_a_buffer_of_any_pitch(pitch):
+    """A single token's row, contiguous and aligned, out of a buffer whose rows lie an odd number of elements apart; results and residual likewise."""
+    K, N = 512, 40
+    w = weights(N, K, 64, seed=3)
+    A, out = torch.full((2, pitch), float("nan"), dtype=BF, device=DEV), torch.full((2, pitch), 3.0, dtype=BF, device=DEV)
+    A[0, :K] = torch.randn(K, generator=generator(4), device=DEV).to(BF)
+    r = torch.randn(2, N + 1, generator=generator(5), device=DEV)[:1, :N]
+    want = check(A[:1, :K].clone(), *w, 64, BF, residual=r.clone())
+    rg.rg_gemv_four(rg.rg_weights_four(w[0], w[1], zeros=w[2], group=64), A[:1, :K], out[:1, 1:N + 1], residual=r)
+    assert torch.equal(out[:1, 1:N + 1], want) and bool((out[0, :1] == 3.0).all()) and bool((out[0, N + 1:] == 3.0).all()) and bool((out[1] == 3.0).all())
