@@ -419,7 +419,7 @@ typedef struct {
 /* C[M][N] = epilogue(A . W^T) with W in four bits.  Per group the products of A with the integers u - zero are summed by a chain of 16-wide
  * tensor-core steps from zero (fp32; the order of k within a group is fixed by this library), times the group's scale in fp32 and onto a
  * part's running sum; K has at most eight parts (of whole 256s, each but the last of equal length), the first four and the rest added in ascending order each,
- * then to one another; then the epilogue of rg_gemm and one rounding.  No weight is narrowed.  A row's bits do not depend on M, strides or
+ * then to one another (a sum that is zero is +0); then the epilogue of rg_gemm and one rounding.  No weight is narrowed.  A row's bits do not depend on M, strides or
  * the run.  Meant for a few rows: the weights are read once for every 40 of them, and from some hundred rows on weights unpacked once for rg_gemm are faster.
  *   A: [M][K] bf16 or fp16, 16-byte aligned, ld a multiple of 8; K a multiple of 32; C, bias, residual: bf16, fp16 or fp32, aligned to their type.
  *   codes: 16-byte aligned; scales: aligned to their type.  M is at most 2^19.  M == 0 or N == 0: RG_OK, nothing launched.  K == 0: RG_ERR_SHAPE.

@@ -4,7 +4,8 @@
 // The inner sum is a chain of 16-wide tensor-core steps from a zero accumulator: u - z is an integer of at most four bits and a sign, exact in bf16 and
 // fp16, so nothing is rounded before the products' fp32 sum.  The scale multiplies a finished group once, in fp32 (fused, onto the running sum of a part of
 // K): no weight is ever narrowed, whatever the scales' type.  A part is a run of whole 256-wide stages, at most eight of them over K; the lower and the
-// upper four are each added in ascending order, and then to one another.  The cut follows from K alone and an accumulator's column is one row of A, so a row's bits do not depend on M.
+// upper four are each added in ascending order, and then to one another, and zero last of all: parts that a form adds as zeros, and another does not, would else tell a
+// sum of -0 (of products below the smallest number) apart.  The cut follows from K alone and an accumulator's column is one row of A, so a row's bits do not depend on M.
 //
 // Weights are the 16 rows of mma.sync's first operand, read straight from the natural order of the codes: a warp's lanes hold whole words of eight codes, and
 // the order of k within a group is the tensor core's own affair as long as A's elements follow it.  tcgen05 would want the unpacked weights in shared or
@@ -100,7 +101,7 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(0), "r"(bar) : "memory");
 }
 
-// The sum of the parts of K: of the lower and of the upper four, each in ascending order.
+// The sum of the parts of K: of the lower and of the upper four, each in ascending order.  The epilogue takes it with zero added.
 __device__ __forceinline__ float join(const float (&q)[PARTS]) {
   return f_add(f_add(f_add(f_add(q[0], q[1]), q[2]), q[3]), f_add(f_add(f_add(q[4], q[5]), q[6]), q[7]));
 }
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
     float q[PARTS];
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) q[i] = i < n_parts ? from[i * rows * (COLS + 1)] : 0.0f;
-    const float v = join(q);
+    const float v = f_add(join(q), 0.0f);
     store_scalar(p.C, p.c_dtype, (int64_t)row * p.ldc + n, apply_epilogue(v, p.epi, row, n));
   }
   if (*abort_flag) {                                   // a wait gave up: let copies in flight end
@@ -496,7 +497,7 @@ __global__ void __launch_bounds__(RW * 32, 2) gemv_w4_rows_kernel(const __grid_c
     } else {
       v = sums[row * (COLS + 1) + col];
     }
-    store_scalar(p.C, p.c_dtype, (int64_t)(m0 + row) * p.ldc + n, apply_epilogue(v, p.epi, m0 + row, n));
+    store_scalar(p.C, p.c_dtype, (int64_t)(m0 + row) * p.ldc + n, apply_epilogue(f_add(v, 0.0f), p.epi, m0 + row, n));
   }
   if (*abort_flag) {                                   // a wait gave up: let copies in flight end
     const uint64_t t0 = globaltimer_ns();

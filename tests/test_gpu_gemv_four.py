@@ -245,3 +245,15 @@ def test_one_row_of_a_buffer_of_any_pitch(pitch):
     want = check(A[:1, :K].clone(), *w, 64, BF, residual=r.clone())
     rg.rg_gemv_four(rg.rg_weights_four(w[0], w[1], zeros=w[2], group=64), A[:1, :K], out[:1, 1:N + 1], residual=r)
     assert torch.equal(out[:1, 1:N + 1], want) and bool((out[0, :1] == 3.0).all()) and bool((out[0, N + 1:] == 3.0).all()) and bool((out[1] == 3.0).all())
+
+
+@pytest.mark.parametrize("out_dtype", [BF, F32])
+@pytest.mark.parametrize("N,K", [(250, 32), (250, 288), (129, 1056), (70, 1312), (333, 2080), (5000, 544), (15000, 1312)])
+def test_sums_that_vanish_have_the_same_zero_in_every_number_of_rows(N, K, out_dtype):
+    """Products below the smallest number of either sign: a group's scaled sum is rounded to a zero with its sign.  One to eight parts of K, whose missing ones some
+    forms add as zeros and others do not; a row's zeros have the same bits in all of them."""
+    codes, _, z = weights(N, K, 32, seed=K)
+    s = torch.full((N, -(-K // 32)), 2.0 ** -100, dtype=F32, device=DEV) * torch.where(torch.arange(N, device=DEV) % 2 == 0, 1.0, -1.0)[:, None]
+    A = torch.full((41, K), 2.0 ** -70, dtype=BF, device=DEV) * torch.where(torch.arange(41, device=DEV) % 3 == 0, 1.0, -1.0)[:, None].to(BF)
+    for M in (1, 2, 4, 5, 8, 17, 33, 41):
+        assert not bool(product(A[:M], codes, s, z, 32, out_dtype).view(torch.int16).any()), M
