@@ -11,7 +11,7 @@
 // the order of k within a group is the tensor core's own affair as long as A's elements follow it.  tcgen05 would want the unpacked weights in shared or
 // tensor memory, a trip that costs more than these few rows' products.  Every warp streams its own stages into shared memory, a TMA box at a time.
 //
-// Two kernels.  One to four rows: a warp copies A's elements along with its codes and never waits for another warp until all its parts are done.
+// Two kernels.  One to four rows (a rule below has the exceptions): a warp copies A's elements along with its codes and never waits for another warp until all its parts are done.
 // More: eight warps share A's elements in shared memory, stage by stage.  28672 x 4096 in groups of 128, a graph of calls on rotating weights, us:
 //   rows          1      2      4      8     16     40
 //   the first    21.3   21.7   22.5   29.7   (71, as a form for 16 rows that reads A's elements from global memory)
@@ -571,16 +571,30 @@ cudaError_t launch_tiles(const rg_weights_four_t* W, const W4Params& p, cudaStre
 }
 // Tiles of 16 rows of weights with eight warps, while all of them fit the GPU at a time, two an SM (4096 x 14336: 14.1 us, 18.4 in tiles of 32; 6144 x 4096, which does
 // not fit: 8.0 and 6.8); then tiles of 32, for which A's elements are read and put in order once, with four warps, or with eight where four leave fewer than
-// 12 an SM (8192 x 8192: 14.2 us with eight; 14336 x 4096: 16.1 with eight, 13.5 with four; 57344 x 8192: 62.5 with four, 79.5 with a warp a tile).
+// 12 an SM (8192 x 8192: 14.2 us with eight; 14336 x 4096: 16.1 with eight, 13.5 with four; 57344 x 8192: 62.5 with four, 79.5 with a warp a tile).  Three and four rows in
+// groups of 32 fill shared memory first: four warps, three CTAs an SM, as soon as eight take more than one wave of two (10240 x 4096: 17.1 us with four, 19.6 and 22.3 with eight).
 template <bool F16, int GROUP>
 cudaError_t launch_few(const rg_weights_four_t* W, const W4Params& p, cudaStream_t st) {
   const int64_t sms = current_device().sms, wide = (p.N + 31) / 32;
   if ((p.N + 15) / 16 <= 2 * sms) return launch_tiles<F16, GROUP, 1, 8>(W, p, st);
-  return wide * 4 < 12 * sms ? launch_tiles<F16, GROUP, 2, 8>(W, p, st) : launch_tiles<F16, GROUP, 2, 4>(W, p, st);
+  const bool eight = GROUP == 32 && p.M > 2 ? wide <= 2 * sms : wide * 4 < 12 * sms;
+  return eight ? launch_tiles<F16, GROUP, 2, 8>(W, p, st) : launch_tiles<F16, GROUP, 2, 4>(W, p, st);
+}
+// Up to four rows the first kernel, but for sizes at which its tiles need a second wave of CTAs for lack of shared memory and the second kernel's need one.  Four rows in groups
+// of 32, tiles that would have eight warps: one CTA fits an SM (4740 x 4096: 13.4 us, the second kernel 13.2; 8704 x 4096: 16.1 and 14.1; 8704 x 14336: 40.5 and 38.2); from 15/8 tiles
+// an SM on clusters of the second kernel find no room in one wave either (9216 x 4096: 16.2 and 22.2).  Three or four rows in groups of 32, four in groups of 64, with four warps: three
+// CTAs an SM, and the second kernel's 148 blocks are four tiles an SM (groups of 32, 18432 x 4096: 28.3 and 23.1 us, 16384 x 8192: 53.1 and 42.4; groups of 64: 19.7 and 17.8; 19072 x 4096 in groups
+// of 32: 29.1 and 40.5; three rows in groups of 64, of which four fit: 16.4 and 17.8).
+template <int GROUP>
+bool takes_few(const W4Params& p) {
+  if (p.M > FEW) return false;
+  const int64_t sms = current_device().sms, wide = (p.N + 31) / 32;
+  if (GROUP == 32 && p.M == 4 && (p.N + 15) / 16 > 2 * sms && wide * 8 <= 15 * sms) return false;
+  return !((GROUP == 32 ? p.M > 2 : GROUP == 64 && p.M == 4) && wide > 3 * sms && wide <= 4 * sms);
 }
 template <bool F16, int GROUP>
 cudaError_t launch_group(const rg_weights_four_t* W, W4Params p, cudaStream_t st) {
-  if (p.M <= FEW) return launch_few<F16, GROUP>(W, p, st);
+  if (takes_few<GROUP>(p)) return launch_few<F16, GROUP>(W, p, st);
   const int passes = (p.M + 39) / 40;                  // over the rows, as even as eights allow
   p.rows = ((p.M + passes - 1) / passes + 7) / 8 * 8;
   switch (p.rows / 8) {

@@ -257,3 +257,37 @@ def test_sums_that_vanish_have_the_same_zero_in_every_number_of_rows(N, K, out_d
     A = torch.full((41, K), 2.0 ** -70, dtype=BF, device=DEV) * torch.where(torch.arange(41, device=DEV) % 3 == 0, 1.0, -1.0)[:, None].to(BF)
     for M in (1, 2, 4, 5, 8, 17, 33, 41):
         assert not bool(product(A[:M], codes, s, z, 32, out_dtype).view(torch.int16).any()), M
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N,K", [(40, 1056), (4736, 288), (4737, 544), (8864, 2080), (8865, 544), (9472, 544), (9473, 2080), (14208, 544), (14209, 1056), (18944, 2080), (18945, 544), (30011, 544)])
+def test_one_to_five_rows_on_weights_of_every_size(N, K, group, dtype):
+    """Either side of every number of weights' rows at which up to five rows of A go to another tile, another number of warps or the other kernel: against the definition,
+    and the same bits whatever comes along."""
+    codes, s, z = weights(N, K, group, seed=N + K)
+    A = torch.randn(6, K, generator=generator(N), device=DEV).to(dtype)
+    full = check(A, codes, s, z, group, F32)
+    for M in (1, 2, 3, 4, 5):
+        assert torch.equal(product(A[:M].contiguous(), codes, s, z, group, F32), full[:M]), M
+        assert torch.equal(product(A[6 - M:].contiguous(), codes, s, z, group, F32, w_static=1), full[6 - M:]), M
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N,K", [(1, 32), (17, 96), (16, 128), (33, 256), (100, 288), (1000, 4096), (65, 2080), (48, 14336), (5, 2048 + 32)])
+@pytest.mark.parametrize("M", [2, 4, 5])
+def test_sizes_and_groups_at_the_border_of_the_kernels(M, N, K, group, zeros):
+    A = torch.randn(M, K, generator=generator(M + N), device=DEV).to(BF)
+    check(A, *weights(N, K, group, zeros=zeros, seed=K), group, BF)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N,K", [(333, 4096), (40, 8224)])
+def test_bits_of_four_and_five_rows(N, K, group, dtype):
+    A = torch.randn(10, K, generator=generator(5), device=DEV).to(dtype)
+    w = weights(N, K, group, seed=6)
+    whole = product(A, *w, group, F32)
+    for lo, hi in ((0, 4), (0, 5), (3, 7), (5, 10), (6, 10)):
+        assert torch.equal(product(A[lo:hi], *w, group, F32), whole[lo:hi])
