@@ -1,6 +1,7 @@
 // The C boundary: argument validation, descriptor canonicalisation and class key, plan
 // selection, and the host-buffer forms.  Nothing here does arithmetic on data.
 #include <algorithm>
+#include <initializer_list>
 #include <string.h>
 #include <utility>
 
@@ -647,19 +648,35 @@ size_t rg_paged_attention_workspace_bytes(const rg_paged_attn_desc_t* d, const r
   return align_up((size_t)tokens * q_heads * n * (size_t)(dim + 2) * sizeof(float), 256);
 }
 
+namespace {
+struct Operands {                                          // what the kernel reads through tensor maps
+  int n = 0;
+  int64_t strides[8], sizes[8];
+  uintptr_t addresses = 0;                                 // all of them, their bits together
+  void add(const void* ptr, std::initializer_list<std::pair<int64_t, int64_t>> dims) {
+    for (const auto& x : dims) { strides[n] = x.first; sizes[n++] = x.second; }
+    addresses |= reinterpret_cast<uintptr_t>(ptr);
+  }
+  // strides, then dimensions that repeat one address (there is no tensor map for them), then addresses
+  rg_status_t check() const {
+    for (int i = 0; i < n; ++i) if (strides[i] % 8) return RG_ERR_ALIGNMENT;
+    for (int i = 0; i < n; ++i) if (strides[i] == 0 && sizes[i] > 1) return RG_ERR_UNSUPPORTED;
+    return addresses & 15 ? RG_ERR_ALIGNMENT : RG_OK;
+  }
+};
+}  // namespace
+
 // what rg_paged_attention and rg_paged_attention_four have in common, once rows, caches and sequences are checked by themselves
-static rg_status_t attend(const rg_paged_attn_desc_t* d, const rg_rows_t* q, rg::PagedAttnArgs a, rg_status_t caches, int64_t pages, int64_t page_size, int64_t kv_heads, const rg_paged_seqs_t* seqs,
+static rg_status_t attend(const rg_paged_attn_desc_t* d, const rg_rows_t* q, rg::PagedAttnArgs a, Operands mapped, int64_t pages, int64_t page_size, int64_t kv_heads, const rg_paged_seqs_t* seqs,
                           const rg_rows_t* out, float* lse, int64_t lse_ld, void* ws, size_t ws_bytes, void* cuda_stream) {
   if (out->dtype != q->dtype && out->dtype != RG_F32) return RG_ERR_SHAPE;
   if (out->tokens != q->tokens || out->heads != q->heads || out->dim != q->dim) return RG_ERR_SHAPE;
   if (q->heads % kv_heads) return RG_ERR_SHAPE;
   if (q->dim % 8 || q->dim > 128 || page_size % 8 || q->heads / kv_heads > 128) return RG_ERR_UNSUPPORTED;
   if (lse && (lse_ld < q->heads || reinterpret_cast<uintptr_t>(lse) % 4)) return RG_ERR_SHAPE;
-  if (caches != RG_OK) return caches;                      // their strides and addresses, after the shapes
-  if (q->token_stride % 8 || q->head_stride % 8) return RG_ERR_ALIGNMENT;
-  // a dimension that repeats one address has no tensor map
-  if ((q->token_stride == 0 && q->tokens > 1) || (q->head_stride == 0 && q->heads > 1)) return RG_ERR_UNSUPPORTED;
-  if (reinterpret_cast<uintptr_t>(q->ptr) & 15) return RG_ERR_ALIGNMENT;
+  mapped.add(q->ptr, {{q->token_stride, q->tokens}, {q->head_stride, q->heads}});
+  const rg_status_t s = mapped.check();
+  if (s != RG_OK) return s;
   const int64_t max_len = pages > 0 ? bound_of_len(seqs, page_size) : 0;
   if (max_len > DIM_LIMIT / 2) return RG_ERR_SHAPE;
   if (q->tokens == 0 || seqs->n_seqs == 0) return RG_OK;
@@ -688,16 +705,11 @@ rg_status_t rg_paged_attention(const rg_paged_attn_desc_t* d, const rg_rows_t* q
   if (k_cache->dtype != q->dtype || v_cache->dtype != q->dtype) return RG_ERR_SHAPE;
   if (k_cache->pages != v_cache->pages || k_cache->page_size != v_cache->page_size || k_cache->heads != v_cache->heads || k_cache->dim != q->dim || v_cache->dim != q->dim)
     return RG_ERR_SHAPE;
-  const int64_t strides[] = {k_cache->page_stride, k_cache->slot_stride, k_cache->head_stride, v_cache->page_stride, v_cache->slot_stride, v_cache->head_stride};
-  // a dimension that repeats one address has no tensor map
-  const int64_t sizes[] = {k_cache->pages, k_cache->page_size, k_cache->heads, v_cache->pages, v_cache->page_size, v_cache->heads};
-  rg_status_t caches = RG_OK;
-  for (int64_t x : strides) if (x % 8) caches = RG_ERR_ALIGNMENT;
-  for (int i = 0; i < 6 && caches == RG_OK; ++i) if (strides[i] == 0 && sizes[i] > 1) caches = RG_ERR_UNSUPPORTED;
-  if (caches == RG_OK && ((reinterpret_cast<uintptr_t>(k_cache->ptr) | reinterpret_cast<uintptr_t>(v_cache->ptr)) & 15)) caches = RG_ERR_ALIGNMENT;
+  Operands mapped;
+  for (const rg_cache_t* c : {k_cache, v_cache}) mapped.add(c->ptr, {{c->page_stride, c->pages}, {c->slot_stride, c->page_size}, {c->head_stride, c->heads}});
   rg::PagedAttnArgs a{};
   a.k = k_cache; a.v = v_cache;
-  return attend(d, q, a, caches, k_cache->pages, k_cache->page_size, k_cache->heads, seqs, out, lse, lse_ld, ws, ws_bytes, cuda_stream);
+  return attend(d, q, a, mapped, k_cache->pages, k_cache->page_size, k_cache->heads, seqs, out, lse, lse_ld, ws, ws_bytes, cuda_stream);
 }
 
 // ------------------------------------------------------------ four bits
@@ -816,7 +828,7 @@ rg_status_t rg_paged_attention_four(const rg_paged_attn_desc_t* d, const rg_rows
   if ((s = check_cache4_pair(k_cache, v_cache)) != RG_OK || k_cache->dim != q->dim) return RG_ERR_SHAPE;
   rg::PagedAttnArgs a{};
   a.k4 = k_cache; a.v4 = v_cache;
-  return attend(d, q, a, RG_OK, k_cache->pages, k_cache->page_size, k_cache->heads, seqs, out, lse, lse_ld, ws, ws_bytes, cuda_stream);
+  return attend(d, q, a, Operands(), k_cache->pages, k_cache->page_size, k_cache->heads, seqs, out, lse, lse_ld, ws, ws_bytes, cuda_stream);
 }
 
 // ------------------------------------------------------------ host-buffer forms

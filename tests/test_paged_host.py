@@ -99,6 +99,16 @@ def test_attention_refuses(status, kw):
     assert attend(**kw) == status
 
 
+@pytest.mark.parametrize("status,kw", [
+    # strides of all operands first, then dimensions that repeat an address, then addresses
+    (ALIGN, {"q": rows(heads=4, head_stride=68), "kc": cache(slot_stride=0)}), (ALIGN, {"q": rows(heads=4, token_stride=260), "vc": cache(page_stride=0)}), (ALIGN, {"q": rows(heads=4, token_stride=0), "vc": cache(head_stride=68)}),
+    (UNSUPPORTED, {"q": rows(heads=4, token_stride=0), "kc": cache(ptr=FAKE + 8)}), (UNSUPPORTED, {"q": rows(heads=4, ptr=FAKE + 8), "vc": cache(head_stride=0)}),
+    (SHAPE, {"lse": FAKE, "lse_ld": 3, "kc": cache(slot_stride=132)}), (SHAPE, {"lse": FAKE, "lse_ld": 3, "q": rows(heads=4, ptr=FAKE + 8)}), (UNSUPPORTED, {"q": rows(heads=258, token_stride=258 * 64 + 4), "out": rows(heads=258)}),
+])
+def test_attention_with_two_faults_names_the_one_that_comes_first(status, kw):
+    assert attend(**kw) == status
+
+
 def test_nothing_to_do_is_fine():
     assert rope(x=rows(0), out=rows(0), pos=pos(cols=0)) == 0
     assert append(k=rows(0), v=rows(0)) == 0 and append(s=seqs(n_seqs=0, block_table=None, seq_lens=None, cu_q=None)) == 0
