@@ -540,7 +540,7 @@ rg_status_t check_positions(const rg_rope_desc_t* d, const rg_tensor_t* pos, int
 extern "C++" {
 template <typename P>
 void set_rotation(P* p, const rg_rope_desc_t* d, const rg_tensor_t* pos, const double* inv_freq) {
-  p->rot = (int32_t)d->rot_dim; p->style = d->style; p->inverse = d->inverse;
+  p->rot = (int32_t)d->rot_dim; p->style = d->style;
   uint32_t end = 0;
   for (int a = 0; a < 3; ++a) {
     if (a < d->n_axes) end += d->sections[a];
@@ -590,6 +590,7 @@ rg_status_t rg_rope(const rg_rope_desc_t* d, const rg_rows_t* x, const rg_tensor
   p.st[0] = {x->ptr, out->ptr, x->token_stride, x->head_stride, 0, out->token_stride, out->head_stride, (int32_t)x->heads, 1, 0};
   p.n_streams = 1; p.tokens = x->tokens; p.d = (int32_t)x->dim;
   set_rotation(&p, d, pos, inv_freq);
+  p.inverse = d->inverse;                                  // the append takes none
   return rg::launch_rope(p, x->dtype, false, static_cast<cudaStream_t>(cuda_stream));
 }
 

@@ -112,7 +112,7 @@ struct Cache4Params {
   Cache4Stream st[3];                  // keys, values, queries
   int32_t n_streams, heads_all;
   int64_t tokens;
-  int32_t d, rot, style, inverse;
+  int32_t d, rot, style;
   int32_t axis_end[3];
   int32_t pos64;
   const void* pos;
