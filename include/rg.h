@@ -420,7 +420,8 @@ typedef struct {
  * tensor-core steps from zero (fp32; the order of k within a group is fixed by this library), times the group's scale in fp32 and onto a
  * part's running sum; K has at most eight parts (of whole 256s, each but the last of equal length), the first four and the rest added in ascending order each,
  * then to one another (a sum that is zero is +0); then the epilogue of rg_gemm and one rounding.  No weight is narrowed.  A row's bits do not depend on M, strides or
- * the run.  Meant for a few rows: the weights are read once for every 40 of them, and from some hundred rows on weights unpacked once for rg_gemm are faster.
+ * the run.  Meant for a few rows: the weights are read once for every 40 of them, so prompts of hundreds of rows want a 16-bit copy of the weights that the
+ * caller keeps, and rg_gemm (nothing here makes one; its weights are rounded, these are not).
  *   A: [M][K] bf16 or fp16, 16-byte aligned, ld a multiple of 8; K a multiple of 32; C, bias, residual: bf16, fp16 or fp32, aligned to their type.
  *   codes: 16-byte aligned; scales: aligned to their type.  M is at most 2^19.  M == 0 or N == 0: RG_OK, nothing launched.  K == 0: RG_ERR_SHAPE.
  * Asynchronous on `cuda_stream`; no workspace. */

@@ -6,11 +6,14 @@
 // the close ones in 64 bits costs more: their code is never in the instruction cache, 3 us in a call of 64 tokens.)  Queries are rotated as rg_rope does it,
 // with its bits.
 //
-// What bounds it: bytes for prompts, latency for single tokens.  A thread takes one group of 16 elements of one row (a query, or a key and a value) and the group
+// What bounds it: for single tokens the latency of place, page, sine in 64 bits and store; for prompts waits for memory that the warps of an SM do not cover and, next to
+// them, instructions (by the counters issue slots 59 % busy appending, 58 % reading; of 11 and 16 cycles that a warp takes for an instruction 4.6 and 7.5 are waits for loads).
+// A thread takes one group of 16 elements of one row (a query, or a key and a value) and the group
 // that the rotation pairs with it: 16-byte loads, several of them in flight, no exchange between threads, and a key's 8 code bytes and its scale byte are
 // a thread's own.  Threads run over two groups, then the CTA's tokens, then the chunks of the head: neighbours write the neighbouring slots of a tile.
 // 8 key heads and 32 query heads of 128 in bf16: 10.5 k tokens of 5 prompts 56 us (4 TB/s; 99.8 with remainders instead of magic sums, 67.5 with a second look at
-// close codes, 63 with queries dealt out as keys are), 64 single tokens 5.3 us.  Reading those tokens back: 17.2 us (4.9 TB/s) and 3.1; two heads of a thread in flight 18.1.
+// close codes, 63 with queries dealt out as keys are; rg_kv_append, which moves more bytes and has no codes to make, 47.5), 64 single tokens 5.3 us (3.7).  Reading those tokens
+// back: 17.2 us (55 MB: 3.2 TB/s, half the copy's rate) and 3.2; two heads of a thread in flight 18.1.
 #include <algorithm>
 #include <type_traits>
 

@@ -1,7 +1,7 @@
 // Values held in four bits: the cache's format (rg_cache_four_t) and the small arithmetic on it that several kernels share.
 //
 // A group is 16 consecutive elements of a head: codes c in -8..7, kept as c + 8, and a scale byte b that stands for s = (8 + b % 8) 2^(b / 8 - 22).
-// c s has at most 4 + 4 significant bits and lies in 2^-22 .. 61440, so it is a bf16 and an fp16 number: nothing is rounded on the way back.
+// c s has at most 4 + 4 significant bits and is 0 or 2^-19 .. 61440 in magnitude, so it is a bf16 and an fp16 number: nothing is rounded on the way back.
 // Every byte is a finite scale: what lies in unused slots cannot be an infinity or a NaN.
 //
 // A block (one page of one head) is a row of tiles of 8 slots, tile_bytes(dim) = 4.5 dim bytes each:
@@ -33,9 +33,9 @@ __device__ __forceinline__ uint32_t scale4_byte(float amax) {
   return (uint32_t)b;
 }
 
-// Eight codes of 16-bit numbers, as they lie in a word, for a scale that reaches their largest magnitude; inv = 1 / s.  x inv is off by 2^-21 at most, so it
-// may miss a border between two codes; it is rounded to a multiple of 2^-15 first, which puts what is next to a border exactly there, and then to an integer, ties to
-// even.  That is exact: x / s is a border or 2^-13 from one (2 x and (2 k + 1) s differ by 2^-8 of the last place of s or more).  The integer stands in the
+// Eight codes of 16-bit numbers, as they lie in a word, for a scale that reaches their largest magnitude; inv = 1 / s.  x inv is off by less than 2^-20 (6.04e-7,
+// all eight mantissas of s and 11 bits of x gone through), so it may miss a border between two codes; it is rounded to a multiple of 2^-15 first, which puts what is next to
+// a border exactly there, and then to an integer, ties to even.  That is exact: x / s is a border or at least 2^-12 from one (11 bits of x against the four of s).  The integer stands in the
 // low bits of a float above 2^23 (the 8 is added there), which is multiplied to its nibble; what stands above the codes adds up to a constant.  Codes of 8
 // become 7 by a minimum in front.
 __device__ __forceinline__ uint32_t codes4(const float* x, float inv) {
@@ -47,7 +47,7 @@ __device__ __forceinline__ uint32_t codes4(const float* x, float inv) {
   }
   return w;
 }
-// The same for numbers in 64 bits.  x inv is off by 2^-48 or so and rounded to a multiple of 2^-40.
+// The same for numbers in 64 bits.  x inv is off by less than 2^-44 (1 / s by 2^-48 of it, x / s at most 7.5) and rounded to a multiple of 2^-40.
 __device__ __forceinline__ uint32_t codes4(const double* x, double inv) {
   uint32_t w = 0u;
 #pragma unroll

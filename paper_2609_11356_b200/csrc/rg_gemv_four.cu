@@ -12,10 +12,10 @@
 // tensor memory, a trip that costs more than these few rows' products.  Every warp streams its own stages into shared memory, a TMA box at a time.
 //
 // Two kernels.  One to four rows (a rule below has the exceptions): a warp copies A's elements along with its codes and never waits for another warp until all its parts are done.
-// More: eight warps share A's elements in shared memory, stage by stage.  28672 x 4096 in groups of 128, a graph of calls on rotating weights, us:
-//   rows          1      2      4      8     16     40
-//   the first    21.3   21.7   22.5   29.7   (71, as a form for 16 rows that reads A's elements from global memory)
-//   the second   26.1   26.2   26.2   26.5   35.7   58.3
+// More: eight warps share A's elements in shared memory, stage by stage.  28672 x 4096 in groups of 128, bf16, zero points, a graph of calls on rotating weights, us:
+//   rows          1      2      3      4      5      8     16     40
+//   the first    21.3   21.6   22.2   22.6
+//   the second                 26.2   26.1   26.2   26.5   31.5   58.6
 // What bounds them: the bytes of the codes would take 9.4 us.  The instructions that unpack them (a mask that makes a float's mantissa of the nibble, and one
 // subtraction, for two codes, with a shift for three of four) keep the half-rate integer pipe busy for 8 us, and 12 to 16 warps of an SM do not cover all
 // waits between them; a grid of 128-row blocks also fills its last wave only in part.
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) gemv_w4_kernel(const _
 // memory (put there, and into the codes' order, once).  The parts of K are shared among the CTAs of a cluster, or are all one CTA's, and are joined over distributed shared
 // memory, every CTA a share of the elements.  How many parts a CTA has (1, 2, 4 or all 8) is the choice with which the waves of CTAs take the fewest stages (below):
 // 16 rows on 128256 x 4096, where many blocks fill the GPU, take 122 us with all parts in a CTA and 173 us with two; on 4096 x 14336, where eight CTAs for each block are
-// needed, 17.1 us.  33 rows on 11009 x 4128 in groups of 32 take 33.5 us (79 with one warp a part and A's elements from global memory).  Reading A's elements two stages
+// needed, 17.1 us.  33 rows on 11009 x 4128 in groups of 32 take 32.4 us (79 with one warp a part and A's elements from global memory).  Reading A's elements two stages
 // ahead instead of one changes nothing; more than 40 rows would leave room for one CTA of an SM only (64 rows on 28672 x 4096: 113 us, as twice 32 rows 94).
 constexpr int RW = 8;                                  // warps
 template <int GROUP, int NT>
@@ -569,9 +569,9 @@ cudaError_t launch_tiles(const rg_weights_four_t* W, const W4Params& p, cudaStre
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, gemv_w4_kernel<F16, GROUP, MT, WARPS>, codes, p);
 }
-// Tiles of 16 rows of weights with eight warps, while all of them fit the GPU at a time, two an SM (4096 x 14336: 14.1 us, 18.4 in tiles of 32; 6144 x 4096, which does
-// not fit: 8.0 and 6.8); then tiles of 32, for which A's elements are read and put in order once, with four warps, or with eight where four leave fewer than
-// 12 an SM (8192 x 8192: 14.2 us with eight; 14336 x 4096: 16.1 with eight, 13.5 with four; 57344 x 8192: 62.5 with four, 79.5 with a warp a tile).  Three and four rows in
+// Tiles of 16 rows of weights with eight warps, while all of them fit the GPU at a time, two an SM (one row, groups of 128: 4096 x 14336 13.3 us, 18.7 in tiles of 32; 6144 x 4096, which
+// does not fit: 10.1 and 8.5); then tiles of 32, for which A's elements are read and put in order once, with four warps, or with eight where four leave fewer than
+// 12 an SM (8192 x 8192: 13.9 us with eight, 19.6 with four; 14336 x 4096: 15.7 with eight, 13.2 with four; 57344 x 8192: 63.2 with four, 79.5 with a warp a tile).  Three and four rows in
 // groups of 32 fill shared memory first: four warps, three CTAs an SM, as soon as eight take more than one wave of two (10240 x 4096: 17.1 us with four, 19.6 and 22.3 with eight).
 template <bool F16, int GROUP>
 cudaError_t launch_few(const rg_weights_four_t* W, const W4Params& p, cudaStream_t st) {

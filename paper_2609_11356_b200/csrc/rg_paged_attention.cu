@@ -642,7 +642,7 @@ __device__ __forceinline__ void unpack32(const Unpack& u, const uint4& codes, ui
   }
 }
 // A key's elements, 32 at a time: `put` takes 16 words and the chunk's number.  `raw`: the block's codes.  WHOLE: heads of so many chunks unrolled.  The kernel for many
-// rows, where two warps unpack, has that (4096-row chunk 1067 us, 1120 as a loop); the one for few rows, where thirty warps run five different pieces of
+// rows, where four warps unpack, has that (4096-row chunk, with two of them: 1067 us, 1120 as a loop); the one for few rows, where thirty warps run five different pieces of
 // code and wait for what does not fit the instruction caches, has a loop (64 single tokens 131 us, 153 unrolled by two, 161 wholly).
 template <int DT, int WHOLE, typename Put>
 __device__ __forceinline__ void unpack_key(const Unpack& u, const uint8_t* raw, int d, int key, Put&& put) {
